@@ -1,0 +1,111 @@
+/*
+ * cocod_lm.h -- operators for workers that train a language model (part of libcocod.so).
+ *
+ * Algorithm 1 of arxiv 1906.12043, Step II asks for every worker's mini-batch gradient; these calls form it for models
+ * made of wide layers and a vocabulary, for all workers of the GPU at once:
+ *
+ *     cocod_grouped_*   products of rows with their own group's weights, forward and backward
+ *     cocod_act_*       activations kept from the forward pass in 8 bits, and their use in the backward pass
+ *     cocod_vocab_*     softmax cross-entropy over a large vocabulary, and its gradient
+ *
+ * Groups.  The rows of all groups (workers, whose mini-batches M_i may differ in size, Section 3.2; or experts) lie one
+ * behind the other in one matrix: row m belongs to group g when offsets[g] <= m < offsets[g + 1].  offsets: device,
+ * G + 1 int32, rising from 0 to M; groups may be empty.  The offsets are only read on the device.  Offsets that do not
+ * rise from 0 to M never lead to an access outside the matrices; the next cocod_lm_check reports them (INVALID).
+ *
+ * Matrices are row-major; a leading dimension (row stride) and a group stride are in elements, so that the weights may be
+ * views of the engine's K x P bf16 copy (cocod_get_bf16_shadow) and the weight gradients views of the K x P fp32
+ * gradients that cocod_local_step takes.  Every base address has to be a multiple of 16 bytes, and so has every stride;
+ * n and k have to be multiples of 8 (INVALID otherwise).
+ *
+ * Precision: bf16 operands, products and sums in fp32, one rounding at the end where the result is bf16.
+ *
+ * Same conventions as cocod.h: int return codes (COCOD_*), device pointers on the device current at create, one host
+ * thread per handle, asynchronous on the given stream.  The calls on one handle use scratch of the handle: order them
+ * (one stream, or events).  Calls can be captured into a CUDA graph.
+ * workspace: device memory lent for the call (until the stream has passed it), 256-byte aligned.
+ */
+#ifndef COCOD_LM_H
+#define COCOD_LM_H
+
+#include <stdint.h>
+
+#include "cocod.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct cocod_lm cocod_lm_handle;
+
+enum { COCOD_BF16 = 0, COCOD_F32 = 1 };      /* type of a result */
+
+#define COCOD_LM_MAX_GROUPS 1024
+
+/* Scratch for tensor maps and flags, about 300 KB.  Errors: INVALID, OOM, CUDA. */
+int cocod_lm_create(cocod_lm_handle **out);
+int cocod_lm_destroy(cocod_lm_handle *h);
+
+/* Synchronise `stream` and report what the kernels of this handle met since the last check: COCOD_ERR_TIMEOUT (a kernel
+ * gave up a wait), COCOD_ERR_INVALID (offsets that do not rise from 0 to M, or a label beyond the vocabulary), COCOD_OK. */
+int cocod_lm_check(cocod_lm_handle *h, cocod_stream_t stream);
+
+/* Number of kernels launched by this handle so far. */
+int64_t cocod_lm_launch_count(const cocod_lm_handle *h);
+
+/* ---------------------------------------------------------------------------------------------
+ * Products by group.  w: G x [n][k] bf16 (ldw >= k, w_stride between groups).
+ *
+ * forward        y[m][j]    = sum_i x[m][i] w[g][j][i]        x: M x k,  y: M x n
+ * input_grad     dx[m][i]   = sum_j dy[m][j] w[g][j][i]       dy: M x n, dx: M x k
+ * weight_grad    dw[g][j][i] = sum_{m in g} dy[m][j] x[m][i]  dw: G x [n][k], written completely (an empty group: 0)
+ *
+ * out_type: COCOD_BF16 or COCOD_F32.  workspace is used to cut long reductions with few results into parts whose sums are
+ * joined in a fixed order; cocod_grouped_workspace says how much a call can use (0 is allowed: no parts). */
+int cocod_grouped_forward(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
+                          const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t w_stride,
+                          void *y, int64_t ldy, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
+                             const void *dy, int64_t lddy, const void *w, int64_t ldw, int64_t w_stride,
+                             void *dx, int64_t lddx, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
+                              const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                              void *dw, int64_t lddw, int64_t dw_stride, int out_type,
+                              void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+enum { COCOD_GROUPED_FORWARD = 0, COCOD_GROUPED_INPUT_GRAD = 1, COCOD_GROUPED_WEIGHT_GRAD = 2 };
+int64_t cocod_grouped_workspace(int which, int G, int64_t M, int64_t n, int64_t k);
+
+/* ---------------------------------------------------------------------------------------------
+ * Activations in 8 bits.  A block is 128 consecutive columns of a row (the last one of a row may be shorter).  With amax
+ * the largest finite magnitude of the block and e the least integer >= -126 with amax <= 127 * 2^e,
+ *     q = sign(x) * max(1, rint(|x| / 2^e)) for x != 0, else 0              (half to even)
+ * stands for q * 2^e: within half a unit of x (within one for |x| < 2^e / 2: the sign of a value always survives, so that
+ * the gate of a ReLU can be taken from it), and exact in bf16.  q = -128 marks a value that was not finite and reads as NaN.
+ *   q      : M x k int8, row stride ldq (a multiple of 16, >= k)
+ *   scales : ceil(k / 128) x M bytes, e + 127
+ *
+ * act_pack       x: M x k bf16 (any k and ldx, any 2-byte alignment; 16-byte aligned rows are faster)
+ * act_unpack     y: M x k bf16
+ * act_relu_grad  dz = (q > 0) ? dh : 0  (NaN where q marks a value that was not finite), dh, dz: M x k bf16; dz may be dh
+ * weight_grad_packed  as cocod_grouped_weight_grad, with x as the checkpoint stands for it. */
+int cocod_act_pack(cocod_lm_handle *h, int64_t M, int64_t k, const void *x, int64_t ldx, int8_t *q, int64_t ldq,
+                   uint8_t *scales, cocod_stream_t stream);
+int cocod_act_unpack(cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, int64_t ldq, const uint8_t *scales,
+                     void *y, int64_t ldy, cocod_stream_t stream);
+int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh, int64_t lddh, const int8_t *q, int64_t ldq,
+                        void *dz, int64_t lddz, cocod_stream_t stream);
+int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
+                                     const void *dy, int64_t lddy, const int8_t *q, int64_t ldq, const uint8_t *scales,
+                                     void *dw, int64_t lddw, int64_t dw_stride, int out_type,
+                                     void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k);
+
+/* Self-test of the bounded waits of the product kernels: one launch (pairs of thread blocks when `pair` is not 0) whose
+ * copies are never issued.  Every wait ends after at most 1.5 * wait_ms (1 .. 2000), COCOD_ERR_TIMEOUT is returned and the
+ * context stays usable. */
+int cocod_grouped_wait_selftest(int wait_ms, int pair, cocod_stream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* COCOD_LM_H */

@@ -1,0 +1,469 @@
+// Products of rows that belong to groups (the workers' mini-batches, of unequal sizes) with each group's own matrix, on
+// the tensor cores of sm_100a.  Row m belongs to group g when offsets[g] <= m < offsets[g + 1]; the offsets live on the
+// device, so a launch does not know how its rows are divided and finds its tiles itself.
+//
+//   rows form    out[m][n]    = sum_k A[m][k] B_g(n, k)      forward (B_g stored [n][k]) and input gradient (stored [k][n])
+//   weight form  out_g[i][j]  = sum_{m in g} A[m][i] B[m][j] weight gradient; the reduction runs over the group's rows
+//
+// One persistent, warp-specialised kernel serves all forms:
+//   * A tile is 256 x 256, computed by a PAIR of CTAs (cta_group::2): each holds 128 rows of A and 128 columns of B per
+//     64-deep block of the reduction (32 KB a stage, six stages), so a pair moves 64 bytes per SM and clock for tensor
+//     cores that need 512 clocks for the block; a single CTA with a tile of its own would need half as much again from
+//     L2.  Problems with few tiles use 128 x 128 tiles and single CTAs (CG = 1): more SMs take part.
+//   * Two accumulators in tensor memory: the epilogue of a tile runs under the products of the next.
+//   * Warps: 0 producer (TMA), 1 issuer of tcgen05.mma (leading CTA of the pair only), 2 tensor memory, 4..11 epilogue.
+//     Every role walks the tile list on its own (Walker); nothing is handed over but barriers.
+//   * An epilogue warp owns 32 rows of its CTA's tile and half of the columns, stages them in shared memory of its own
+//     (4 KB, TMA swizzle) and hands them to the store engine; rows behind the end of a group are some other group's, so a
+//     warp whose rows end inside a group's last tile stores the valid ones itself.
+// Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
+// with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
+// Every wait is bounded, as in cocod_gemm_sm100.cuh.
+#pragma once
+#include "cocod_gemm_sm100.cuh"
+
+namespace cocod {
+namespace lm {
+
+using namespace cocod::gemm;
+
+constexpr int EPI_WARPS = 8, GROUPED_THREADS = 128 + 32 * EPI_WARPS;
+constexpr int RING = 6;                                             // stages of 32 KB
+constexpr int OUT_BYTES = 4096;                                     // staging of an epilogue warp: 32 rows of 128 bytes
+constexpr int GROUPED_SMEM = RING * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 512;
+constexpr int ERR_OFFSETS = 100;                                    // error_flag: the offsets do not rise from 0 to the number of rows
+constexpr int ERR_LABEL = 101;                                      // error_flag: a label beyond the vocabulary
+
+enum Out {
+    OUT_BF16 = 0,
+    OUT_F32 = 1,
+    OUT_ADD_F32 = 2,       // added to what is there
+};
+
+struct GroupedParams {
+    const int *offsets;                // [groups + 1], device
+    int groups;
+    int total_rows;                    // offsets[groups] has to be this
+    int row0, rows;                    // this launch takes rows row0 .. row0 + rows - 1; A and out start at row row0
+    int n;                             // columns of out
+    int kdim;                          // rows form: length of the reduction.  Weight form: rows of out_g
+    int tiles_n;
+    int splits;                        // the reduction is cut into this many parts; part s writes out at index s (weight form: s * groups + g)
+    void *out;                         // rows form: for the rows of a partial tile
+    long long ld_out, split_stride;    // elements
+    const float *row_scale;            // rows form, optional: factor of every row (0: the row is 0 whatever the product is)
+    const CUtensorMap *group_maps;     // weight form: A and B of group g at 2 g and 2 g + 1
+    int *error_flag;
+    unsigned long long wait_ns;        // 0 = WAIT_LIMIT_NS
+    int debug_no_loads;                // self-test: the producer issues nothing
+};
+
+// ------------------------------------------------------------------------------------------ PTX wrappers
+__device__ __forceinline__ void mbar_arrive_local(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)      // a shared::cluster address
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void acquire_map(const CUtensorMap *map)
+{
+    asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(map) : "memory");
+}
+// A tile load of one CTA of a pair; its bytes are counted at `bar` (a shared::cluster address: the leading CTA's barrier).
+template <int CG>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    if (CG == 1)
+        tma_load_3d(dst, map, bar, x, y, z);
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 "
+                     "[%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+template <int CG> __device__ __forceinline__ void tmem_alloc_g(uint32_t slot, uint32_t cols)
+{
+    if (CG == 1) {
+        tmem_alloc(slot, cols);
+        tmem_relinquish();
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG> __device__ __forceinline__ void tmem_dealloc_g(uint32_t taddr, uint32_t cols)
+{
+    if (CG == 1) tmem_dealloc(taddr, cols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void umma_g(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    if (CG == 1)
+        umma_bf16(tmem_d, adesc, bdesc, idesc, accumulate);
+    else
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "setp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrive at the barrier (in both CTAs of a pair) once all products issued so far are complete.
+template <int CG> __device__ __forceinline__ void umma_commit_g(uint32_t bar)
+{
+    if (CG == 1)
+        umma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+template <int CG> __device__ __forceinline__ uint32_t cta_rank()
+{
+    if (CG == 1) return 0;
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// Instruction descriptor: fp32 accumulator, bf16 operands, M = 128 per CTA, operand majors as given.
+template <int CG, int TN, bool A_MN, bool B_MN> __host__ __device__ constexpr uint32_t grouped_idesc()
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
+           ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
+}
+
+// ------------------------------------------------------------------------------------------ tiles
+struct Tile {
+    int g;             // group
+    int m0, m1;        // rows form: first row of the tile, end of the group (both counted from row0).  Weight form: first row of out_g, -
+    int n0;            // first column
+    int kb0, kb1;      // blocks of the reduction (64 each)
+    int split;
+};
+
+// Rows of group g within this launch, counted from row0; any content of offsets gives a range inside [0, rows].
+__device__ __forceinline__ void group_range(const GroupedParams &p, int g, int &lo, int &hi)
+{
+    lo = min(max(p.offsets[g] - p.row0, 0), p.rows);
+    hi = min(max(p.offsets[g + 1] - p.row0, lo), p.rows);
+}
+
+// Within a group, tiles go in bands of eight tile rows, column by column: the CTAs that run at the same time share their
+// operands through L2.
+__device__ __forceinline__ void in_band(int i, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int band = i / (8 * tiles_n), r = i - band * 8 * tiles_n;
+    const int high = min(8, tiles_m - band * 8);
+    tn = r / high;
+    tm = band * 8 + r - tn * high;
+}
+
+// The tile list of a launch, read in rising order by a whole warp.  In the rows form a group has as many tile rows as its
+// rows fill; 32 groups are looked at together, one per lane.
+template <int TM, int TN, bool WG> struct Walker {
+    const GroupedParams &p;
+    int lane, gb = 0, base = 0, lo = 0, hi = 0, cnt = 0, incl = 0, total = 0;
+    __device__ Walker(const GroupedParams &params, int lane_) : p(params), lane(lane_)
+    {
+        if (!WG) load();
+    }
+    __device__ void load()
+    {
+        const int g = gb + lane;
+        lo = hi = cnt = 0;
+        if (g < p.groups) {
+            group_range(p, g, lo, hi);
+            cnt = (hi - lo + TM - 1) / TM * p.tiles_n * p.splits;
+        }
+        incl = cnt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        total = __shfl_sync(0xffffffffu, incl, 31);
+    }
+    __device__ bool find(int t, Tile &tile)
+    {
+        int i, tiles_m;
+        if (WG) {
+            tiles_m = (p.kdim + TM - 1) / TM;
+            const int per = tiles_m * p.tiles_n * p.splits;
+            tile.g = t / per;
+            if (tile.g >= p.groups) return false;
+            i = t - tile.g * per;
+            group_range(p, tile.g, lo, hi);
+        } else {
+            while (t >= base + total) {
+                base += total;
+                gb += 32;
+                if (gb >= p.groups) return false;
+                load();
+            }
+            const int l = __ffs(__ballot_sync(0xffffffffu, t < base + incl)) - 1;
+            tile.g = gb + l;
+            i = t - base - __shfl_sync(0xffffffffu, incl - cnt, l);
+            tile.m0 = __shfl_sync(0xffffffffu, lo, l);
+            tile.m1 = __shfl_sync(0xffffffffu, hi, l);
+            tiles_m = (tile.m1 - tile.m0 + TM - 1) / TM;
+        }
+        const int per_split = tiles_m * p.tiles_n;
+        tile.split = i / per_split;
+        i -= tile.split * per_split;
+        int tm, tn;
+        in_band(i, tiles_m, p.tiles_n, tm, tn);
+        tile.n0 = tn * TN;
+        int blocks;
+        if (WG) {
+            tile.m0 = tm * TM;
+            tile.m1 = p.kdim;
+            blocks = (hi - lo + BK - 1) / BK;
+        } else {
+            tile.m0 += tm * TM;
+            blocks = (p.kdim + BK - 1) / BK;
+        }
+        tile.kb0 = (int)((long long)blocks * tile.split / p.splits);
+        tile.kb1 = (int)((long long)blocks * (tile.split + 1) / p.splits);
+        return true;
+    }
+};
+
+// ------------------------------------------------------------------------------------------ kernel
+// Tensor maps (all three-dimensional, innermost dimension contiguous, 128-byte swizzle):
+//   A, B with the reduction innermost: boxes of 64 x 128 rows; A or B with it second: boxes of 64 x 64, two per operand.
+//   out: boxes of 32 rows x 128 bytes; third index = group (weight form) or part of the reduction.
+template <int CG, int TN, bool WG, bool B_MN, int OUT>
+__global__ void __launch_bounds__(GROUPED_THREADS, 1)
+grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+             const __grid_constant__ CUtensorMap map_out, const GroupedParams p)
+{
+    constexpr int TM = 128 * CG;
+    constexpr bool A_MN = WG;
+    static_assert(TN / CG == 128, "each CTA holds 128 columns of B");
+    extern __shared__ uint8_t grouped_smem[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(grouped_smem) + 1023) & ~(uintptr_t)1023);
+    uint8_t *outs = smem + RING * STAGE_BYTES;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(outs + EPI_WARPS * OUT_BYTES);
+    const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + RING), accf0 = smem_u32(bars + 2 * RING), acce0 = smem_u32(bars + 2 * RING + 2);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * RING + 4);
+    volatile int *abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cta_rank<CG>();
+    const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
+    const uint32_t smem_base = smem_u32(smem);
+    const unsigned long long limit = p.wait_ns ? p.wait_ns : WAIT_LIMIT_NS;
+
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_out) : "memory");
+        for (int s = 0; s < RING; ++s) {
+            mbar_init(full0 + 8 * s, 1);
+            mbar_init(empty0 + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(accf0 + 8 * s, 1);
+            mbar_init(acce0 + 8 * s, EPI_WARPS * CG);
+        }
+        *abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    if (warp == 2) tmem_alloc_g<CG>(smem_u32(tmem_slot), 2 * TN);
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_launch_dependents();
+    pdl_wait();
+
+    int failed = 0;
+    if (warp == 0) {
+        // ---- producer
+        Walker<TM, TN, WG> walk(p, lane);
+        if (blockIdx.x == 0 && p.error_flag != nullptr) {
+            bool bad = false;
+            for (int g = lane; g < p.groups; g += 32)
+                bad |= p.offsets[g + 1] < p.offsets[g] || (g == 0 && p.offsets[0] != 0) || (g == p.groups - 1 && p.offsets[p.groups] != p.total_rows);
+            if (bad) atomicExch(p.error_flag, ERR_OFFSETS);
+        }
+        Tile t;
+        unsigned it = 0;
+        int last_g = -1;
+        for (int i = cluster; walk.find(i, t); i += clusters) {
+            if (lane == 0 && !p.debug_no_loads) {
+                const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
+                if (WG && t.g != last_g) {
+                    acquire_map(ma);
+                    acquire_map(mb);
+                    last_g = t.g;
+                }
+                const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
+                for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+                    const unsigned s = it % RING, use = it / RING;
+                    if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * STAGE_BYTES);
+                    const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
+                    const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+                    if (A_MN) {
+                        load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
+                        load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
+                    } else {
+                        load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
+                    }
+                    if (B_MN) {
+                        load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
+                        load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
+                    } else {
+                        load_tile<CG>(db, mb, bar, kb * BK, n0, zb);
+                    }
+                }
+            }
+            if (__any_sync(0xffffffffu, failed)) break;
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ---- issuer of the products
+        constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B_MN>();
+        constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B_MN ? 2048u : 32u;
+        Walker<TM, TN, WG> walk(p, lane);
+        Tile t;
+        unsigned it = 0, ai = 0;
+        for (int i = cluster; walk.find(i, t); i += clusters) {
+            if (t.kb0 == t.kb1) continue;
+            if (lane == 0) {
+                const unsigned a = ai & 1, use = ai >> 1;
+                if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) failed = 2;
+                tc_fence_after();
+                for (int kb = t.kb0; kb < t.kb1 && !failed; ++kb, ++it) {
+                    const unsigned s = it % RING;
+                    if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
+                    tc_fence_after();
+                    const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+#pragma unroll
+                    for (int k = 0; k < BK / UMMA_K; ++k)
+                        umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B_MN), idesc,
+                                   (kb > t.kb0 || k > 0) ? 1u : 0u);
+                    umma_commit_g<CG>(empty0 + 8 * s);
+                }
+                if (!failed) umma_commit_g<CG>(accf0 + 8 * a);
+            }
+            ++ai;
+            if (__any_sync(0xffffffffu, failed)) break;
+        }
+    } else if (warp >= 4) {
+        // ---- epilogue: rows 32 (warp % 4) .. + 31 of the CTA's 128, columns of one half of the tile
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        uint8_t *stage = outs + (warp - 4) * OUT_BYTES;
+        Walker<TM, TN, WG> walk(p, lane);
+        Tile t;
+        unsigned ai = 0;
+        for (int i = cluster; walk.find(i, t); i += clusters) {
+            const bool any = t.kb0 < t.kb1;
+            const unsigned a = ai & 1;
+            if (any) {
+                const bool ok = mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2);
+                if (!__all_sync(0xffffffffu, ok)) { failed = 3; break; }
+                tc_fence_after();
+                ++ai;
+            }
+            const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
+            const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
+            const int z = WG ? t.split * p.groups + t.g : t.split;
+            const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * TN + half * (TN / 2);
+            float scale = 1.0f;
+            if (!WG && p.row_scale != nullptr && lane < valid) scale = p.row_scale[m + lane];
+            constexpr int CHUNK = OUT == OUT_BF16 ? 64 : 32;                 // 128 bytes of a row
+#pragma unroll 1
+            for (int c = 0; c < TN / 2; c += CHUNK) {
+                uint32_t r[CHUNK];
+                if (any) {
+                    tmem_ld32(tacc + c, *reinterpret_cast<uint32_t (*)[32]>(r));
+                    if (CHUNK == 64) tmem_ld32(tacc + c + 32, *reinterpret_cast<uint32_t (*)[32]>(r + CHUNK - 32));
+                    tmem_ld_wait();
+                    if (c + CHUNK == TN / 2) {            // the accumulator may be overwritten
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (CG == 1) mbar_arrive_local(acce0 + 8 * a);
+                            else mbar_arrive_cluster(map_to_rank(acce0 + 8 * a, 0));
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < CHUNK; ++j) r[j] = 0u;
+                }
+                const int col = t.n0 + half * (TN / 2) + c;
+                if (valid <= 0 || col >= p.n || (OUT == OUT_ADD_F32 && !any)) continue;
+                if (!WG && p.row_scale != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < CHUNK; ++j) r[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(r[j]) * scale);
+                }
+                if (lane == 0) tma_store_wait_read<0>();     // the last store has read the staging
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint4 v;
+                    if (OUT == OUT_BF16) {
+                        const int b = j * 8 < CHUNK ? j * 8 : 0;
+                        v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
+                                       pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
+                    } else {
+                        v = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+                    }
+                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = v;
+                }
+                if (WG || valid >= 32) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(stage), col, m, z);
+                        else tma_store_3d(&map_out, smem_u32(stage), col, m, z);
+                        tma_store_commit();
+                    }
+                } else {
+                    __syncwarp();
+                    constexpr int ES = OUT == OUT_BF16 ? 2 : 4, PER = 16 / ES;
+                    uint8_t *dst = static_cast<uint8_t *>(p.out) + (t.split * p.split_stride + (long long)m * p.ld_out + col) * ES;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const int row = q * 4 + (lane >> 3), piece = lane & 7;
+                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ (row & 7)) << 4));
+                        if (row < valid && col + piece * PER < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + piece * 16) = v;
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) tma_store_wait_read<0>();
+    }
+    if (failed) {
+        *abort = 1;
+        if (p.error_flag != nullptr) atomicExch(p.error_flag, 200 + failed);
+        // copies in flight land within microseconds; this CTA's shared memory outlives them
+        for (const unsigned long long t0 = now_ns(); now_ns() - t0 < 1000000ull;) { }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    if (warp == 2) tmem_dealloc_g<CG>(tmem_base, 2 * TN);
+}
+
+}  // namespace lm
+}  // namespace cocod

@@ -1,0 +1,454 @@
+// Operators for workers that train a language model: products of rows with their own group's weights, activations in
+// 8 bits, softmax cross-entropy over a large vocabulary.  Declared in include/cocod_lm.h.
+#include "cocod_lm.h"
+#include "cocod_act8.cuh"
+#include "cocod_grouped_sm100.cuh"
+#include "cocod_host.h"
+
+#include <algorithm>
+#include <new>
+
+struct cocod_lm {
+    CUtensorMap *group_maps = nullptr;     // device: two per group
+    int *flag = nullptr;                   // device: what the kernels met
+    long long launches = 0;
+};
+
+namespace {
+
+using namespace cocod;
+using namespace cocod::lm;
+using bf16 = __nv_bfloat16;
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int sm_count()
+{
+    static int count[MAX_DEVICES] = {};
+    const int dev = current_device();
+    if (dev < 0) return 0;
+    if (count[dev] == 0 && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        count[dev] = 0;
+    }
+    return count[dev];
+}
+
+// A row-major matrix, or one per group.
+struct Matrix {
+    const void *data;
+    int64_t ld, stride;                    // elements; stride: between groups
+    int elem;                              // bytes of an element: 2 (bf16) or 4 (fp32)
+};
+
+// Three-dimensional map {columns, rows, groups}; a box is 128 bytes of `box_rows` rows.
+bool encode(CUtensorMap *m, const Matrix &x, uint64_t cols, uint64_t rows, uint64_t groups, uint32_t box_rows)
+{
+    EncodeTiledFn enc = get_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {cols, rows, groups};
+    const cuuint64_t strides[2] = {(cuuint64_t)x.ld * x.elem, (cuuint64_t)(groups > 1 ? x.stride : (int64_t)rows * x.ld) * x.elem};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / x.elem), box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return enc(m, x.elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void *>(x.data), dims,
+               strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// ------------------------------------------------------------------------------------------ small kernels
+// The tensor maps of every group's rows of A and B (the weight form reduces over them): the maps of the whole matrices
+// with the first row moved to the group's first row and the number of rows set to the group's.
+__global__ void __launch_bounds__(32)
+make_group_maps(const __grid_constant__ CUtensorMap whole_a, const __grid_constant__ CUtensorMap whole_b, const char *a, long long lda_bytes,
+                const char *b, long long ldb_bytes, const GroupedParams p, CUtensorMap *maps)
+{
+    __shared__ __align__(128) CUtensorMap map;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int g = blockIdx.x >> 1, which = blockIdx.x & 1, lane = threadIdx.x;
+    int lo, hi;
+    group_range(p, g, lo, hi);
+    reinterpret_cast<uint32_t *>(&map)[lane] = reinterpret_cast<const uint32_t *>(which ? &whole_b : &whole_a)[lane];
+    __syncwarp();
+    if (lane == 0) {
+        const uint64_t first = reinterpret_cast<uint64_t>(which ? b + lo * ldb_bytes : a + lo * lda_bytes);
+        asm volatile("tensormap.replace.tile.global_address.shared::cta.b1024.b64 [%0], %1;" ::"r"(smem_u32(&map)), "l"(first) : "memory");
+        asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(smem_u32(&map)), "r"(max(hi - lo, 1)) : "memory");
+    }
+    __syncwarp();
+    asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;"
+                 ::"l"(maps + 2 * g + which), "r"(smem_u32(&map)) : "memory");
+}
+
+// The parts of a reduction that was cut: out = part 0 + part 1 + ... in this order, for `rows` rows of n columns (n a
+// multiple of 4); row r of the result is row r % per_group of group r / per_group.
+template <bool BF16_OUT>
+__global__ void __launch_bounds__(256)
+join_parts(const float *parts, long long part_stride, int count, void *out, long long ld, long long group_stride, long long per_group,
+           long long rows, int n)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int quads = n / 4;
+    const long long total = rows * quads;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+        const long long r = i / quads, c = (i - r * quads) * 4;
+        const float *src = parts + r * n + c;
+        float4 s = *reinterpret_cast<const float4 *>(src);
+        for (int k = 1; k < count; ++k) {
+            const float4 v = *reinterpret_cast<const float4 *>(src + k * part_stride);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const long long at = (r / per_group) * group_stride + (r % per_group) * ld + c;
+        if (BF16_OUT) *reinterpret_cast<uint2 *>(static_cast<bf16 *>(out) + at) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+        else *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = s;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launching the products
+template <int CG, int TN, bool WG, bool B_MN, int OUT>
+cudaError_t launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const GroupedParams &p, int64_t tiles, cudaStream_t s)
+{
+    static bool configured[MAX_DEVICES] = {};
+    const int dev = current_device(), sms = sm_count();
+    if (dev < 0 || sms < 2) return cudaErrorInvalidDevice;
+    auto kernel = grouped_gemm<CG, TN, WG, B_MN, OUT>;
+    if (!configured[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GROUPED_SMEM);
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(tiles, sms / CG) * CG));
+    cfg.blockDim = dim3(GROUPED_THREADS);
+    cfg.dynamicSmemBytes = GROUPED_SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, out, p);
+}
+
+enum Form { FORWARD = COCOD_GROUPED_FORWARD, INPUT_GRAD = COCOD_GROUPED_INPUT_GRAD, WEIGHT_GRAD = COCOD_GROUPED_WEIGHT_GRAD };
+
+// How a product is cut into tiles and parts.
+struct Cut {
+    bool pair;             // 256 x 256 tiles by pairs of CTAs, else 128 x 128 by single ones
+    int splits;
+    int64_t tiles;         // at most
+};
+// rows x cols results (rows form: `groups` groups may each end in a tile of their own; weight form: per group), reductions of
+// `depth` (weight form: on average).
+Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t depth, int64_t workspace_bytes)
+{
+    Cut best{};
+    double best_cost = 1e300;
+    const int sms = std::max(sm_count(), 2);
+    for (int pair = 0; pair < 2; ++pair) {
+        const int64_t t = pair ? 256 : 128, slots = pair ? sms / 2 : sms;
+        const int64_t row_tiles = form == WEIGHT_GRAD ? groups * ceil_div(rows, t)
+                                                      : std::min(rows, ceil_div(rows, t) + (groups > 1 ? groups - 1 : 0));
+        const int64_t tiles = row_tiles * ceil_div(cols, t);
+        const int64_t blocks = std::max<int64_t>(1, ceil_div(depth, 64));
+        const int64_t out_bytes = (form == WEIGHT_GRAD ? groups * rows : rows) * cols * 4;
+        for (int64_t splits = 1; splits <= 64 && (splits == 1 || (blocks / splits >= 4 && splits * out_bytes <= workspace_bytes)); splits *= 2) {
+            const int64_t waves = ceil_div(tiles * splits, slots);
+            const double cost = waves * (ceil_div(blocks, splits) * (pair ? 0.30 : 0.25) + 2.0) + (splits > 1 ? 3.0 + splits * out_bytes / 3e6 : 0.0);
+            if (cost < best_cost) {
+                best_cost = cost;
+                best = Cut{pair != 0, (int)splits, tiles * splits};
+            }
+        }
+    }
+    return best;
+}
+
+template <bool WG, bool B_MN>
+cudaError_t launch_form(const Cut &c, int out, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GroupedParams &p, cudaStream_t s)
+{
+    if (c.pair)
+        return out == OUT_BF16 ? launch_tiles<2, 256, WG, B_MN, OUT_BF16>(a, b, o, p, c.tiles, s)
+                               : launch_tiles<2, 256, WG, B_MN, OUT_F32>(a, b, o, p, c.tiles, s);
+    return out == OUT_BF16 ? launch_tiles<1, 128, WG, B_MN, OUT_BF16>(a, b, o, p, c.tiles, s)
+                           : launch_tiles<1, 128, WG, B_MN, OUT_F32>(a, b, o, p, c.tiles, s);
+}
+
+#define TRY_CUDA(call) do { if ((call) != cudaSuccess) { cudaGetLastError(); return COCOD_ERR_CUDA; } ++h->launches; } while (0)
+
+int join(cocod_lm *h, const float *parts, int64_t part_stride, int count, const Matrix &out, int64_t per_group, int64_t rows, int64_t n, cudaStream_t s)
+{
+    const int64_t quads = rows * (n / 4);
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(quads, 256), 8 * (int64_t)sm_count()));
+    void *dst = const_cast<void *>(out.data);
+    TRY_CUDA(out.elem == 2 ? launch_dependent(true, join_parts<true>, grid, dim3(256), 0, s, parts, (long long)part_stride, count, dst, (long long)out.ld, (long long)out.stride, (long long)per_group, (long long)rows, (int)n)
+                           : launch_dependent(true, join_parts<false>, grid, dim3(256), 0, s, parts, (long long)part_stride, count, dst, (long long)out.ld, (long long)out.stride, (long long)per_group, (long long)rows, (int)n));
+    return COCOD_OK;
+}
+
+// rows form: out (M x cols) = A (M x depth) times B_g (cols x depth for FORWARD, depth x cols for INPUT_GRAD)
+int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, int64_t M, int64_t cols, int64_t depth, const Matrix &A, const Matrix &B,
+             const Matrix &out, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+{
+    if (M == 0) return COCOD_OK;
+    const Cut cut = choose_cut(form, G, M, cols, depth, workspace_bytes);
+    Matrix dst = out;
+    if (cut.splits > 1) dst = Matrix{workspace, cols, M * cols, 4};
+    CUtensorMap a, b, o;
+    const bool ok = encode(&a, A, depth, M, 1, 128) &&
+                    (form == FORWARD ? encode(&b, B, depth, cols, G, 128) : encode(&b, B, cols, depth, G, 64)) &&
+                    encode(&o, dst, cols, M, cut.splits, 32);
+    if (!ok) return COCOD_ERR_CUDA;
+    GroupedParams p{};
+    p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)depth;
+    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits;
+    p.out = const_cast<void *>(dst.data); p.ld_out = dst.ld; p.split_stride = dst.stride;
+    p.error_flag = h->flag;
+    TRY_CUDA(form == FORWARD ? (launch_form<false, false>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s))
+                             : (launch_form<false, true>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s)));
+    if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), M * cols, cut.splits, out, M, M, cols, s);
+    return COCOD_OK;
+}
+
+// weight form: out_g (rows x cols) = sum over the group's rows m of A[m][.]^T B[m][.]
+int run_weights(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
+                const Matrix &out, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+{
+    const Cut cut = choose_cut(WEIGHT_GRAD, G, rows, cols, ceil_div(std::max<int64_t>(M, 1), G), workspace_bytes);
+    Matrix dst = out, a_rows = A, b_rows = B;
+    if (cut.splits > 1) dst = Matrix{workspace, cols, rows * cols, 4};
+    if (M == 0) a_rows.data = b_rows.data = h->group_maps;      // nothing is read
+    CUtensorMap a, b, o;
+    if (!encode(&a, a_rows, rows, std::max<int64_t>(M, 1), 1, 64) || !encode(&b, b_rows, cols, std::max<int64_t>(M, 1), 1, 64) ||
+        !encode(&o, dst, cols, rows, (uint64_t)G * cut.splits, 32))
+        return COCOD_ERR_CUDA;
+    GroupedParams p{};
+    p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
+    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits;
+    p.group_maps = h->group_maps; p.error_flag = h->flag;
+    TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, b, static_cast<const char *>(A.data), (long long)A.ld * 2,
+                              static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps));
+    TRY_CUDA((launch_form<true, true>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s)));
+    if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), (int64_t)G * rows * cols, cut.splits, out, rows, (int64_t)G * rows, cols, s);
+    return COCOD_OK;
+}
+
+// ------------------------------------------------------------------------------------------ checks of arguments
+constexpr int64_t MAX_DIM = (1ll << 31) - 1024;
+bool good_rows(const void *p, int64_t ld, int64_t cols, int64_t M, int elem)
+{
+    return (M == 0 || p != nullptr) && aligned16(p) && ld >= cols && (ld * elem) % 16 == 0 && ld < (1ll << 36);
+}
+bool good_groups(const void *p, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int G, int elem)
+{
+    return p != nullptr && aligned16(p) && ld >= cols && (ld * elem) % 16 == 0 && ld < (1ll << 36) &&
+           (G == 1 || (stride >= (rows - 1) * ld + cols && (stride * elem) % 16 == 0 && stride < (1ll << 37)));
+}
+bool good_shape(const cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *workspace, int64_t workspace_bytes)
+{
+    return h && G >= 1 && G <= COCOD_LM_MAX_GROUPS && offsets && (reinterpret_cast<uintptr_t>(offsets) & 3u) == 0 && M >= 0 && M <= MAX_DIM &&
+           n >= 8 && n <= MAX_DIM && n % 8 == 0 && k >= 8 && k <= MAX_DIM && k % 8 == 0 && workspace_bytes >= 0 &&
+           (workspace_bytes == 0 || (workspace != nullptr && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0));
+}
+inline int size_of(int type) { return type == COCOD_BF16 ? 2 : type == COCOD_F32 ? 4 : 0; }
+
+}  // namespace
+
+extern "C" {
+
+int cocod_lm_create(cocod_lm_handle **out)
+{
+    if (!out) return COCOD_ERR_INVALID;
+    if (!get_encoder()) return COCOD_ERR_CUDA;
+    cocod_lm *h = new (std::nothrow) cocod_lm();
+    if (!h) return COCOD_ERR_OOM;
+    cudaError_t e = cudaMalloc((void **)&h->group_maps, 2 * COCOD_LM_MAX_GROUPS * sizeof(CUtensorMap));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
+    if (e == cudaSuccess) e = cudaMemset(h->flag, 0, 256);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        if (h->group_maps) cudaFree(h->group_maps);
+        if (h->flag) cudaFree(h->flag);
+        delete h;
+        return e == cudaErrorMemoryAllocation ? COCOD_ERR_OOM : COCOD_ERR_CUDA;
+    }
+    *out = h;
+    return COCOD_OK;
+}
+
+int cocod_lm_destroy(cocod_lm_handle *h)
+{
+    if (!h) return COCOD_OK;
+    cudaDeviceSynchronize();
+    cudaFree(h->group_maps);
+    cudaFree(h->flag);
+    delete h;
+    return COCOD_OK;
+}
+
+int cocod_lm_check(cocod_lm_handle *h, cocod_stream_t stream)
+{
+    if (!h) return COCOD_ERR_INVALID;
+    cudaStream_t s = (cudaStream_t)stream;
+    int f = 0;
+    if (cudaMemcpyAsync(&f, h->flag, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
+        return COCOD_ERR_CUDA;
+    if (f == 0) return COCOD_OK;
+    if (cudaMemsetAsync(h->flag, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return COCOD_ERR_CUDA;
+    return f == ERR_OFFSETS || f == ERR_LABEL ? COCOD_ERR_INVALID : COCOD_ERR_TIMEOUT;
+}
+
+int64_t cocod_lm_launch_count(const cocod_lm_handle *h) { return h ? h->launches : -1; }
+
+int64_t cocod_grouped_workspace(int which, int G, int64_t M, int64_t n, int64_t k)
+{
+    if (which < FORWARD || which > WEIGHT_GRAD || G < 1 || G > COCOD_LM_MAX_GROUPS || M < 0 || M > MAX_DIM || n < 8 || n > MAX_DIM || k < 8 || k > MAX_DIM)
+        return COCOD_ERR_INVALID;
+    const int64_t any = 1ll << 62;
+    const Cut c = which == FORWARD ? choose_cut(FORWARD, G, M, n, k, any)
+                  : which == INPUT_GRAD ? choose_cut(INPUT_GRAD, G, M, k, n, any)
+                                        : choose_cut(WEIGHT_GRAD, G, n, k, ceil_div(std::max<int64_t>(M, 1), G), any);
+    if (c.splits == 1) return 0;
+    return c.splits * 4 * (which == FORWARD ? M * n : which == INPUT_GRAD ? M * k : G * n * k);
+}
+
+int cocod_grouped_forward(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *x, int64_t ldx,
+                          const void *w, int64_t ldw, int64_t w_stride, void *y, int64_t ldy, int out_type, void *workspace,
+                          int64_t workspace_bytes, cocod_stream_t stream)
+{
+    const int es = size_of(out_type);
+    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(x, ldx, k, M, 2) ||
+        !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(y, ldy, n, M, es))
+        return COCOD_ERR_INVALID;
+    return run_rows(h, FORWARD, G, offsets, M, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, workspace,
+                    workspace_bytes, (cudaStream_t)stream);
+}
+
+int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy, int64_t lddy,
+                             const void *w, int64_t ldw, int64_t w_stride, void *dx, int64_t lddx, int out_type, void *workspace,
+                             int64_t workspace_bytes, cocod_stream_t stream)
+{
+    const int es = size_of(out_type);
+    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) ||
+        !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(dx, lddx, k, M, es))
+        return COCOD_ERR_INVALID;
+    return run_rows(h, INPUT_GRAD, G, offsets, M, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, workspace,
+                    workspace_bytes, (cudaStream_t)stream);
+}
+
+int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy, int64_t lddy,
+                              const void *x, int64_t ldx, void *dw, int64_t lddw, int64_t dw_stride, int out_type, void *workspace,
+                              int64_t workspace_bytes, cocod_stream_t stream)
+{
+    const int es = size_of(out_type);
+    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) || !good_rows(x, ldx, k, M, 2) ||
+        !good_groups(dw, lddw, dw_stride, n, k, G, es))
+        return COCOD_ERR_INVALID;
+    return run_weights(h, G, offsets, M, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, workspace,
+                       workspace_bytes, (cudaStream_t)stream);
+}
+
+static bool good_act(const cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, int64_t ldq)
+{
+    return h && M >= 0 && M <= MAX_DIM && k >= 1 && k <= 65535ll * ACT_BLOCK && (M == 0 || q) && aligned16(q) && ldq % 16 == 0 && ldq >= k &&
+           ldq < (1ll << 36);
+}
+static bool good_bf16(const void *p, int64_t ld, int64_t M, int64_t k)
+{
+    return (M == 0 || p) && (reinterpret_cast<uintptr_t>(p) & 1u) == 0 && ld >= k && ld < (1ll << 36);
+}
+
+int cocod_act_pack(cocod_lm_handle *h, int64_t M, int64_t k, const void *x, int64_t ldx, int8_t *q, int64_t ldq, uint8_t *scales,
+                   cocod_stream_t stream)
+{
+    if (!good_act(h, M, k, q, ldq) || !good_bf16(x, ldx, M, k) || (M > 0 && !scales)) return COCOD_ERR_INVALID;
+    if (M == 0) return COCOD_OK;
+    const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
+    TRY_CUDA(launch_dependent(true, act_pack, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(x), (long long)ldx, q,
+                              (long long)ldq, scales, (long long)M, (long long)k, (int)(aligned16(x) && ldx % 8 == 0)));
+    return COCOD_OK;
+}
+
+int cocod_act_unpack(cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, int64_t ldq, const uint8_t *scales, void *y, int64_t ldy,
+                     cocod_stream_t stream)
+{
+    if (!good_act(h, M, k, q, ldq) || !good_bf16(y, ldy, M, k) || (M > 0 && !scales)) return COCOD_ERR_INVALID;
+    if (M == 0) return COCOD_OK;
+    const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
+    TRY_CUDA(launch_dependent(true, act_unpack, grid, dim3(256), 0, (cudaStream_t)stream, q, (long long)ldq, scales, static_cast<bf16 *>(y),
+                              (long long)ldy, (long long)M, (long long)k, (int)(aligned16(y) && ldy % 8 == 0)));
+    return COCOD_OK;
+}
+
+int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh, int64_t lddh, const int8_t *q, int64_t ldq, void *dz,
+                        int64_t lddz, cocod_stream_t stream)
+{
+    if (!good_act(h, M, k, q, ldq) || !good_bf16(dh, lddh, M, k) || !good_bf16(dz, lddz, M, k)) return COCOD_ERR_INVALID;
+    if (M == 0) return COCOD_OK;
+    const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
+    TRY_CUDA(launch_dependent(true, act_relu_grad, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(dh), (long long)lddh, q,
+                              (long long)ldq, static_cast<bf16 *>(dz), (long long)lddz, (long long)M, (long long)k,
+                              (int)(aligned16(dh) && aligned16(dz) && lddh % 8 == 0 && lddz % 8 == 0)));
+    return COCOD_OK;
+}
+
+int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k)
+{
+    const int64_t parts = cocod_grouped_workspace(COCOD_GROUPED_WEIGHT_GRAD, G, M, n, k);
+    return parts < 0 ? parts : ceil_div(M * k * 2, 256) * 256 + parts;
+}
+
+int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy,
+                                     int64_t lddy, const int8_t *q, int64_t ldq, const uint8_t *scales, void *dw, int64_t lddw,
+                                     int64_t dw_stride, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream)
+{
+    const int es = size_of(out_type);
+    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) || !good_act(h, M, k, q, ldq) ||
+        (M > 0 && !scales) || !good_groups(dw, lddw, dw_stride, n, k, G, es))
+        return COCOD_ERR_INVALID;
+    const int64_t wide = ceil_div(M * k * 2, 256) * 256;
+    if (workspace_bytes < wide) return COCOD_ERR_TOO_LARGE;
+    if (int rc = cocod_act_unpack(h, M, k, q, ldq, scales, workspace, k, stream)) return rc;
+    return run_weights(h, G, offsets, M, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es},
+                       static_cast<char *>(workspace) + wide, workspace_bytes - wide, (cudaStream_t)stream);
+}
+
+int cocod_grouped_wait_selftest(int wait_ms, int pair, cocod_stream_t stream)
+{
+    if (wait_ms < 1 || wait_ms > 2000) return COCOD_ERR_INVALID;
+    struct Scratch {                       // of this call only
+        char *p = nullptr;
+        ~Scratch() { if (p) cudaFree(p); }
+    } sc;
+    cudaStream_t s = (cudaStream_t)stream;
+    constexpr size_t BYTES = 512 * 512 * 4;
+    if (cudaMalloc((void **)&sc.p, BYTES + 512) != cudaSuccess) { cudaGetLastError(); return COCOD_ERR_OOM; }
+    int *flag = reinterpret_cast<int *>(sc.p + BYTES), *offsets = flag + 32;
+    const int32_t two[2] = {0, 512};
+    if (cudaMemsetAsync(sc.p, 0, BYTES + 512, s) != cudaSuccess ||
+        cudaMemcpyAsync(offsets, two, sizeof(two), cudaMemcpyHostToDevice, s) != cudaSuccess)
+        return COCOD_ERR_CUDA;
+    const Matrix m{sc.p, 512, 512 * 512, 2};
+    CUtensorMap a, b, o;
+    if (!encode(&a, m, 512, 512, 1, 128) || !encode(&b, m, 512, 512, 1, 128) || !encode(&o, m, 512, 512, 1, 32)) return COCOD_ERR_CUDA;
+    GroupedParams p{};
+    p.offsets = offsets; p.groups = 1; p.total_rows = 512; p.rows = 512; p.n = 512; p.kdim = 512; p.splits = 1;
+    p.tiles_n = pair ? 2 : 4; p.out = sc.p; p.ld_out = 512; p.error_flag = flag;
+    p.wait_ns = (unsigned long long)wait_ms * 1000000ull;
+    p.debug_no_loads = 1;
+    // two CTAs (one pair), so that several tiles wait for each
+    const cudaError_t e = pair ? launch_tiles<2, 256, false, false, OUT_BF16>(a, b, o, p, 1, s) : launch_tiles<1, 128, false, false, OUT_BF16>(a, b, o, p, 2, s);
+    int f = 0;
+    if (e != cudaSuccess || cudaMemcpyAsync(&f, flag, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+        cudaGetLastError();
+        return COCOD_ERR_CUDA;
+    }
+    return f ? COCOD_ERR_TIMEOUT : COCOD_OK;
+}
+
+}  // extern "C"

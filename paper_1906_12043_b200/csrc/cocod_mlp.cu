@@ -20,6 +20,7 @@
 #include "cocod_gemm_update_sm100.cuh"
 #include "cocod_mlp_chain_sm100.cuh"
 #include "cocod_internal.h"
+#include "cocod_host.h"
 
 #include <algorithm>
 #include <cstdio>
@@ -30,28 +31,8 @@
 namespace {
 
 using bf16 = __nv_bfloat16;
+using namespace cocod;
 using namespace cocod::gemm;
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encoder()
-{
-    static EncodeTiledFn fn = nullptr;
-    static bool tried = false;
-    if (!tried) {
-        tried = true;
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-        else
-            cudaGetLastError();
-    }
-    return fn;
-}
 
 // 3-D maps over a batched row-major matrix: dims {cols (contiguous), rows, workers}.  `box_rows` is
 // 128 for a K-major operand tile, 64 for an MN-major one; a box is 64 bf16 columns wide (128 bytes,
@@ -91,32 +72,6 @@ bool map_out(CUtensorMap *m, float *base, uint64_t cols, uint64_t rows, uint64_t
     return enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Facts that belong to a device (function attributes set, SM count, scratch of the stand-alone GEMM call) are
-// cached per device, indexed by the current device: one process may drive engines on several GPUs.
-constexpr int MAX_DEVICES = 64;
-inline int current_device()
-{
-    int d = 0;
-    if (cudaGetDevice(&d) != cudaSuccess || d < 0 || d >= MAX_DEVICES) return -1;
-    return d;
-}
-
-// Launch with the programmatic-serialization attribute: the kernel may become resident (and run the
-// part of its prologue that precedes pdl_wait()) while the previous kernel in the stream drains.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(bool pdl, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
-                             Args &&...args)
-{
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
 template <int EPI, bool A_MN, bool B_MN>

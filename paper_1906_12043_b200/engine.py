@@ -67,6 +67,21 @@ SIGNATURES = {
     "cocod_kernel_mean": (_i, [_vp, _i, _i64, _vp, _vp, _vp]),
     "cocod_kernel_merge": (_i, [_vp, _vp, _vp, _i, _i64, _vp]),
     "cocod_kernel_local_step_host_noalloc": (_i, [_vp, _vp, _vp, _vp, _i64, _f, _f, _f, _vp]),
+    # include/cocod_lm.h (bound by lm.py)
+    "cocod_lm_create": (_i, [ctypes.POINTER(_vp)]),
+    "cocod_lm_destroy": (_i, [_vp]),
+    "cocod_lm_check": (_i, [_vp, _vp]),
+    "cocod_lm_launch_count": (_i64, [_vp]),
+    "cocod_grouped_forward": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i, _vp, _i64, _vp]),
+    "cocod_grouped_input_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i, _vp, _i64, _vp]),
+    "cocod_grouped_weight_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
+    "cocod_grouped_workspace": (_i64, [_i, _i, _i64, _i64, _i64]),
+    "cocod_act_pack": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "cocod_act_unpack": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "cocod_act_relu_grad": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "cocod_grouped_weight_grad_packed": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
+    "cocod_grouped_packed_workspace": (_i64, [_i, _i64, _i64, _i64]),
+    "cocod_grouped_wait_selftest": (_i, [_i, _i, _vp]),
 }
 
 _lib = None
