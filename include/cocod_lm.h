@@ -100,6 +100,31 @@ int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *o
                                      void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
 int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k);
 
+/* ---------------------------------------------------------------------------------------------
+ * Softmax cross-entropy over a vocabulary of V entries, each group with an output matrix w[g] (V x D) of its own:
+ *     l[r][v] = sum_i x[r][i] w[g][v][i],   row_loss[r] = log sum_v exp(l[r][v]) - l[r][label_r],
+ *     loss[g] = sum over the group's rows of a_r row_loss[r],
+ *     dx[r] = a_r sum_v (softmax - onehot)[r][v] w[g][v],   dw[g][v] = sum_r a_r (softmax - onehot)[r][v] x[r].
+ * a_r = row_weights[r], or, where row_weights is NULL, 1 / (rows of the group that take part): the mean.
+ * Rows whose label is negative (or whose weight is 0) take no part whatever they hold: row_loss and dx are 0 there.  A
+ * group of which no row takes part has loss 0 and dw 0.  A label >= V is reported by cocod_lm_check; its row takes no part.
+ *   x: M x D bf16;  w: bf16;  labels: M int32;  row_weights: M fp32 or NULL;  loss: G fp32;  row_loss: M fp32
+ *   dx: M x D bf16;  dw: G x [V][D], bf16 or fp32, written completely.  V: any; D: a multiple of 8.
+ * The logits are never written.  cocod_vocab_loss keeps two numbers for each row and 64 or 128 entries; cocod_vocab_loss_grad keeps
+ * exp(l - l[label]) in bf16 for as many rows at a time as the workspace holds (at least 256, or all), and adds up dw over
+ * these passes in fp32.  cocod_vocab_workspace: the bytes for one pass over all rows, or, if that is more than `limit`,
+ * for the most rows that stay within it (more than `limit` if not even the fewest do); less: COCOD_ERR_TOO_LARGE.
+ * Precision: the exponentials and a_r x / sum are rounded to bf16 as operands of the gradients' products (each term of a
+ * gradient carries a relative error of up to 2^-8, also where dw is fp32); the losses are formed in fp32. */
+int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_grad, int dw_type, int64_t limit);
+int cocod_vocab_loss(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const void *x, int64_t ldx,
+                     const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, float *loss,
+                     float *row_loss, void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+int cocod_vocab_loss_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const void *x, int64_t ldx,
+                          const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, float *loss,
+                          float *row_loss, void *dx, int64_t lddx, void *dw, int64_t lddw, int64_t dw_stride, int dw_type,
+                          void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+
 /* Self-test of the bounded waits of the product kernels: one launch (pairs of thread blocks when `pair` is not 0) whose
  * copies are never issued.  Every wait ends after at most 1.5 * wait_ms (1 .. 2000), COCOD_ERR_TIMEOUT is returned and the
  * context stays usable. */

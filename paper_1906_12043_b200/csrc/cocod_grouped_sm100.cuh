@@ -38,7 +38,11 @@ enum Out {
     OUT_BF16 = 0,
     OUT_F32 = 1,
     OUT_ADD_F32 = 2,       // added to what is there
+    // rows form, the vocabulary's logits l = h w^T: nothing of l is written, but for every row r with reference c_r and label t_r
+    OUT_VOCAB = 3,         // u[r][v] = exp(l - c_r) in bf16, 0 at v = t_r, and for each half of a tile sum_v u (in fp32) and max_v l, v != t_r
+    OUT_VOCAB_SUMS = 4,    // only the sums and maxima
 };
+__host__ __device__ constexpr bool is_vocab(int out) { return out == OUT_VOCAB || out == OUT_VOCAB_SUMS; }
 
 struct GroupedParams {
     const int *offsets;                // [groups + 1], device
@@ -53,6 +57,13 @@ struct GroupedParams {
     long long ld_out, split_stride;    // elements
     const float *row_scale;            // rows form, optional: factor of every row (0: the row is 0 whatever the product is)
     const CUtensorMap *group_maps;     // weight form: A and B of group g at 2 g and 2 g + 1
+    // OUT_VOCAB, OUT_VOCAB_SUMS (rows counted from row0)
+    const float *ref;                  // c_r
+    const int *label;                  // t_r; negative: the row takes no part (u = 0)
+    float2 *sums;                      // [half tiles][ld_sums]: {sum, max}
+    int ld_sums;
+    const int *redo;                   // optional: only tiles with a row whose entry is not 0, and nothing at all if *redo_any is 0
+    const int *redo_any;
     int *error_flag;
     unsigned long long wait_ns;        // 0 = WAIT_LIMIT_NS
     int debug_no_loads;                // self-test: the producer issues nothing
@@ -243,6 +254,21 @@ template <int TM, int TN, bool WG> struct Walker {
     }
 };
 
+// Whether a second pass over the logits takes this tile (all roles of both CTAs see the same).
+template <int TM> __device__ __forceinline__ bool redo_tile(const GroupedParams &p, const Tile &t, int lane)
+{
+    bool any = false;
+    for (int r = t.m0 + lane; r < min(t.m0 + TM, t.m1); r += 32) any |= p.redo[r] != 0;
+    return __any_sync(0xffffffffu, any);
+}
+
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // ------------------------------------------------------------------------------------------ kernel
 // Tensor maps (all three-dimensional, innermost dimension contiguous, 128-byte swizzle):
 //   A, B with the reduction innermost: boxes of 64 x 128 rows; A or B with it second: boxes of 64 x 64, two per operand.
@@ -292,6 +318,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t tmem_base = *tmem_slot;
     pdl_launch_dependents();
     pdl_wait();
+    // a second pass over the logits that no row needs has no tiles
+    const int first = is_vocab(OUT) && p.redo != nullptr && *p.redo_any == 0 ? 0x7fffffff : cluster;
 
     int failed = 0;
     if (warp == 0) {
@@ -306,7 +334,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         Tile t;
         unsigned it = 0;
         int last_g = -1;
-        for (int i = cluster; walk.find(i, t); i += clusters) {
+        for (int i = first; walk.find(i, t); i += clusters) {
+            if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
             if (lane == 0 && !p.debug_no_loads) {
                 const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
                 if (WG && t.g != last_g) {
@@ -344,7 +373,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         Walker<TM, TN, WG> walk(p, lane);
         Tile t;
         unsigned it = 0, ai = 0;
-        for (int i = cluster; walk.find(i, t); i += clusters) {
+        for (int i = first; walk.find(i, t); i += clusters) {
+            if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
             if (t.kb0 == t.kb1) continue;
             if (lane == 0) {
                 const unsigned a = ai & 1, use = ai >> 1;
@@ -373,7 +403,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         Walker<TM, TN, WG> walk(p, lane);
         Tile t;
         unsigned ai = 0;
-        for (int i = cluster; walk.find(i, t); i += clusters) {
+        for (int i = first; walk.find(i, t); i += clusters) {
+            if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
             const bool any = t.kb0 < t.kb1;
             const unsigned a = ai & 1;
             if (any) {
@@ -388,7 +419,14 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * TN + half * (TN / 2);
             float scale = 1.0f;
             if (!WG && p.row_scale != nullptr && lane < valid) scale = p.row_scale[m + lane];
-            constexpr int CHUNK = OUT == OUT_BF16 ? 64 : 32;                 // 128 bytes of a row
+            constexpr bool HALF_WORDS = OUT == OUT_BF16 || is_vocab(OUT);
+            constexpr int CHUNK = HALF_WORDS ? 64 : 32;                      // 128 bytes of a row
+            float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
+            int label = -1;
+            if (is_vocab(OUT) && lane < valid) {
+                label = p.label[m + lane];
+                if (label >= 0) ref = p.ref[m + lane];
+            }
 #pragma unroll 1
             for (int c = 0; c < TN / 2; c += CHUNK) {
                 uint32_t r[CHUNK];
@@ -410,6 +448,28 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
                 const int col = t.n0 + half * (TN / 2) + c;
                 if (valid <= 0 || col >= p.n || (OUT == OUT_ADD_F32 && !any)) continue;
+                if (is_vocab(OUT)) {
+                    // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
+                    const int end = label < 0 ? 0 : p.n - col, at = label - col;
+                    if (__any_sync(0xffffffffu, end < CHUNK || (at >= 0 && at < CHUNK))) {
+#pragma unroll
+                        for (int j = 0; j < CHUNK; ++j) if (j >= end || j == at) r[j] = 0xff800000u;
+                    }
+                    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < CHUNK; ++j) {
+                        const float l = __uint_as_float(r[j]);
+                        most = fmaxf(most, l);
+                        const float e = exp2_approx((l - ref) * 1.4426950408889634f);
+                        s4[j & 3] += e;
+                        r[j] = __float_as_uint(e);
+                    }
+                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    if (c + CHUNK == TN / 2 || col + CHUNK >= p.n) {          // the last columns of this half
+                        if (lane < valid) p.sums[(long long)(t.n0 / (TN / 2) + half) * p.ld_sums + m + lane] = make_float2(sum, most);
+                    }
+                    if (OUT == OUT_VOCAB_SUMS) continue;
+                }
                 if (!WG && p.row_scale != nullptr) {
 #pragma unroll
                     for (int j = 0; j < CHUNK; ++j) r[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(r[j]) * scale);
@@ -419,7 +479,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint4 v;
-                    if (OUT == OUT_BF16) {
+                    if (HALF_WORDS) {
                         const int b = j * 8 < CHUNK ? j * 8 : 0;
                         v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
                                        pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
@@ -438,7 +498,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     }
                 } else {
                     __syncwarp();
-                    constexpr int ES = OUT == OUT_BF16 ? 2 : 4, PER = 16 / ES;
+                    constexpr int ES = HALF_WORDS ? 2 : 4, PER = 16 / ES;
                     uint8_t *dst = static_cast<uint8_t *>(p.out) + (t.split * p.split_stride + (long long)m * p.ld_out + col) * ES;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {

@@ -3,6 +3,7 @@
 #include "cocod_lm.h"
 #include "cocod_act8.cuh"
 #include "cocod_grouped_sm100.cuh"
+#include "cocod_vocab.cuh"
 #include "cocod_host.h"
 
 #include <algorithm>
@@ -191,10 +192,16 @@ int join(cocod_lm *h, const float *parts, int64_t part_stride, int count, const 
     return COCOD_OK;
 }
 
+// Which rows of the batch a call takes: row0 .. row0 + rows - 1 of total (A, out and row_scale start at row0).
+struct Window {
+    int64_t row0, rows, total;
+};
+
 // rows form: out (M x cols) = A (M x depth) times B_g (cols x depth for FORWARD, depth x cols for INPUT_GRAD)
-int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, int64_t M, int64_t cols, int64_t depth, const Matrix &A, const Matrix &B,
-             const Matrix &out, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window &win, int64_t cols, int64_t depth, const Matrix &A, const Matrix &B,
+             const Matrix &out, const float *row_scale, void *workspace, int64_t workspace_bytes, cudaStream_t s)
 {
+    const int64_t M = win.rows;
     if (M == 0) return COCOD_OK;
     const Cut cut = choose_cut(form, G, M, cols, depth, workspace_bytes);
     Matrix dst = out;
@@ -205,8 +212,8 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, int64_t M, i
                     encode(&o, dst, cols, M, cut.splits, 32);
     if (!ok) return COCOD_ERR_CUDA;
     GroupedParams p{};
-    p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)depth;
-    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits;
+    p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)depth;
+    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits; p.row_scale = row_scale;
     p.out = const_cast<void *>(dst.data); p.ld_out = dst.ld; p.split_stride = dst.stride;
     p.error_flag = h->flag;
     TRY_CUDA(form == FORWARD ? (launch_form<false, false>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s))
@@ -216,9 +223,12 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, int64_t M, i
 }
 
 // weight form: out_g (rows x cols) = sum over the group's rows m of A[m][.]^T B[m][.]
-int run_weights(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
-                const Matrix &out, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+// (add: added to what out, fp32, holds)
+int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
+                const Matrix &out, bool add, void *workspace, int64_t workspace_bytes, cudaStream_t s)
 {
+    const int64_t M = win.rows;
+    if (add) workspace_bytes = 0;
     const Cut cut = choose_cut(WEIGHT_GRAD, G, rows, cols, ceil_div(std::max<int64_t>(M, 1), G), workspace_bytes);
     Matrix dst = out, a_rows = A, b_rows = B;
     if (cut.splits > 1) dst = Matrix{workspace, cols, rows * cols, 4};
@@ -228,13 +238,140 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t r
         !encode(&o, dst, cols, rows, (uint64_t)G * cut.splits, 32))
         return COCOD_ERR_CUDA;
     GroupedParams p{};
-    p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
+    p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
     p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits;
     p.group_maps = h->group_maps; p.error_flag = h->flag;
     TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, b, static_cast<const char *>(A.data), (long long)A.ld * 2,
                               static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps));
+    if (add) {
+        TRY_CUDA((cut.pair ? launch_tiles<2, 256, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)
+                           : launch_tiles<1, 128, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)));
+        return COCOD_OK;
+    }
     TRY_CUDA((launch_form<true, true>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s)));
     if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), (int64_t)G * rows * cols, cut.splits, out, rows, (int64_t)G * rows, cols, s);
+    return COCOD_OK;
+}
+
+// ------------------------------------------------------------------------------------------ vocabulary
+// How a call's workspace is laid out when `at_once` rows are taken together.
+struct VocabLayout {
+    int64_t label, own, ref, share, any;       // whole batch: byte offsets
+    int64_t rho, redo, sums, u, hs;            // rows of one pass
+    int64_t total32;                           // fp32 gradient of the weights, if it is summed over passes and wanted in bf16
+    int64_t parts;                             // what is left: parts of cut reductions
+    int64_t bytes, ldu, n_sums;
+};
+VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int dw_elem, int64_t at_once)
+{
+    VocabLayout l{};
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { const int64_t here = at; at += ceil_div(bytes, 256) * 256; return here; };
+    l.label = take(4 * M);
+    l.own = take(4 * M);
+    l.ref = take(4 * M);
+    l.share = take(4 * G);
+    l.any = take(256);
+    l.redo = take(4 * at_once);
+    l.n_sums = ceil_div(V, 128) * 2;           // (as many as the smaller tiles give)
+    l.sums = take(8 * at_once * l.n_sums);
+    l.ldu = ceil_div(V, 64) * 64;
+    if (grad) {
+        l.rho = take(4 * at_once);
+        l.u = take(2 * at_once * l.ldu);
+        l.hs = take(2 * at_once * D);
+        if (at_once < M && dw_elem == 2) l.total32 = take(4 * G * V * D);
+    }
+    l.parts = l.bytes = at;
+    return l;
+}
+// The most rows that fit, 0 if not even the fewest do.
+int64_t vocab_rows(int G, int64_t M, int64_t V, int64_t D, bool grad, int dw_elem, int64_t bytes)
+{
+    if (vocab_layout(G, M, V, D, grad, dw_elem, M).bytes <= bytes) return M;
+    int64_t lo = 0, hi = ceil_div(M, 256);     // in units of 256 rows: lo fits, hi does not
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) / 2;
+        if (vocab_layout(G, M, V, D, grad, dw_elem, mid * 256).bytes <= bytes) lo = mid; else hi = mid;
+    }
+    return lo * 256;
+}
+
+struct VocabGrad {
+    Matrix dh, dw;
+};
+
+int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const Matrix &x, const Matrix &w, const int32_t *labels,
+              const float *row_weight, float *loss, float *row_loss, const VocabGrad *grad, char *ws, int64_t workspace_bytes, cudaStream_t s)
+{
+    const int dw_elem = grad ? grad->dw.elem : 0;
+    const int64_t at_once = M ? vocab_rows(G, M, V, D, grad != nullptr, dw_elem, workspace_bytes) : 0;
+    if (M && at_once == 0) return COCOD_ERR_TOO_LARGE;
+    const VocabLayout l = vocab_layout(G, M, V, D, grad != nullptr, dw_elem, at_once);
+    if (l.bytes > workspace_bytes) return COCOD_ERR_TOO_LARGE;
+    VocabRows v{};
+    v.offsets = offsets; v.groups = G; v.total = (int)M; v.vocab = (int)V; v.width = (int)D; v.labels = labels; v.row_weight = row_weight;
+    v.h = static_cast<const bf16 *>(x.data); v.ldh = x.ld;
+    v.w = static_cast<const bf16 *>(w.data); v.ldw = w.ld; v.w_stride = w.stride;
+    v.label = reinterpret_cast<int *>(ws + l.label); v.own = reinterpret_cast<float *>(ws + l.own);
+    v.ref = reinterpret_cast<float *>(ws + l.ref); v.share = reinterpret_cast<float *>(ws + l.share);
+    v.error_flag = h->flag;
+    int *any = reinterpret_cast<int *>(ws + l.any);
+    const int row_blocks = (int)ceil_div(M, 8);
+    TRY_CUDA(launch_dependent(true, vocab_target, dim3(row_blocks + G), dim3(256), 0, s, v, row_blocks));
+    for (int64_t row0 = 0; row0 < M; row0 += at_once) {
+        const Window win{row0, std::min(at_once, M - row0), M};
+        const Matrix hx{static_cast<const bf16 *>(x.data) + row0 * x.ld, x.ld, 0, 2};
+        if (cudaMemsetAsync(any, 0, sizeof(int), s) != cudaSuccess) return COCOD_ERR_CUDA;
+        const Cut cut = choose_cut(FORWARD, G, win.rows, V, D, 0);
+        const Matrix u{ws + l.u, l.ldu, 0, 2};
+        CUtensorMap a, b, o;
+        if (!encode(&a, hx, D, win.rows, 1, 128) || !encode(&b, w, D, V, G, 128) || !encode(&o, grad ? u : hx, grad ? V : D, win.rows, 1, 32))
+            return COCOD_ERR_CUDA;
+        GroupedParams p{};
+        p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.row0 = (int)row0; p.rows = (int)win.rows; p.n = (int)V; p.kdim = (int)D;
+        p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.splits = 1;
+        p.out = ws + l.u; p.ld_out = l.ldu; p.error_flag = h->flag;
+        p.ref = v.ref + row0; p.label = v.label + row0; p.sums = reinterpret_cast<float2 *>(ws + l.sums); p.ld_sums = (int)win.rows;
+        FinishParams f{};
+        f.v = v; f.row0 = (int)row0; f.rows = (int)win.rows; f.sums = p.sums; f.ld_sums = p.ld_sums;
+        f.n_sums = (int)ceil_div(V, cut.pair ? 128 : 64);
+        f.row_loss = row_loss; f.redo = reinterpret_cast<int *>(ws + l.redo); f.redo_any = any;
+        if (grad) {
+            f.rho = reinterpret_cast<float *>(ws + l.rho);
+            f.u = reinterpret_cast<bf16 *>(ws + l.u); f.ldu = l.ldu;
+            f.hs = reinterpret_cast<bf16 *>(ws + l.hs);
+        }
+        for (int pass = 0; pass < 2; ++pass) {
+            p.redo = pass ? f.redo : nullptr;
+            p.redo_any = any;
+            f.second = pass;
+            if (grad)
+                TRY_CUDA((cut.pair ? launch_tiles<2, 256, false, false, OUT_VOCAB>(a, b, o, p, cut.tiles, s)
+                                   : launch_tiles<1, 128, false, false, OUT_VOCAB>(a, b, o, p, cut.tiles, s)));
+            else
+                TRY_CUDA((cut.pair ? launch_tiles<2, 256, false, false, OUT_VOCAB_SUMS>(a, b, o, p, cut.tiles, s)
+                                   : launch_tiles<1, 128, false, false, OUT_VOCAB_SUMS>(a, b, o, p, cut.tiles, s)));
+            TRY_CUDA(launch_dependent(true, vocab_finish, dim3((unsigned)ceil_div(win.rows, FINISH_ROWS)), dim3(32 * FINISH_WARPS), 0, s, f));
+        }
+        if (!grad) continue;
+        char *parts = ws + l.parts;
+        const int64_t parts_bytes = workspace_bytes - l.parts;
+        const Matrix dh{static_cast<const bf16 *>(grad->dh.data) + row0 * grad->dh.ld, grad->dh.ld, 0, 2};
+        if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, parts, parts_bytes, s)) return rc;
+        const Matrix hs{ws + l.hs, D, 0, 2};
+        const bool several = at_once < M;
+        const Matrix dst = several && dw_elem == 2 ? Matrix{ws + l.total32, D, V * D, 4} : grad->dw;
+        if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, dst, several && row0 > 0, parts, parts_bytes, s)) return rc;
+        if (several && dw_elem == 2 && row0 + at_once >= M) {
+            if (int rc = join(h, reinterpret_cast<const float *>(ws + l.total32), 0, 1, grad->dw, V, G * V, D, s)) return rc;
+        }
+    }
+    if (M == 0 && grad) {
+        const Matrix none{h->group_maps, D, 0, 2};
+        if (int rc = run_weights(h, G, offsets, Window{0, 0, 0}, V, D, Matrix{h->group_maps, ceil_div(V, 8) * 8, 0, 2}, none, grad->dw, false, nullptr, 0, s)) return rc;
+    }
+    TRY_CUDA(launch_dependent(true, vocab_mean, dim3(G), dim3(256), 0, s, v, static_cast<const float *>(row_loss), loss));
     return COCOD_OK;
 }
 
@@ -325,7 +462,7 @@ int cocod_grouped_forward(cocod_lm_handle *h, int G, const int32_t *offsets, int
     if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(y, ldy, n, M, es))
         return COCOD_ERR_INVALID;
-    return run_rows(h, FORWARD, G, offsets, M, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, workspace,
+    return run_rows(h, FORWARD, G, offsets, Window{0, M, M}, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, nullptr, workspace,
                     workspace_bytes, (cudaStream_t)stream);
 }
 
@@ -337,7 +474,7 @@ int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, 
     if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) ||
         !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(dx, lddx, k, M, es))
         return COCOD_ERR_INVALID;
-    return run_rows(h, INPUT_GRAD, G, offsets, M, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, workspace,
+    return run_rows(h, INPUT_GRAD, G, offsets, Window{0, M, M}, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, nullptr, workspace,
                     workspace_bytes, (cudaStream_t)stream);
 }
 
@@ -349,7 +486,7 @@ int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets,
     if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(dw, lddw, dw_stride, n, k, G, es))
         return COCOD_ERR_INVALID;
-    return run_weights(h, G, offsets, M, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, workspace,
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, workspace,
                        workspace_bytes, (cudaStream_t)stream);
 }
 
@@ -414,8 +551,62 @@ int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *o
     const int64_t wide = ceil_div(M * k * 2, 256) * 256;
     if (workspace_bytes < wide) return COCOD_ERR_TOO_LARGE;
     if (int rc = cocod_act_unpack(h, M, k, q, ldq, scales, workspace, k, stream)) return rc;
-    return run_weights(h, G, offsets, M, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es},
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false,
                        static_cast<char *>(workspace) + wide, workspace_bytes - wide, (cudaStream_t)stream);
+}
+
+int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_grad, int dw_type, int64_t limit)
+{
+    const int es = with_grad ? size_of(dw_type) : 2;
+    if (G < 1 || G > COCOD_LM_MAX_GROUPS || M < 0 || M > MAX_DIM || V < 1 || V > MAX_DIM || D < 8 || D > MAX_DIM || D % 8 || !es || limit < 0)
+        return COCOD_ERR_INVALID;
+    const int64_t all = vocab_layout(G, M, V, D, with_grad != 0, es, M).bytes;
+    int64_t bytes = all;
+    if (all > limit) {
+        const int64_t rows = vocab_rows(G, M, V, D, with_grad != 0, es, limit);
+        bytes = vocab_layout(G, M, V, D, with_grad != 0, es, std::max<int64_t>(rows, std::min<int64_t>(M, 256))).bytes;
+    }
+    if (with_grad && M > 0) {              // a short batch gains by cutting the long reductions
+        const int64_t any = 1ll << 62;
+        const Cut dh = choose_cut(INPUT_GRAD, G, M, D, V, any), dw = choose_cut(WEIGHT_GRAD, G, V, D, ceil_div(M, G), any);
+        const int64_t parts = std::max<int64_t>(dh.splits > 1 ? dh.splits * 4 * M * D : 0, dw.splits > 1 ? dw.splits * 4 * G * V * D : 0);
+        bytes += std::min(parts, std::max<int64_t>(limit - bytes, 0));
+    }
+    return bytes;
+}
+
+static bool good_vocab(const cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const void *x, int64_t ldx,
+                       const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, const float *loss,
+                       const float *row_loss, const void *workspace, int64_t workspace_bytes)
+{
+    return good_shape(h, G, offsets, M, 8, D, workspace, workspace_bytes) && workspace && V >= 1 && V <= MAX_DIM && good_rows(x, ldx, D, M, 2) &&
+           good_groups(w, ldw, w_stride, V, D, G, 2) && (M == 0 || (labels && row_loss)) && loss &&
+           ((reinterpret_cast<uintptr_t>(labels) | reinterpret_cast<uintptr_t>(row_weights) | reinterpret_cast<uintptr_t>(loss) |
+             reinterpret_cast<uintptr_t>(row_loss)) & 3u) == 0;
+}
+
+int cocod_vocab_loss(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const void *x, int64_t ldx,
+                     const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, float *loss,
+                     float *row_loss, void *workspace, int64_t workspace_bytes, cocod_stream_t stream)
+{
+    if (!good_vocab(h, G, offsets, M, V, D, x, ldx, w, ldw, w_stride, labels, row_weights, loss, row_loss, workspace, workspace_bytes))
+        return COCOD_ERR_INVALID;
+    return run_vocab(h, G, offsets, M, V, D, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, labels, row_weights, loss, row_loss, nullptr,
+                     static_cast<char *>(workspace), workspace_bytes, (cudaStream_t)stream);
+}
+
+int cocod_vocab_loss_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const void *x, int64_t ldx,
+                          const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, float *loss,
+                          float *row_loss, void *dx, int64_t lddx, void *dw, int64_t lddw, int64_t dw_stride, int dw_type, void *workspace,
+                          int64_t workspace_bytes, cocod_stream_t stream)
+{
+    const int es = size_of(dw_type);
+    if (!good_vocab(h, G, offsets, M, V, D, x, ldx, w, ldw, w_stride, labels, row_weights, loss, row_loss, workspace, workspace_bytes) || !es ||
+        !good_rows(dx, lddx, D, M, 2) || !good_groups(dw, lddw, dw_stride, V, D, G, es))
+        return COCOD_ERR_INVALID;
+    const VocabGrad grad{Matrix{dx, lddx, 0, 2}, Matrix{dw, lddw, dw_stride, es}};
+    return run_vocab(h, G, offsets, M, V, D, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, labels, row_weights, loss, row_loss, &grad,
+                     static_cast<char *>(workspace), workspace_bytes, (cudaStream_t)stream);
 }
 
 int cocod_grouped_wait_selftest(int wait_ms, int pair, cocod_stream_t stream)

@@ -1,0 +1,227 @@
+// Softmax cross-entropy over a large vocabulary: what is left besides the three products.
+//
+// With c_r the reference of row r (its label's own logit, l[r][t]), S_r = sum_{v != t} exp(l - c_r) and D_r = S_r + exp(l[r][t] - c_r):
+//     loss_r            = log D_r + c_r - l[r][t]            ( = log1p(S_r) for that reference)
+//     d loss_r / d l    = softmax - onehot = u[r][v] / D_r   with u = exp(l - c_r) for v != t and u[r][t] = -S_r
+// The row's factor rho_r = a_r / D_r (a_r: the row's share in the loss) is not needed before the sums are complete, and
+// it is one number per row: it is the epilogue's factor in dh = rho (u w), and goes into h in dw = u^T (rho h).  So the
+// exponentials are written once, next to the sums, and read by the two products as they are; no pass over them between.
+// The label's own entry is the one whose value hangs on the sums; this file's vocab_finish puts it in.
+// u in bf16 has 8 bits everywhere: -S_r is formed from the sum, not as a difference from one.  A row's largest entry of
+// softmax - onehot is as a rule its label's: the factor that goes into h is rho_r S_r / bf16(S_r), so that the label's term of dw
+// carries one rounding (of rho h) and not two; the factor of dh stays rho_r.
+// When loss_r > 50, exp(l - c_r) could leave bf16's range or rho_r fp32's: such a row is done again relative to its largest logit.
+#pragma once
+#include "cocod_grouped_sm100.cuh"
+
+namespace cocod {
+namespace lm {
+
+constexpr int FINISH_ROWS = 32, FINISH_WARPS = 16;
+using bf16_t = __nv_bfloat16;
+constexpr float SUM_LIMIT = 5.0e21f;         // about exp(50)
+
+struct VocabRows {
+    const int *offsets;                // [groups + 1]
+    int groups, total;                 // total: all rows
+    int vocab, width;
+    const int *labels;                 // [total], the caller's
+    const float *row_weight;           // [total] or nullptr: 1 / (rows of the group that have a label)
+    const __nv_bfloat16 *h;            // [total][ldh]
+    long long ldh;
+    const __nv_bfloat16 *w;            // [groups][vocab][ldw]
+    long long ldw, w_stride;
+    int *label;                        // [total]: negative where the row takes no part
+    float *own;                        // [total]: the label's logit
+    float *ref;                        // [total]: c_r
+    float *share;                      // [groups]: 1 / rows with a label
+    int *error_flag;
+};
+
+__device__ __forceinline__ int group_of(const int *offsets, int groups, int r)      // -1: in no group
+{
+    if (r < offsets[0] || r >= offsets[groups]) return -1;
+    int lo = 0, hi = groups;           // offsets[lo] <= r < offsets[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (offsets[mid] <= r) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// One warp per row: the label's logit.  The last `groups` blocks count the rows of a group that have a label.
+__global__ void __launch_bounds__(256)
+vocab_target(const VocabRows p, int row_blocks)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x >= row_blocks) {
+        const int g = blockIdx.x - row_blocks;
+        const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
+        __shared__ int part[8];
+        int n = 0;
+        for (int r = lo + threadIdx.x; r < hi; r += 256) {
+            const int t = p.labels[r];
+            n += t >= 0 && t < p.vocab && (p.row_weight == nullptr || p.row_weight[r] != 0.0f);
+        }
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) part[warp] = n;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int i = 1; i < 8; ++i) n += part[i];
+            p.share[g] = 1.0f / (float)max(n, 1);
+        }
+        return;
+    }
+    const long long r = (long long)blockIdx.x * 8 + warp;
+    if (r >= p.total) return;
+    const int g = group_of(p.offsets, p.groups, (int)r);
+    int t = p.labels[r];
+    if (t >= p.vocab) {
+        if (lane == 0 && p.error_flag != nullptr) atomicExch(p.error_flag, ERR_LABEL);
+        t = -1;
+    }
+    if (g < 0 || (p.row_weight != nullptr && p.row_weight[r] == 0.0f)) t = -1;
+    float s = 0.0f;
+    if (t >= 0) {
+        const uint4 *a = reinterpret_cast<const uint4 *>(p.h + r * p.ldh);
+        const uint4 *b = reinterpret_cast<const uint4 *>(p.w + g * p.w_stride + t * p.ldw);
+#pragma unroll 4
+        for (int i = lane; i < p.width / 8; i += 32) {
+            const uint4 x = a[i], y = b[i];
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s = fmaf(__uint_as_float(xs[j] << 16), __uint_as_float(ys[j] << 16), s);
+                s = fmaf(__uint_as_float(xs[j] & 0xffff0000u), __uint_as_float(ys[j] & 0xffff0000u), s);
+            }
+        }
+    }
+    s = warp_sum(s);
+    if (lane == 0) {
+        p.label[r] = t < 0 ? -1 : t;
+        p.own[r] = s;
+        p.ref[r] = s;
+    }
+}
+
+struct FinishParams {
+    VocabRows v;
+    int row0, rows;                    // of this launch; u, sums, rho, redo and hs start at row0
+    const float2 *sums;
+    int n_sums, ld_sums;
+    float *row_loss;                   // [total]
+    float *rho;                        // [rows], nullptr: the loss alone is wanted
+    __nv_bfloat16 *u;                  // [rows][ldu]
+    long long ldu;
+    __nv_bfloat16 *hs;                 // [rows][width]: rho h
+    int *redo, *redo_any;              // first pass: set; second pass: nothing is done if *redo_any is 0
+    int second;
+};
+
+// 32 rows per CTA: their sums, losses and factors, the label's entry of u, and rho h.
+__global__ void __launch_bounds__(32 * FINISH_WARPS)
+vocab_finish(const FinishParams p)
+{
+    __shared__ float2 part[FINISH_WARPS][FINISH_ROWS];
+    __shared__ float factor[FINISH_ROWS];
+    pdl_launch_dependents();
+    pdl_wait();
+    if (p.second && *p.redo_any == 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int first = blockIdx.x * FINISH_ROWS, row = first + lane;        // counted from row0
+    float s = 0.0f, most = __uint_as_float(0xff800000u);
+    if (row < p.rows) {
+#pragma unroll 4
+        for (int i = warp; i < p.n_sums; i += FINISH_WARPS) {
+            const float2 v = p.sums[(long long)i * p.ld_sums + row];
+            s += v.x;
+            most = fmaxf(most, v.y);
+        }
+    }
+    part[warp][lane] = make_float2(s, most);
+    __syncthreads();
+    if (warp == 0) {
+        float rho = 0.0f, scale = 0.0f;
+        int again = 0;
+        if (row < p.rows) {
+            const int r = p.row0 + row, t = p.v.label[r];
+            float loss = 0.0f;
+            if (t >= 0) {
+                for (int i = 1; i < FINISH_WARPS; ++i) {
+                    s += part[i][lane].x;
+                    most = fmaxf(most, part[i][lane].y);
+                }
+                const float own = p.v.own[r], ref = p.v.ref[r];
+                const float et = own == ref ? 1.0f : expf(own - ref);
+                loss = own == ref ? log1pf(s) : logf(s + et) + (ref - own);
+                if (!p.second && !(s <= SUM_LIMIT)) {
+                    again = 1;
+                    p.v.ref[r] = most;
+                    *p.redo_any = 1;
+                }
+                if (p.rho != nullptr) {
+                    const float a = p.v.row_weight != nullptr ? p.v.row_weight[r] : p.v.share[group_of(p.v.offsets, p.v.groups, r)];
+                    rho = a / (s + et);
+                    const bf16_t entry = __float2bfloat16_rn(-s);
+                    const float kept = -__bfloat162float(entry);
+                    p.u[row * p.ldu + t] = entry;
+                    scale = kept > 0.0f && kept <= 3.0e38f ? rho * (s / kept) : rho;
+                }
+            }
+            p.row_loss[r] = loss;
+            if (!p.second) p.redo[row] = again;
+            if (p.rho != nullptr) p.rho[row] = rho;
+        }
+        factor[lane] = scale;
+    }
+    if (p.rho == nullptr) return;
+    __syncthreads();
+    const int vecs = p.v.width / 8, rows = min(FINISH_ROWS, p.rows - first);
+    for (int i = threadIdx.x; i < rows * vecs; i += 32 * FINISH_WARPS) {
+        const int rr = i / vecs, c = i - rr * vecs;
+        const float f = factor[rr];
+        uint4 o = make_uint4(0, 0, 0, 0);
+        if (f != 0.0f) {               // (a row that takes no part is 0 whatever it holds)
+            const uint4 x = reinterpret_cast<const uint4 *>(p.v.h + (long long)(p.row0 + first + rr) * p.v.ldh)[c];
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+            uint32_t os[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) os[j] = pack_bf16x2(__uint_as_float(xs[j] << 16) * f, __uint_as_float(xs[j] & 0xffff0000u) * f);
+            o = make_uint4(os[0], os[1], os[2], os[3]);
+        }
+        reinterpret_cast<uint4 *>(p.hs + (long long)(first + rr) * p.v.width)[c] = o;
+    }
+}
+
+// loss[g] = sum of the rows' losses with their shares; one block per group, sums in a fixed order.
+__global__ void __launch_bounds__(256)
+vocab_mean(const VocabRows p, const float *row_loss, float *loss)
+{
+    __shared__ float part[8];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int g = blockIdx.x;
+    const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
+    float s = 0.0f;
+    for (int r = lo + threadIdx.x; r < hi; r += 256)
+        if (p.label[r] >= 0) s += p.row_weight != nullptr ? p.row_weight[r] * row_loss[r] : row_loss[r];
+    s = warp_sum(s);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) s += part[i];
+        loss[g] = p.row_weight != nullptr ? s : s * p.share[g];
+    }
+}
+
+}  // namespace lm
+}  // namespace cocod

@@ -9,6 +9,7 @@ device memory and streams.  No CPU fallback.
     dw = ops.grouped_weight_grad(dy, x, offsets)         # x: a tensor or the PackedActivations of one
     kept = ops.act_pack(x)                               # 8 bits per value until the backward pass
     dz = ops.act_relu_grad(dh, kept)                     # dh where the kept activation is positive
+    loss, row_loss, dx, dw = ops.vocab_loss_grad(x, w, labels, offsets)
 """
 from __future__ import annotations
 
@@ -56,7 +57,10 @@ class PackedActivations:
 class LMOps:
     """The operators, with the scratch their kernels share: order the calls of one object (one stream, or events)."""
 
-    def __init__(self):
+    def __init__(self, workspace_limit: int = 2 << 30):
+        """workspace_limit: bytes that a call of the vocabulary operators may take for what it keeps of the rows it works on
+        at a time (a longer batch is worked on in several passes)."""
+        self.workspace_limit = int(workspace_limit)
         if not torch.cuda.is_available():
             raise RuntimeError("the language-model operators need a CUDA device (there is no CPU fallback)")
         self._lib = _E.load()
@@ -208,6 +212,48 @@ class LMOps:
         zp, lddz = self._rows(out, "out", M, k, align=0)
         self._call("cocod_act_relu_grad", M, k, dp, lddh, qp, ldq, zp, lddz)
         return out
+
+    # ------------------------------------------------------------------------------------------ vocabulary
+    def _vector(self, t, name, n, dtype):
+        if t.dim() != 1 or t.dtype is not dtype or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device.type != "cuda" \
+                or t.device.index != self._device:
+            raise ValueError(f"{name}: need {n} contiguous {dtype} on cuda:{self._device}")
+        return t.data_ptr()
+
+    def _vocab(self, x, w, labels, offsets, row_weights):
+        G, V, D = w.shape
+        M = x.shape[0]
+        xp, ldx = self._rows(x, "x", cols=D)
+        wp, ldw, gs = self._groups(w, "w")
+        wt = None if row_weights is None else self._vector(row_weights, "row_weights", M, torch.float32)
+        loss = torch.empty(G, dtype=torch.float32, device=x.device)
+        row_loss = torch.empty(M, dtype=torch.float32, device=x.device)
+        return loss, row_loss, (G, self._offsets(offsets, G), M, V, D, xp, ldx, wp, ldw, gs, self._vector(labels, "labels", M, torch.int32), wt,
+                                loss.data_ptr(), row_loss.data_ptr())
+
+    def vocab_loss(self, x, w, labels, offsets, row_weights=None):
+        """(loss of each group, loss of each row) of softmax cross-entropy with logits x w[g]^T.  x: M x D bf16, w: G x V x D bf16,
+        labels: M int32, negative for rows that take no part; the mean over a group's other rows, or the sum weighted by
+        row_weights (M float32)."""
+        loss, row_loss, args = self._vocab(x, w, labels, offsets, row_weights)
+        G, _, M, V, D = args[:5]
+        ws = self._scratch(self._lib.cocod_vocab_workspace(G, M, V, D, 0, BF16, self.workspace_limit))
+        self._call("cocod_vocab_loss", *args, ws.data_ptr(), ws.numel())
+        return loss, row_loss
+
+    def vocab_loss_grad(self, x, w, labels, offsets, row_weights=None, dw=None, dw_dtype=None):
+        """(loss, row_loss, dx, dw): vocab_loss and the gradients of the groups' losses.  dw: G x V x D, bf16 (as w) or float32, for
+        example a view of the K x P gradients that Engine.local_step takes."""
+        dtype = self._type(dw, dw_dtype or (None if dw is not None else torch.bfloat16))
+        loss, row_loss, args = self._vocab(x, w, labels, offsets, row_weights)
+        G, _, M, V, D = args[:5]
+        dx = torch.empty((M, D), dtype=torch.bfloat16, device=x.device)
+        if dw is None:
+            dw = torch.empty((G, V, D), dtype=dtype, device=x.device)
+        dp, lddw, gs = self._groups(dw, "dw", (G, V, D), dtype)
+        ws = self._scratch(self._lib.cocod_vocab_workspace(G, M, V, D, 1, _TYPES[dtype], self.workspace_limit))
+        self._call("cocod_vocab_loss_grad", *args, dx.data_ptr(), D, dp, lddw, gs, _TYPES[dtype], ws.data_ptr(), ws.numel())
+        return loss, row_loss, dx, dw
 
     # ------------------------------------------------------------------------------------------ the rest
     def check(self):
