@@ -16,6 +16,11 @@
 //   * An epilogue warp owns 32 rows of its CTA's tile and half of the columns, stages them in shared memory of its own
 //     (4 KB, TMA swizzle) and hands them to the store engine; rows behind the end of a group are some other group's, so a
 //     warp whose rows end inside a group's last tile stores the valid ones itself.
+// The tensor cores cut the accumulator's last bits off with every step they add: the sum of 2048 products came out 2.1e-6 too
+// small, four times fp32's rounding error, and the loss grows with the length.  Where the result leaves as fp32, a reduction
+// is therefore cut into parts of 512: each goes to the other accumulator, and the epilogue adds it, rounding to nearest, to
+// sums that it holds in registers (half a tile row per thread; the epilogue warps take the registers that the others give
+// up).  A bf16 result does not show the difference.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
 // with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
 // Every wait is bounded, as in cocod_gemm_sm100.cuh.
@@ -28,9 +33,10 @@ namespace lm {
 using namespace cocod::gemm;
 
 constexpr int EPI_WARPS = 8, GROUPED_THREADS = 128 + 32 * EPI_WARPS;
-constexpr int RING = 6;                                             // stages of 32 KB
-constexpr int OUT_BYTES = 4096;                                     // staging of an epilogue warp: 32 rows of 128 bytes
+constexpr int RING = 5;                                             // stages of 32 KB
+constexpr int OUT_BYTES = 2 * 4096;                                 // staging of an epilogue warp: twice 32 rows of 128 bytes
 constexpr int GROUPED_SMEM = RING * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 512;
+constexpr int PART_BLOCKS = 8;                                      // fp32 results: blocks of 64 summed by the tensor cores at a time
 constexpr int ERR_OFFSETS = 100;                                    // error_flag: the offsets do not rise from 0 to the number of rows
 constexpr int ERR_LABEL = 101;                                      // error_flag: a label beyond the vocabulary
 
@@ -42,6 +48,7 @@ enum Out {
     OUT_VOCAB = 3,         // u[r][v] = exp(l - c_r) in bf16, 0 at v = t_r, and for each half of a tile sum_v u (in fp32) and max_v l, v != t_r
     OUT_VOCAB_SUMS = 4,    // only the sums and maxima
 };
+__host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32; }
 __host__ __device__ constexpr bool is_vocab(int out) { return out == OUT_VOCAB || out == OUT_VOCAB_SUMS; }
 
 struct GroupedParams {
@@ -144,6 +151,9 @@ template <int CG> __device__ __forceinline__ void umma_commit_g(uint32_t bar)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                      ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
+// Registers per thread from here on, for all warps of a warpgroup.  The launch holds 384 x 168 = 64512 of them: 128 x 40 + 256 x 232.
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int CG> __device__ __forceinline__ uint32_t cta_rank()
 {
     if (CG == 1) return 0;
@@ -322,195 +332,242 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const int first = is_vocab(OUT) && p.redo != nullptr && *p.redo_any == 0 ? 0x7fffffff : cluster;
 
     int failed = 0;
-    if (warp == 0) {
-        // ---- producer
-        Walker<TM, TN, WG> walk(p, lane);
-        if (blockIdx.x == 0 && p.error_flag != nullptr) {
-            bool bad = false;
-            for (int g = lane; g < p.groups; g += 32)
-                bad |= p.offsets[g + 1] < p.offsets[g] || (g == 0 && p.offsets[0] != 0) || (g == p.groups - 1 && p.offsets[p.groups] != p.total_rows);
-            if (bad) atomicExch(p.error_flag, ERR_OFFSETS);
-        }
-        Tile t;
-        unsigned it = 0;
-        int last_g = -1;
-        for (int i = first; walk.find(i, t); i += clusters) {
-            if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
-            if (lane == 0 && !p.debug_no_loads) {
-                const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
-                if (WG && t.g != last_g) {
-                    acquire_map(ma);
-                    acquire_map(mb);
-                    last_g = t.g;
-                }
-                const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
-                for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-                    const unsigned s = it % RING, use = it / RING;
-                    if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
-                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * STAGE_BYTES);
-                    const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
-                    const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
-                    if (A_MN) {
-                        load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
-                        load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
-                    } else {
-                        load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
-                    }
-                    if (B_MN) {
-                        load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
-                        load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
-                    } else {
-                        load_tile<CG>(db, mb, bar, kb * BK, n0, zb);
-                    }
-                }
-            }
-            if (__any_sync(0xffffffffu, failed)) break;
-        }
-    } else if (warp == 1 && rank == 0) {
-        // ---- issuer of the products
-        constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B_MN>();
-        constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B_MN ? 2048u : 32u;
-        Walker<TM, TN, WG> walk(p, lane);
-        Tile t;
-        unsigned it = 0, ai = 0;
-        for (int i = first; walk.find(i, t); i += clusters) {
-            if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
-            if (t.kb0 == t.kb1) continue;
-            if (lane == 0) {
-                const unsigned a = ai & 1, use = ai >> 1;
-                if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) failed = 2;
-                tc_fence_after();
-                for (int kb = t.kb0; kb < t.kb1 && !failed; ++kb, ++it) {
-                    const unsigned s = it % RING;
-                    if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
-                    tc_fence_after();
-                    const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
-#pragma unroll
-                    for (int k = 0; k < BK / UMMA_K; ++k)
-                        umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B_MN), idesc,
-                                   (kb > t.kb0 || k > 0) ? 1u : 0u);
-                    umma_commit_g<CG>(empty0 + 8 * s);
-                }
-                if (!failed) umma_commit_g<CG>(accf0 + 8 * a);
-            }
-            ++ai;
-            if (__any_sync(0xffffffffu, failed)) break;
-        }
-    } else if (warp >= 4) {
+    if (warp >= 4) {
+        if (is_f32(OUT)) take_registers<232>();
         // ---- epilogue: rows 32 (warp % 4) .. + 31 of the CTA's 128, columns of one half of the tile
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        uint8_t *stage = outs + (warp - 4) * OUT_BYTES;
+        uint8_t *staging = outs + (warp - 4) * OUT_BYTES;
+        constexpr int HALF = TN / 2, CHUNK = is_f32(OUT) ? 32 : 64, CHUNKS = HALF / CHUNK;      // a chunk: 128 bytes of a row
+        constexpr int ES = is_f32(OUT) ? 4 : 2, PER = 16 / ES;
         Walker<TM, TN, WG> walk(p, lane);
-        Tile t;
-        unsigned ai = 0;
+        Tile t{};
+        unsigned ai = 0, stores = 0;
+        // The staging is used in turns: a thread that writes one of the two buffers has seen the store before last read.
+        auto stage_and_store = [&](const uint32_t (&r)[CHUNK], int col, int m, int valid, int z) {
+            uint8_t *stage = staging + (stores++ & 1) * 4096;
+            if (lane == 0) tma_store_wait_read<1>();
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint4 v;
+                if (is_f32(OUT)) {
+                    const int b = j * 4;
+                    v = make_uint4(r[b], r[b + 1], r[b + 2], r[b + 3]);
+                } else {
+                    const int b = j * 8 < CHUNK ? j * 8 : 0;
+                    v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
+                                   pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
+                }
+                *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = v;
+            }
+            if (WG || valid >= 32) {
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(stage), col, m, z);
+                    else tma_store_3d(&map_out, smem_u32(stage), col, m, z);
+                }
+            } else {
+                __syncwarp();
+                uint8_t *dst = static_cast<uint8_t *>(p.out) + (t.split * p.split_stride + (long long)m * p.ld_out + col) * ES;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const int row = q * 4 + (lane >> 3), piece = lane & 7;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ (row & 7)) << 4));
+                    if (row < valid && col + piece * PER < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + piece * 16) = v;
+                }
+                __syncwarp();
+            }
+            if (lane == 0) tma_store_commit();
+        };
+        auto release = [&](unsigned a) {          // this warp has read the accumulator
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 1) mbar_arrive_local(acce0 + 8 * a);
+                else mbar_arrive_cluster(map_to_rank(acce0 + 8 * a, 0));
+            }
+        };
         for (int i = first; walk.find(i, t); i += clusters) {
             if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
-            const bool any = t.kb0 < t.kb1;
-            const unsigned a = ai & 1;
-            if (any) {
-                const bool ok = mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2);
-                if (!__all_sync(0xffffffffu, ok)) { failed = 3; break; }
-                tc_fence_after();
-                ++ai;
-            }
             const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
             const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
             const int z = WG ? t.split * p.groups + t.g : t.split;
-            const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + a * TN + half * (TN / 2);
+            const int col0 = t.n0 + half * HALF;
+            const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * HALF;
             float scale = 1.0f;
             if (!WG && p.row_scale != nullptr && lane < valid) scale = p.row_scale[m + lane];
-            constexpr bool HALF_WORDS = OUT == OUT_BF16 || is_vocab(OUT);
-            constexpr int CHUNK = HALF_WORDS ? 64 : 32;                      // 128 bytes of a row
-            float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
-            int label = -1;
-            if (is_vocab(OUT) && lane < valid) {
-                label = p.label[m + lane];
-                if (label >= 0) ref = p.ref[m + lane];
-            }
-#pragma unroll 1
-            for (int c = 0; c < TN / 2; c += CHUNK) {
-                uint32_t r[CHUNK];
+            auto scaled = [&](uint32_t x) { return scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(x) * scale); };
+            if constexpr (is_f32(OUT)) {
+                uint32_t acc[CHUNKS][32];
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) acc[c][j] = 0u;
+                for (int k0 = t.kb0; k0 < t.kb1; k0 += PART_BLOCKS, ++ai) {
+                    const unsigned a = ai & 1;
+                    if (!__all_sync(0xffffffffu, mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2))) { failed = 3; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        uint32_t r[32];
+                        tmem_ld32(tacc + a * TN + c * 32, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[c][j] = __float_as_uint(__uint_as_float(acc[c][j]) + __uint_as_float(r[j]));
+                    }
+                    release(a);
+                }
+                if (failed) break;
+                if (valid <= 0 || (OUT == OUT_ADD_F32 && t.kb0 == t.kb1)) continue;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    if (col0 + c * 32 >= p.n) continue;
+                    if (!WG && p.row_scale != nullptr) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[c][j] = scaled(acc[c][j]);
+                    }
+                    stage_and_store(acc[c], col0 + c * 32, m, valid, z);
+                }
+            } else {
+                const bool any = t.kb0 < t.kb1;
+                const unsigned a = ai & 1;
                 if (any) {
-                    tmem_ld32(tacc + c, *reinterpret_cast<uint32_t (*)[32]>(r));
-                    if (CHUNK == 64) tmem_ld32(tacc + c + 32, *reinterpret_cast<uint32_t (*)[32]>(r + CHUNK - 32));
-                    tmem_ld_wait();
-                    if (c + CHUNK == TN / 2) {            // the accumulator may be overwritten
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (CG == 1) mbar_arrive_local(acce0 + 8 * a);
-                            else mbar_arrive_cluster(map_to_rank(acce0 + 8 * a, 0));
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < CHUNK; ++j) r[j] = 0u;
+                    if (!__all_sync(0xffffffffu, mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2))) { failed = 3; break; }
+                    tc_fence_after();
+                    ++ai;
                 }
-                const int col = t.n0 + half * (TN / 2) + c;
-                if (valid <= 0 || col >= p.n || (OUT == OUT_ADD_F32 && !any)) continue;
-                if (is_vocab(OUT)) {
-                    // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
-                    const int end = label < 0 ? 0 : p.n - col, at = label - col;
-                    if (__any_sync(0xffffffffu, end < CHUNK || (at >= 0 && at < CHUNK))) {
-#pragma unroll
-                        for (int j = 0; j < CHUNK; ++j) if (j >= end || j == at) r[j] = 0xff800000u;
-                    }
-                    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < CHUNK; ++j) {
-                        const float l = __uint_as_float(r[j]);
-                        most = fmaxf(most, l);
-                        const float e = exp2_approx((l - ref) * 1.4426950408889634f);
-                        s4[j & 3] += e;
-                        r[j] = __float_as_uint(e);
-                    }
-                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                    if (c + CHUNK == TN / 2 || col + CHUNK >= p.n) {          // the last columns of this half
-                        if (lane < valid) p.sums[(long long)(t.n0 / (TN / 2) + half) * p.ld_sums + m + lane] = make_float2(sum, most);
-                    }
-                    if (OUT == OUT_VOCAB_SUMS) continue;
+                float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
+                int label = -1;
+                if (is_vocab(OUT) && lane < valid) {
+                    label = p.label[m + lane];
+                    if (label >= 0) ref = p.ref[m + lane];
                 }
-                if (!WG && p.row_scale != nullptr) {
-#pragma unroll
-                    for (int j = 0; j < CHUNK; ++j) r[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(r[j]) * scale);
-                }
-                if (lane == 0) tma_store_wait_read<0>();     // the last store has read the staging
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint4 v;
-                    if (HALF_WORDS) {
-                        const int b = j * 8 < CHUNK ? j * 8 : 0;
-                        v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
-                                       pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
+#pragma unroll 1
+                for (int c = 0; c < CHUNKS; ++c) {
+                    uint32_t r[CHUNK];
+                    if (any) {
+                        tmem_ld32(tacc + a * TN + c * CHUNK, *reinterpret_cast<uint32_t (*)[32]>(r));
+                        tmem_ld32(tacc + a * TN + c * CHUNK + 32, *reinterpret_cast<uint32_t (*)[32]>(r + CHUNK - 32));
+                        tmem_ld_wait();
+                        if (c == CHUNKS - 1) release(a);
                     } else {
-                        v = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
-                    }
-                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = v;
-                }
-                if (WG || valid >= 32) {
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(stage), col, m, z);
-                        else tma_store_3d(&map_out, smem_u32(stage), col, m, z);
-                        tma_store_commit();
-                    }
-                } else {
-                    __syncwarp();
-                    constexpr int ES = HALF_WORDS ? 2 : 4, PER = 16 / ES;
-                    uint8_t *dst = static_cast<uint8_t *>(p.out) + (t.split * p.split_stride + (long long)m * p.ld_out + col) * ES;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const int row = q * 4 + (lane >> 3), piece = lane & 7;
-                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ (row & 7)) << 4));
-                        if (row < valid && col + piece * PER < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + piece * 16) = v;
+                        for (int j = 0; j < CHUNK; ++j) r[j] = 0u;
                     }
-                    __syncwarp();
+                    const int col = col0 + c * CHUNK;
+                    if (valid <= 0 || col >= p.n) continue;
+                    if (is_vocab(OUT)) {
+                        // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
+                        const int end = label < 0 ? 0 : p.n - col, at = label - col;
+                        if (__any_sync(0xffffffffu, end < CHUNK || (at >= 0 && at < CHUNK))) {
+#pragma unroll
+                            for (int j = 0; j < CHUNK; ++j) if (j >= end || j == at) r[j] = 0xff800000u;
+                        }
+                        float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int j = 0; j < CHUNK; ++j) {
+                            const float l = __uint_as_float(r[j]);
+                            most = fmaxf(most, l);
+                            const float e = exp2_approx((l - ref) * 1.4426950408889634f);
+                            s4[j & 3] += e;
+                            r[j] = __float_as_uint(e);
+                        }
+                        sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                        if (c == CHUNKS - 1 || col + CHUNK >= p.n) {          // the last columns of this half
+                            if (lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
+                        }
+                        if (OUT == OUT_VOCAB_SUMS) continue;
+                    } else if (!WG && p.row_scale != nullptr) {
+#pragma unroll
+                        for (int j = 0; j < CHUNK; ++j) r[j] = scaled(r[j]);
+                    }
+                    stage_and_store(r, col, m, valid, z);
                 }
             }
         }
         if (lane == 0) tma_store_wait_read<0>();
+    } else {
+        if (is_f32(OUT)) give_registers<40>();
+        if (warp == 0) {
+            // ---- producer
+            Walker<TM, TN, WG> walk(p, lane);
+            if (blockIdx.x == 0 && p.error_flag != nullptr) {
+                bool bad = false;
+                for (int g = lane; g < p.groups; g += 32)
+                    bad |= p.offsets[g + 1] < p.offsets[g] || (g == 0 && p.offsets[0] != 0) || (g == p.groups - 1 && p.offsets[p.groups] != p.total_rows);
+                if (bad) atomicExch(p.error_flag, ERR_OFFSETS);
+            }
+            Tile t;
+            unsigned it = 0;
+            int last_g = -1;
+            for (int i = first; walk.find(i, t); i += clusters) {
+                if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
+                if (lane == 0 && !p.debug_no_loads) {
+                    const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
+                    if (WG && t.g != last_g) {
+                        acquire_map(ma);
+                        acquire_map(mb);
+                        last_g = t.g;
+                    }
+                    const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
+                    for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+                        const unsigned s = it % RING, use = it / RING;
+                        if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
+                        if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * STAGE_BYTES);
+                        const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
+                        const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+                        if (A_MN) {
+                            load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
+                            load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
+                        } else {
+                            load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
+                        }
+                        if (B_MN) {
+                            load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
+                            load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
+                        } else {
+                            load_tile<CG>(db, mb, bar, kb * BK, n0, zb);
+                        }
+                    }
+                }
+                if (__any_sync(0xffffffffu, failed)) break;
+            }
+        } else if (warp == 1 && rank == 0) {
+            // ---- issuer of the products
+            constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B_MN>();
+            constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B_MN ? 2048u : 32u;
+            Walker<TM, TN, WG> walk(p, lane);
+            Tile t;
+            unsigned it = 0, ai = 0;
+            for (int i = first; walk.find(i, t); i += clusters) {
+                if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
+                if (t.kb0 == t.kb1) continue;
+                if (lane == 0) {
+                    for (int k0 = t.kb0; k0 < t.kb1 && !failed; ++ai) {
+                        const int k1 = is_f32(OUT) ? min(k0 + PART_BLOCKS, t.kb1) : t.kb1;
+                        const unsigned a = ai & 1, use = ai >> 1;
+                        if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) { failed = 2; break; }
+                        tc_fence_after();
+                        for (int kb = k0; kb < k1; ++kb, ++it) {
+                            const unsigned s = it % RING;
+                            if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
+                            tc_fence_after();
+                            const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+#pragma unroll
+                            for (int k = 0; k < BK / UMMA_K; ++k)
+                                umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B_MN), idesc,
+                                           (kb > k0 || k > 0) ? 1u : 0u);
+                            umma_commit_g<CG>(empty0 + 8 * s);
+                        }
+                        if (failed) break;
+                        umma_commit_g<CG>(accf0 + 8 * a);
+                        k0 = k1;
+                    }
+                }
+                if (__any_sync(0xffffffffu, failed)) break;
+            }
+        }
     }
     if (failed) {
         *abort = 1;

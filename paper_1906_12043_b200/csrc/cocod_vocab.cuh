@@ -140,7 +140,7 @@ vocab_finish(const FinishParams p)
     const int first = blockIdx.x * FINISH_ROWS, row = first + lane;        // counted from row0
     float s = 0.0f, most = __uint_as_float(0xff800000u);
     if (row < p.rows) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = warp; i < p.n_sums; i += FINISH_WARPS) {
             const float2 v = p.sums[(long long)i * p.ld_sums + row];
             s += v.x;
