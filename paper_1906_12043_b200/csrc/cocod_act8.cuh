@@ -68,31 +68,48 @@ act_pack(const __nv_bfloat16 *x, long long ldx, int8_t *q, long long ldq, uint8_
     const long long c = (long long)blockIdx.y * ACT_BLOCK + (threadIdx.x & 7) * 16;
     uint32_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (m < M) load16(x + m * ldx, c, k, vec, v);
-    uint32_t amax = 0;                  // bf16 magnitudes compare like whole numbers
+    uint32_t amax2 = 0;                 // bf16 magnitudes compare like whole numbers, two at a time
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t lo = v[j] & 0x7fff, hi = v[j] >> 16 & 0x7fff;
-        amax = max(amax, max(lo < 0x7f80 ? lo : 0, hi < 0x7f80 ? hi : 0));
+    for (int j = 0; j < 8; ++j) amax2 = __vmaxu2(amax2, v[j] & 0x7fff7fffu);
+    uint32_t amax = max(amax2 & 0xffff, amax2 >> 16);
+    const bool plain = amax < 0x7f80;   // none of this thread's values is infinite or NaN
+    if (!plain) {
+        amax = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t lo = v[j] & 0x7fff, hi = v[j] >> 16 & 0x7fff;
+            amax = max(amax, max(lo < 0x7f80 ? lo : 0, hi < 0x7f80 ? hi : 0));
+        }
     }
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     const int biased = block_exponent(amax);
-    // 1 / 2^e is exact down to e = -126 and up to the largest e, 122.  There the largest values would round up to 2^128,
-    // which bf16 does not hold: they stop at 63 units.
-    const float inv = power_of_two(254 - biased), most = biased == 122 + 127 ? 63.0f : 127.0f;
+    const float inv = power_of_two(254 - biased);       // 2^-e: exact from e = -126 up to the largest e, 122
+    // With |y| = |x| 2^-e <= 127, y + 1.5 2^23 rounds y to a whole number, half to even, and holds it in its low byte; |y| below
+    // 3/4 counts as 3/4, which rounds to 1, unless it is 0.
     uint32_t packed[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        packed[j] = 0;
+        uint32_t b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t bits = (v[2 * j + (i >> 1)] >> (16 * (i & 1))) & 0xffff;
-            const float a = __uint_as_float(bits << 16);
-            float r = fminf(rintf(fabsf(a) * inv), most);
-            if (a != 0.0f) r = fmaxf(r, 1.0f);
-            int b = a < 0.0f ? -(int)r : (int)r;
-            if ((bits & 0x7fff) >= 0x7f80) b = -128;
-            packed[j] |= ((uint32_t)b & 0xff) << (8 * i);
+            const uint32_t w = v[2 * j + (i >> 1)];
+            const float a = __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+            const float y = copysignf(fmaxf(fabsf(a * inv), 0.75f), a);
+            b[i] = a == 0.0f ? 0u : __float_as_uint(y + 12582912.0f);
+        }
+        packed[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    }
+    if (!plain || biased == 122 + 127) {
+        // The rare cases, value by value: the marker; and, where e is 122, the largest values would round up to 2^128, which bf16
+        // does not hold: they stop at 63 units.
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t bits = (v[j >> 1] >> (16 * (j & 1))) & 0xffff;
+            int n = (int8_t)(packed[j >> 2] >> (8 * (j & 3)));
+            if (biased == 122 + 127) n = min(max(n, -63), 63);
+            if ((bits & 0x7fff) >= 0x7f80) n = -128;
+            packed[j >> 2] = (packed[j >> 2] & ~(0xffu << (8 * (j & 3)))) | ((uint32_t)n & 0xff) << (8 * (j & 3));
         }
     }
     if (m < M && c < k) *reinterpret_cast<uint4 *>(q + m * ldq + c) = make_uint4(packed[0], packed[1], packed[2], packed[3]);

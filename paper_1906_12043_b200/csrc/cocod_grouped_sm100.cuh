@@ -18,9 +18,11 @@
 //     warp whose rows end inside a group's last tile stores the valid ones itself.
 // The tensor cores cut the accumulator's last bits off with every step they add: the sum of 2048 products came out 2.1e-6 too
 // small, four times fp32's rounding error, and the loss grows with the length.  Where the result leaves as fp32, a reduction
-// is therefore cut into parts of 512: each goes to the other accumulator, and the epilogue adds it, rounding to nearest, to
-// sums that it holds in registers (half a tile row per thread; the epilogue warps take the registers that the others give
-// up).  A bf16 result does not show the difference.
+// is therefore cut into parts of 768 (logits: 2048): each goes to the other accumulator, and the epilogue adds it, rounding to
+// nearest, to sums that it holds in registers (half a tile row per thread; the epilogue warps take the registers that the
+// others give up).  8192 x 8192 x 8192 in fp32: 774 us without, 788 in parts of 1024, 823 in parts of 512 (the epilogue's
+// reads of tensor memory hold the products up for about 400 clocks a part); error 7e-7 at 768, 1.0e-6 at 1024.  A bf16 result does not show
+// the difference.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
 // with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
 // Every wait is bounded, as in cocod_gemm_sm100.cuh.
@@ -36,7 +38,6 @@ constexpr int EPI_WARPS = 8, GROUPED_THREADS = 128 + 32 * EPI_WARPS;
 constexpr int RING = 5;                                             // stages of 32 KB
 constexpr int OUT_BYTES = 2 * 4096;                                 // staging of an epilogue warp: twice 32 rows of 128 bytes
 constexpr int GROUPED_SMEM = RING * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 512;
-constexpr int PART_BLOCKS = 8;                                      // fp32 results: blocks of 64 summed by the tensor cores at a time
 constexpr int ERR_OFFSETS = 100;                                    // error_flag: the offsets do not rise from 0 to the number of rows
 constexpr int ERR_LABEL = 101;                                      // error_flag: a label beyond the vocabulary
 
@@ -50,6 +51,8 @@ enum Out {
 };
 __host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32; }
 __host__ __device__ constexpr bool is_vocab(int out) { return out == OUT_VOCAB || out == OUT_VOCAB_SUMS; }
+// Blocks of 64 that the tensor cores sum at a time.
+__host__ __device__ constexpr int part_blocks(int out) { return is_f32(out) ? 12 : is_vocab(out) ? 32 : 1 << 24; }
 
 struct GroupedParams {
     const int *offsets;                // [groups + 1], device
@@ -151,7 +154,7 @@ template <int CG> __device__ __forceinline__ void umma_commit_g(uint32_t bar)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                      ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// Registers per thread from here on, for all warps of a warpgroup.  The launch holds 384 x 168 = 64512 of them: 128 x 40 + 256 x 232.
+// Registers per thread from here on, for all warps of a warpgroup.  The launch holds 384 x 168 = 64512 of them: 128 x 56 + 256 x 224.
 template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int CG> __device__ __forceinline__ uint32_t cta_rank()
@@ -333,7 +336,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 
     int failed = 0;
     if (warp >= 4) {
-        if (is_f32(OUT)) take_registers<232>();
+        take_registers<224>();
         // ---- epilogue: rows 32 (warp % 4) .. + 31 of the CTA's 128, columns of one half of the tile
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         uint8_t *staging = outs + (warp - 4) * OUT_BYTES;
@@ -397,98 +400,75 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * HALF;
             float scale = 1.0f;
             if (!WG && p.row_scale != nullptr && lane < valid) scale = p.row_scale[m + lane];
-            auto scaled = [&](uint32_t x) { return scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(x) * scale); };
-            if constexpr (is_f32(OUT)) {
-                uint32_t acc[CHUNKS][32];
+            uint32_t acc[CHUNKS][CHUNK];
+            for (int k0 = t.kb0; k0 < t.kb1; k0 += part_blocks(OUT), ++ai) {
+                const unsigned a = ai & 1;
+                if (!__all_sync(0xffffffffu, mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2))) { failed = 3; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < HALF; c += 32) {
+                    uint32_t(&sum)[32] = *reinterpret_cast<uint32_t (*)[32]>(&acc[c / CHUNK][c % CHUNK]);
+                    if (k0 == t.kb0) {
+                        tmem_ld32(tacc + a * TN + c, sum);
+                    } else {
+                        uint32_t r[32];
+                        tmem_ld32(tacc + a * TN + c, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(r[j]));
+                    }
+                }
+                tmem_ld_wait();
+                release(a);
+            }
+            if (failed) break;
+            if (valid <= 0 || (OUT == OUT_ADD_F32 && t.kb0 == t.kb1)) continue;
+            if (t.kb0 == t.kb1) {
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) acc[c][j] = 0u;
-                for (int k0 = t.kb0; k0 < t.kb1; k0 += PART_BLOCKS, ++ai) {
-                    const unsigned a = ai & 1;
-                    if (!__all_sync(0xffffffffu, mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2))) { failed = 3; break; }
-                    tc_fence_after();
-#pragma unroll
-                    for (int c = 0; c < CHUNKS; ++c) {
-                        uint32_t r[32];
-                        tmem_ld32(tacc + a * TN + c * 32, r);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[c][j] = __float_as_uint(__uint_as_float(acc[c][j]) + __uint_as_float(r[j]));
-                    }
-                    release(a);
-                }
-                if (failed) break;
-                if (valid <= 0 || (OUT == OUT_ADD_F32 && t.kb0 == t.kb1)) continue;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) {
-                    if (col0 + c * 32 >= p.n) continue;
-                    if (!WG && p.row_scale != nullptr) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[c][j] = scaled(acc[c][j]);
-                    }
-                    stage_and_store(acc[c], col0 + c * 32, m, valid, z);
-                }
-            } else {
-                const bool any = t.kb0 < t.kb1;
-                const unsigned a = ai & 1;
-                if (any) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2))) { failed = 3; break; }
-                    tc_fence_after();
-                    ++ai;
-                }
-                float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
-                int label = -1;
-                if (is_vocab(OUT) && lane < valid) {
-                    label = p.label[m + lane];
-                    if (label >= 0) ref = p.ref[m + lane];
-                }
-#pragma unroll 1
-                for (int c = 0; c < CHUNKS; ++c) {
-                    uint32_t r[CHUNK];
-                    if (any) {
-                        tmem_ld32(tacc + a * TN + c * CHUNK, *reinterpret_cast<uint32_t (*)[32]>(r));
-                        tmem_ld32(tacc + a * TN + c * CHUNK + 32, *reinterpret_cast<uint32_t (*)[32]>(r + CHUNK - 32));
-                        tmem_ld_wait();
-                        if (c == CHUNKS - 1) release(a);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < CHUNK; ++j) r[j] = 0u;
-                    }
-                    const int col = col0 + c * CHUNK;
-                    if (valid <= 0 || col >= p.n) continue;
-                    if (is_vocab(OUT)) {
-                        // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
-                        const int end = label < 0 ? 0 : p.n - col, at = label - col;
-                        if (__any_sync(0xffffffffu, end < CHUNK || (at >= 0 && at < CHUNK))) {
-#pragma unroll
-                            for (int j = 0; j < CHUNK; ++j) if (j >= end || j == at) r[j] = 0xff800000u;
-                        }
-                        float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int j = 0; j < CHUNK; ++j) {
-                            const float l = __uint_as_float(r[j]);
-                            most = fmaxf(most, l);
-                            const float e = exp2_approx((l - ref) * 1.4426950408889634f);
-                            s4[j & 3] += e;
-                            r[j] = __float_as_uint(e);
-                        }
-                        sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                        if (c == CHUNKS - 1 || col + CHUNK >= p.n) {          // the last columns of this half
-                            if (lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
-                        }
-                        if (OUT == OUT_VOCAB_SUMS) continue;
-                    } else if (!WG && p.row_scale != nullptr) {
-#pragma unroll
-                        for (int j = 0; j < CHUNK; ++j) r[j] = scaled(r[j]);
-                    }
-                    stage_and_store(r, col, m, valid, z);
-                }
+                    for (int j = 0; j < CHUNK; ++j) acc[c][j] = 0u;
             }
+            float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
+            int label = -1;
+            if (is_vocab(OUT) && lane < valid) {
+                label = p.label[m + lane];
+                if (label >= 0) ref = p.ref[m + lane];
+            }
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                const int col = col0 + c * CHUNK;
+                if (col >= p.n) continue;
+                uint32_t (&r)[CHUNK] = acc[c];
+                if (is_vocab(OUT)) {
+                    // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
+                    const int end = label < 0 ? 0 : p.n - col, at = label - col;
+                    if (__any_sync(0xffffffffu, end < CHUNK || (at >= 0 && at < CHUNK))) {
+#pragma unroll
+                        for (int j = 0; j < CHUNK; ++j) if (j >= end || j == at) r[j] = 0xff800000u;
+                    }
+                    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < CHUNK; ++j) {
+                        const float l = __uint_as_float(r[j]);
+                        most = fmaxf(most, l);
+                        const float e = exp2_approx((l - ref) * 1.4426950408889634f);
+                        s4[j & 3] += e;
+                        r[j] = __float_as_uint(e);
+                    }
+                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    if (OUT == OUT_VOCAB_SUMS) continue;
+                } else if (!WG && p.row_scale != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < CHUNK; ++j) r[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(r[j]) * scale);
+                }
+                stage_and_store(r, col, m, valid, z);
+            }
+            if (is_vocab(OUT) && col0 < p.n && lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
         }
         if (lane == 0) tma_store_wait_read<0>();
     } else {
-        if (is_f32(OUT)) give_registers<40>();
+        give_registers<56>();
         if (warp == 0) {
             // ---- producer
             Walker<TM, TN, WG> walk(p, lane);
@@ -545,7 +525,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (t.kb0 == t.kb1) continue;
                 if (lane == 0) {
                     for (int k0 = t.kb0; k0 < t.kb1 && !failed; ++ai) {
-                        const int k1 = is_f32(OUT) ? min(k0 + PART_BLOCKS, t.kb1) : t.kb1;
+                        const int k1 = min(k0 + part_blocks(OUT), t.kb1);
                         const unsigned a = ai & 1, use = ai >> 1;
                         if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) { failed = 2; break; }
                         tc_fence_after();

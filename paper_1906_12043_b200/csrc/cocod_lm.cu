@@ -118,7 +118,11 @@ cudaError_t launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUten
     auto kernel = grouped_gemm<CG, TN, WG, B_MN, OUT>;
     if (!configured[dev]) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GROUPED_SMEM);
+        // The epilogue warps wait for the registers that the others give up: the launch has to hold their sum.
+        cudaFuncAttributes attr{};
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, kernel);
         if (e != cudaSuccess) return e;
+        if (attr.numRegs < 168) return cudaErrorLaunchOutOfResources;
         configured[dev] = true;
     }
     cudaLaunchConfig_t cfg{};
@@ -324,7 +328,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
         const Window win{row0, std::min(at_once, M - row0), M};
         const Matrix hx{static_cast<const bf16 *>(x.data) + row0 * x.ld, x.ld, 0, 2};
         if (cudaMemsetAsync(any, 0, sizeof(int), s) != cudaSuccess) return COCOD_ERR_CUDA;
-        const Cut cut = choose_cut(FORWARD, G, win.rows, V, D, 0);
+        const Cut cut = choose_cut(FORWARD, G, M, V, D, 0);      // by the whole batch: the passes change no sum's order
         const Matrix u{ws + l.u, l.ldu, 0, 2};
         CUtensorMap a, b, o;
         if (!encode(&a, hx, D, win.rows, 1, 128) || !encode(&b, w, D, V, G, 128) || !encode(&o, grad ? u : hx, grad ? V : D, win.rows, 1, 32))
@@ -565,7 +569,7 @@ int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_g
     int64_t bytes = all;
     if (all > limit) {
         const int64_t rows = vocab_rows(G, M, V, D, with_grad != 0, es, limit);
-        bytes = vocab_layout(G, M, V, D, with_grad != 0, es, std::max<int64_t>(rows, std::min<int64_t>(M, 256))).bytes;
+        bytes = std::min(all, vocab_layout(G, M, V, D, with_grad != 0, es, std::max<int64_t>(rows, std::min<int64_t>(M, 256))).bytes);
     }
     if (with_grad && M > 0) {              // a short batch gains by cutting the long reductions
         const int64_t any = 1ll << 62;
