@@ -187,6 +187,26 @@ __device__ __forceinline__ void group_range(const GroupedParams &p, int g, int &
     hi = min(max(p.offsets[g + 1] - p.row0, lo), p.rows);
 }
 
+// The tensor map of group g's rows (the weight form reduces over them): the map of the whole matrix with the first row moved to
+// the group's first and the number of rows set to the group's.  One warp; `map` is scratch in shared memory.
+__device__ __forceinline__ void write_group_map(const CUtensorMap &whole, const char *base, long long ld_bytes, const GroupedParams &p, int g,
+                                                CUtensorMap *dst, CUtensorMap &map)
+{
+    const int lane = threadIdx.x & 31;
+    int lo, hi;
+    group_range(p, g, lo, hi);
+    reinterpret_cast<uint32_t *>(&map)[lane] = reinterpret_cast<const uint32_t *>(&whole)[lane];
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("tensormap.replace.tile.global_address.shared::cta.b1024.b64 [%0], %1;"
+                     ::"r"(smem_u32(&map)), "l"(reinterpret_cast<uint64_t>(base + lo * ld_bytes)) : "memory");
+        asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(smem_u32(&map)), "r"(max(hi - lo, 1)) : "memory");
+    }
+    __syncwarp();
+    asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;"
+                 ::"l"(dst), "r"(smem_u32(&map)) : "memory");
+}
+
 // Within a group, tiles go in bands of eight tile rows, column by column: the CTAs that run at the same time share their
 // operands through L2.
 __device__ __forceinline__ void in_band(int i, int tiles_m, int tiles_n, int &tm, int &tn)
@@ -307,6 +327,11 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t smem_base = smem_u32(smem);
     const unsigned long long limit = p.wait_ns ? p.wait_ns : WAIT_LIMIT_NS;
 
+    if (is_vocab(OUT) && p.redo != nullptr) {     // a second pass over the logits that no row needs
+        pdl_launch_dependents();
+        pdl_wait();
+        if (*p.redo_any == 0) return;
+    }
     if (threadIdx.x == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
@@ -331,8 +356,6 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t tmem_base = *tmem_slot;
     pdl_launch_dependents();
     pdl_wait();
-    // a second pass over the logits that no row needs has no tiles
-    const int first = is_vocab(OUT) && p.redo != nullptr && *p.redo_any == 0 ? 0x7fffffff : cluster;
 
     int failed = 0;
     if (warp >= 4) {
@@ -391,7 +414,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 else mbar_arrive_cluster(map_to_rank(acce0 + 8 * a, 0));
             }
         };
-        for (int i = first; walk.find(i, t); i += clusters) {
+        for (int i = cluster; walk.find(i, t); i += clusters) {
             if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
             const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
             const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
@@ -481,7 +504,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             Tile t;
             unsigned it = 0;
             int last_g = -1;
-            for (int i = first; walk.find(i, t); i += clusters) {
+            for (int i = cluster; walk.find(i, t); i += clusters) {
                 if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
                 if (lane == 0 && !p.debug_no_loads) {
                     const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
@@ -520,7 +543,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             Walker<TM, TN, WG> walk(p, lane);
             Tile t;
             unsigned it = 0, ai = 0;
-            for (int i = first; walk.find(i, t); i += clusters) {
+            for (int i = cluster; walk.find(i, t); i += clusters) {
                 if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
                 if (t.kb0 == t.kb1) continue;
                 if (lane == 0) {

@@ -7,6 +7,7 @@
 #include "cocod_host.h"
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 struct cocod_lm {
@@ -58,8 +59,7 @@ bool encode(CUtensorMap *m, const Matrix &x, uint64_t cols, uint64_t rows, uint6
 }
 
 // ------------------------------------------------------------------------------------------ small kernels
-// The tensor maps of every group's rows of A and B (the weight form reduces over them): the maps of the whole matrices
-// with the first row moved to the group's first row and the number of rows set to the group's.
+// Block 2 g + i: the tensor map of group g's rows of A (i = 0) or B.
 __global__ void __launch_bounds__(32)
 make_group_maps(const __grid_constant__ CUtensorMap whole_a, const __grid_constant__ CUtensorMap whole_b, const char *a, long long lda_bytes,
                 const char *b, long long ldb_bytes, const GroupedParams p, CUtensorMap *maps)
@@ -67,19 +67,9 @@ make_group_maps(const __grid_constant__ CUtensorMap whole_a, const __grid_consta
     __shared__ __align__(128) CUtensorMap map;
     pdl_launch_dependents();
     pdl_wait();
-    const int g = blockIdx.x >> 1, which = blockIdx.x & 1, lane = threadIdx.x;
-    int lo, hi;
-    group_range(p, g, lo, hi);
-    reinterpret_cast<uint32_t *>(&map)[lane] = reinterpret_cast<const uint32_t *>(which ? &whole_b : &whole_a)[lane];
-    __syncwarp();
-    if (lane == 0) {
-        const uint64_t first = reinterpret_cast<uint64_t>(which ? b + lo * ldb_bytes : a + lo * lda_bytes);
-        asm volatile("tensormap.replace.tile.global_address.shared::cta.b1024.b64 [%0], %1;" ::"r"(smem_u32(&map)), "l"(first) : "memory");
-        asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(smem_u32(&map)), "r"(max(hi - lo, 1)) : "memory");
-    }
-    __syncwarp();
-    asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;"
-                 ::"l"(maps + 2 * g + which), "r"(smem_u32(&map)) : "memory");
+    const int g = blockIdx.x >> 1;
+    if (blockIdx.x & 1) write_group_map(whole_b, b, ldb_bytes, p, g, maps + 2 * g + 1, map);
+    else write_group_map(whole_a, a, lda_bytes, p, g, maps + 2 * g, map);
 }
 
 // The parts of a reduction that was cut: out = part 0 + part 1 + ... in this order, for `rows` rows of n columns (n a
@@ -149,8 +139,11 @@ struct Cut {
     int splits;
     int64_t tiles;         // at most
 };
-// rows x cols results (rows form: `groups` groups may each end in a tile of their own; weight form: per group), reductions of
-// `depth` (weight form: on average).
+// rows x cols results (rows form: `groups` groups share the rows; weight form: per group), reductions of `depth` (weight form: on
+// average).  The choice minimises an estimate in microseconds, fitted to measurements: a launch 3.5 (pairs 4.5), a tile 1.5 (2.0)
+// and for each block of 64 of its reduction 0.16 (0.28), or, when all SMs load at the same time, 0.34 (0.40): 4096 x 4096 x 4096
+// takes 153 us in single tiles and 98 in pairs, 128 x 18944 x 512 7.4 and 10.0.  A cut reduction pays for writing its parts and
+// for joining them.
 Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t depth, int64_t workspace_bytes)
 {
     Cut best{};
@@ -158,17 +151,20 @@ Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t de
     const int sms = std::max(sm_count(), 2);
     for (int pair = 0; pair < 2; ++pair) {
         const int64_t t = pair ? 256 : 128, slots = pair ? sms / 2 : sms;
-        const int64_t row_tiles = form == WEIGHT_GRAD ? groups * ceil_div(rows, t)
-                                                      : std::min(rows, ceil_div(rows, t) + (groups > 1 ? groups - 1 : 0));
-        const int64_t tiles = row_tiles * ceil_div(cols, t);
-        const int64_t blocks = std::max<int64_t>(1, ceil_div(depth, 64));
+        // rows form: how the rows are divided is not known here; every group ends inside a tile, half a tile on average
+        const int64_t most = form == WEIGHT_GRAD ? groups * ceil_div(rows, t) : std::min(rows, ceil_div(rows, t) + groups - 1);
+        const double likely = form == WEIGHT_GRAD || groups == 1 ? (double)most
+                                                                 : std::max((double)std::min(groups, rows), (double)rows / t + 0.5 * groups);
+        const int64_t col_tiles = ceil_div(cols, t), blocks = std::max<int64_t>(1, ceil_div(depth, 64));
         const int64_t out_bytes = (form == WEIGHT_GRAD ? groups * rows : rows) * cols * 4;
         for (int64_t splits = 1; splits <= 64 && (splits == 1 || (blocks / splits >= 4 && splits * out_bytes <= workspace_bytes)); splits *= 2) {
-            const int64_t waves = ceil_div(tiles * splits, slots);
-            const double cost = waves * (ceil_div(blocks, splits) * (pair ? 0.30 : 0.25) + 2.0) + (splits > 1 ? 3.0 + splits * out_bytes / 3e6 : 0.0);
+            const double tiles = likely * col_tiles * splits, waves = std::ceil(tiles / slots), busy = std::min(1.0, tiles / slots);
+            const double block = pair ? std::max(0.28, 0.40 * busy) : std::max(0.16, 0.34 * busy);
+            const double cost = (pair ? 4.5 : 3.5) + waves * (ceil_div(blocks, splits) * block + (pair ? 2.0 : 1.5)) +
+                                (splits > 1 ? 2.5 + splits * out_bytes / 4e6 : 0.0);
             if (cost < best_cost) {
                 best_cost = cost;
-                best = Cut{pair != 0, (int)splits, tiles * splits};
+                best = Cut{pair != 0, (int)splits, most * col_tiles * splits};
             }
         }
     }
@@ -228,9 +224,9 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window
 }
 
 // weight form: out_g (rows x cols) = sum over the group's rows m of A[m][.]^T B[m][.]
-// (add: added to what out, fp32, holds)
+// (add: added to what out, fp32, holds;  maps_ready: a kernel before this one has written the groups' maps)
 int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
-                const Matrix &out, bool add, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+                const Matrix &out, bool add, bool maps_ready, void *workspace, int64_t workspace_bytes, cudaStream_t s)
 {
     const int64_t M = win.rows;
     if (add) workspace_bytes = 0;
@@ -246,8 +242,9 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, i
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
     p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits;
     p.group_maps = h->group_maps; p.error_flag = h->flag;
-    TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, b, static_cast<const char *>(A.data), (long long)A.ld * 2,
-                              static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps));
+    if (!maps_ready)
+        TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, b, static_cast<const char *>(A.data),
+                                  (long long)A.ld * 2, static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps));
     if (add) {
         TRY_CUDA((cut.pair ? launch_tiles<2, 256, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)
                            : launch_tiles<1, 128, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)));
@@ -320,63 +317,64 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
     v.w = static_cast<const bf16 *>(w.data); v.ldw = w.ld; v.w_stride = w.stride;
     v.label = reinterpret_cast<int *>(ws + l.label); v.own = reinterpret_cast<float *>(ws + l.own);
     v.ref = reinterpret_cast<float *>(ws + l.ref); v.share = reinterpret_cast<float *>(ws + l.share);
+    v.redo_any = reinterpret_cast<int *>(ws + l.any);
     v.error_flag = h->flag;
-    int *any = reinterpret_cast<int *>(ws + l.any);
-    const int row_blocks = (int)ceil_div(M, 8);
-    TRY_CUDA(launch_dependent(true, vocab_target, dim3(row_blocks + G), dim3(256), 0, s, v, row_blocks));
-    for (int64_t row0 = 0; row0 < M; row0 += at_once) {
+    const Cut cut = choose_cut(FORWARD, G, M, V, D, 0);      // by the whole batch: the passes change no sum's order
+    const bool several = at_once < M;
+    int64_t row0 = 0;
+    do {                                   // (no rows at all: one pass, for the results' zeros)
         const Window win{row0, std::min(at_once, M - row0), M};
-        const Matrix hx{static_cast<const bf16 *>(x.data) + row0 * x.ld, x.ld, 0, 2};
-        if (cudaMemsetAsync(any, 0, sizeof(int), s) != cudaSuccess) return COCOD_ERR_CUDA;
-        const Cut cut = choose_cut(FORWARD, G, M, V, D, 0);      // by the whole batch: the passes change no sum's order
-        const Matrix u{ws + l.u, l.ldu, 0, 2};
-        CUtensorMap a, b, o;
-        if (!encode(&a, hx, D, win.rows, 1, 128) || !encode(&b, w, D, V, G, 128) || !encode(&o, grad ? u : hx, grad ? V : D, win.rows, 1, 32))
+        const int64_t rows = std::max<int64_t>(win.rows, 1);
+        const Matrix hx{M ? static_cast<const bf16 *>(x.data) + row0 * x.ld : (const void *)h->group_maps, M ? x.ld : D, 0, 2};
+        const Matrix u{grad ? ws + l.u : (char *)h->group_maps, l.ldu, 0, 2}, hs{grad ? ws + l.hs : (char *)h->group_maps, D, 0, 2};
+        CUtensorMap a, b, o, u_rows, hs_rows;
+        if (!encode(&a, hx, D, rows, 1, 128) || !encode(&b, w, D, V, G, 128) || !encode(&o, grad ? u : hx, grad ? V : D, rows, 1, 32) ||
+            !encode(&u_rows, u, V, rows, 1, 64) || !encode(&hs_rows, hs, D, rows, 1, 64))
             return COCOD_ERR_CUDA;
         GroupedParams p{};
         p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.row0 = (int)row0; p.rows = (int)win.rows; p.n = (int)V; p.kdim = (int)D;
         p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.splits = 1;
         p.out = ws + l.u; p.ld_out = l.ldu; p.error_flag = h->flag;
         p.ref = v.ref + row0; p.label = v.label + row0; p.sums = reinterpret_cast<float2 *>(ws + l.sums); p.ld_sums = (int)win.rows;
+        const int row_blocks = (int)ceil_div(win.rows, 8);
+        TRY_CUDA(launch_dependent(true, vocab_begin, dim3(row_blocks + G), dim3(256), 0, s, u_rows, hs_rows, static_cast<const char *>(u.data),
+                                  (long long)u.ld * 2, static_cast<const char *>(hs.data), (long long)hs.ld * 2, p,
+                                  grad ? h->group_maps : (CUtensorMap *)nullptr, v, row_blocks));
         FinishParams f{};
         f.v = v; f.row0 = (int)row0; f.rows = (int)win.rows; f.sums = p.sums; f.ld_sums = p.ld_sums;
         f.n_sums = (int)ceil_div(V, cut.pair ? 128 : 64);
-        f.row_loss = row_loss; f.redo = reinterpret_cast<int *>(ws + l.redo); f.redo_any = any;
+        f.row_loss = row_loss; f.redo = reinterpret_cast<int *>(ws + l.redo);
+        f.loss = row0 + win.rows >= M ? loss : nullptr;
         if (grad) {
             f.rho = reinterpret_cast<float *>(ws + l.rho);
             f.u = reinterpret_cast<bf16 *>(ws + l.u); f.ldu = l.ldu;
             f.hs = reinterpret_cast<bf16 *>(ws + l.hs);
         }
+        const dim3 finish_grid((unsigned)ceil_div(rows, FINISH_ROWS));
         for (int pass = 0; pass < 2; ++pass) {
             p.redo = pass ? f.redo : nullptr;
-            p.redo_any = any;
+            p.redo_any = v.redo_any;
             f.second = pass;
-            if (grad)
+            if (win.rows > 0 && grad)
                 TRY_CUDA((cut.pair ? launch_tiles<2, 256, false, false, OUT_VOCAB>(a, b, o, p, cut.tiles, s)
                                    : launch_tiles<1, 128, false, false, OUT_VOCAB>(a, b, o, p, cut.tiles, s)));
-            else
+            else if (win.rows > 0)
                 TRY_CUDA((cut.pair ? launch_tiles<2, 256, false, false, OUT_VOCAB_SUMS>(a, b, o, p, cut.tiles, s)
                                    : launch_tiles<1, 128, false, false, OUT_VOCAB_SUMS>(a, b, o, p, cut.tiles, s)));
-            TRY_CUDA(launch_dependent(true, vocab_finish, dim3((unsigned)ceil_div(win.rows, FINISH_ROWS)), dim3(32 * FINISH_WARPS), 0, s, f));
+            TRY_CUDA(launch_dependent(true, vocab_finish, finish_grid, dim3(32 * FINISH_WARPS), 0, s, f));
         }
-        if (!grad) continue;
-        char *parts = ws + l.parts;
-        const int64_t parts_bytes = workspace_bytes - l.parts;
-        const Matrix dh{static_cast<const bf16 *>(grad->dh.data) + row0 * grad->dh.ld, grad->dh.ld, 0, 2};
-        if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, parts, parts_bytes, s)) return rc;
-        const Matrix hs{ws + l.hs, D, 0, 2};
-        const bool several = at_once < M;
-        const Matrix dst = several && dw_elem == 2 ? Matrix{ws + l.total32, D, V * D, 4} : grad->dw;
-        if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, dst, several && row0 > 0, parts, parts_bytes, s)) return rc;
-        if (several && dw_elem == 2 && row0 + at_once >= M) {
-            if (int rc = join(h, reinterpret_cast<const float *>(ws + l.total32), 0, 1, grad->dw, V, G * V, D, s)) return rc;
+        if (grad) {
+            char *parts = ws + l.parts;
+            const int64_t parts_bytes = workspace_bytes - l.parts;
+            const Matrix dh{static_cast<const bf16 *>(grad->dh.data) + row0 * grad->dh.ld, grad->dh.ld, 0, 2};
+            if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, parts, parts_bytes, s)) return rc;
+            const Matrix dst = several && dw_elem == 2 ? Matrix{ws + l.total32, D, V * D, 4} : grad->dw;
+            if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, dst, several && row0 > 0, true, parts, parts_bytes, s)) return rc;
         }
-    }
-    if (M == 0 && grad) {
-        const Matrix none{h->group_maps, D, 0, 2};
-        if (int rc = run_weights(h, G, offsets, Window{0, 0, 0}, V, D, Matrix{h->group_maps, ceil_div(V, 8) * 8, 0, 2}, none, grad->dw, false, nullptr, 0, s)) return rc;
-    }
-    TRY_CUDA(launch_dependent(true, vocab_mean, dim3(G), dim3(256), 0, s, v, static_cast<const float *>(row_loss), loss));
+        row0 += win.rows;
+    } while (row0 < M);
+    if (grad && several && dw_elem == 2)
+        return join(h, reinterpret_cast<const float *>(ws + l.total32), 0, 1, grad->dw, V, G * V, D, s);
     return COCOD_OK;
 }
 
@@ -491,7 +489,7 @@ int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets,
     if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(dw, lddw, dw_stride, n, k, G, es))
         return COCOD_ERR_INVALID;
-    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, workspace,
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false, workspace,
                        workspace_bytes, (cudaStream_t)stream);
 }
 
@@ -556,7 +554,7 @@ int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *o
     const int64_t wide = ceil_div(M * k * 2, 256) * 256;
     if (workspace_bytes < wide) return COCOD_ERR_TOO_LARGE;
     if (int rc = cocod_act_unpack(h, M, k, q, ldq, scales, workspace, k, stream)) return rc;
-    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false,
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false,
                        static_cast<char *>(workspace) + wide, workspace_bytes - wide, (cudaStream_t)stream);
 }
 

@@ -18,7 +18,6 @@ namespace cocod {
 namespace lm {
 
 constexpr int FINISH_ROWS = 32, FINISH_WARPS = 16;
-using bf16_t = __nv_bfloat16;
 constexpr float SUM_LIMIT = 5.0e21f;         // about exp(50)
 
 struct VocabRows {
@@ -35,6 +34,7 @@ struct VocabRows {
     float *own;                        // [total]: the label's logit
     float *ref;                        // [total]: c_r
     float *share;                      // [groups]: 1 / rows with a label
+    int *redo_any;                     // whether a row needs the second pass; [1]: blocks of vocab_finish that are through
     int *error_flag;
 };
 
@@ -56,17 +56,23 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// One warp per row: the label's logit.  The last `groups` blocks count the rows of a group that have a label.
+// One warp per row: the label's logit.  The last `groups` blocks count the rows of a group that have a label, and, where the
+// gradient is wanted (maps != nullptr), write the tensor maps of the group's rows of u and of rho h.
 __global__ void __launch_bounds__(256)
-vocab_target(const VocabRows p, int row_blocks)
+vocab_begin(const __grid_constant__ CUtensorMap whole_u, const __grid_constant__ CUtensorMap whole_hs, const char *u, long long ldu_bytes,
+            const char *hs, long long ldhs_bytes, const GroupedParams window, CUtensorMap *maps, const VocabRows p, int row_blocks)
 {
+    __shared__ __align__(128) CUtensorMap map[2];
+    __shared__ int part[8];
     pdl_launch_dependents();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x >= row_blocks) {
         const int g = blockIdx.x - row_blocks;
+        if (g == 0 && threadIdx.x < 2) p.redo_any[threadIdx.x] = 0;
+        if (maps != nullptr && warp == 6) write_group_map(whole_u, u, ldu_bytes, window, g, maps + 2 * g, map[0]);
+        if (maps != nullptr && warp == 7) write_group_map(whole_hs, hs, ldhs_bytes, window, g, maps + 2 * g + 1, map[1]);
         const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
-        __shared__ int part[8];
         int n = 0;
         for (int r = lo + threadIdx.x; r < hi; r += 256) {
             const int t = p.labels[r];
@@ -81,8 +87,8 @@ vocab_target(const VocabRows p, int row_blocks)
         }
         return;
     }
-    const long long r = (long long)blockIdx.x * 8 + warp;
-    if (r >= p.total) return;
+    const long long r = window.row0 + (long long)blockIdx.x * 8 + warp;
+    if (r >= window.row0 + window.rows) return;
     const int g = group_of(p.offsets, p.groups, (int)r);
     int t = p.labels[r];
     if (t >= p.vocab) {
@@ -123,9 +129,27 @@ struct FinishParams {
     __nv_bfloat16 *u;                  // [rows][ldu]
     long long ldu;
     __nv_bfloat16 *hs;                 // [rows][width]: rho h
-    int *redo, *redo_any;              // first pass: set; second pass: nothing is done if *redo_any is 0
-    int second;
+    int *redo;                         // first pass: set
+    float *loss;                       // [groups], second pass over the last rows: the means; else nullptr
+    int second;                        // second pass: no row is looked at again if *v.redo_any is 0
 };
+
+// loss[g] = sum of the rows' losses with their shares, by one block; one warp per group, sums in a fixed order.
+__device__ __forceinline__ void vocab_mean(const VocabRows &p, const float *row_loss, float *loss)
+{
+    const int lane = threadIdx.x & 31;
+    for (int g = threadIdx.x >> 5; g < p.groups; g += FINISH_WARPS) {
+        const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
+        float s = 0.0f;
+#pragma unroll 8
+        for (int r = lo + lane; r < hi; r += 32) {
+            const float v = __ldcg(row_loss + r);
+            s += p.row_weight == nullptr ? v : v == 0.0f ? 0.0f : p.row_weight[r] * v;
+        }
+        s = warp_sum(s);
+        if (lane == 0) loss[g] = p.row_weight != nullptr ? s : s * p.share[g];
+    }
+}
 
 // 32 rows per CTA: their sums, losses and factors, the label's entry of u, and rho h.
 __global__ void __launch_bounds__(32 * FINISH_WARPS)
@@ -135,7 +159,10 @@ vocab_finish(const FinishParams p)
     __shared__ float factor[FINISH_ROWS];
     pdl_launch_dependents();
     pdl_wait();
-    if (p.second && *p.redo_any == 0) return;
+    if (p.second && *p.v.redo_any == 0) {          // (the losses are complete: the first block adds them up)
+        if (blockIdx.x == 0 && p.loss != nullptr) vocab_mean(p.v, p.row_loss, p.loss);
+        return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int first = blockIdx.x * FINISH_ROWS, row = first + lane;        // counted from row0
     float s = 0.0f, most = __uint_as_float(0xff800000u);
@@ -166,12 +193,12 @@ vocab_finish(const FinishParams p)
                 if (!p.second && !(s <= SUM_LIMIT)) {
                     again = 1;
                     p.v.ref[r] = most;
-                    *p.redo_any = 1;
+                    *p.v.redo_any = 1;
                 }
                 if (p.rho != nullptr) {
                     const float a = p.v.row_weight != nullptr ? p.v.row_weight[r] : p.v.share[group_of(p.v.offsets, p.v.groups, r)];
                     rho = a / (s + et);
-                    const bf16_t entry = __float2bfloat16_rn(-s);
+                    const __nv_bfloat16 entry = __float2bfloat16_rn(-s);
                     const float kept = -__bfloat162float(entry);
                     p.u[row * p.ldu + t] = entry;
                     scale = kept > 0.0f && kept <= 3.0e38f ? rho * (s / kept) : rho;
@@ -182,6 +209,18 @@ vocab_finish(const FinishParams p)
             if (p.rho != nullptr) p.rho[row] = rho;
         }
         factor[lane] = scale;
+    }
+    if (p.second && p.loss != nullptr) {           // the last block to get here adds the losses up
+        __shared__ int last;
+        if (warp == 0) {
+            __threadfence();
+            if (lane == 0) last = atomicAdd(p.v.redo_any + 1, 1) == (int)gridDim.x - 1;
+        }
+        __syncthreads();
+        if (last) {
+            __threadfence();
+            vocab_mean(p.v, p.row_loss, p.loss);
+        }
     }
     if (p.rho == nullptr) return;
     __syncthreads();
@@ -199,27 +238,6 @@ vocab_finish(const FinishParams p)
             o = make_uint4(os[0], os[1], os[2], os[3]);
         }
         reinterpret_cast<uint4 *>(p.hs + (long long)(first + rr) * p.v.width)[c] = o;
-    }
-}
-
-// loss[g] = sum of the rows' losses with their shares; one block per group, sums in a fixed order.
-__global__ void __launch_bounds__(256)
-vocab_mean(const VocabRows p, const float *row_loss, float *loss)
-{
-    __shared__ float part[8];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int g = blockIdx.x;
-    const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
-    float s = 0.0f;
-    for (int r = lo + threadIdx.x; r < hi; r += 256)
-        if (p.label[r] >= 0) s += p.row_weight != nullptr ? p.row_weight[r] * row_loss[r] : row_loss[r];
-    s = warp_sum(s);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) s += part[i];
-        loss[g] = p.row_weight != nullptr ? s : s * p.share[g];
     }
 }
 

@@ -24,6 +24,10 @@ FORWARD, INPUT_GRAD, WEIGHT_GRAD = 0, 1, 2
 BLOCK = 128                      # columns that share a scale in an 8-bit checkpoint
 MAX_GROUPS = 1024
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_SIZES = {torch.bfloat16: 2, torch.float32: 4, torch.int8: 1}
+PARTS_BYTES = 32 << 20           # kept by every LMOps for the parts of reductions that are cut
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _round_up(n: int, m: int) -> int:
@@ -70,63 +74,51 @@ class LMOps:
             raise _E.CocodError(rc, "cocod_lm_create")
         self._h = h
         self._device = torch.cuda.current_device()
+        self._parts = torch.empty(PARTS_BYTES, dtype=torch.uint8, device=self._device)
+        self._parts_at = self._parts.data_ptr()
 
     # ------------------------------------------------------------------------------------------ arguments
-    def _rows(self, t, name, M=None, cols=None, dtype=torch.bfloat16, align=16):
-        """(address, row stride) of a matrix with contiguous rows."""
-        if t.dim() != 2 or t.dtype is not dtype or t.device.type != "cuda" or t.device.index != self._device:
-            raise ValueError(f"{name}: need a two-dimensional {dtype} tensor on cuda:{self._device}, the current device at creation")
-        if (M is not None and t.shape[0] != M) or (cols is not None and t.shape[1] != cols):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, need {M if M is not None else 'any'} x {cols if cols is not None else 'any'}")
-        if t.shape[1] > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name}: rows have to be contiguous")
-        ld = t.stride(0) if t.shape[0] > 1 else _round_up(t.shape[1], 16)
-        if align and (t.data_ptr() % align or ld * t.element_size() % align):
-            raise ValueError(f"{name}: rows have to start at multiples of {align} bytes")
-        if ld < t.shape[1]:
-            raise ValueError(f"{name}: rows overlap")
-        return t.data_ptr(), ld
+    def _rows(self, t, name, M, cols, dtype=torch.bfloat16, align=16):
+        """(address, row stride) of an M x cols matrix with contiguous rows that start at multiples of `align` bytes."""
+        if t.dtype is dtype and t.get_device() == self._device and t.shape == (M, cols):
+            ld, step = t.stride()
+            if M <= 1:
+                ld = _round_up(cols, 16)
+            at = t.data_ptr()
+            if (step == 1 or cols == 1) and ld >= cols and not (at | ld * _SIZES[dtype]) % align:
+                return at, ld
+        raise ValueError(f"{name}: need {M} x {cols} {dtype} on cuda:{self._device} (the current device at creation), rows contiguous, not "
+                         f"overlapping and starting at multiples of {align} bytes; got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
 
-    def _groups(self, t, name, shape=None, dtype=torch.bfloat16):
-        """(address, row stride, group stride) of one matrix per group."""
-        if t.dim() != 3 or t.dtype is not dtype or t.device.type != "cuda" or t.device.index != self._device:
-            raise ValueError(f"{name}: need a three-dimensional {dtype} tensor on cuda:{self._device}, the current device at creation")
-        if shape is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
-        G, n, k = t.shape
-        if k > 1 and t.stride(2) != 1:
-            raise ValueError(f"{name}: rows have to be contiguous")
-        ld = t.stride(1) if n > 1 else _round_up(k, 8)
-        gs = t.stride(0) if G > 1 else n * ld
-        if t.data_ptr() % 16 or ld * t.element_size() % 16 or gs * t.element_size() % 16:
-            raise ValueError(f"{name}: rows and groups have to start at multiples of 16 bytes")
-        if ld < k or gs < (n - 1) * ld + k:
-            raise ValueError(f"{name}: rows or groups overlap")
-        return t.data_ptr(), ld, gs
+    def _groups(self, t, name, G, n, k, dtype=torch.bfloat16):
+        """(address, row stride, group stride) of one n x k matrix per group."""
+        if t.dtype is dtype and t.get_device() == self._device and t.shape == (G, n, k):
+            gs, ld, step = t.stride()
+            if n == 1:
+                ld = _round_up(k, 8)
+            if G == 1:
+                gs = n * ld
+            at, size = t.data_ptr(), _SIZES[dtype]
+            if (step == 1 or k == 1) and ld >= k and gs >= (n - 1) * ld + k and not (at | ld * size | gs * size) % 16:
+                return at, ld, gs
+        raise ValueError(f"{name}: need {G} x {n} x {k} {dtype} on cuda:{self._device} (the current device at creation), rows contiguous, rows and "
+                         f"groups not overlapping and starting at multiples of 16 bytes; got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
 
-    def _offsets(self, offsets, G):
-        if offsets.dim() != 1 or offsets.dtype is not torch.int32 or offsets.shape[0] != G + 1 or not offsets.is_contiguous() \
-                or offsets.device.type != "cuda" or offsets.device.index != self._device:
-            raise ValueError(f"offsets: need {G + 1} contiguous int32 on cuda:{self._device} (one more than there are groups)")
-        return offsets.data_ptr()
-
-    def _type(self, out, out_dtype):
-        dtype = out.dtype if out is not None else out_dtype
-        if dtype not in _TYPES or (out is not None and out_dtype not in (None, dtype)):
-            raise ValueError(f"result type {out_dtype if out is None else (out.dtype, out_dtype)}: bfloat16 or float32")
-        return dtype
-
-    def _scratch(self, nbytes):
-        if nbytes < 0:
-            raise ValueError("sizes outside the operators' range")
-        return torch.empty(nbytes, dtype=torch.uint8, device=self._device) if nbytes else None
+    def _vector(self, t, name, n, dtype):
+        if t.dtype is dtype and t.get_device() == self._device and t.shape == (n,) and (n <= 1 or t.stride() == (1,)):
+            return t.data_ptr()
+        raise ValueError(f"{name}: need {n} contiguous {dtype} on cuda:{self._device} (the current device at creation); got {tuple(t.shape)} "
+                         f"{t.dtype} on {t.device}")
 
     @staticmethod
-    def _addr(t):
-        return None if t is None else t.data_ptr()
+    def _type(out, out_dtype, usual):
+        dtype = out_dtype or (usual if out is None else out.dtype)
+        if dtype not in _TYPES or (out is not None and out.dtype is not dtype):
+            raise ValueError(f"result type {dtype}{'' if out is None else f' for a result of {out.dtype}'}: bfloat16 or float32, as the result")
+        return dtype
 
-    def _call(self, name, *args):
-        rc = getattr(self._lib, name)(self._h, *args, torch.cuda.current_stream(self._device).cuda_stream)
+    def _call(self, name, function, *args):
+        rc = function(self._h, *args, _raw_stream(self._device))
         if rc != _E.OK:
             raise _E.CocodError(rc, name)
 
@@ -136,99 +128,88 @@ class LMOps:
         """y[m] = w[g] x[m] for the rows m of every group g.  x: M x k bf16, w: G x n x k bf16 (any group and row stride),
         offsets: G + 1 int32.  Rows behind offsets[G] are not written."""
         G, n, k = w.shape
-        return self._rows_product("cocod_grouped_forward", FORWARD, x, "x", k, n, w, G, n, k, offsets, out, out_dtype)
+        M = x.shape[0]
+        dtype = self._type(out, out_dtype, torch.bfloat16)
+        if out is None:
+            out = x.new_empty((M, n), dtype=dtype)
+        self._call("cocod_grouped_forward", self._lib.cocod_grouped_forward, G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k,
+                   *self._rows(x, "x", M, k), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, n, dtype), _TYPES[dtype],
+                   self._parts_at, PARTS_BYTES)
+        return out
 
     def grouped_input_grad(self, dy, w, offsets, out=None, out_dtype=None):
         """dx[m] = w[g]^T dy[m]: the gradient of grouped_forward's input.  dy: M x n bf16."""
         G, n, k = w.shape
-        return self._rows_product("cocod_grouped_input_grad", INPUT_GRAD, dy, "dy", n, k, w, G, n, k, offsets, out, out_dtype)
-
-    def _rows_product(self, name, which, a, a_name, depth, cols, w, G, n, k, offsets, out, out_dtype):
-        dtype = self._type(out, out_dtype or (None if out is not None else torch.bfloat16))
-        ap, lda = self._rows(a, a_name, cols=depth)
-        wp, ldw, gs = self._groups(w, "w")
-        M = a.shape[0]
-        op = self._offsets(offsets, G)
+        M = dy.shape[0]
+        dtype = self._type(out, out_dtype, torch.bfloat16)
         if out is None:
-            out = torch.empty((M, cols), dtype=dtype, device=a.device)
-        yp, ldy = self._rows(out, "out", M, cols, dtype)
-        ws = self._scratch(self._lib.cocod_grouped_workspace(which, G, M, n, k))
-        self._call(name, G, op, M, n, k, ap, lda, wp, ldw, gs, yp, ldy, _TYPES[dtype], self._addr(ws), 0 if ws is None else ws.numel())
+            out = dy.new_empty((M, k), dtype=dtype)
+        self._call("cocod_grouped_input_grad", self._lib.cocod_grouped_input_grad, G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k,
+                   *self._rows(dy, "dy", M, n), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, k, dtype), _TYPES[dtype],
+                   self._parts_at, PARTS_BYTES)
         return out
 
     def grouped_weight_grad(self, dy, x, offsets, out=None, out_dtype=None):
         """dw[g] = sum over the group's rows of dy[m] x[m]^T: the gradient of grouped_forward's weights, G x n x k, 0 for an
         empty group.  x: M x k bf16, or the PackedActivations kept of it.  out: any group and row stride, e.g. a view of the
         K x P gradients that Engine.local_step takes."""
-        dtype = self._type(out, out_dtype or (None if out is not None else torch.float32))
-        packed = isinstance(x, PackedActivations)
         M, k = x.shape
-        dp, lddy = self._rows(dy, "dy", M=M)
         n, G = dy.shape[1], offsets.shape[0] - 1
-        op = self._offsets(offsets, G)
+        dtype = self._type(out, out_dtype, torch.float32)
         if out is None:
-            out = torch.empty((G, n, k), dtype=dtype, device=dy.device)
-        wp, ldw, gs = self._groups(out, "out", (G, n, k), dtype)
-        if packed:
-            qp, ldq = self._rows(x.q, "x.q", M, k, torch.int8)
+            out = dy.new_empty((G, n, k), dtype=dtype)
+        shape = (G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k)
+        if isinstance(x, PackedActivations):
             ws = self._scratch(self._lib.cocod_grouped_packed_workspace(G, M, n, k))
-            self._call("cocod_grouped_weight_grad_packed", G, op, M, n, k, dp, lddy, qp, ldq, x.scales.data_ptr(), wp, ldw, gs, _TYPES[dtype],
-                       self._addr(ws), 0 if ws is None else ws.numel())
+            self._call("cocod_grouped_weight_grad_packed", self._lib.cocod_grouped_weight_grad_packed, *shape, *self._rows(dy, "dy", M, n),
+                       *self._rows(x.q, "x.q", M, k, torch.int8), x.scales.data_ptr(), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype],
+                       None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
         else:
-            xp, ldx = self._rows(x, "x")
-            ws = self._scratch(self._lib.cocod_grouped_workspace(WEIGHT_GRAD, G, M, n, k))
-            self._call("cocod_grouped_weight_grad", G, op, M, n, k, dp, lddy, xp, ldx, wp, ldw, gs, _TYPES[dtype], self._addr(ws),
-                       0 if ws is None else ws.numel())
+            self._call("cocod_grouped_weight_grad", self._lib.cocod_grouped_weight_grad, *shape, *self._rows(dy, "dy", M, n),
+                       *self._rows(x, "x", M, k), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype], self._parts_at, PARTS_BYTES)
         return out
+
+    def _scratch(self, nbytes):
+        if nbytes < 0:
+            raise ValueError("sizes outside the operators' range")
+        return torch.empty(nbytes, dtype=torch.uint8, device=self._device) if nbytes else None
 
     # ------------------------------------------------------------------------------------------ activations in 8 bits
     def act_pack(self, x, out=None):
         """The 8-bit form of x (M x k bf16)."""
         M, k = x.shape
-        xp, ldx = self._rows(x, "x", align=0)
         if out is None:
             out = PackedActivations(M, k, x.device)
-        qp, ldq = self._rows(out.q, "out.q", M, k, torch.int8)
-        self._call("cocod_act_pack", M, k, xp, ldx, qp, ldq, out.scales.data_ptr())
+        self._call("cocod_act_pack", self._lib.cocod_act_pack, M, k, *self._rows(x, "x", M, k, align=1),
+                   *self._rows(out.q, "out.q", M, k, torch.int8), out.scales.data_ptr())
         return out
 
     def act_unpack(self, packed, out=None):
         """The bf16 values that a checkpoint stands for."""
         M, k = packed.shape
         if out is None:
-            out = torch.empty((M, k), dtype=torch.bfloat16, device=packed.q.device)
-        qp, ldq = self._rows(packed.q, "packed.q", M, k, torch.int8)
-        yp, ldy = self._rows(out, "out", M, k, align=0)
-        self._call("cocod_act_unpack", M, k, qp, ldq, packed.scales.data_ptr(), yp, ldy)
+            out = packed.q.new_empty((M, k), dtype=torch.bfloat16)
+        self._call("cocod_act_unpack", self._lib.cocod_act_unpack, M, k, *self._rows(packed.q, "packed.q", M, k, torch.int8),
+                   packed.scales.data_ptr(), *self._rows(out, "out", M, k, align=1))
         return out
 
     def act_relu_grad(self, dh, packed, out=None):
         """dz = dh where the kept activation is positive, 0 elsewhere (NaN where it was not finite).  out may be dh."""
         M, k = packed.shape
         if out is None:
-            out = torch.empty((M, k), dtype=torch.bfloat16, device=dh.device)
-        dp, lddh = self._rows(dh, "dh", M, k, align=0)
-        qp, ldq = self._rows(packed.q, "packed.q", M, k, torch.int8)
-        zp, lddz = self._rows(out, "out", M, k, align=0)
-        self._call("cocod_act_relu_grad", M, k, dp, lddh, qp, ldq, zp, lddz)
+            out = dh.new_empty((M, k))
+        self._call("cocod_act_relu_grad", self._lib.cocod_act_relu_grad, M, k, *self._rows(dh, "dh", M, k, align=1),
+                   *self._rows(packed.q, "packed.q", M, k, torch.int8), *self._rows(out, "out", M, k, align=1))
         return out
 
     # ------------------------------------------------------------------------------------------ vocabulary
-    def _vector(self, t, name, n, dtype):
-        if t.dim() != 1 or t.dtype is not dtype or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device.type != "cuda" \
-                or t.device.index != self._device:
-            raise ValueError(f"{name}: need {n} contiguous {dtype} on cuda:{self._device}")
-        return t.data_ptr()
-
     def _vocab(self, x, w, labels, offsets, row_weights):
         G, V, D = w.shape
         M = x.shape[0]
-        xp, ldx = self._rows(x, "x", cols=D)
-        wp, ldw, gs = self._groups(w, "w")
-        wt = None if row_weights is None else self._vector(row_weights, "row_weights", M, torch.float32)
-        loss = torch.empty(G, dtype=torch.float32, device=x.device)
-        row_loss = torch.empty(M, dtype=torch.float32, device=x.device)
-        return loss, row_loss, (G, self._offsets(offsets, G), M, V, D, xp, ldx, wp, ldw, gs, self._vector(labels, "labels", M, torch.int32), wt,
+        loss, row_loss = x.new_empty(G, dtype=torch.float32), x.new_empty(M, dtype=torch.float32)
+        return loss, row_loss, (G, self._vector(offsets, "offsets", G + 1, torch.int32), M, V, D, *self._rows(x, "x", M, D),
+                                *self._groups(w, "w", G, V, D), self._vector(labels, "labels", M, torch.int32),
+                                None if row_weights is None else self._vector(row_weights, "row_weights", M, torch.float32),
                                 loss.data_ptr(), row_loss.data_ptr())
 
     def vocab_loss(self, x, w, labels, offsets, row_weights=None):
@@ -238,27 +219,27 @@ class LMOps:
         loss, row_loss, args = self._vocab(x, w, labels, offsets, row_weights)
         G, _, M, V, D = args[:5]
         ws = self._scratch(self._lib.cocod_vocab_workspace(G, M, V, D, 0, BF16, self.workspace_limit))
-        self._call("cocod_vocab_loss", *args, ws.data_ptr(), ws.numel())
+        self._call("cocod_vocab_loss", self._lib.cocod_vocab_loss, *args, ws.data_ptr(), ws.numel())
         return loss, row_loss
 
     def vocab_loss_grad(self, x, w, labels, offsets, row_weights=None, dw=None, dw_dtype=None):
         """(loss, row_loss, dx, dw): vocab_loss and the gradients of the groups' losses.  dw: G x V x D, bf16 (as w) or float32, for
         example a view of the K x P gradients that Engine.local_step takes."""
-        dtype = self._type(dw, dw_dtype or (None if dw is not None else torch.bfloat16))
+        dtype = self._type(dw, dw_dtype, torch.bfloat16)
         loss, row_loss, args = self._vocab(x, w, labels, offsets, row_weights)
         G, _, M, V, D = args[:5]
-        dx = torch.empty((M, D), dtype=torch.bfloat16, device=x.device)
+        dx = x.new_empty((M, D))
         if dw is None:
-            dw = torch.empty((G, V, D), dtype=dtype, device=x.device)
-        dp, lddw, gs = self._groups(dw, "dw", (G, V, D), dtype)
+            dw = x.new_empty((G, V, D), dtype=dtype)
         ws = self._scratch(self._lib.cocod_vocab_workspace(G, M, V, D, 1, _TYPES[dtype], self.workspace_limit))
-        self._call("cocod_vocab_loss_grad", *args, dx.data_ptr(), D, dp, lddw, gs, _TYPES[dtype], ws.data_ptr(), ws.numel())
+        self._call("cocod_vocab_loss_grad", self._lib.cocod_vocab_loss_grad, *args, dx.data_ptr(), D,
+                   *self._groups(dw, "dw", G, V, D, dtype), _TYPES[dtype], ws.data_ptr(), ws.numel())
         return loss, row_loss, dx, dw
 
     # ------------------------------------------------------------------------------------------ the rest
     def check(self):
         """Synchronise the current stream; raise if a kernel gave up a wait or met offsets or labels out of range."""
-        rc = self._lib.cocod_lm_check(self._h, torch.cuda.current_stream(self._device).cuda_stream)
+        rc = self._lib.cocod_lm_check(self._h, _raw_stream(self._device))
         if rc != _E.OK:
             raise _E.CocodError(rc, "cocod_lm_check")
 
