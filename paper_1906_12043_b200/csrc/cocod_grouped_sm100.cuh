@@ -11,8 +11,9 @@
 //     cores that need 512 clocks for the block; a single CTA with a tile of its own would need half as much again from
 //     L2.  Problems with few tiles use 128 x 128 tiles and single CTAs (CG = 1): more SMs take part.
 //   * Two accumulators in tensor memory: the epilogue of a tile runs under the products of the next.
-//   * Warps: 0 producer (TMA), 1 issuer of tcgen05.mma (leading CTA of the pair only), 2 tensor memory, 4..11 epilogue.
-//     Every role walks the tile list on its own (Walker); nothing is handed over but barriers.
+//   * Warps: 0 producer (TMA), 1 issuer of tcgen05.mma (leading CTA of the pair only), 2 tensor memory, 3 scheduler, 4..11 epilogue.
+//     The scheduler reads the tile list (Walker) some tiles ahead and leaves them in shared memory; when every role found
+//     its tiles itself, the producer's pause for it emptied the ring: 3000 clocks a tile.
 //   * An epilogue warp owns 32 rows of its CTA's tile and half of the columns, stages them in shared memory of its own
 //     (4 KB, TMA swizzle) and hands them to the store engine; rows behind the end of a group are some other group's, so a
 //     warp whose rows end inside a group's last tile stores the valid ones itself.
@@ -37,6 +38,7 @@ using namespace cocod::gemm;
 constexpr int EPI_WARPS = 8, GROUPED_THREADS = 128 + 32 * EPI_WARPS;
 constexpr int RING = 5;                                             // stages of 32 KB
 constexpr int OUT_BYTES = 2 * 4096;                                 // staging of an epilogue warp: twice 32 rows of 128 bytes
+constexpr int AHEAD = 4;                                            // tiles that the scheduler may be ahead
 constexpr int GROUPED_SMEM = RING * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 512;
 constexpr int ERR_OFFSETS = 100;                                    // error_flag: the offsets do not rise from 0 to the number of rows
 constexpr int ERR_LABEL = 101;                                      // error_flag: a label beyond the vocabulary
@@ -172,12 +174,13 @@ template <int CG, int TN, bool A_MN, bool B_MN> __host__ __device__ constexpr ui
 }
 
 // ------------------------------------------------------------------------------------------ tiles
-struct Tile {
-    int g;             // group
+struct __align__(16) Tile {
+    int g;             // group; negative: there are no more tiles
     int m0, m1;        // rows form: first row of the tile, end of the group (both counted from row0).  Weight form: first row of out_g, -
     int n0;            // first column
     int kb0, kb1;      // blocks of the reduction (64 each)
     int split;
+    int unused;
 };
 
 // Rows of group g within this launch, counted from row0; any content of offsets gives a range inside [0, rows].
@@ -319,7 +322,9 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     uint8_t *outs = smem + RING * STAGE_BYTES;
     uint64_t *bars = reinterpret_cast<uint64_t *>(outs + EPI_WARPS * OUT_BYTES);
     const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + RING), accf0 = smem_u32(bars + 2 * RING), acce0 = smem_u32(bars + 2 * RING + 2);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * RING + 4);
+    const uint32_t tilef0 = smem_u32(bars + 2 * RING + 4), tilee0 = smem_u32(bars + 2 * RING + 4 + AHEAD);
+    Tile *tiles = reinterpret_cast<Tile *>(bars + 2 * RING + 4 + 2 * AHEAD);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(tiles + AHEAD);
     volatile int *abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cta_rank<CG>();
@@ -344,6 +349,10 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             mbar_init(accf0 + 8 * s, 1);
             mbar_init(acce0 + 8 * s, EPI_WARPS * CG);
         }
+        for (int s = 0; s < AHEAD; ++s) {
+            mbar_init(tilef0 + 8 * s, 1);
+            mbar_init(tilee0 + 8 * s, 1 + (rank == 0 ? 1 : 0) + EPI_WARPS);      // producer, issuer, epilogue
+        }
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
@@ -358,6 +367,20 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     pdl_wait();
 
     int failed = 0;
+    // The next tile of a role's warp, in the scheduler's order; false at the end of the list (or when a wait gives up).
+    unsigned turn = 0;
+    auto next_tile = [&](Tile &t) {
+        const unsigned s = turn % AHEAD;
+        if (!__all_sync(0xffffffffu, mbar_wait(tilef0 + 8 * s, (turn / AHEAD) & 1, abort, limit))) { failed = 4; return false; }
+        ++turn;
+        const int4 *src = reinterpret_cast<const int4 *>(tiles + s);
+        const int4 a = src[0], b = src[1];
+        t.g = a.x; t.m0 = a.y; t.m1 = a.z; t.n0 = a.w;
+        t.kb0 = b.x; t.kb1 = b.y; t.split = b.z;
+        __syncwarp();
+        if (lane == 0) mbar_arrive_local(tilee0 + 8 * s);
+        return t.g >= 0;
+    };
     if (warp >= 4) {
         take_registers<224>();
         // ---- epilogue: rows 32 (warp % 4) .. + 31 of the CTA's 128, columns of one half of the tile
@@ -365,7 +388,6 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         uint8_t *staging = outs + (warp - 4) * OUT_BYTES;
         constexpr int HALF = TN / 2, CHUNK = is_f32(OUT) ? 32 : 64, CHUNKS = HALF / CHUNK;      // a chunk: 128 bytes of a row
         constexpr int ES = is_f32(OUT) ? 4 : 2, PER = 16 / ES;
-        Walker<TM, TN, WG> walk(p, lane);
         Tile t{};
         unsigned ai = 0, stores = 0;
         // The staging is used in turns: a thread that writes one of the two buffers has seen the store before last read.
@@ -414,8 +436,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 else mbar_arrive_cluster(map_to_rank(acce0 + 8 * a, 0));
             }
         };
-        for (int i = cluster; walk.find(i, t); i += clusters) {
-            if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
+        while (next_tile(t)) {
             const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
             const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
             const int z = WG ? t.split * p.groups + t.g : t.split;
@@ -423,6 +444,12 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * HALF;
             float scale = 1.0f;
             if (!WG && p.row_scale != nullptr && lane < valid) scale = p.row_scale[m + lane];
+            float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
+            int label = -1;
+            if (is_vocab(OUT) && lane < valid) {
+                label = p.label[m + lane];
+                if (label >= 0) ref = p.ref[m + lane];
+            }
             uint32_t acc[CHUNKS][CHUNK];
             for (int k0 = t.kb0; k0 < t.kb1; k0 += part_blocks(OUT), ++ai) {
                 const unsigned a = ai & 1;
@@ -451,12 +478,6 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                     for (int j = 0; j < CHUNK; ++j) acc[c][j] = 0u;
-            }
-            float ref = 0.0f, sum = 0.0f, most = __uint_as_float(0xff800000u);
-            int label = -1;
-            if (is_vocab(OUT) && lane < valid) {
-                label = p.label[m + lane];
-                if (label >= 0) ref = p.ref[m + lane];
             }
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
@@ -494,18 +515,10 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         give_registers<56>();
         if (warp == 0) {
             // ---- producer
-            Walker<TM, TN, WG> walk(p, lane);
-            if (blockIdx.x == 0 && p.error_flag != nullptr) {
-                bool bad = false;
-                for (int g = lane; g < p.groups; g += 32)
-                    bad |= p.offsets[g + 1] < p.offsets[g] || (g == 0 && p.offsets[0] != 0) || (g == p.groups - 1 && p.offsets[p.groups] != p.total_rows);
-                if (bad) atomicExch(p.error_flag, ERR_OFFSETS);
-            }
             Tile t;
             unsigned it = 0;
             int last_g = -1;
-            for (int i = cluster; walk.find(i, t); i += clusters) {
-                if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
+            while (next_tile(t)) {
                 if (lane == 0 && !p.debug_no_loads) {
                     const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
                     if (WG && t.g != last_g) {
@@ -540,11 +553,9 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             // ---- issuer of the products
             constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B_MN>();
             constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B_MN ? 2048u : 32u;
-            Walker<TM, TN, WG> walk(p, lane);
             Tile t;
             unsigned it = 0, ai = 0;
-            for (int i = cluster; walk.find(i, t); i += clusters) {
-                if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
+            while (next_tile(t)) {
                 if (t.kb0 == t.kb1) continue;
                 if (lane == 0) {
                     for (int k0 = t.kb0; k0 < t.kb1 && !failed; ++ai) {
@@ -569,6 +580,29 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     }
                 }
                 if (__any_sync(0xffffffffu, failed)) break;
+            }
+        } else if (warp == 3) {
+            // ---- scheduler
+            if (blockIdx.x == 0 && p.error_flag != nullptr) {
+                bool bad = false;
+                for (int g = lane; g < p.groups; g += 32)
+                    bad |= p.offsets[g + 1] < p.offsets[g] || (g == 0 && p.offsets[0] != 0) || (g == p.groups - 1 && p.offsets[p.groups] != p.total_rows);
+                if (bad) atomicExch(p.error_flag, ERR_OFFSETS);
+            }
+            Walker<TM, TN, WG> walk(p, lane);
+            for (int i = cluster;; i += clusters) {
+                Tile t{};
+                if (!walk.find(i, t)) t.g = -1;
+                else if (is_vocab(OUT) && p.redo != nullptr && !redo_tile<TM>(p, t, lane)) continue;
+                const unsigned s = turn % AHEAD;
+                if (turn >= AHEAD && !__all_sync(0xffffffffu, mbar_wait(tilee0 + 8 * s, (turn / AHEAD - 1) & 1, abort, limit))) { failed = 5; break; }
+                ++turn;
+                if (lane == 0) {
+                    reinterpret_cast<int4 *>(tiles + s)[0] = make_int4(t.g, t.m0, t.m1, t.n0);
+                    reinterpret_cast<int4 *>(tiles + s)[1] = make_int4(t.kb0, t.kb1, t.split, 0);
+                    mbar_arrive_local(tilef0 + 8 * s);
+                }
+                if (t.g < 0) break;
             }
         }
     }
