@@ -47,14 +47,15 @@ enum Out {
     OUT_BF16 = 0,
     OUT_F32 = 1,
     OUT_ADD_F32 = 2,       // added to what is there
+    OUT_PART = 5,          // fp32 parts of a sum that will be bf16
     // rows form, the vocabulary's logits l = h w^T: nothing of l is written, but for every row r with reference c_r and label t_r
     OUT_VOCAB = 3,         // u[r][v] = exp(l - c_r) in bf16, 0 at v = t_r, and for each half of a tile sum_v u (in fp32) and max_v l, v != t_r
     OUT_VOCAB_SUMS = 4,    // only the sums and maxima
 };
-__host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32; }
+__host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32 || out == OUT_PART; }
 __host__ __device__ constexpr bool is_vocab(int out) { return out == OUT_VOCAB || out == OUT_VOCAB_SUMS; }
 // Blocks of 64 that the tensor cores sum at a time.
-__host__ __device__ constexpr int part_blocks(int out) { return is_f32(out) ? 12 : is_vocab(out) ? 32 : 1 << 24; }
+__host__ __device__ constexpr int part_blocks(int out) { return out == OUT_F32 || out == OUT_ADD_F32 ? 12 : is_vocab(out) ? 32 : 1 << 24; }
 
 struct GroupedParams {
     const int *offsets;                // [groups + 1], device
@@ -92,9 +93,11 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)      // a shared::cluster address
+// Arrive at a barrier of the pair, given by its shared::cluster address.  It orders this thread's accesses within the CTA only:
+// what is handed over is tensor memory, whose reads are complete.  (Release at cluster scope took 1200 to 2000 clocks.)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync()
 {
@@ -387,46 +390,53 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         uint8_t *staging = outs + (warp - 4) * OUT_BYTES;
         constexpr int HALF = TN / 2, CHUNK = is_f32(OUT) ? 32 : 64, CHUNKS = HALF / CHUNK;      // a chunk: 128 bytes of a row
-        constexpr int ES = is_f32(OUT) ? 4 : 2, PER = 16 / ES;
+        constexpr int ES = is_f32(OUT) ? 4 : 2, PER = 16 / ES, AT_ONCE = CHUNKS < 2 ? 1 : 2;
         Tile t{};
-        unsigned ai = 0, stores = 0;
-        // The staging is used in turns: a thread that writes one of the two buffers has seen the store before last read.
-        auto stage_and_store = [&](const uint32_t (&r)[CHUNK], int col, int m, int valid, int z) {
-            uint8_t *stage = staging + (stores++ & 1) * 4096;
-            if (lane == 0) tma_store_wait_read<1>();
+        unsigned ai = 0;
+        // Up to two chunks at a time go through the warp's staging: one wait for the store engine's reads, one fence.
+        auto stage_and_store = [&](const uint32_t (&r0)[CHUNK], const uint32_t (&r1)[CHUNK], int col, int m, int valid, int z) {
+            if (lane == 0) tma_store_wait_read<0>();
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint4 v;
-                if (is_f32(OUT)) {
-                    const int b = j * 4;
-                    v = make_uint4(r[b], r[b + 1], r[b + 2], r[b + 3]);
-                } else {
-                    const int b = j * 8 < CHUNK ? j * 8 : 0;
-                    v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
-                                   pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
+            for (int h = 0; h < AT_ONCE; ++h) {
+                const uint32_t(&r)[CHUNK] = h == AT_ONCE - 1 ? r1 : r0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint4 v;
+                    if (is_f32(OUT)) {
+                        const int b = j * 4;
+                        v = make_uint4(r[b], r[b + 1], r[b + 2], r[b + 3]);
+                    } else {
+                        const int b = j * 8 < CHUNK ? j * 8 : 0;
+                        v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
+                                       pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
+                    }
+                    *reinterpret_cast<uint4 *>(staging + h * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) = v;
                 }
-                *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = v;
             }
             if (WG || valid >= 32) {
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(stage), col, m, z);
-                    else tma_store_3d(&map_out, smem_u32(stage), col, m, z);
+#pragma unroll
+                    for (int h = 0; h < AT_ONCE; ++h) {
+                        if (col + h * CHUNK >= p.n) break;
+                        if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, z);
+                        else tma_store_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, z);
+                    }
+                    tma_store_commit();
                 }
             } else {
                 __syncwarp();
                 uint8_t *dst = static_cast<uint8_t *>(p.out) + (t.split * p.split_stride + (long long)m * p.ld_out + col) * ES;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int row = q * 4 + (lane >> 3), piece = lane & 7;
-                    const uint4 v = *reinterpret_cast<const uint4 *>(stage + row * 128 + ((piece ^ (row & 7)) << 4));
-                    if (row < valid && col + piece * PER < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + piece * 16) = v;
+                for (int q = 0; q < 8 * AT_ONCE; ++q) {
+                    const int row = (q & 7) * 4 + (lane >> 3), piece = lane & 7, c = (q >> 3) * CHUNK + piece * PER;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(staging + (q >> 3) * 4096 + row * 128 + ((piece ^ (row & 7)) << 4));
+                    if (row < valid && col + c < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + c * ES) = v;
                 }
                 __syncwarp();
             }
-            if (lane == 0) tma_store_commit();
         };
         auto release = [&](unsigned a) {          // this warp has read the accumulator
             tc_fence_before();
@@ -482,9 +492,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const int col = col0 + c * CHUNK;
-                if (col >= p.n) continue;
                 uint32_t (&r)[CHUNK] = acc[c];
-                if (is_vocab(OUT)) {
+                if (is_vocab(OUT) && col < p.n) {
                     // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
                     const int end = label < 0 ? 0 : p.n - col, at = label - col;
                     if (__any_sync(0xffffffffu, end < CHUNK || (at >= 0 && at < CHUNK))) {
@@ -501,12 +510,13 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         r[j] = __float_as_uint(e);
                     }
                     sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                    if (OUT == OUT_VOCAB_SUMS) continue;
-                } else if (!WG && p.row_scale != nullptr) {
+                } else if (!WG && !is_vocab(OUT) && p.row_scale != nullptr) {
 #pragma unroll
                     for (int j = 0; j < CHUNK; ++j) r[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(r[j]) * scale);
                 }
-                stage_and_store(r, col, m, valid, z);
+                const int c0 = c + 1 - AT_ONCE;           // AT_ONCE chunks, this one the last, are stored together
+                if (OUT != OUT_VOCAB_SUMS && (c + 1) % AT_ONCE == 0 && col0 + c0 * CHUNK < p.n)
+                    stage_and_store(acc[c0 < 0 ? 0 : c0], r, col0 + c0 * CHUNK, m, valid, z);
             }
             if (is_vocab(OUT) && col0 < p.n && lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
         }

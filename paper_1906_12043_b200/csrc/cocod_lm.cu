@@ -172,13 +172,12 @@ Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t de
 }
 
 template <bool WG, bool B_MN>
-cudaError_t launch_form(const Cut &c, int out, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GroupedParams &p, cudaStream_t s)
+cudaError_t launch_form(const Cut &c, const Matrix &out, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GroupedParams &p, cudaStream_t s)
 {
-    if (c.pair)
-        return out == OUT_BF16 ? launch_tiles<2, 256, WG, B_MN, OUT_BF16>(a, b, o, p, c.tiles, s)
-                               : launch_tiles<2, 256, WG, B_MN, OUT_F32>(a, b, o, p, c.tiles, s);
-    return out == OUT_BF16 ? launch_tiles<1, 128, WG, B_MN, OUT_BF16>(a, b, o, p, c.tiles, s)
-                           : launch_tiles<1, 128, WG, B_MN, OUT_F32>(a, b, o, p, c.tiles, s);
+#define FORM(OUT) (c.pair ? launch_tiles<2, 256, WG, B_MN, OUT>(a, b, o, p, c.tiles, s) : launch_tiles<1, 128, WG, B_MN, OUT>(a, b, o, p, c.tiles, s))
+    if (out.elem == 4) return FORM(OUT_F32);
+    return c.splits > 1 ? FORM(OUT_PART) : FORM(OUT_BF16);
+#undef FORM
 }
 
 #define TRY_CUDA(call) do { if ((call) != cudaSuccess) { cudaGetLastError(); return COCOD_ERR_CUDA; } ++h->launches; } while (0)
@@ -217,8 +216,8 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window
     p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits; p.row_scale = row_scale;
     p.out = const_cast<void *>(dst.data); p.ld_out = dst.ld; p.split_stride = dst.stride;
     p.error_flag = h->flag;
-    TRY_CUDA(form == FORWARD ? (launch_form<false, false>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s))
-                             : (launch_form<false, true>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s)));
+    TRY_CUDA(form == FORWARD ? (launch_form<false, false>(cut, out, a, b, o, p, s))
+                             : (launch_form<false, true>(cut, out, a, b, o, p, s)));
     if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), M * cols, cut.splits, out, M, M, cols, s);
     return COCOD_OK;
 }
@@ -250,7 +249,7 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, i
                            : launch_tiles<1, 128, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)));
         return COCOD_OK;
     }
-    TRY_CUDA((launch_form<true, true>(cut, dst.elem == 2 ? OUT_BF16 : OUT_F32, a, b, o, p, s)));
+    TRY_CUDA((launch_form<true, true>(cut, out, a, b, o, p, s)));
     if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), (int64_t)G * rows * cols, cut.splits, out, rows, (int64_t)G * rows, cols, s);
     return COCOD_OK;
 }

@@ -134,20 +134,32 @@ struct FinishParams {
     int second;                        // second pass: no row is looked at again if *v.redo_any is 0
 };
 
-// loss[g] = sum of the rows' losses with their shares, by one block; one warp per group, sums in a fixed order.
+// loss[g] = sum of the rows' losses with their shares, by one block in a fixed order: a group's rows are shared out over as many
+// warps as there are for each group.
 __device__ __forceinline__ void vocab_mean(const VocabRows &p, const float *row_loss, float *loss)
 {
-    const int lane = threadIdx.x & 31;
-    for (int g = threadIdx.x >> 5; g < p.groups; g += FINISH_WARPS) {
-        const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
+    __shared__ float part[FINISH_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per = p.groups >= FINISH_WARPS ? 1 : FINISH_WARPS / p.groups, at_once = FINISH_WARPS / per;
+    for (int g0 = 0; g0 < p.groups; g0 += at_once) {
+        const int g = g0 + warp / per;
         float s = 0.0f;
+        if (g < p.groups && warp < at_once * per) {
+            const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
 #pragma unroll 8
-        for (int r = lo + lane; r < hi; r += 32) {
-            const float v = __ldcg(row_loss + r);
-            s += p.row_weight == nullptr ? v : v == 0.0f ? 0.0f : p.row_weight[r] * v;
+            for (int r = lo + (warp % per) * 32 + lane; r < hi; r += 32 * per) {
+                const float v = __ldcg(row_loss + r);
+                s += p.row_weight == nullptr ? v : v == 0.0f ? 0.0f : p.row_weight[r] * v;
+            }
         }
         s = warp_sum(s);
-        if (lane == 0) loss[g] = p.row_weight != nullptr ? s : s * p.share[g];
+        __syncthreads();
+        if (lane == 0) part[warp] = s;
+        __syncthreads();
+        if (lane == 0 && warp % per == 0 && g < p.groups && warp < at_once * per) {
+            for (int i = 1; i < per; ++i) s += part[warp + i];
+            loss[g] = p.row_weight != nullptr ? s : s * p.share[g];
+        }
     }
 }
 
