@@ -370,16 +370,26 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     pdl_wait();
 
     int failed = 0;
-    // The next tile of a role's warp, in the scheduler's order; false at the end of the list (or when a wait gives up).
+    // The next tile in the scheduler's order, for one thread (the producer, the issuer) or a whole warp; false at the end of the
+    // list (or when a wait gives up).
     unsigned turn = 0;
-    auto next_tile = [&](Tile &t) {
-        const unsigned s = turn % AHEAD;
-        if (!__all_sync(0xffffffffu, mbar_wait(tilef0 + 8 * s, (turn / AHEAD) & 1, abort, limit))) { failed = 4; return false; }
-        ++turn;
-        const int4 *src = reinterpret_cast<const int4 *>(tiles + s);
+    auto read_tile = [&](Tile &t) {
+        const int4 *src = reinterpret_cast<const int4 *>(tiles + turn++ % AHEAD);
         const int4 a = src[0], b = src[1];
         t.g = a.x; t.m0 = a.y; t.m1 = a.z; t.n0 = a.w;
         t.kb0 = b.x; t.kb1 = b.y; t.split = b.z;
+    };
+    auto next_tile = [&](Tile &t) {
+        const unsigned s = turn % AHEAD;
+        if (!mbar_wait(tilef0 + 8 * s, (turn / AHEAD) & 1, abort, limit)) { failed = 4; return false; }
+        read_tile(t);
+        mbar_arrive_local(tilee0 + 8 * s);
+        return t.g >= 0;
+    };
+    auto next_tile_warp = [&](Tile &t) {
+        const unsigned s = turn % AHEAD;
+        if (!__all_sync(0xffffffffu, mbar_wait(tilef0 + 8 * s, (turn / AHEAD) & 1, abort, limit))) { failed = 4; return false; }
+        read_tile(t);
         __syncwarp();
         if (lane == 0) mbar_arrive_local(tilee0 + 8 * s);
         return t.g >= 0;
@@ -446,7 +456,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 else mbar_arrive_cluster(map_to_rank(acce0 + 8 * a, 0));
             }
         };
-        while (next_tile(t)) {
+        while (next_tile_warp(t)) {
             const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
             const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
             const int z = WG ? t.split * p.groups + t.g : t.split;
@@ -524,72 +534,66 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     } else {
         give_registers<56>();
         if (warp == 0) {
-            // ---- producer
+            // ---- producer (one thread: a warp's own synchronisation at every tile cost the ring 300 clocks)
             Tile t;
             unsigned it = 0;
             int last_g = -1;
-            while (next_tile(t)) {
-                if (lane == 0 && !p.debug_no_loads) {
-                    const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
-                    if (WG && t.g != last_g) {
-                        acquire_map(ma);
-                        acquire_map(mb);
-                        last_g = t.g;
+            while (lane == 0 && !failed && next_tile(t)) {
+                if (p.debug_no_loads) continue;
+                const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
+                if (WG && t.g != last_g) {
+                    acquire_map(ma);
+                    acquire_map(mb);
+                    last_g = t.g;
+                }
+                const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
+                for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+                    const unsigned s = it % RING, use = it / RING;
+                    if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * STAGE_BYTES);
+                    const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
+                    const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+                    if (A_MN) {
+                        load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
+                        load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
+                    } else {
+                        load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
                     }
-                    const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
-                    for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-                        const unsigned s = it % RING, use = it / RING;
-                        if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
-                        if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * STAGE_BYTES);
-                        const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
-                        const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
-                        if (A_MN) {
-                            load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
-                            load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
-                        } else {
-                            load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
-                        }
-                        if (B_MN) {
-                            load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
-                            load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
-                        } else {
-                            load_tile<CG>(db, mb, bar, kb * BK, n0, zb);
-                        }
+                    if (B_MN) {
+                        load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
+                        load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
+                    } else {
+                        load_tile<CG>(db, mb, bar, kb * BK, n0, zb);
                     }
                 }
-                if (__any_sync(0xffffffffu, failed)) break;
             }
         } else if (warp == 1 && rank == 0) {
-            // ---- issuer of the products
+            // ---- issuer of the products (one thread)
             constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B_MN>();
             constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B_MN ? 2048u : 32u;
             Tile t;
             unsigned it = 0, ai = 0;
-            while (next_tile(t)) {
-                if (t.kb0 == t.kb1) continue;
-                if (lane == 0) {
-                    for (int k0 = t.kb0; k0 < t.kb1 && !failed; ++ai) {
-                        const int k1 = min(k0 + part_blocks(OUT), t.kb1);
-                        const unsigned a = ai & 1, use = ai >> 1;
-                        if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) { failed = 2; break; }
+            while (lane == 0 && !failed && next_tile(t)) {
+                for (int k0 = t.kb0; k0 < t.kb1; ++ai) {
+                    const int k1 = min(k0 + part_blocks(OUT), t.kb1);
+                    const unsigned a = ai & 1, use = ai >> 1;
+                    if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) { failed = 2; break; }
+                    tc_fence_after();
+                    for (int kb = k0; kb < k1; ++kb, ++it) {
+                        const unsigned s = it % RING;
+                        if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
                         tc_fence_after();
-                        for (int kb = k0; kb < k1; ++kb, ++it) {
-                            const unsigned s = it % RING;
-                            if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
-                            tc_fence_after();
-                            const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+                        const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
 #pragma unroll
-                            for (int k = 0; k < BK / UMMA_K; ++k)
-                                umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B_MN), idesc,
-                                           (kb > k0 || k > 0) ? 1u : 0u);
-                            umma_commit_g<CG>(empty0 + 8 * s);
-                        }
-                        if (failed) break;
-                        umma_commit_g<CG>(accf0 + 8 * a);
-                        k0 = k1;
+                        for (int k = 0; k < BK / UMMA_K; ++k)
+                            umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B_MN), idesc,
+                                       (kb > k0 || k > 0) ? 1u : 0u);
+                        umma_commit_g<CG>(empty0 + 8 * s);
                     }
+                    if (failed) break;
+                    umma_commit_g<CG>(accf0 + 8 * a);
+                    k0 = k1;
                 }
-                if (__any_sync(0xffffffffu, failed)) break;
             }
         } else if (warp == 3) {
             // ---- scheduler

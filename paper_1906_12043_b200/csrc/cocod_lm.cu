@@ -87,7 +87,7 @@ join_parts(const float *parts, long long part_stride, int count, void *out, long
         const long long r = i / quads, c = (i - r * quads) * 4;
         const float *src = parts + r * n + c;
         float4 s = *reinterpret_cast<const float4 *>(src);
-#pragma unroll 8
+#pragma unroll 16
         for (int k = 1; k < count; ++k) {
             const float4 v = *reinterpret_cast<const float4 *>(src + k * part_stride);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;

@@ -178,6 +178,15 @@ vocab_finish(const FinishParams p)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int first = blockIdx.x * FINISH_ROWS, row = first + lane;        // counted from row0
     float s = 0.0f, most = __uint_as_float(0xff800000u);
+    int t = -1;                        // what the first warp needs later is asked for now
+    float own = 0.0f, ref = 0.0f, share = 0.0f;
+    if (warp == 0 && row < p.rows) {
+        t = p.v.label[p.row0 + row];
+        own = p.v.own[p.row0 + row];
+        ref = p.v.ref[p.row0 + row];
+        const int g = group_of(p.v.offsets, p.v.groups, p.row0 + row);
+        if (p.rho != nullptr && g >= 0) share = p.v.row_weight != nullptr ? p.v.row_weight[p.row0 + row] : p.v.share[g];
+    }
     if (row < p.rows) {
 #pragma unroll 8
         for (int i = warp; i < p.n_sums; i += FINISH_WARPS) {
@@ -192,14 +201,14 @@ vocab_finish(const FinishParams p)
         float rho = 0.0f, scale = 0.0f;
         int again = 0;
         if (row < p.rows) {
-            const int r = p.row0 + row, t = p.v.label[r];
+            const int r = p.row0 + row;
             float loss = 0.0f;
             if (t >= 0) {
+#pragma unroll
                 for (int i = 1; i < FINISH_WARPS; ++i) {
                     s += part[i][lane].x;
                     most = fmaxf(most, part[i][lane].y);
                 }
-                const float own = p.v.own[r], ref = p.v.ref[r];
                 const float et = own == ref ? 1.0f : expf(own - ref);
                 loss = own == ref ? log1pf(s) : logf(s + et) + (ref - own);
                 if (!p.second && !(s <= SUM_LIMIT)) {
@@ -208,8 +217,7 @@ vocab_finish(const FinishParams p)
                     *p.v.redo_any = 1;
                 }
                 if (p.rho != nullptr) {
-                    const float a = p.v.row_weight != nullptr ? p.v.row_weight[r] : p.v.share[group_of(p.v.offsets, p.v.groups, r)];
-                    rho = a / (s + et);
+                    rho = share / (s + et);
                     const __nv_bfloat16 entry = __float2bfloat16_rn(-s);
                     const float kept = -__bfloat162float(entry);
                     p.u[row * p.ldu + t] = entry;
