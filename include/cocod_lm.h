@@ -42,7 +42,7 @@ enum { COCOD_BF16 = 0, COCOD_F32 = 1 };      /* type of a result */
 
 #define COCOD_LM_MAX_GROUPS 1024
 
-/* Scratch for tensor maps and flags, about 300 KB.  Errors: INVALID, OOM, CUDA. */
+/* Allocates the kernels' scratch (tensor maps, flags, parts of sums), about 20 MB.  Errors: INVALID, OOM, CUDA. */
 int cocod_lm_create(cocod_lm_handle **out);
 int cocod_lm_destroy(cocod_lm_handle *h);
 
@@ -60,20 +60,17 @@ int64_t cocod_lm_launch_count(const cocod_lm_handle *h);
  * input_grad     dx[m][i]   = sum_j dy[m][j] w[g][j][i]       dy: M x n, dx: M x k
  * weight_grad    dw[g][j][i] = sum_{m in g} dy[m][j] x[m][i]  dw: G x [n][k], written completely (an empty group: 0)
  *
- * out_type: COCOD_BF16 or COCOD_F32.  workspace is used to cut long reductions with few results into parts whose sums are
- * joined in a fixed order; cocod_grouped_workspace says how much a call can use (0 is allowed: no parts). */
+ * out_type: COCOD_BF16 or COCOD_F32.  Long reductions may be cut into parts whose sums are joined in a fixed order; results do not
+ * change from call to call. */
 int cocod_grouped_forward(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
                           const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t w_stride,
-                          void *y, int64_t ldy, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+                          void *y, int64_t ldy, int out_type, cocod_stream_t stream);
 int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
                              const void *dy, int64_t lddy, const void *w, int64_t ldw, int64_t w_stride,
-                             void *dx, int64_t lddx, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+                             void *dx, int64_t lddx, int out_type, cocod_stream_t stream);
 int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k,
                               const void *dy, int64_t lddy, const void *x, int64_t ldx,
-                              void *dw, int64_t lddw, int64_t dw_stride, int out_type,
-                              void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
-enum { COCOD_GROUPED_FORWARD = 0, COCOD_GROUPED_INPUT_GRAD = 1, COCOD_GROUPED_WEIGHT_GRAD = 2 };
-int64_t cocod_grouped_workspace(int which, int G, int64_t M, int64_t n, int64_t k);
+                              void *dw, int64_t lddw, int64_t dw_stride, int out_type, cocod_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Activations in 8 bits.  A block is 128 consecutive columns of a row (the last one of a row may be shorter).  With amax
@@ -98,7 +95,7 @@ int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *o
                                      const void *dy, int64_t lddy, const int8_t *q, int64_t ldq, const uint8_t *scales,
                                      void *dw, int64_t lddw, int64_t dw_stride, int out_type,
                                      void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
-int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k);
+int64_t cocod_grouped_packed_workspace(int64_t M, int64_t k);
 
 /* ---------------------------------------------------------------------------------------------
  * Softmax cross-entropy over a vocabulary of V entries, each group with an output matrix w[g] (V x D) of its own:

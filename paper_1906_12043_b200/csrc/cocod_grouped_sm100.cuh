@@ -26,6 +26,9 @@
 // the difference.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
 // with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
+// The number of tiles is seldom a multiple of the CTA pairs.  The tiles of the last, incomplete wave (all of them when there are few)
+// are cut along the reduction into as many parts as keep every pair busy; a part leaves as fp32 in scratch, at most one per
+// pair, and join_parts adds the parts of a tile up in a fixed order.  5.2 waves of tiles take 5.2 and not 6 times a tile.
 // Every wait is bounded, as in cocod_gemm_sm100.cuh.
 #pragma once
 #include "cocod_gemm_sm100.cuh"
@@ -47,15 +50,14 @@ enum Out {
     OUT_BF16 = 0,
     OUT_F32 = 1,
     OUT_ADD_F32 = 2,       // added to what is there
-    OUT_PART = 5,          // fp32 parts of a sum that will be bf16
     // rows form, the vocabulary's logits l = h w^T: nothing of l is written, but for every row r with reference c_r and label t_r
     OUT_VOCAB = 3,         // u[r][v] = exp(l - c_r) in bf16, 0 at v = t_r, and for each half of a tile sum_v u (in fp32) and max_v l, v != t_r
     OUT_VOCAB_SUMS = 4,    // only the sums and maxima
 };
-__host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32 || out == OUT_PART; }
+__host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32; }
 __host__ __device__ constexpr bool is_vocab(int out) { return out == OUT_VOCAB || out == OUT_VOCAB_SUMS; }
 // Blocks of 64 that the tensor cores sum at a time.
-__host__ __device__ constexpr int part_blocks(int out) { return out == OUT_F32 || out == OUT_ADD_F32 ? 12 : is_vocab(out) ? 32 : 1 << 24; }
+__host__ __device__ constexpr int part_blocks(int out) { return is_f32(out) ? 12 : is_vocab(out) ? 32 : 1 << 24; }
 
 struct GroupedParams {
     const int *offsets;                // [groups + 1], device
@@ -65,11 +67,13 @@ struct GroupedParams {
     int n;                             // columns of out
     int kdim;                          // rows form: length of the reduction.  Weight form: rows of out_g
     int tiles_n;
-    int splits;                        // the reduction is cut into this many parts; part s writes out at index s (weight form: s * groups + g)
-    void *out;                         // rows form: for the rows of a partial tile
-    long long ld_out, split_stride;    // elements
+    int band;                          // tile rows that are walked together, column by column
+    int max_parts;                     // a tile of the last wave is cut into at most this many parts (1: none is)
+    void *out;                         // for the rows of a partial tile, and for join_parts
+    long long ld_out, out_stride;      // elements; out_stride (weight form): between groups
     const float *row_scale;            // rows form, optional: factor of every row (0: the row is 0 whatever the product is)
     const CUtensorMap *group_maps;     // weight form: A and B of group g at 2 g and 2 g + 1
+    const int *order;                  // weight form: the groups, those with the most rows first
     // OUT_VOCAB, OUT_VOCAB_SUMS (rows counted from row0)
     const float *ref;                  // c_r
     const int *label;                  // t_r; negative: the row takes no part (u = 0)
@@ -182,7 +186,7 @@ struct __align__(16) Tile {
     int m0, m1;        // rows form: first row of the tile, end of the group (both counted from row0).  Weight form: first row of out_g, -
     int n0;            // first column
     int kb0, kb1;      // blocks of the reduction (64 each)
-    int split;
+    int slot;          // negative: a whole tile; else a part of one, number `slot` in the scratch
     int unused;
 };
 
@@ -213,23 +217,62 @@ __device__ __forceinline__ void write_group_map(const CUtensorMap &whole, const 
                  ::"l"(dst), "r"(smem_u32(&map)) : "memory");
 }
 
-// Within a group, tiles go in bands of eight tile rows, column by column: the CTAs that run at the same time share their
-// operands through L2.
-__device__ __forceinline__ void in_band(int i, int tiles_m, int tiles_n, int &tm, int &tn)
+// The place of group g when the groups are ordered by their rows, most first (one warp).
+__device__ __forceinline__ int group_rank(const GroupedParams &p, int g)
 {
-    const int band = i / (8 * tiles_n), r = i - band * 8 * tiles_n;
-    const int high = min(8, tiles_m - band * 8);
-    tn = r / high;
-    tm = band * 8 + r - tn * high;
+    int lo, hi, rank = 0;
+    group_range(p, g, lo, hi);
+    const int mine = hi - lo;
+    for (int j = threadIdx.x & 31; j < p.groups; j += 32) {
+        group_range(p, j, lo, hi);
+        rank += hi - lo > mine || (hi - lo == mine && j < g);
+    }
+    return __reduce_add_sync(0xffffffffu, rank);
 }
 
-// The tile list of a launch, read in rising order by a whole warp.  In the rows form a group has as many tile rows as its
-// rows fill; 32 groups are looked at together, one per lane.
+// Within a group, tiles go in bands of tile rows, column by column: the CTAs that run at the same time share their operands
+// through L2.
+__device__ __forceinline__ void in_band(int i, int high, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int band = i / (high * tiles_n), r = i - band * high * tiles_n;
+    const int here = min(high, tiles_m - band * high);
+    tn = r / here;
+    tm = band * high + r - tn * here;
+}
+
+// The list of a launch, read in rising order by a whole warp: first the tiles of the complete waves, then the parts of the last
+// wave's tiles, then (weight form) the tiles of groups without rows.  In the rows form a group has as many tile rows as its rows
+// fill; 32 groups are looked at together, one per lane.
 template <int TM, int TN, bool WG> struct Walker {
     const GroupedParams &p;
     int lane, gb = 0, base = 0, lo = 0, hi = 0, cnt = 0, incl = 0, total = 0;
-    __device__ Walker(const GroupedParams &params, int lane_) : p(params), lane(lane_)
+    int whole = 0x7fffffff, cut = 0, parts = 1;
+    __device__ Walker(const GroupedParams &params, int lane_, int clusters) : p(params), lane(lane_)
     {
+        int tiles = 0;
+        if (WG) {
+            for (int g0 = 0; g0 < p.groups; g0 += 32) {
+                if (g0 + lane < p.groups) group_range(p, g0 + lane, lo, hi);
+                tiles += __popc(__ballot_sync(0xffffffffu, g0 + lane < p.groups && hi > lo));
+            }
+            tiles *= (p.kdim + TM - 1) / TM * p.tiles_n;
+            whole = tiles;
+        } else if (p.max_parts > 1) {
+            for (gb = 0; gb < p.groups; gb += 32) {
+                load();
+                tiles += total;
+            }
+            gb = 0;
+            whole = tiles;
+        }
+        if (p.max_parts > 1) {
+            const int rest = tiles % clusters;
+            parts = rest ? min(clusters / rest, p.max_parts) : 1;
+            if (parts > 1) {
+                cut = rest;
+                whole = tiles - rest;
+            }
+        }
         if (!WG) load();
     }
     __device__ void load()
@@ -238,7 +281,7 @@ template <int TM, int TN, bool WG> struct Walker {
         lo = hi = cnt = 0;
         if (g < p.groups) {
             group_range(p, g, lo, hi);
-            cnt = (hi - lo + TM - 1) / TM * p.tiles_n * p.splits;
+            cnt = (hi - lo + TM - 1) / TM * p.tiles_n;
         }
         incl = cnt;
 #pragma unroll
@@ -250,13 +293,27 @@ template <int TM, int TN, bool WG> struct Walker {
     }
     __device__ bool find(int t, Tile &tile)
     {
-        int i, tiles_m;
+        int part = 0, of = 1, tiles_m;
+        tile.slot = -1;
+        if (t >= whole) {
+            const int u = t - whole;
+            if (u < cut * parts) {
+                part = u % parts;
+                of = parts;
+                tile.slot = u;
+                t = whole + u / parts;
+            } else if (WG) {
+                t = whole + cut + u - cut * parts;
+            } else {
+                return false;
+            }
+        }
         if (WG) {
             tiles_m = (p.kdim + TM - 1) / TM;
-            const int per = tiles_m * p.tiles_n * p.splits;
-            tile.g = t / per;
-            if (tile.g >= p.groups) return false;
-            i = t - tile.g * per;
+            const int per = tiles_m * p.tiles_n, at = t / per;
+            if (at >= p.groups) return false;
+            tile.g = p.order[at];
+            t -= at * per;
             group_range(p, tile.g, lo, hi);
         } else {
             while (t >= base + total) {
@@ -267,16 +324,13 @@ template <int TM, int TN, bool WG> struct Walker {
             }
             const int l = __ffs(__ballot_sync(0xffffffffu, t < base + incl)) - 1;
             tile.g = gb + l;
-            i = t - base - __shfl_sync(0xffffffffu, incl - cnt, l);
+            t -= base + __shfl_sync(0xffffffffu, incl - cnt, l);
             tile.m0 = __shfl_sync(0xffffffffu, lo, l);
             tile.m1 = __shfl_sync(0xffffffffu, hi, l);
             tiles_m = (tile.m1 - tile.m0 + TM - 1) / TM;
         }
-        const int per_split = tiles_m * p.tiles_n;
-        tile.split = i / per_split;
-        i -= tile.split * per_split;
         int tm, tn;
-        in_band(i, tiles_m, p.tiles_n, tm, tn);
+        in_band(t, p.band, tiles_m, p.tiles_n, tm, tn);
         tile.n0 = tn * TN;
         int blocks;
         if (WG) {
@@ -287,8 +341,8 @@ template <int TM, int TN, bool WG> struct Walker {
             tile.m0 += tm * TM;
             blocks = (p.kdim + BK - 1) / BK;
         }
-        tile.kb0 = (int)((long long)blocks * tile.split / p.splits);
-        tile.kb1 = (int)((long long)blocks * (tile.split + 1) / p.splits);
+        tile.kb0 = (int)((long long)blocks * part / of);
+        tile.kb1 = (int)((long long)blocks * (part + 1) / of);
         return true;
     }
 };
@@ -311,11 +365,12 @@ __device__ __forceinline__ float exp2_approx(float x)
 // ------------------------------------------------------------------------------------------ kernel
 // Tensor maps (all three-dimensional, innermost dimension contiguous, 128-byte swizzle):
 //   A, B with the reduction innermost: boxes of 64 x 128 rows; A or B with it second: boxes of 64 x 64, two per operand.
-//   out: boxes of 32 rows x 128 bytes; third index = group (weight form) or part of the reduction.
+//   out: boxes of 32 rows x 128 bytes; third index = group (weight form).  parts: the scratch as an fp32 matrix of TN columns, TM
+//   rows for each part, boxes of 32 x 32.
 template <int CG, int TN, bool WG, bool B_MN, int OUT>
 __global__ void __launch_bounds__(GROUPED_THREADS, 1)
 grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-             const __grid_constant__ CUtensorMap map_out, const GroupedParams p)
+             const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_parts, const GroupedParams p)
 {
     constexpr int TM = 128 * CG;
     constexpr bool A_MN = WG;
@@ -377,7 +432,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const int4 *src = reinterpret_cast<const int4 *>(tiles + turn++ % AHEAD);
         const int4 a = src[0], b = src[1];
         t.g = a.x; t.m0 = a.y; t.m1 = a.z; t.n0 = a.w;
-        t.kb0 = b.x; t.kb1 = b.y; t.split = b.z;
+        t.kb0 = b.x; t.kb1 = b.y; t.slot = b.z;
     };
     auto next_tile = [&](Tile &t) {
         const unsigned s = turn % AHEAD;
@@ -404,26 +459,25 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         Tile t{};
         unsigned ai = 0;
         // Up to two chunks at a time go through the warp's staging: one wait for the store engine's reads, one fence.
-        auto stage_and_store = [&](const uint32_t (&r0)[CHUNK], const uint32_t (&r1)[CHUNK], int col, int m, int valid, int z) {
+        auto staging_free = [&]() {
             if (lane == 0) tma_store_wait_read<0>();
             __syncwarp();
+        };
+        auto stage_f32 = [&](const uint32_t (&r)[32], int h) {
 #pragma unroll
-            for (int h = 0; h < AT_ONCE; ++h) {
-                const uint32_t(&r)[CHUNK] = h == AT_ONCE - 1 ? r1 : r0;
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<uint4 *>(staging + h * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                    make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+        };
+        auto stage_bf16 = [&](const uint32_t (&r)[64], int h) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint4 v;
-                    if (is_f32(OUT)) {
-                        const int b = j * 4;
-                        v = make_uint4(r[b], r[b + 1], r[b + 2], r[b + 3]);
-                    } else {
-                        const int b = j * 8 < CHUNK ? j * 8 : 0;
-                        v = make_uint4(pack_bf16x2(__uint_as_float(r[b]), __uint_as_float(r[b + 1])), pack_bf16x2(__uint_as_float(r[b + 2]), __uint_as_float(r[b + 3])),
-                                       pack_bf16x2(__uint_as_float(r[b + 4]), __uint_as_float(r[b + 5])), pack_bf16x2(__uint_as_float(r[b + 6]), __uint_as_float(r[b + 7])));
-                    }
-                    *reinterpret_cast<uint4 *>(staging + h * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) = v;
-                }
-            }
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<uint4 *>(staging + h * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                    make_uint4(pack_bf16x2(__uint_as_float(r[8 * j]), __uint_as_float(r[8 * j + 1])), pack_bf16x2(__uint_as_float(r[8 * j + 2]), __uint_as_float(r[8 * j + 3])),
+                               pack_bf16x2(__uint_as_float(r[8 * j + 4]), __uint_as_float(r[8 * j + 5])), pack_bf16x2(__uint_as_float(r[8 * j + 6]), __uint_as_float(r[8 * j + 7])));
+        };
+        // The staged chunks to out: row m, column col.
+        auto store = [&](int col, int m, int valid) {
             if (WG || valid >= 32) {
                 fence_async_smem();
                 __syncwarp();
@@ -431,14 +485,14 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                     for (int h = 0; h < AT_ONCE; ++h) {
                         if (col + h * CHUNK >= p.n) break;
-                        if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, z);
-                        else tma_store_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, z);
+                        if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, t.g);
+                        else tma_store_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, WG ? t.g : 0);
                     }
                     tma_store_commit();
                 }
             } else {
                 __syncwarp();
-                uint8_t *dst = static_cast<uint8_t *>(p.out) + (t.split * p.split_stride + (long long)m * p.ld_out + col) * ES;
+                uint8_t *dst = static_cast<uint8_t *>(p.out) + ((long long)m * p.ld_out + col) * ES;
 #pragma unroll
                 for (int q = 0; q < 8 * AT_ONCE; ++q) {
                     const int row = (q & 7) * 4 + (lane >> 3), piece = lane & 7, c = (q >> 3) * CHUNK + piece * PER;
@@ -459,7 +513,6 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         while (next_tile_warp(t)) {
             const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
             const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
-            const int z = WG ? t.split * p.groups + t.g : t.split;
             const int col0 = t.n0 + half * HALF;
             const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * HALF;
             float scale = 1.0f;
@@ -470,14 +523,14 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 label = p.label[m + lane];
                 if (label >= 0) ref = p.ref[m + lane];
             }
-            uint32_t acc[CHUNKS][CHUNK];
+            uint32_t acc[HALF];
             for (int k0 = t.kb0; k0 < t.kb1; k0 += part_blocks(OUT), ++ai) {
                 const unsigned a = ai & 1;
                 if (!__all_sync(0xffffffffu, mbar_wait(accf0 + 8 * a, (ai >> 1) & 1, abort, limit + limit / 2))) { failed = 3; break; }
                 tc_fence_after();
 #pragma unroll
                 for (int c = 0; c < HALF; c += 32) {
-                    uint32_t(&sum)[32] = *reinterpret_cast<uint32_t (*)[32]>(&acc[c / CHUNK][c % CHUNK]);
+                    uint32_t(&sum)[32] = *reinterpret_cast<uint32_t (*)[32]>(&acc[c]);
                     if (k0 == t.kb0) {
                         tmem_ld32(tacc + a * TN + c, sum);
                     } else {
@@ -492,17 +545,36 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 release(a);
             }
             if (failed) break;
-            if (valid <= 0 || (OUT == OUT_ADD_F32 && t.kb0 == t.kb1)) continue;
+            if (valid <= 0 || (OUT == OUT_ADD_F32 && t.kb0 == t.kb1 && t.slot < 0)) continue;
             if (t.kb0 == t.kb1) {
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
+                for (int j = 0; j < HALF; ++j) acc[j] = 0u;
+            }
+            if (!WG && !is_vocab(OUT) && p.row_scale != nullptr) {
 #pragma unroll
-                    for (int j = 0; j < CHUNK; ++j) acc[c][j] = 0u;
+                for (int j = 0; j < HALF; ++j) acc[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(acc[j]) * scale);
+            }
+            if (!is_vocab(OUT) && t.slot >= 0) {         // a part: fp32, in the scratch
+#pragma unroll
+                for (int c = 0; c < HALF; c += 64) {
+                    staging_free();
+                    stage_f32(*reinterpret_cast<const uint32_t (*)[32]>(&acc[c]), 0);
+                    stage_f32(*reinterpret_cast<const uint32_t (*)[32]>(&acc[c + 32]), 1);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            tma_store_3d(&map_parts, smem_u32(staging) + h * 4096, half * HALF + c + h * 32, t.slot * TM + (int)rank * 128 + quarter * 32, 0);
+                        tma_store_commit();
+                    }
+                }
+                continue;
             }
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const int col = col0 + c * CHUNK;
-                uint32_t (&r)[CHUNK] = acc[c];
+                uint32_t (&r)[CHUNK] = *reinterpret_cast<uint32_t (*)[CHUNK]>(&acc[c * CHUNK]);
                 if (is_vocab(OUT) && col < p.n) {
                     // logits that do not count become -inf: the label's, those behind the vocabulary, rows without a label
                     const int end = label < 0 ? 0 : p.n - col, at = label - col;
@@ -520,13 +592,14 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         r[j] = __float_as_uint(e);
                     }
                     sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                } else if (!WG && !is_vocab(OUT) && p.row_scale != nullptr) {
-#pragma unroll
-                    for (int j = 0; j < CHUNK; ++j) r[j] = scale == 0.0f ? 0u : __float_as_uint(__uint_as_float(r[j]) * scale);
                 }
-                const int c0 = c + 1 - AT_ONCE;           // AT_ONCE chunks, this one the last, are stored together
-                if (OUT != OUT_VOCAB_SUMS && (c + 1) % AT_ONCE == 0 && col0 + c0 * CHUNK < p.n)
-                    stage_and_store(acc[c0 < 0 ? 0 : c0], r, col0 + c0 * CHUNK, m, valid, z);
+                if (OUT == OUT_VOCAB_SUMS) continue;
+                const int h = c % AT_ONCE;
+                if (col - h * CHUNK >= p.n) continue;
+                if (h == 0) staging_free();
+                if constexpr (is_f32(OUT)) stage_f32(r, h);
+                else stage_bf16(r, h);
+                if (h == AT_ONCE - 1) store(col - h * CHUNK, m, valid);
             }
             if (is_vocab(OUT) && col0 < p.n && lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
         }
@@ -603,7 +676,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     bad |= p.offsets[g + 1] < p.offsets[g] || (g == 0 && p.offsets[0] != 0) || (g == p.groups - 1 && p.offsets[p.groups] != p.total_rows);
                 if (bad) atomicExch(p.error_flag, ERR_OFFSETS);
             }
-            Walker<TM, TN, WG> walk(p, lane);
+            Walker<TM, TN, WG> walk(p, lane, clusters);
             for (int i = cluster;; i += clusters) {
                 Tile t{};
                 if (!walk.find(i, t)) t.g = -1;
@@ -613,7 +686,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 ++turn;
                 if (lane == 0) {
                     reinterpret_cast<int4 *>(tiles + s)[0] = make_int4(t.g, t.m0, t.m1, t.n0);
-                    reinterpret_cast<int4 *>(tiles + s)[1] = make_int4(t.kb0, t.kb1, t.split, 0);
+                    reinterpret_cast<int4 *>(tiles + s)[1] = make_int4(t.kb0, t.kb1, t.slot, 0);
                     mbar_arrive_local(tilef0 + 8 * s);
                 }
                 if (t.g < 0) break;
@@ -631,6 +704,39 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     __syncthreads();
     if (CG == 2) cluster_sync();
     if (warp == 2) tmem_dealloc_g<CG>(tmem_base, 2 * TN);
+}
+
+// The tiles that were cut: block (x, y) adds the parts of the x-th of them up, for 256 groups of four results, and writes them to out.
+template <int TM, int TN, bool WG, int OUT>
+__global__ void __launch_bounds__(256)
+join_parts(const GroupedParams p, const float *scratch, int clusters)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    Walker<TM, TN, WG> walk(p, threadIdx.x & 31, clusters);
+    Tile t;
+    if ((int)blockIdx.x >= walk.cut || !walk.find(walk.whole + blockIdx.x * walk.parts, t)) return;
+    constexpr int QUADS = TN / 4;
+    const int i = blockIdx.y * 256 + threadIdx.x, row = i / QUADS, c = (i % QUADS) * 4;
+    if (t.m0 + row >= t.m1 || t.n0 + c >= p.n) return;
+    const float *src = scratch + (long long)t.slot * (TM * TN) + row * TN + c;
+    float4 s = *reinterpret_cast<const float4 *>(src);
+#pragma unroll 16
+    for (int k = 1; k < walk.parts; ++k) {
+        const float4 v = *reinterpret_cast<const float4 *>(src + (long long)k * (TM * TN));
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const long long at = (WG ? t.g * p.out_stride : 0) + (t.m0 + row) * p.ld_out + t.n0 + c;
+    if (OUT == OUT_BF16) {
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + at) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+    } else {
+        float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at);
+        if (OUT == OUT_ADD_F32) {
+            const float4 v = *dst;
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        *dst = s;
+    }
 }
 
 }  // namespace lm

@@ -12,6 +12,8 @@
 
 struct cocod_lm {
     CUtensorMap *group_maps = nullptr;     // device: two per group
+    int *order = nullptr;                  // device: the groups by size
+    float *parts = nullptr;                // device: parts of tiles, 256 x 256 for each pair of CTAs
     int *flag = nullptr;                   // device: what the kernels met
     long long launches = 0;
 };
@@ -59,25 +61,27 @@ bool encode(CUtensorMap *m, const Matrix &x, uint64_t cols, uint64_t rows, uint6
 }
 
 // ------------------------------------------------------------------------------------------ small kernels
-// Block 2 g + i: the tensor map of group g's rows of A (i = 0) or B.
+// Block 2 g + i: the tensor map of group g's rows of A (i = 0) or B; and the group's place by size.
 __global__ void __launch_bounds__(32)
 make_group_maps(const __grid_constant__ CUtensorMap whole_a, const __grid_constant__ CUtensorMap whole_b, const char *a, long long lda_bytes,
-                const char *b, long long ldb_bytes, const GroupedParams p, CUtensorMap *maps)
+                const char *b, long long ldb_bytes, const GroupedParams p, CUtensorMap *maps, int *order)
 {
     __shared__ __align__(128) CUtensorMap map;
     pdl_launch_dependents();
     pdl_wait();
     const int g = blockIdx.x >> 1;
-    if (blockIdx.x & 1) write_group_map(whole_b, b, ldb_bytes, p, g, maps + 2 * g + 1, map);
-    else write_group_map(whole_a, a, lda_bytes, p, g, maps + 2 * g, map);
+    if (blockIdx.x & 1) {
+        write_group_map(whole_b, b, ldb_bytes, p, g, maps + 2 * g + 1, map);
+    } else {
+        write_group_map(whole_a, a, lda_bytes, p, g, maps + 2 * g, map);
+        const int rank = group_rank(p, g);
+        if (threadIdx.x == 0) order[rank] = g;
+    }
 }
 
-// The parts of a reduction that was cut: out = part 0 + part 1 + ... in this order, for `rows` rows of n columns (n a
-// multiple of 4); row r of the result is row r % per_group of group r / per_group.
-template <bool BF16_OUT>
+// out = bf16(sums), for `rows` rows of n columns (n a multiple of 4); row r of the result is row r % per_group of group r / per_group.
 __global__ void __launch_bounds__(256)
-join_parts(const float *parts, long long part_stride, int count, void *out, long long ld, long long group_stride, long long per_group,
-           long long rows, int n)
+round_sums(const float *sums, bf16 *out, long long ld, long long group_stride, long long per_group, long long rows, int n)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -85,66 +89,29 @@ join_parts(const float *parts, long long part_stride, int count, void *out, long
     const long long total = rows * quads;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
         const long long r = i / quads, c = (i - r * quads) * 4;
-        const float *src = parts + r * n + c;
-        float4 s = *reinterpret_cast<const float4 *>(src);
-#pragma unroll 16
-        for (int k = 1; k < count; ++k) {
-            const float4 v = *reinterpret_cast<const float4 *>(src + k * part_stride);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        const long long at = (r / per_group) * group_stride + (r % per_group) * ld + c;
-        if (BF16_OUT) *reinterpret_cast<uint2 *>(static_cast<bf16 *>(out) + at) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
-        else *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = s;
+        const float4 s = *reinterpret_cast<const float4 *>(sums + r * n + c);
+        *reinterpret_cast<uint2 *>(out + (r / per_group) * group_stride + (r % per_group) * ld + c) =
+            make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
     }
 }
 
 // ------------------------------------------------------------------------------------------ launching the products
-template <int CG, int TN, bool WG, bool B_MN, int OUT>
-cudaError_t launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const GroupedParams &p, int64_t tiles, cudaStream_t s)
-{
-    static bool configured[MAX_DEVICES] = {};
-    const int dev = current_device(), sms = sm_count();
-    if (dev < 0 || sms < 2) return cudaErrorInvalidDevice;
-    auto kernel = grouped_gemm<CG, TN, WG, B_MN, OUT>;
-    if (!configured[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GROUPED_SMEM);
-        // The epilogue warps wait for the registers that the others give up: the launch has to hold their sum.
-        cudaFuncAttributes attr{};
-        if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, kernel);
-        if (e != cudaSuccess) return e;
-        if (attr.numRegs < 168) return cudaErrorLaunchOutOfResources;
-        configured[dev] = true;
-    }
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(tiles, sms / CG) * CG));
-    cfg.blockDim = dim3(GROUPED_THREADS);
-    cfg.dynamicSmemBytes = GROUPED_SMEM;
-    cfg.stream = s;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = CG;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, out, p);
-}
+#define TRY_CUDA(call) do { if ((call) != cudaSuccess) { cudaGetLastError(); return COCOD_ERR_CUDA; } ++h->launches; } while (0)
 
-enum Form { FORWARD = COCOD_GROUPED_FORWARD, INPUT_GRAD = COCOD_GROUPED_INPUT_GRAD, WEIGHT_GRAD = COCOD_GROUPED_WEIGHT_GRAD };
+enum Form { FORWARD, INPUT_GRAD, WEIGHT_GRAD };
 
 // How a product is cut into tiles and parts.
 struct Cut {
     bool pair;             // 256 x 256 tiles by pairs of CTAs, else 128 x 128 by single ones
-    int splits;
+    int max_parts;         // of a tile of the last wave
     int64_t tiles;         // at most
+    int band;              // GroupedParams::band
 };
 // rows x cols results (rows form: `groups` groups share the rows; weight form: per group), reductions of `depth` (weight form: on
 // average).  The choice minimises an estimate in microseconds, fitted to measurements: a launch 3.5 (pairs 4.5), a tile 1.5 (2.0)
 // and for each block of 64 of its reduction 0.16 (0.28), or, when all SMs load at the same time, 0.34 (0.40): 4096 x 4096 x 4096
-// takes 153 us in single tiles and 98 in pairs, 128 x 18944 x 512 7.4 and 10.0.  A cut reduction pays for writing its parts and
-// for joining them.
-Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t depth, int64_t workspace_bytes)
+// takes 153 us in single tiles and 98 in pairs, 128 x 18944 x 512 7.4 and 10.0.  Joining the parts of tiles is another launch.
+Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t depth, bool parts_allowed)
 {
     Cut best{};
     double best_cost = 1e300;
@@ -156,40 +123,82 @@ Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t de
         const double likely = form == WEIGHT_GRAD || groups == 1 ? (double)most
                                                                  : std::max((double)std::min(groups, rows), (double)rows / t + 0.5 * groups);
         const int64_t col_tiles = ceil_div(cols, t), blocks = std::max<int64_t>(1, ceil_div(depth, 64));
-        const int64_t out_bytes = (form == WEIGHT_GRAD ? groups * rows : rows) * cols * 4;
-        for (int64_t splits = 1; splits <= 64 && (splits == 1 || (blocks / splits >= 4 && splits * out_bytes <= workspace_bytes)); splits *= 2) {
-            const double tiles = likely * col_tiles * splits, waves = std::ceil(tiles / slots), busy = std::min(1.0, tiles / slots);
-            const double block = pair ? std::max(0.28, 0.40 * busy) : std::max(0.16, 0.34 * busy);
-            const double cost = (pair ? 4.5 : 3.5) + waves * (ceil_div(blocks, splits) * block + (pair ? 2.0 : 1.5)) +
-                                (splits > 1 ? 2.5 + splits * out_bytes / 4e6 : 0.0);
-            if (cost < best_cost) {
+        const int64_t tiles = std::max<int64_t>(1, (int64_t)(likely * col_tiles)), full = tiles / slots, rest = tiles % slots;
+        const double busy = std::min(1.0, (double)tiles / slots);
+        const double block = pair ? std::max(0.28, 0.40 * busy) : std::max(0.16, 0.34 * busy), tile = pair ? 2.0 : 1.5;
+        // A's tile rows of a band stay in L2 while B passes by; where all of B fits, or A's do not, eight are enough
+        const int64_t row_bytes = t * depth * 2;
+        const bool b_fits = cols * depth * 2 <= (40 << 20);
+        const int band = (int)std::max<int64_t>(8, std::min<int64_t>(b_fits ? 8 : (40 << 20) / std::max<int64_t>(row_bytes, 1), 1 << 16));
+        // (joining takes about 0.09 us for each part: more parts than this cost more than they save)
+        const int64_t sensible = (int64_t)std::sqrt(blocks * (pair ? 0.28 : 0.16) / 0.09) + 1, bound = std::min(blocks / 4, std::max<int64_t>(sensible, 2));
+        const int64_t most_parts = rest > 0 && parts_allowed ? std::min(slots / rest, bound) : 1;
+        for (int cut = 0; cut < 2; ++cut) {
+            const int64_t parts = cut ? most_parts : 1;
+            if (cut && parts < 2) break;
+            const double busy_rest = std::min(1.0, (double)rest * parts / slots);
+            const double block_rest = pair ? std::max(0.28, 0.40 * busy_rest) : std::max(0.16, 0.34 * busy_rest);
+            const double cost = (pair ? 4.5 : 3.5) + full * (blocks * block + tile) + (rest ? ceil_div(blocks, parts) * block_rest + tile : 0.0) +
+                                (parts > 1 ? 3.0 + parts * 0.09 + rest * parts * t * t * 4 / 8e6 : 0.0);
+            // A cut has to promise a sixth: under load the GPU is at its power limit, where idle SMs leave the busy ones a higher clock
+            // (4096 x 4096 x 4096: 3.5 instead of 4 waves, and 105 us instead of 101)
+            if (cost * (parts > 1 ? 7.0 / 6.0 : 1.0) < best_cost) {
                 best_cost = cost;
-                best = Cut{pair != 0, (int)splits, most * col_tiles * splits};
+                // (the kernel counts the tiles itself and cuts by what it finds)
+                best = Cut{pair != 0, cut ? (int)std::max<int64_t>(bound, 2) : 1, most * col_tiles, band};
             }
         }
     }
     return best;
 }
 
-template <bool WG, bool B_MN>
-cudaError_t launch_form(const Cut &c, const Matrix &out, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GroupedParams &p, cudaStream_t s)
+template <int CG, int TN, bool WG, bool B_MN, int OUT>
+int launch_tiles(cocod_lm *h, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const GroupedParams &p, int64_t tiles, cudaStream_t s)
 {
-#define FORM(OUT) (c.pair ? launch_tiles<2, 256, WG, B_MN, OUT>(a, b, o, p, c.tiles, s) : launch_tiles<1, 128, WG, B_MN, OUT>(a, b, o, p, c.tiles, s))
-    if (out.elem == 4) return FORM(OUT_F32);
-    return c.splits > 1 ? FORM(OUT_PART) : FORM(OUT_BF16);
-#undef FORM
+    static bool configured[MAX_DEVICES] = {};
+    const int dev = current_device(), sms = sm_count();
+    if (dev < 0 || sms < 2) return COCOD_ERR_CUDA;
+    auto kernel = grouped_gemm<CG, TN, WG, B_MN, OUT>;
+    if (!configured[dev]) {
+        // The epilogue warps wait for the registers that the others give up: the launch has to hold their sum.
+        cudaFuncAttributes attr{};
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GROUPED_SMEM) != cudaSuccess ||
+            cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs < 168) {
+            cudaGetLastError();
+            return COCOD_ERR_CUDA;
+        }
+        configured[dev] = true;
+    }
+    const int clusters = (int)(p.max_parts > 1 ? sms / CG : std::min<int64_t>(tiles, sms / CG));
+    CUtensorMap parts = out;
+    if (p.max_parts > 1 && !encode(&parts, Matrix{h->parts, TN, 0, 4}, TN, (uint64_t)clusters * 128 * CG, 1, 32)) return COCOD_ERR_CUDA;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)clusters * CG);
+    cfg.blockDim = dim3(GROUPED_THREADS);
+    cfg.dynamicSmemBytes = GROUPED_SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    TRY_CUDA(cudaLaunchKernelEx(&cfg, kernel, a, b, out, parts, p));
+    if constexpr (!is_vocab(OUT)) {
+        // a wave has at most half its tiles cut, so that every one gets two parts
+        if (p.max_parts > 1)
+            TRY_CUDA(launch_dependent(true, join_parts<128 * CG, TN, WG, OUT>, dim3((unsigned)std::min<int64_t>(tiles, clusters / 2), 128 * CG * TN / 1024),
+                                      dim3(256), 0, s, p, static_cast<const float *>(h->parts), clusters));
+    }
+    return COCOD_OK;
 }
 
-#define TRY_CUDA(call) do { if ((call) != cudaSuccess) { cudaGetLastError(); return COCOD_ERR_CUDA; } ++h->launches; } while (0)
-
-int join(cocod_lm *h, const float *parts, int64_t part_stride, int count, const Matrix &out, int64_t per_group, int64_t rows, int64_t n, cudaStream_t s)
+template <bool WG, bool B_MN, int OUT>
+int launch_form(cocod_lm *h, const Cut &c, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GroupedParams &p, cudaStream_t s)
 {
-    const int64_t quads = rows * (n / 4);
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(quads, 256), 8 * (int64_t)sm_count()));
-    void *dst = const_cast<void *>(out.data);
-    TRY_CUDA(out.elem == 2 ? launch_dependent(true, join_parts<true>, grid, dim3(256), 0, s, parts, (long long)part_stride, count, dst, (long long)out.ld, (long long)out.stride, (long long)per_group, (long long)rows, (int)n)
-                           : launch_dependent(true, join_parts<false>, grid, dim3(256), 0, s, parts, (long long)part_stride, count, dst, (long long)out.ld, (long long)out.stride, (long long)per_group, (long long)rows, (int)n));
-    return COCOD_OK;
+    return c.pair ? launch_tiles<2, 256, WG, B_MN, OUT>(h, a, b, o, p, c.tiles, s) : launch_tiles<1, 128, WG, B_MN, OUT>(h, a, b, o, p, c.tiles, s);
 }
 
 // Which rows of the batch a call takes: row0 .. row0 + rows - 1 of total (A, out and row_scale start at row0).
@@ -199,59 +208,48 @@ struct Window {
 
 // rows form: out (M x cols) = A (M x depth) times B_g (cols x depth for FORWARD, depth x cols for INPUT_GRAD)
 int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window &win, int64_t cols, int64_t depth, const Matrix &A, const Matrix &B,
-             const Matrix &out, const float *row_scale, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+             const Matrix &out, const float *row_scale, cudaStream_t s)
 {
     const int64_t M = win.rows;
     if (M == 0) return COCOD_OK;
-    const Cut cut = choose_cut(form, G, M, cols, depth, workspace_bytes);
-    Matrix dst = out;
-    if (cut.splits > 1) dst = Matrix{workspace, cols, M * cols, 4};
+    const Cut cut = choose_cut(form, G, M, cols, depth, true);
     CUtensorMap a, b, o;
     const bool ok = encode(&a, A, depth, M, 1, 128) &&
-                    (form == FORWARD ? encode(&b, B, depth, cols, G, 128) : encode(&b, B, cols, depth, G, 64)) &&
-                    encode(&o, dst, cols, M, cut.splits, 32);
+                    (form == FORWARD ? encode(&b, B, depth, cols, G, 128) : encode(&b, B, cols, depth, G, 64)) && encode(&o, out, cols, M, 1, 32);
     if (!ok) return COCOD_ERR_CUDA;
     GroupedParams p{};
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)depth;
-    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits; p.row_scale = row_scale;
-    p.out = const_cast<void *>(dst.data); p.ld_out = dst.ld; p.split_stride = dst.stride;
+    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = cut.max_parts; p.row_scale = row_scale;
+    p.out = const_cast<void *>(out.data); p.ld_out = out.ld;
     p.error_flag = h->flag;
-    TRY_CUDA(form == FORWARD ? (launch_form<false, false>(cut, out, a, b, o, p, s))
-                             : (launch_form<false, true>(cut, out, a, b, o, p, s)));
-    if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), M * cols, cut.splits, out, M, M, cols, s);
-    return COCOD_OK;
+    if (form == FORWARD)
+        return out.elem == 2 ? launch_form<false, false, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<false, false, OUT_F32>(h, cut, a, b, o, p, s);
+    return out.elem == 2 ? launch_form<false, true, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<false, true, OUT_F32>(h, cut, a, b, o, p, s);
 }
 
 // weight form: out_g (rows x cols) = sum over the group's rows m of A[m][.]^T B[m][.]
-// (add: added to what out, fp32, holds;  maps_ready: a kernel before this one has written the groups' maps)
+// (add: added to what out, fp32, holds;  maps_ready: a kernel before this one has written the groups' maps and order)
 int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
-                const Matrix &out, bool add, bool maps_ready, void *workspace, int64_t workspace_bytes, cudaStream_t s)
+                const Matrix &out, bool add, bool maps_ready, cudaStream_t s)
 {
     const int64_t M = win.rows;
-    if (add) workspace_bytes = 0;
-    const Cut cut = choose_cut(WEIGHT_GRAD, G, rows, cols, ceil_div(std::max<int64_t>(M, 1), G), workspace_bytes);
-    Matrix dst = out, a_rows = A, b_rows = B;
-    if (cut.splits > 1) dst = Matrix{workspace, cols, rows * cols, 4};
+    const Cut cut = choose_cut(WEIGHT_GRAD, G, rows, cols, ceil_div(std::max<int64_t>(M, 1), G), true);
+    Matrix a_rows = A, b_rows = B;
     if (M == 0) a_rows.data = b_rows.data = h->group_maps;      // nothing is read
     CUtensorMap a, b, o;
     if (!encode(&a, a_rows, rows, std::max<int64_t>(M, 1), 1, 64) || !encode(&b, b_rows, cols, std::max<int64_t>(M, 1), 1, 64) ||
-        !encode(&o, dst, cols, rows, (uint64_t)G * cut.splits, 32))
+        !encode(&o, out, cols, rows, (uint64_t)G, 32))
         return COCOD_ERR_CUDA;
     GroupedParams p{};
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
-    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.splits = cut.splits;
-    p.group_maps = h->group_maps; p.error_flag = h->flag;
+    p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = cut.max_parts;
+    p.out = const_cast<void *>(out.data); p.ld_out = out.ld; p.out_stride = out.stride;
+    p.group_maps = h->group_maps; p.order = h->order; p.error_flag = h->flag;
     if (!maps_ready)
         TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, b, static_cast<const char *>(A.data),
-                                  (long long)A.ld * 2, static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps));
-    if (add) {
-        TRY_CUDA((cut.pair ? launch_tiles<2, 256, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)
-                           : launch_tiles<1, 128, true, true, OUT_ADD_F32>(a, b, o, p, cut.tiles, s)));
-        return COCOD_OK;
-    }
-    TRY_CUDA((launch_form<true, true>(cut, out, a, b, o, p, s)));
-    if (cut.splits > 1) return join(h, static_cast<const float *>(workspace), (int64_t)G * rows * cols, cut.splits, out, rows, (int64_t)G * rows, cols, s);
-    return COCOD_OK;
+                                  (long long)A.ld * 2, static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps, h->order));
+    if (add) return launch_form<true, true, OUT_ADD_F32>(h, cut, a, b, o, p, s);
+    return out.elem == 2 ? launch_form<true, true, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<true, true, OUT_F32>(h, cut, a, b, o, p, s);
 }
 
 // ------------------------------------------------------------------------------------------ vocabulary
@@ -260,7 +258,6 @@ struct VocabLayout {
     int64_t label, own, ref, share, any;       // whole batch: byte offsets
     int64_t rho, redo, sums, u, hs;            // rows of one pass
     int64_t total32;                           // fp32 gradient of the weights, if it is summed over passes and wanted in bf16
-    int64_t parts;                             // what is left: parts of cut reductions
     int64_t bytes, ldu, n_sums;
 };
 VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int dw_elem, int64_t at_once)
@@ -283,7 +280,7 @@ VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int 
         l.hs = take(2 * at_once * D);
         if (at_once < M && dw_elem == 2) l.total32 = take(4 * G * V * D);
     }
-    l.parts = l.bytes = at;
+    l.bytes = at;
     return l;
 }
 // The most rows that fit, 0 if not even the fewest do.
@@ -318,7 +315,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
     v.ref = reinterpret_cast<float *>(ws + l.ref); v.share = reinterpret_cast<float *>(ws + l.share);
     v.redo_any = reinterpret_cast<int *>(ws + l.any);
     v.error_flag = h->flag;
-    const Cut cut = choose_cut(FORWARD, G, M, V, D, 0);      // by the whole batch: the passes change no sum's order
+    const Cut cut = choose_cut(FORWARD, G, M, V, D, false);  // by the whole batch: the passes change no sum's order
     const bool several = at_once < M;
     int64_t row0 = 0;
     do {                                   // (no rows at all: one pass, for the results' zeros)
@@ -332,13 +329,13 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
             return COCOD_ERR_CUDA;
         GroupedParams p{};
         p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.row0 = (int)row0; p.rows = (int)win.rows; p.n = (int)V; p.kdim = (int)D;
-        p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.splits = 1;
+        p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = 1;
         p.out = ws + l.u; p.ld_out = l.ldu; p.error_flag = h->flag;
         p.ref = v.ref + row0; p.label = v.label + row0; p.sums = reinterpret_cast<float2 *>(ws + l.sums); p.ld_sums = (int)win.rows;
         const int row_blocks = (int)ceil_div(win.rows, 8);
         TRY_CUDA(launch_dependent(true, vocab_begin, dim3(row_blocks + G), dim3(256), 0, s, u_rows, hs_rows, static_cast<const char *>(u.data),
                                   (long long)u.ld * 2, static_cast<const char *>(hs.data), (long long)hs.ld * 2, p,
-                                  grad ? h->group_maps : (CUtensorMap *)nullptr, v, row_blocks));
+                                  grad ? h->group_maps : (CUtensorMap *)nullptr, h->order, v, row_blocks));
         FinishParams f{};
         f.v = v; f.row0 = (int)row0; f.rows = (int)win.rows; f.sums = p.sums; f.ld_sums = p.ld_sums;
         f.n_sums = (int)ceil_div(V, cut.pair ? 128 : 64);
@@ -354,26 +351,24 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
             p.redo = pass ? f.redo : nullptr;
             p.redo_any = v.redo_any;
             f.second = pass;
-            if (win.rows > 0 && grad)
-                TRY_CUDA((cut.pair ? launch_tiles<2, 256, false, false, OUT_VOCAB>(a, b, o, p, cut.tiles, s)
-                                   : launch_tiles<1, 128, false, false, OUT_VOCAB>(a, b, o, p, cut.tiles, s)));
-            else if (win.rows > 0)
-                TRY_CUDA((cut.pair ? launch_tiles<2, 256, false, false, OUT_VOCAB_SUMS>(a, b, o, p, cut.tiles, s)
-                                   : launch_tiles<1, 128, false, false, OUT_VOCAB_SUMS>(a, b, o, p, cut.tiles, s)));
+            if (win.rows > 0) {
+                if (int rc = grad ? launch_form<false, false, OUT_VOCAB>(h, cut, a, b, o, p, s) : launch_form<false, false, OUT_VOCAB_SUMS>(h, cut, a, b, o, p, s))
+                    return rc;
+            }
             TRY_CUDA(launch_dependent(true, vocab_finish, finish_grid, dim3(32 * FINISH_WARPS), 0, s, f));
         }
         if (grad) {
-            char *parts = ws + l.parts;
-            const int64_t parts_bytes = workspace_bytes - l.parts;
             const Matrix dh{static_cast<const bf16 *>(grad->dh.data) + row0 * grad->dh.ld, grad->dh.ld, 0, 2};
-            if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, parts, parts_bytes, s)) return rc;
+            if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, s)) return rc;
             const Matrix dst = several && dw_elem == 2 ? Matrix{ws + l.total32, D, V * D, 4} : grad->dw;
-            if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, dst, several && row0 > 0, true, parts, parts_bytes, s)) return rc;
+            if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, dst, several && row0 > 0, true, s)) return rc;
         }
         row0 += win.rows;
     } while (row0 < M);
     if (grad && several && dw_elem == 2)
-        return join(h, reinterpret_cast<const float *>(ws + l.total32), 0, 1, grad->dw, V, G * V, D, s);
+        TRY_CUDA(launch_dependent(true, round_sums, dim3((unsigned)std::min<int64_t>(ceil_div(G * V * D / 4, 256), 8 * (int64_t)sm_count())), dim3(256), 0, s,
+                                  reinterpret_cast<const float *>(ws + l.total32), static_cast<bf16 *>(const_cast<void *>(grad->dw.data)),
+                                  (long long)grad->dw.ld, (long long)grad->dw.stride, (long long)V, (long long)(G * V), (int)D));
     return COCOD_OK;
 }
 
@@ -388,11 +383,16 @@ bool good_groups(const void *p, int64_t ld, int64_t stride, int64_t rows, int64_
     return p != nullptr && aligned16(p) && ld >= cols && (ld * elem) % 16 == 0 && ld < (1ll << 36) &&
            (G == 1 || (stride >= (rows - 1) * ld + cols && (stride * elem) % 16 == 0 && stride < (1ll << 37)));
 }
-bool good_shape(const cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *workspace, int64_t workspace_bytes)
+bool good_shape(const cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k)
 {
     return h && G >= 1 && G <= COCOD_LM_MAX_GROUPS && offsets && (reinterpret_cast<uintptr_t>(offsets) & 3u) == 0 && M >= 0 && M <= MAX_DIM &&
-           n >= 8 && n <= MAX_DIM && n % 8 == 0 && k >= 8 && k <= MAX_DIM && k % 8 == 0 && workspace_bytes >= 0 &&
-           (workspace_bytes == 0 || (workspace != nullptr && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0));
+           n >= 8 && n <= MAX_DIM && n % 8 == 0 && k >= 8 && k <= MAX_DIM && k % 8 == 0;
+}
+void lm_free(cocod_lm *h)
+{
+    void *ptrs[] = {h->group_maps, h->order, h->parts, h->flag};
+    for (void *p : ptrs) if (p) cudaFree(p);
+    delete h;
 }
 inline int size_of(int type) { return type == COCOD_BF16 ? 2 : type == COCOD_F32 ? 4 : 0; }
 
@@ -407,13 +407,13 @@ int cocod_lm_create(cocod_lm_handle **out)
     cocod_lm *h = new (std::nothrow) cocod_lm();
     if (!h) return COCOD_ERR_OOM;
     cudaError_t e = cudaMalloc((void **)&h->group_maps, 2 * COCOD_LM_MAX_GROUPS * sizeof(CUtensorMap));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->order, COCOD_LM_MAX_GROUPS * sizeof(int));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->parts, (size_t)(sm_count() / 2 + 1) * 256 * 256 * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
     if (e == cudaSuccess) e = cudaMemset(h->flag, 0, 256);
     if (e != cudaSuccess) {
         cudaGetLastError();
-        if (h->group_maps) cudaFree(h->group_maps);
-        if (h->flag) cudaFree(h->flag);
-        delete h;
+        lm_free(h);
         return e == cudaErrorMemoryAllocation ? COCOD_ERR_OOM : COCOD_ERR_CUDA;
     }
     *out = h;
@@ -424,9 +424,7 @@ int cocod_lm_destroy(cocod_lm_handle *h)
 {
     if (!h) return COCOD_OK;
     cudaDeviceSynchronize();
-    cudaFree(h->group_maps);
-    cudaFree(h->flag);
-    delete h;
+    lm_free(h);
     return COCOD_OK;
 }
 
@@ -444,52 +442,38 @@ int cocod_lm_check(cocod_lm_handle *h, cocod_stream_t stream)
 
 int64_t cocod_lm_launch_count(const cocod_lm_handle *h) { return h ? h->launches : -1; }
 
-int64_t cocod_grouped_workspace(int which, int G, int64_t M, int64_t n, int64_t k)
-{
-    if (which < FORWARD || which > WEIGHT_GRAD || G < 1 || G > COCOD_LM_MAX_GROUPS || M < 0 || M > MAX_DIM || n < 8 || n > MAX_DIM || k < 8 || k > MAX_DIM)
-        return COCOD_ERR_INVALID;
-    const int64_t any = 1ll << 62;
-    const Cut c = which == FORWARD ? choose_cut(FORWARD, G, M, n, k, any)
-                  : which == INPUT_GRAD ? choose_cut(INPUT_GRAD, G, M, k, n, any)
-                                        : choose_cut(WEIGHT_GRAD, G, n, k, ceil_div(std::max<int64_t>(M, 1), G), any);
-    if (c.splits == 1) return 0;
-    return c.splits * 4 * (which == FORWARD ? M * n : which == INPUT_GRAD ? M * k : G * n * k);
-}
-
 int cocod_grouped_forward(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *x, int64_t ldx,
-                          const void *w, int64_t ldw, int64_t w_stride, void *y, int64_t ldy, int out_type, void *workspace,
-                          int64_t workspace_bytes, cocod_stream_t stream)
+                          const void *w, int64_t ldw, int64_t w_stride, void *y, int64_t ldy, int out_type,
+                          cocod_stream_t stream)
 {
     const int es = size_of(out_type);
-    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(x, ldx, k, M, 2) ||
+    if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(y, ldy, n, M, es))
         return COCOD_ERR_INVALID;
-    return run_rows(h, FORWARD, G, offsets, Window{0, M, M}, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, nullptr, workspace,
-                    workspace_bytes, (cudaStream_t)stream);
+    return run_rows(h, FORWARD, G, offsets, Window{0, M, M}, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, nullptr, (cudaStream_t)stream);
 }
 
 int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy, int64_t lddy,
-                             const void *w, int64_t ldw, int64_t w_stride, void *dx, int64_t lddx, int out_type, void *workspace,
-                             int64_t workspace_bytes, cocod_stream_t stream)
+                             const void *w, int64_t ldw, int64_t w_stride, void *dx, int64_t lddx, int out_type,
+                             cocod_stream_t stream)
 {
     const int es = size_of(out_type);
-    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) ||
+    if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) ||
         !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(dx, lddx, k, M, es))
         return COCOD_ERR_INVALID;
-    return run_rows(h, INPUT_GRAD, G, offsets, Window{0, M, M}, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, nullptr, workspace,
-                    workspace_bytes, (cudaStream_t)stream);
+    return run_rows(h, INPUT_GRAD, G, offsets, Window{0, M, M}, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, nullptr, (cudaStream_t)stream);
 }
 
 int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy, int64_t lddy,
-                              const void *x, int64_t ldx, void *dw, int64_t lddw, int64_t dw_stride, int out_type, void *workspace,
-                              int64_t workspace_bytes, cocod_stream_t stream)
+                              const void *x, int64_t ldx, void *dw, int64_t lddw, int64_t dw_stride, int out_type,
+                              cocod_stream_t stream)
 {
     const int es = size_of(out_type);
-    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) || !good_rows(x, ldx, k, M, 2) ||
+    if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(dw, lddw, dw_stride, n, k, G, es))
         return COCOD_ERR_INVALID;
-    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false, workspace,
-                       workspace_bytes, (cudaStream_t)stream);
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false,
+                       (cudaStream_t)stream);
 }
 
 static bool good_act(const cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, int64_t ldq)
@@ -536,25 +520,21 @@ int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh
     return COCOD_OK;
 }
 
-int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k)
-{
-    const int64_t parts = cocod_grouped_workspace(COCOD_GROUPED_WEIGHT_GRAD, G, M, n, k);
-    return parts < 0 ? parts : ceil_div(M * k * 2, 256) * 256 + parts;
-}
+int64_t cocod_grouped_packed_workspace(int64_t M, int64_t k) { return M < 0 || M > MAX_DIM || k < 1 || k > MAX_DIM ? COCOD_ERR_INVALID : ceil_div(M * k * 2, 256) * 256; }
 
 int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy,
                                      int64_t lddy, const int8_t *q, int64_t ldq, const uint8_t *scales, void *dw, int64_t lddw,
                                      int64_t dw_stride, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream)
 {
     const int es = size_of(out_type);
-    if (!good_shape(h, G, offsets, M, n, k, workspace, workspace_bytes) || !es || !good_rows(dy, lddy, n, M, 2) || !good_act(h, M, k, q, ldq) ||
+    if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) || !good_act(h, M, k, q, ldq) ||
         (M > 0 && !scales) || !good_groups(dw, lddw, dw_stride, n, k, G, es))
         return COCOD_ERR_INVALID;
-    const int64_t wide = ceil_div(M * k * 2, 256) * 256;
-    if (workspace_bytes < wide) return COCOD_ERR_TOO_LARGE;
+    if (M > 0 && (!workspace || !aligned16(workspace))) return COCOD_ERR_INVALID;
+    if (workspace_bytes < M * k * 2) return COCOD_ERR_TOO_LARGE;
     if (int rc = cocod_act_unpack(h, M, k, q, ldq, scales, workspace, k, stream)) return rc;
     return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false,
-                       static_cast<char *>(workspace) + wide, workspace_bytes - wide, (cudaStream_t)stream);
+                       (cudaStream_t)stream);
 }
 
 int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_grad, int dw_type, int64_t limit)
@@ -568,12 +548,6 @@ int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_g
         const int64_t rows = vocab_rows(G, M, V, D, with_grad != 0, es, limit);
         bytes = std::min(all, vocab_layout(G, M, V, D, with_grad != 0, es, std::max<int64_t>(rows, std::min<int64_t>(M, 256))).bytes);
     }
-    if (with_grad && M > 0) {              // a short batch gains by cutting the long reductions
-        const int64_t any = 1ll << 62;
-        const Cut dh = choose_cut(INPUT_GRAD, G, M, D, V, any), dw = choose_cut(WEIGHT_GRAD, G, V, D, ceil_div(M, G), any);
-        const int64_t parts = std::max<int64_t>(dh.splits > 1 ? dh.splits * 4 * M * D : 0, dw.splits > 1 ? dw.splits * 4 * G * V * D : 0);
-        bytes += std::min(parts, std::max<int64_t>(limit - bytes, 0));
-    }
     return bytes;
 }
 
@@ -581,7 +555,7 @@ static bool good_vocab(const cocod_lm_handle *h, int G, const int32_t *offsets, 
                        const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, const float *loss,
                        const float *row_loss, const void *workspace, int64_t workspace_bytes)
 {
-    return good_shape(h, G, offsets, M, 8, D, workspace, workspace_bytes) && workspace && V >= 1 && V <= MAX_DIM && good_rows(x, ldx, D, M, 2) &&
+    return good_shape(h, G, offsets, M, 8, D) && workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0 && workspace_bytes >= 0 && V >= 1 && V <= MAX_DIM && good_rows(x, ldx, D, M, 2) &&
            good_groups(w, ldw, w_stride, V, D, G, 2) && (M == 0 || (labels && row_loss)) && loss &&
            ((reinterpret_cast<uintptr_t>(labels) | reinterpret_cast<uintptr_t>(row_weights) | reinterpret_cast<uintptr_t>(loss) |
              reinterpret_cast<uintptr_t>(row_loss)) & 3u) == 0;
@@ -630,14 +604,15 @@ int cocod_grouped_wait_selftest(int wait_ms, int pair, cocod_stream_t stream)
     CUtensorMap a, b, o;
     if (!encode(&a, m, 512, 512, 1, 128) || !encode(&b, m, 512, 512, 1, 128) || !encode(&o, m, 512, 512, 1, 32)) return COCOD_ERR_CUDA;
     GroupedParams p{};
-    p.offsets = offsets; p.groups = 1; p.total_rows = 512; p.rows = 512; p.n = 512; p.kdim = 512; p.splits = 1;
+    p.offsets = offsets; p.groups = 1; p.total_rows = 512; p.rows = 512; p.n = 512; p.kdim = 512; p.band = 8; p.max_parts = 1;
     p.tiles_n = pair ? 2 : 4; p.out = sc.p; p.ld_out = 512; p.error_flag = flag;
     p.wait_ns = (unsigned long long)wait_ms * 1000000ull;
     p.debug_no_loads = 1;
     // two CTAs (one pair), so that several tiles wait for each
-    const cudaError_t e = pair ? launch_tiles<2, 256, false, false, OUT_BF16>(a, b, o, p, 1, s) : launch_tiles<1, 128, false, false, OUT_BF16>(a, b, o, p, 2, s);
+    cocod_lm scratch;
+    const int rc = pair ? launch_tiles<2, 256, false, false, OUT_BF16>(&scratch, a, b, o, p, 1, s) : launch_tiles<1, 128, false, false, OUT_BF16>(&scratch, a, b, o, p, 2, s);
     int f = 0;
-    if (e != cudaSuccess || cudaMemcpyAsync(&f, flag, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+    if (rc != COCOD_OK || cudaMemcpyAsync(&f, flag, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaGetLastError();
         return COCOD_ERR_CUDA;
     }

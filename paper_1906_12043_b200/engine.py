@@ -72,15 +72,14 @@ SIGNATURES = {
     "cocod_lm_destroy": (_i, [_vp]),
     "cocod_lm_check": (_i, [_vp, _vp]),
     "cocod_lm_launch_count": (_i64, [_vp]),
-    "cocod_grouped_forward": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i, _vp, _i64, _vp]),
-    "cocod_grouped_input_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i, _vp, _i64, _vp]),
-    "cocod_grouped_weight_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
-    "cocod_grouped_workspace": (_i64, [_i, _i, _i64, _i64, _i64]),
+    "cocod_grouped_forward": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i, _vp]),
+    "cocod_grouped_input_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i, _vp]),
+    "cocod_grouped_weight_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i, _vp]),
     "cocod_act_pack": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
     "cocod_act_unpack": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
     "cocod_act_relu_grad": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
     "cocod_grouped_weight_grad_packed": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
-    "cocod_grouped_packed_workspace": (_i64, [_i, _i64, _i64, _i64]),
+    "cocod_grouped_packed_workspace": (_i64, [_i64, _i64]),
     "cocod_vocab_workspace": (_i64, [_i, _i64, _i64, _i64, _i, _i, _i64]),
     "cocod_vocab_loss": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "cocod_vocab_loss_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp,

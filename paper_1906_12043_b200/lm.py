@@ -20,12 +20,10 @@ import torch
 from . import engine as _E
 
 BF16, F32 = 0, 1
-FORWARD, INPUT_GRAD, WEIGHT_GRAD = 0, 1, 2
 BLOCK = 128                      # columns that share a scale in an 8-bit checkpoint
 MAX_GROUPS = 1024
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _SIZES = {torch.bfloat16: 2, torch.float32: 4, torch.int8: 1}
-PARTS_BYTES = 32 << 20           # kept by every LMOps for the parts of reductions that are cut
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -74,8 +72,6 @@ class LMOps:
             raise _E.CocodError(rc, "cocod_lm_create")
         self._h = h
         self._device = torch.cuda.current_device()
-        self._parts = torch.empty(PARTS_BYTES, dtype=torch.uint8, device=self._device)
-        self._parts_at = self._parts.data_ptr()
 
     # ------------------------------------------------------------------------------------------ arguments
     def _rows(self, t, name, M, cols, dtype=torch.bfloat16, align=16):
@@ -133,8 +129,7 @@ class LMOps:
         if out is None:
             out = x.new_empty((M, n), dtype=dtype)
         self._call("cocod_grouped_forward", self._lib.cocod_grouped_forward, G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k,
-                   *self._rows(x, "x", M, k), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, n, dtype), _TYPES[dtype],
-                   self._parts_at, PARTS_BYTES)
+                   *self._rows(x, "x", M, k), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, n, dtype), _TYPES[dtype])
         return out
 
     def grouped_input_grad(self, dy, w, offsets, out=None, out_dtype=None):
@@ -145,8 +140,7 @@ class LMOps:
         if out is None:
             out = dy.new_empty((M, k), dtype=dtype)
         self._call("cocod_grouped_input_grad", self._lib.cocod_grouped_input_grad, G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k,
-                   *self._rows(dy, "dy", M, n), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, k, dtype), _TYPES[dtype],
-                   self._parts_at, PARTS_BYTES)
+                   *self._rows(dy, "dy", M, n), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, k, dtype), _TYPES[dtype])
         return out
 
     def grouped_weight_grad(self, dy, x, offsets, out=None, out_dtype=None):
@@ -160,13 +154,13 @@ class LMOps:
             out = dy.new_empty((G, n, k), dtype=dtype)
         shape = (G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k)
         if isinstance(x, PackedActivations):
-            ws = self._scratch(self._lib.cocod_grouped_packed_workspace(G, M, n, k))
+            ws = self._scratch(self._lib.cocod_grouped_packed_workspace(M, k))
             self._call("cocod_grouped_weight_grad_packed", self._lib.cocod_grouped_weight_grad_packed, *shape, *self._rows(dy, "dy", M, n),
                        *self._rows(x.q, "x.q", M, k, torch.int8), x.scales.data_ptr(), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype],
                        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
         else:
             self._call("cocod_grouped_weight_grad", self._lib.cocod_grouped_weight_grad, *shape, *self._rows(dy, "dy", M, n),
-                       *self._rows(x, "x", M, k), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype], self._parts_at, PARTS_BYTES)
+                       *self._rows(x, "x", M, k), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype])
         return out
 
     def _scratch(self, nbytes):

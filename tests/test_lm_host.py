@@ -18,8 +18,8 @@ def test_calls_without_a_handle_are_refused(lib):
     assert lib.cocod_lm_check(None, None) == ERR_INVALID
     assert lib.cocod_lm_launch_count(None) == -1
     for f in (lib.cocod_grouped_forward, lib.cocod_grouped_input_grad):
-        assert f(None, 1, 16, 8, 8, 8, 16, 8, 16, 8, 64, 16, 8, 0, None, 0, None) == ERR_INVALID
-    assert lib.cocod_grouped_weight_grad(None, 1, 16, 8, 8, 8, 16, 8, 16, 8, 16, 8, 64, 0, None, 0, None) == ERR_INVALID
+        assert f(None, 1, 16, 8, 8, 8, 16, 8, 16, 8, 64, 16, 8, 0, None) == ERR_INVALID
+    assert lib.cocod_grouped_weight_grad(None, 1, 16, 8, 8, 8, 16, 8, 16, 8, 16, 8, 64, 0, None) == ERR_INVALID
     assert lib.cocod_grouped_weight_grad_packed(None, 1, 16, 8, 8, 8, 16, 8, 16, 16, 16, 16, 8, 64, 0, None, 0, None) == ERR_INVALID
     assert lib.cocod_act_pack(None, 1, 8, 16, 8, 16, 16, 16, None) == ERR_INVALID
     assert lib.cocod_act_unpack(None, 1, 8, 16, 16, 16, 16, 8, None) == ERR_INVALID
@@ -31,9 +31,6 @@ def test_calls_without_a_handle_are_refused(lib):
 
 
 def test_sizes_out_of_range_are_refused(lib):
-    for args in ((3, 1, 8, 8, 8), (0, 0, 8, 8, 8), (0, 1025, 8, 8, 8), (0, 1, -1, 8, 8), (0, 1, 8, 0, 8), (0, 1, 8, 8, 1 << 31)):
-        assert lib.cocod_grouped_workspace(*args) < 0
-    assert lib.cocod_grouped_packed_workspace(0, 8, 8, 8) < 0
     for args in ((0, 8, 8, 8, 1, 0, 0), (1, -1, 8, 8, 1, 0, 0), (1, 8, 0, 8, 1, 0, 0), (1, 8, 8, 12, 1, 0, 0), (1, 8, 8, 8, 1, 2, 0), (1, 8, 8, 8, 1, 0, -1)):
         assert lib.cocod_vocab_workspace(*args) < 0
 
