@@ -77,14 +77,17 @@ int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets,
  * the largest finite magnitude of the block and e the least integer >= -126 with amax <= 127 * 2^e,
  *     q = sign(x) * max(1, rint(|x| / 2^e)) for x != 0, else 0              (half to even)
  * stands for q * 2^e: within half a unit of x (within one for |x| < 2^e / 2: the sign of a value always survives, so that
- * the gate of a ReLU can be taken from it), and exact in bf16.  q = -128 marks a value that was not finite and reads as NaN.
+ * the gate of a ReLU can be taken from it), and exact in bf16.  q = -128 marks a value that was not finite; a block that holds
+ * one has scale byte 255 and reads as NaN.
  *   q      : M x k int8, row stride ldq (a multiple of 16, >= k)
- *   scales : ceil(k / 128) x M bytes, e + 127
+ *   scales : ceil(k / 128) x M bytes, e + 127 (or 255)
  *
  * act_pack       x: M x k bf16 (any k and ldx, any 2-byte alignment; 16-byte aligned rows are faster)
  * act_unpack     y: M x k bf16
  * act_relu_grad  dz = (q > 0) ? dh : 0  (NaN where q marks a value that was not finite), dh, dz: M x k bf16; dz may be dh
- * weight_grad_packed  as cocod_grouped_weight_grad, with x as the checkpoint stands for it. */
+ * weight_grad_packed  as cocod_grouped_weight_grad, with x as the checkpoint stands for it.  With a workspace of M * k * 2 bytes the
+ *   checkpoint is turned into bf16 there first, otherwise inside the product; the results are the same.
+ *   cocod_grouped_packed_workspace: the bytes with which the call is faster (0 where it is faster without). */
 int cocod_act_pack(cocod_lm_handle *h, int64_t M, int64_t k, const void *x, int64_t ldx, int8_t *q, int64_t ldq,
                    uint8_t *scales, cocod_stream_t stream);
 int cocod_act_unpack(cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, int64_t ldq, const uint8_t *scales,
@@ -95,7 +98,7 @@ int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *o
                                      const void *dy, int64_t lddy, const int8_t *q, int64_t ldq, const uint8_t *scales,
                                      void *dw, int64_t lddw, int64_t dw_stride, int out_type,
                                      void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
-int64_t cocod_grouped_packed_workspace(int64_t M, int64_t k);
+int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k);
 
 /* ---------------------------------------------------------------------------------------------
  * Softmax cross-entropy over a vocabulary of V entries, each group with an output matrix w[g] (V x D) of its own:

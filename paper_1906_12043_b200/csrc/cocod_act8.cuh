@@ -113,7 +113,8 @@ act_pack(const __nv_bfloat16 *x, long long ldx, int8_t *q, long long ldq, uint8_
         }
     }
     if (m < M && c < k) *reinterpret_cast<uint4 *>(q + m * ldq + c) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-    if ((threadIdx.x & 7) == 0) exps[threadIdx.x >> 3] = (uint8_t)biased;
+    const bool all_finite = __all_sync(0xffu << (threadIdx.x & 24), plain);      // of the eight threads of this block of columns
+    if ((threadIdx.x & 7) == 0) exps[threadIdx.x >> 3] = all_finite ? (uint8_t)biased : 255;
     __syncthreads();
     const long long mm = (long long)blockIdx.x * ACT_ROWS + threadIdx.x;
     if (threadIdx.x < ACT_ROWS && mm < M) scales[(long long)blockIdx.y * M + mm] = exps[threadIdx.x];
@@ -126,17 +127,18 @@ __device__ __forceinline__ __nv_bfloat162 pair_of(uint32_t two)       // bytes 0
     const uint32_t t = (two & 0x007f007fu) | 0x43004300u, s = (two & 0x00800080u) | 0x43004300u;
     return __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&t), *reinterpret_cast<const __nv_bfloat162 *>(&s));
 }
-// Four 8-bit values as two bf16 pairs, times the power of two.
+// Four 8-bit values as two bf16 pairs, times the unit.
 __device__ __forceinline__ void widen4(uint32_t b, __nv_bfloat162 unit, uint32_t &lo, uint32_t &hi)
 {
     __nv_bfloat162 a = __hmul2(pair_of(__byte_perm(b, 0, 0x4140)), unit), c = __hmul2(pair_of(__byte_perm(b, 0, 0x4342)), unit);
     lo = *reinterpret_cast<uint32_t *>(&a);
     hi = *reinterpret_cast<uint32_t *>(&c);
-    const uint32_t bad = __vcmpeq4(b, 0x80808080u);               // the marker reads as NaN
-    if (bad) {
-        lo |= __byte_perm(bad, 0, 0x1100) & 0x7fff7fffu;
-        hi |= __byte_perm(bad, 0, 0x3322) & 0x7fff7fffu;
-    }
+}
+// The unit that a scale byte stands for, twice: the exponent field of bf16 starts at bit 7; 255 is NaN (255 << 7 alone would be infinite).
+__device__ __forceinline__ __nv_bfloat162 unit_of(uint32_t scale)
+{
+    const uint32_t bits = scale * 0x00800080u | (scale == 255u ? 0x00400040u : 0u);
+    return *reinterpret_cast<const __nv_bfloat162 *>(&bits);
 }
 
 __global__ void __launch_bounds__(256)
@@ -147,7 +149,7 @@ act_unpack(const int8_t *q, long long ldq, const uint8_t *scales, __nv_bfloat16 
     const long long c = (long long)blockIdx.y * ACT_BLOCK + (threadIdx.x & 7) * 16;
     if (m >= M || c >= k) return;
     const uint4 b = *reinterpret_cast<const uint4 *>(q + m * ldq + c);
-    const __nv_bfloat162 unit = __float2bfloat162_rn(power_of_two(scales[(long long)blockIdx.y * M + m]));
+    const __nv_bfloat162 unit = unit_of(scales[(long long)blockIdx.y * M + m]);
     uint32_t v[8];
     widen4(b.x, unit, v[0], v[1]);
     widen4(b.y, unit, v[2], v[3]);

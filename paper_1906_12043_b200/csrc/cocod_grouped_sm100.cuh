@@ -26,11 +26,14 @@
 // the difference.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
 // with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
+// The weight gradient can take B as an 8-bit checkpoint (B_Q8): TMA brings the bytes, an idle warp their scales, and four more warps write
+// the bf16 operand tile, exactly (a whole number times a power of two), with zeros behind the group's end.
 // The number of tiles is seldom a multiple of the CTA pairs.  The tiles of the last, incomplete wave (all of them when there are few)
 // are cut along the reduction into as many parts as keep every pair busy; a part leaves as fp32 in scratch, at most one per
 // pair, and join_parts adds the parts of a tile up in a fixed order.  5.2 waves of tiles take 5.2 and not 6 times a tile.
 // Every wait is bounded, as in cocod_gemm_sm100.cuh.
 #pragma once
+#include "cocod_act8.cuh"
 #include "cocod_gemm_sm100.cuh"
 
 namespace cocod {
@@ -38,11 +41,25 @@ namespace lm {
 
 using namespace cocod::gemm;
 
-constexpr int EPI_WARPS = 8, GROUPED_THREADS = 128 + 32 * EPI_WARPS;
-constexpr int RING = 5;                                             // stages of 32 KB
+enum Operand { B_K = 0, B_MN = 1, B_Q8 = 2 };                       // B: reduction innermost; second; second and in 8 bits
+
+constexpr int EPI_WARPS = 8, CONV_WARPS = 8;
+__host__ __device__ constexpr int grouped_threads(int b) { return 128 + 32 * EPI_WARPS + (b == B_Q8 ? 32 * CONV_WARPS : 0); }
+constexpr int Q_BYTES = 64 * 128;                                   // 8-bit values of a block of the reduction
+__host__ __device__ constexpr int ring(int b) { return b == B_Q8 ? 4 : 5; }                  // stages
+__host__ __device__ constexpr int stage_bytes(int b) { return STAGE_BYTES + (b == B_Q8 ? Q_BYTES : 0); }
 constexpr int OUT_BYTES = 2 * 4096;                                 // staging of an epilogue warp: twice 32 rows of 128 bytes
 constexpr int AHEAD = 4;                                            // tiles that the scheduler may be ahead
-constexpr int GROUPED_SMEM = RING * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 512;
+constexpr int GROUPED_SMEM = 5 * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 1024;
+static_assert(ring(B_Q8) * stage_bytes(B_Q8) <= 5 * STAGE_BYTES, "the stages with 8-bit values take the same room");
+// Registers per thread: what a launch holds, and what the warps 0..3, the epilogue and the converting warps keep of it.
+__host__ __device__ constexpr int launch_registers(int b) { return b == B_Q8 ? 96 : 168; }
+__host__ __device__ constexpr int few_registers(int b) { return b == B_Q8 ? 48 : 64; }
+__host__ __device__ constexpr int epilogue_registers(int b) { return b == B_Q8 ? 160 : 216; }
+constexpr int CONV_REGISTERS = 56;
+static_assert(128 * few_registers(B_K) + 32 * EPI_WARPS * epilogue_registers(B_K) <= grouped_threads(B_K) * launch_registers(B_K), "a warp would wait for ever");
+static_assert(128 * few_registers(B_Q8) + 32 * CONV_WARPS * CONV_REGISTERS + 32 * EPI_WARPS * epilogue_registers(B_Q8) <=
+              grouped_threads(B_Q8) * launch_registers(B_Q8), "a warp would wait for ever");
 constexpr int ERR_OFFSETS = 100;                                    // error_flag: the offsets do not rise from 0 to the number of rows
 constexpr int ERR_LABEL = 101;                                      // error_flag: a label beyond the vocabulary
 
@@ -74,6 +91,7 @@ struct GroupedParams {
     const float *row_scale;            // rows form, optional: factor of every row (0: the row is 0 whatever the product is)
     const CUtensorMap *group_maps;     // weight form: A and B of group g at 2 g and 2 g + 1
     const int *order;                  // weight form: the groups, those with the most rows first
+    const uint8_t *scales;             // B_Q8: [ceil(n / 128)][total_rows], exponents + 127
     // OUT_VOCAB, OUT_VOCAB_SUMS (rows counted from row0)
     const float *ref;                  // c_r
     const int *label;                  // t_r; negative: the row takes no part (u = 0)
@@ -163,7 +181,7 @@ template <int CG> __device__ __forceinline__ void umma_commit_g(uint32_t bar)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                      ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// Registers per thread from here on, for all warps of a warpgroup.  The launch holds 384 x 168 = 64512 of them: 128 x 56 + 256 x 224.
+// Registers per thread from here on, for all warps of a warpgroup.
 template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int CG> __device__ __forceinline__ uint32_t cta_rank()
@@ -183,11 +201,12 @@ template <int CG, int TN, bool A_MN, bool B_MN> __host__ __device__ constexpr ui
 // ------------------------------------------------------------------------------------------ tiles
 struct __align__(16) Tile {
     int g;             // group; negative: there are no more tiles
-    int m0, m1;        // rows form: first row of the tile, end of the group (both counted from row0).  Weight form: first row of out_g, -
+    int m0, m1;        // rows form: first row of the tile, end of the group (both counted from row0).  Weight form: first row of out_g,
+                       // end of the group
     int n0;            // first column
     int kb0, kb1;      // blocks of the reduction (64 each)
     int slot;          // negative: a whole tile; else a part of one, number `slot` in the scratch
-    int unused;
+    int lo;            // weight form: the group's first row
 };
 
 // Rows of group g within this launch, counted from row0; any content of offsets gives a range inside [0, rows].
@@ -335,7 +354,8 @@ template <int TM, int TN, bool WG> struct Walker {
         int blocks;
         if (WG) {
             tile.m0 = tm * TM;
-            tile.m1 = p.kdim;
+            tile.m1 = hi;
+            tile.lo = lo;
             blocks = (hi - lo + BK - 1) / BK;
         } else {
             tile.m0 += tm * TM;
@@ -364,25 +384,29 @@ __device__ __forceinline__ float exp2_approx(float x)
 
 // ------------------------------------------------------------------------------------------ kernel
 // Tensor maps (all three-dimensional, innermost dimension contiguous, 128-byte swizzle):
-//   A, B with the reduction innermost: boxes of 64 x 128 rows; A or B with it second: boxes of 64 x 64, two per operand.
+//   A, B with the reduction innermost: boxes of 64 x 128 rows; A or B with it second: boxes of 64 x 64, two per operand; B in 8
+//   bits: boxes of 128 x 64 rows, not swizzled.
 //   out: boxes of 32 rows x 128 bytes; third index = group (weight form).  parts: the scratch as an fp32 matrix of TN columns, TM
 //   rows for each part, boxes of 32 x 32.
-template <int CG, int TN, bool WG, bool B_MN, int OUT>
-__global__ void __launch_bounds__(GROUPED_THREADS, 1)
+template <int CG, int TN, bool WG, int B, int OUT>
+__global__ void __launch_bounds__(grouped_threads(B), 1)
 grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
              const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_parts, const GroupedParams p)
 {
-    constexpr int TM = 128 * CG;
-    constexpr bool A_MN = WG;
+    constexpr int TM = 128 * CG, RING = ring(B), STAGE = stage_bytes(B);
+    constexpr bool A_MN = WG, QB = B == B_Q8;
     static_assert(TN / CG == 128, "each CTA holds 128 columns of B");
     extern __shared__ uint8_t grouped_smem[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(grouped_smem) + 1023) & ~(uintptr_t)1023);
-    uint8_t *outs = smem + RING * STAGE_BYTES;
+    uint8_t *outs = smem + RING * STAGE;
     uint64_t *bars = reinterpret_cast<uint64_t *>(outs + EPI_WARPS * OUT_BYTES);
     const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + RING), accf0 = smem_u32(bars + 2 * RING), acce0 = smem_u32(bars + 2 * RING + 2);
     const uint32_t tilef0 = smem_u32(bars + 2 * RING + 4), tilee0 = smem_u32(bars + 2 * RING + 4 + AHEAD);
     Tile *tiles = reinterpret_cast<Tile *>(bars + 2 * RING + 4 + 2 * AHEAD);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(tiles + AHEAD);
+    uint64_t *bbars = reinterpret_cast<uint64_t *>(tiles + AHEAD);
+    const uint32_t bfull0 = smem_u32(bbars), qfull0 = smem_u32(bbars + RING);      // B_Q8: the bf16 tile is written; bytes and scales are there
+    uint8_t *unit_bytes = reinterpret_cast<uint8_t *>(bbars + 2 * RING);           // B_Q8: scales of the 64 rows of every stage
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(unit_bytes + 64 * RING);
     volatile int *abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cta_rank<CG>();
@@ -402,6 +426,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         for (int s = 0; s < RING; ++s) {
             mbar_init(full0 + 8 * s, 1);
             mbar_init(empty0 + 8 * s, 1);
+            mbar_init(bfull0 + 8 * s, CONV_WARPS * CG);
+            mbar_init(qfull0 + 8 * s, 2);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(accf0 + 8 * s, 1);
@@ -409,7 +435,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         }
         for (int s = 0; s < AHEAD; ++s) {
             mbar_init(tilef0 + 8 * s, 1);
-            mbar_init(tilee0 + 8 * s, 1 + (rank == 0 ? 1 : 0) + EPI_WARPS);      // producer, issuer, epilogue
+            mbar_init(tilee0 + 8 * s, 1 + (rank == 0 ? 1 : 0) + EPI_WARPS + (QB ? CONV_WARPS + 1 : 0));      // producer, issuer, epilogue, converters, scales
         }
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -432,7 +458,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const int4 *src = reinterpret_cast<const int4 *>(tiles + turn++ % AHEAD);
         const int4 a = src[0], b = src[1];
         t.g = a.x; t.m0 = a.y; t.m1 = a.z; t.n0 = a.w;
-        t.kb0 = b.x; t.kb1 = b.y; t.slot = b.z;
+        t.kb0 = b.x; t.kb1 = b.y; t.slot = b.z; t.lo = b.w;
     };
     auto next_tile = [&](Tile &t) {
         const unsigned s = turn % AHEAD;
@@ -449,8 +475,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         if (lane == 0) mbar_arrive_local(tilee0 + 8 * s);
         return t.g >= 0;
     };
-    if (warp >= 4) {
-        take_registers<224>();
+    if (warp >= 4 && warp < 4 + EPI_WARPS) {
+        take_registers<epilogue_registers(B)>();
         // ---- epilogue: rows 32 (warp % 4) .. + 31 of the CTA's 128, columns of one half of the tile
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         uint8_t *staging = outs + (warp - 4) * OUT_BYTES;
@@ -512,7 +538,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         };
         while (next_tile_warp(t)) {
             const int m = t.m0 + (int)rank * 128 + quarter * 32;            // first row of this warp
-            const int valid = t.m1 - m;                                      // rows of the group (matrix) from there on
+            const int valid = (WG ? p.kdim : t.m1) - m;                     // rows of the group (matrix) from there on
             const int col0 = t.n0 + half * HALF;
             const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * HALF;
             float scale = 1.0f;
@@ -534,11 +560,14 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     if (k0 == t.kb0) {
                         tmem_ld32(tacc + a * TN + c, sum);
                     } else {
-                        uint32_t r[32];
-                        tmem_ld32(tacc + a * TN + c, r);
-                        tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) sum[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(r[j]));
+                        for (int e = 0; e < 32; e += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(tacc + a * TN + c + e, r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sum[e + j] = __float_as_uint(__uint_as_float(sum[e + j]) + __uint_as_float(r[j]));
+                        }
                     }
                 }
                 tmem_ld_wait();
@@ -604,8 +633,52 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (is_vocab(OUT) && col0 < p.n && lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
         }
         if (lane == 0) tma_store_wait_read<0>();
+    } else if (QB && warp >= 4 + EPI_WARPS) {
+        // ---- converters: warp c takes rows 8 c .. + 7 of a block of the reduction.  A lane takes columns 8 j .. + 7 and 64 + 8 j .. + 7 of two of
+        // them, the two halves of a row in turns by its parity, so that no two lanes meet in a bank.
+        give_registers<CONV_REGISTERS>();
+        constexpr int MINE = 64 / (4 * CONV_WARPS);            // rows of a lane
+        const int first = (warp - 4 - EPI_WARPS) * (64 / CONV_WARPS) + (lane >> 3), j = lane & 7, odd = first & 1;
+        Tile t;
+        unsigned it = 0;
+        while (next_tile_warp(t)) {
+            for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+                const unsigned s = it % RING;
+                if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * s, (it / RING) & 1, abort, limit))) { failed = 6; break; }
+                uint8_t *db = smem + s * STAGE + A_BYTES;
+                const uint8_t *q = db + B_BYTES;
+                uint2 v[MINE][2];
+                uint32_t scale[MINE];
+#pragma unroll
+                for (int i = 0; i < MINE; ++i) {
+                    const int r = first + 4 * i;
+                    v[i][0] = *reinterpret_cast<const uint2 *>(q + r * 128 + odd * 64 + j * 8);
+                    v[i][1] = *reinterpret_cast<const uint2 *>(q + r * 128 + (1 - odd) * 64 + j * 8);
+                    scale[i] = unit_bytes[s * 64 + r];
+                }
+#pragma unroll
+                for (int i = 0; i < MINE; ++i) {
+                    const int r = first + 4 * i;
+                    const __nv_bfloat162 unit = unit_of(scale[i]);             // (0 behind the group: 0 times any whole number)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint4 w;
+                        widen4(v[i][h].x, unit, w.x, w.y);
+                        widen4(v[i][h].y, unit, w.z, w.w);
+                        *reinterpret_cast<uint4 *>(db + (h ^ odd) * (BK * 128) + r * 128 + ((j ^ (r & 7)) << 4)) = w;
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 1) mbar_arrive_local(bfull0 + 8 * s);
+                    else mbar_arrive_cluster(map_to_rank(bfull0 + 8 * s, 0));
+                }
+            }
+            if (failed) break;
+        }
     } else {
-        give_registers<56>();
+        give_registers<few_registers(B)>();
         if (warp == 0) {
             // ---- producer (one thread: a warp's own synchronisation at every tile cost the ring 300 clocks)
             Tile t;
@@ -613,26 +686,29 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             int last_g = -1;
             while (lane == 0 && !failed && next_tile(t)) {
                 if (p.debug_no_loads) continue;
-                const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG ? ma + 1 : &map_b;
+                const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG && !QB ? ma + 1 : &map_b;
                 if (WG && t.g != last_g) {
                     acquire_map(ma);
-                    acquire_map(mb);
+                    if (!QB) acquire_map(mb);
                     last_g = t.g;
                 }
                 const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
                 for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
                     const unsigned s = it % RING, use = it / RING;
                     if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
-                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * STAGE_BYTES);
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * (QB ? A_BYTES : STAGE_BYTES));
                     const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
-                    const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+                    const uint32_t da = smem_base + s * STAGE, db = da + A_BYTES;
                     if (A_MN) {
                         load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
                         load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
                     } else {
                         load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
                     }
-                    if (B_MN) {
+                    if (QB) {
+                        mbar_expect_tx(qfull0 + 8 * s, Q_BYTES);
+                        tma_load_3d(db + B_BYTES, &map_b, qfull0 + 8 * s, n0, t.lo + kb * BK, 0);
+                    } else if (B == B_MN) {
                         load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
                         load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
                     } else {
@@ -642,8 +718,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             }
         } else if (warp == 1 && rank == 0) {
             // ---- issuer of the products (one thread)
-            constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B_MN>();
-            constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B_MN ? 2048u : 32u;
+            constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B != B_K>();
+            constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B != B_K ? 2048u : 32u;
             Tile t;
             unsigned it = 0, ai = 0;
             while (lane == 0 && !failed && next_tile(t)) {
@@ -655,11 +731,12 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     for (int kb = k0; kb < k1; ++kb, ++it) {
                         const unsigned s = it % RING;
                         if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
+                        if (QB && !mbar_wait(bfull0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
                         tc_fence_after();
-                        const uint32_t da = smem_base + s * STAGE_BYTES, db = da + A_BYTES;
+                        const uint32_t da = smem_base + s * STAGE, db = da + A_BYTES;
 #pragma unroll
                         for (int k = 0; k < BK / UMMA_K; ++k)
-                            umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B_MN), idesc,
+                            umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B != B_K), idesc,
                                        (kb > k0 || k > 0) ? 1u : 0u);
                         umma_commit_g<CG>(empty0 + 8 * s);
                     }
@@ -667,6 +744,25 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     umma_commit_g<CG>(accf0 + 8 * a);
                     k0 = k1;
                 }
+            }
+        } else if (QB && warp == 2) {
+            // ---- the scales of every block's 64 rows, 0 behind the group and behind the columns
+            Tile t;
+            unsigned it = 0;
+            while (next_tile_warp(t)) {
+                const int n0 = t.n0 + (int)rank * 128, rows = n0 < p.n ? t.m1 - t.lo : 0;
+                const uint8_t *scale = p.scales + (long long)(n0 / ACT_BLOCK) * p.total_rows + t.lo;
+                for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+                    const unsigned s = it % RING, use = it / RING;
+                    const int r = kb * BK + lane;
+                    const uint8_t a = r < rows ? scale[r] : 0, b = r + 32 < rows ? scale[r + 32] : 0;
+                    if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit))) { failed = 7; break; }
+                    unit_bytes[s * 64 + lane] = a;
+                    unit_bytes[s * 64 + lane + 32] = b;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_local(qfull0 + 8 * s);
+                }
+                if (failed) break;
             }
         } else if (warp == 3) {
             // ---- scheduler
@@ -686,7 +782,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 ++turn;
                 if (lane == 0) {
                     reinterpret_cast<int4 *>(tiles + s)[0] = make_int4(t.g, t.m0, t.m1, t.n0);
-                    reinterpret_cast<int4 *>(tiles + s)[1] = make_int4(t.kb0, t.kb1, t.slot, 0);
+                    reinterpret_cast<int4 *>(tiles + s)[1] = make_int4(t.kb0, t.kb1, t.slot, t.lo);
                     mbar_arrive_local(tilef0 + 8 * s);
                 }
                 if (t.g < 0) break;

@@ -43,7 +43,7 @@ int sm_count()
 struct Matrix {
     const void *data;
     int64_t ld, stride;                    // elements; stride: between groups
-    int elem;                              // bytes of an element: 2 (bf16) or 4 (fp32)
+    int elem;                              // bytes of an element: 1 (8-bit checkpoint), 2 (bf16) or 4 (fp32)
 };
 
 // Three-dimensional map {columns, rows, groups}; a box is 128 bytes of `box_rows` rows.
@@ -55,8 +55,9 @@ bool encode(CUtensorMap *m, const Matrix &x, uint64_t cols, uint64_t rows, uint6
     const cuuint64_t strides[2] = {(cuuint64_t)x.ld * x.elem, (cuuint64_t)(groups > 1 ? x.stride : (int64_t)rows * x.ld) * x.elem};
     const cuuint32_t box[3] = {(cuuint32_t)(128 / x.elem), box_rows, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
-    return enc(m, x.elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void *>(x.data), dims,
-               strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    const CUtensorMapDataType type = x.elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : x.elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    return enc(m, type, 3, const_cast<void *>(x.data), dims,
+               strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, x.elem == 1 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -109,7 +110,7 @@ struct Cut {
 };
 // rows x cols results (rows form: `groups` groups share the rows; weight form: per group), reductions of `depth` (weight form: on
 // average).  The choice minimises an estimate in microseconds, fitted to measurements: a launch 3.5 (pairs 4.5), a tile 1.5 (2.0)
-// and for each block of 64 of its reduction 0.16 (0.28), or, when all SMs load at the same time, 0.34 (0.40): 4096 x 4096 x 4096
+// and for each block of 64 of its reduction 0.28 (0.33), or, when all SMs load at the same time, 0.34 (0.40): 4096 x 4096 x 4096
 // takes 153 us in single tiles and 98 in pairs, 128 x 18944 x 512 7.4 and 10.0.  Joining the parts of tiles is another launch.
 Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t depth, bool parts_allowed)
 {
@@ -125,19 +126,19 @@ Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t de
         const int64_t col_tiles = ceil_div(cols, t), blocks = std::max<int64_t>(1, ceil_div(depth, 64));
         const int64_t tiles = std::max<int64_t>(1, (int64_t)(likely * col_tiles)), full = tiles / slots, rest = tiles % slots;
         const double busy = std::min(1.0, (double)tiles / slots);
-        const double block = pair ? std::max(0.28, 0.40 * busy) : std::max(0.16, 0.34 * busy), tile = pair ? 2.0 : 1.5;
+        const double block = pair ? std::max(0.33, 0.40 * busy) : std::max(0.28, 0.34 * busy), tile = pair ? 2.0 : 1.5;
         // A's tile rows of a band stay in L2 while B passes by; where all of B fits, or A's do not, eight are enough
         const int64_t row_bytes = t * depth * 2;
         const bool b_fits = cols * depth * 2 <= (40 << 20);
         const int band = (int)std::max<int64_t>(8, std::min<int64_t>(b_fits ? 8 : (40 << 20) / std::max<int64_t>(row_bytes, 1), 1 << 16));
         // (joining takes about 0.09 us for each part: more parts than this cost more than they save)
-        const int64_t sensible = (int64_t)std::sqrt(blocks * (pair ? 0.28 : 0.16) / 0.09) + 1, bound = std::min(blocks / 4, std::max<int64_t>(sensible, 2));
+        const int64_t sensible = (int64_t)std::sqrt(blocks * (pair ? 0.33 : 0.28) / 0.09) + 1, bound = std::min(blocks / 4, std::max<int64_t>(sensible, 2));
         const int64_t most_parts = rest > 0 && parts_allowed ? std::min(slots / rest, bound) : 1;
         for (int cut = 0; cut < 2; ++cut) {
             const int64_t parts = cut ? most_parts : 1;
             if (cut && parts < 2) break;
             const double busy_rest = std::min(1.0, (double)rest * parts / slots);
-            const double block_rest = pair ? std::max(0.28, 0.40 * busy_rest) : std::max(0.16, 0.34 * busy_rest);
+            const double block_rest = pair ? std::max(0.33, 0.40 * busy_rest) : std::max(0.28, 0.34 * busy_rest);
             const double cost = (pair ? 4.5 : 3.5) + full * (blocks * block + tile) + (rest ? ceil_div(blocks, parts) * block_rest + tile : 0.0) +
                                 (parts > 1 ? 3.0 + parts * 0.09 + rest * parts * t * t * 4 / 8e6 : 0.0);
             // A cut has to promise a sixth: under load the GPU is at its power limit, where idle SMs leave the busy ones a higher clock
@@ -152,18 +153,18 @@ Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t de
     return best;
 }
 
-template <int CG, int TN, bool WG, bool B_MN, int OUT>
+template <int CG, int TN, bool WG, int B, int OUT>
 int launch_tiles(cocod_lm *h, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const GroupedParams &p, int64_t tiles, cudaStream_t s)
 {
     static bool configured[MAX_DEVICES] = {};
     const int dev = current_device(), sms = sm_count();
     if (dev < 0 || sms < 2) return COCOD_ERR_CUDA;
-    auto kernel = grouped_gemm<CG, TN, WG, B_MN, OUT>;
+    auto kernel = grouped_gemm<CG, TN, WG, B, OUT>;
     if (!configured[dev]) {
         // The epilogue warps wait for the registers that the others give up: the launch has to hold their sum.
         cudaFuncAttributes attr{};
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GROUPED_SMEM) != cudaSuccess ||
-            cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs < 168) {
+            cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs < launch_registers(B)) {
             cudaGetLastError();
             return COCOD_ERR_CUDA;
         }
@@ -174,7 +175,7 @@ int launch_tiles(cocod_lm *h, const CUtensorMap &a, const CUtensorMap &b, const 
     if (p.max_parts > 1 && !encode(&parts, Matrix{h->parts, TN, 0, 4}, TN, (uint64_t)clusters * 128 * CG, 1, 32)) return COCOD_ERR_CUDA;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)clusters * CG);
-    cfg.blockDim = dim3(GROUPED_THREADS);
+    cfg.blockDim = dim3(grouped_threads(B));
     cfg.dynamicSmemBytes = GROUPED_SMEM;
     cfg.stream = s;
     cudaLaunchAttribute at[2];
@@ -195,10 +196,10 @@ int launch_tiles(cocod_lm *h, const CUtensorMap &a, const CUtensorMap &b, const 
     return COCOD_OK;
 }
 
-template <bool WG, bool B_MN, int OUT>
+template <bool WG, int B, int OUT>
 int launch_form(cocod_lm *h, const Cut &c, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GroupedParams &p, cudaStream_t s)
 {
-    return c.pair ? launch_tiles<2, 256, WG, B_MN, OUT>(h, a, b, o, p, c.tiles, s) : launch_tiles<1, 128, WG, B_MN, OUT>(h, a, b, o, p, c.tiles, s);
+    return c.pair ? launch_tiles<2, 256, WG, B, OUT>(h, a, b, o, p, c.tiles, s) : launch_tiles<1, 128, WG, B, OUT>(h, a, b, o, p, c.tiles, s);
 }
 
 // Which rows of the batch a call takes: row0 .. row0 + rows - 1 of total (A, out and row_scale start at row0).
@@ -223,14 +224,15 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window
     p.out = const_cast<void *>(out.data); p.ld_out = out.ld;
     p.error_flag = h->flag;
     if (form == FORWARD)
-        return out.elem == 2 ? launch_form<false, false, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<false, false, OUT_F32>(h, cut, a, b, o, p, s);
-    return out.elem == 2 ? launch_form<false, true, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<false, true, OUT_F32>(h, cut, a, b, o, p, s);
+        return out.elem == 2 ? launch_form<false, B_K, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<false, B_K, OUT_F32>(h, cut, a, b, o, p, s);
+    return out.elem == 2 ? launch_form<false, B_MN, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<false, B_MN, OUT_F32>(h, cut, a, b, o, p, s);
 }
 
 // weight form: out_g (rows x cols) = sum over the group's rows m of A[m][.]^T B[m][.]
-// (add: added to what out, fp32, holds;  maps_ready: a kernel before this one has written the groups' maps and order)
+// (scales: B is an 8-bit checkpoint;  add: added to what out, fp32, holds;  maps_ready: a kernel before this one has
+// written the groups' maps and order)
 int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
-                const Matrix &out, bool add, bool maps_ready, cudaStream_t s)
+                const uint8_t *scales, const Matrix &out, bool add, bool maps_ready, cudaStream_t s)
 {
     const int64_t M = win.rows;
     const Cut cut = choose_cut(WEIGHT_GRAD, G, rows, cols, ceil_div(std::max<int64_t>(M, 1), G), true);
@@ -244,12 +246,14 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, i
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
     p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = cut.max_parts;
     p.out = const_cast<void *>(out.data); p.ld_out = out.ld; p.out_stride = out.stride;
-    p.group_maps = h->group_maps; p.order = h->order; p.error_flag = h->flag;
-    if (!maps_ready)
-        TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, b, static_cast<const char *>(A.data),
-                                  (long long)A.ld * 2, static_cast<const char *>(B.data), (long long)B.ld * 2, p, h->group_maps, h->order));
-    if (add) return launch_form<true, true, OUT_ADD_F32>(h, cut, a, b, o, p, s);
-    return out.elem == 2 ? launch_form<true, true, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<true, true, OUT_F32>(h, cut, a, b, o, p, s);
+    p.group_maps = h->group_maps; p.order = h->order; p.scales = scales; p.error_flag = h->flag;
+    if (!maps_ready)                       // (a checkpoint needs none: what lies behind its group becomes zeros in the conversion)
+        TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, scales ? a : b, static_cast<const char *>(A.data),
+                                  (long long)A.ld * 2, static_cast<const char *>(scales ? A.data : B.data), (long long)(scales ? A.ld : B.ld) * 2, p, h->group_maps, h->order));
+    if (scales)
+        return out.elem == 2 ? launch_form<true, B_Q8, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<true, B_Q8, OUT_F32>(h, cut, a, b, o, p, s);
+    if (add) return launch_form<true, B_MN, OUT_ADD_F32>(h, cut, a, b, o, p, s);
+    return out.elem == 2 ? launch_form<true, B_MN, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<true, B_MN, OUT_F32>(h, cut, a, b, o, p, s);
 }
 
 // ------------------------------------------------------------------------------------------ vocabulary
@@ -352,7 +356,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
             p.redo_any = v.redo_any;
             f.second = pass;
             if (win.rows > 0) {
-                if (int rc = grad ? launch_form<false, false, OUT_VOCAB>(h, cut, a, b, o, p, s) : launch_form<false, false, OUT_VOCAB_SUMS>(h, cut, a, b, o, p, s))
+                if (int rc = grad ? launch_form<false, B_K, OUT_VOCAB>(h, cut, a, b, o, p, s) : launch_form<false, B_K, OUT_VOCAB_SUMS>(h, cut, a, b, o, p, s))
                     return rc;
             }
             TRY_CUDA(launch_dependent(true, vocab_finish, finish_grid, dim3(32 * FINISH_WARPS), 0, s, f));
@@ -361,7 +365,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
             const Matrix dh{static_cast<const bf16 *>(grad->dh.data) + row0 * grad->dh.ld, grad->dh.ld, 0, 2};
             if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, s)) return rc;
             const Matrix dst = several && dw_elem == 2 ? Matrix{ws + l.total32, D, V * D, 4} : grad->dw;
-            if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, dst, several && row0 > 0, true, s)) return rc;
+            if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, nullptr, dst, several && row0 > 0, true, s)) return rc;
         }
         row0 += win.rows;
     } while (row0 < M);
@@ -472,7 +476,7 @@ int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets,
     if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(dw, lddw, dw_stride, n, k, G, es))
         return COCOD_ERR_INVALID;
-    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false,
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{x, ldx, 0, 2}, nullptr, Matrix{dw, lddw, dw_stride, es}, false, false,
                        (cudaStream_t)stream);
 }
 
@@ -520,21 +524,39 @@ int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh
     return COCOD_OK;
 }
 
-int64_t cocod_grouped_packed_workspace(int64_t M, int64_t k) { return M < 0 || M > MAX_DIM || k < 1 || k > MAX_DIM ? COCOD_ERR_INVALID : ceil_div(M * k * 2, 256) * 256; }
+// Whether a checkpoint is better turned into bf16 once, by a kernel before the product, than inside it.  The conversion costs the
+// product about 0.18 us for every block of 64 of a tile's reduction (4 groups of 8192 rows, 2048 x 4096 results: 603 us against
+// 538 with the kernel before it, which takes 74); the kernel costs a launch and 3 bytes a value at 5.4 TB/s (16 groups of
+// 128 rows, 1024 x 1024 results: 25.2 us against 23.1 with the conversion inside).
+static bool widen_first(int G, int64_t M, int64_t n, int64_t k)
+{
+    const int64_t depth = ceil_div(std::max<int64_t>(M, 1), G);
+    const Cut cut = choose_cut(WEIGHT_GRAD, G, n, k, depth, true);
+    const double waves = std::ceil((double)cut.tiles / (cut.pair ? sm_count() / 2 : std::max(sm_count(), 1)));
+    return waves * ceil_div(depth, 64) * 0.18 > 4.0 + 3.0 * M * k / 5.4e6;
+}
+
+int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k)
+{
+    if (G < 1 || G > COCOD_LM_MAX_GROUPS || M < 0 || M > MAX_DIM || n < 8 || n > MAX_DIM || k < 8 || k > MAX_DIM) return COCOD_ERR_INVALID;
+    return sm_count() > 1 && widen_first(G, M, n, k) ? M * k * 2 : 0;
+}
 
 int cocod_grouped_weight_grad_packed(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy,
                                      int64_t lddy, const int8_t *q, int64_t ldq, const uint8_t *scales, void *dw, int64_t lddw,
                                      int64_t dw_stride, int out_type, void *workspace, int64_t workspace_bytes, cocod_stream_t stream)
 {
     const int es = size_of(out_type);
-    if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) || !good_act(h, M, k, q, ldq) ||
-        (M > 0 && !scales) || !good_groups(dw, lddw, dw_stride, n, k, G, es))
+    if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) || !good_act(h, M, k, q, ldq) || (M > 0 && !scales) ||
+        !good_groups(dw, lddw, dw_stride, n, k, G, es) || workspace_bytes < 0 || (workspace_bytes > 0 && (!workspace || !aligned16(workspace))))
         return COCOD_ERR_INVALID;
-    if (M > 0 && (!workspace || !aligned16(workspace))) return COCOD_ERR_INVALID;
-    if (workspace_bytes < M * k * 2) return COCOD_ERR_TOO_LARGE;
-    if (int rc = cocod_act_unpack(h, M, k, q, ldq, scales, workspace, k, stream)) return rc;
-    return run_weights(h, G, offsets, Window{0, M, M}, n, k, Matrix{dy, lddy, 0, 2}, Matrix{workspace, k, 0, 2}, Matrix{dw, lddw, dw_stride, es}, false, false,
-                       (cudaStream_t)stream);
+    const Matrix A{dy, lddy, 0, 2}, out{dw, lddw, dw_stride, es};
+    if (M > 0 && workspace_bytes >= M * k * 2) {
+        if (int rc = cocod_act_unpack(h, M, k, q, ldq, scales, workspace, k, stream)) return rc;
+        return run_weights(h, G, offsets, Window{0, M, M}, n, k, A, Matrix{workspace, k, 0, 2}, nullptr, out, false, false, (cudaStream_t)stream);
+    }
+    const uint8_t *any = reinterpret_cast<const uint8_t *>(h->flag);      // (no rows: nothing is read)
+    return run_weights(h, G, offsets, Window{0, M, M}, n, k, A, Matrix{q, ldq, 0, 1}, M > 0 ? scales : any, out, false, false, (cudaStream_t)stream);
 }
 
 int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_grad, int dw_type, int64_t limit)
@@ -610,7 +632,7 @@ int cocod_grouped_wait_selftest(int wait_ms, int pair, cocod_stream_t stream)
     p.debug_no_loads = 1;
     // two CTAs (one pair), so that several tiles wait for each
     cocod_lm scratch;
-    const int rc = pair ? launch_tiles<2, 256, false, false, OUT_BF16>(&scratch, a, b, o, p, 1, s) : launch_tiles<1, 128, false, false, OUT_BF16>(&scratch, a, b, o, p, 2, s);
+    const int rc = pair ? launch_tiles<2, 256, false, B_K, OUT_BF16>(&scratch, a, b, o, p, 1, s) : launch_tiles<1, 128, false, B_K, OUT_BF16>(&scratch, a, b, o, p, 2, s);
     int f = 0;
     if (rc != COCOD_OK || cudaMemcpyAsync(&f, flag, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaGetLastError();

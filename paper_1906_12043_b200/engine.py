@@ -79,7 +79,7 @@ SIGNATURES = {
     "cocod_act_unpack": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
     "cocod_act_relu_grad": (_i, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
     "cocod_grouped_weight_grad_packed": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
-    "cocod_grouped_packed_workspace": (_i64, [_i64, _i64]),
+    "cocod_grouped_packed_workspace": (_i64, [_i, _i64, _i64, _i64]),
     "cocod_vocab_workspace": (_i64, [_i, _i64, _i64, _i64, _i, _i, _i64]),
     "cocod_vocab_loss": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "cocod_vocab_loss_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp,

@@ -34,7 +34,8 @@ def _round_up(n: int, m: int) -> int:
 
 class PackedActivations:
     """M x k activations in 8 bits: q (int8, rows 16-byte aligned) counts units of 2 ** (scales - 127), one unit for each
-    128 columns of a row; scales is ceil(k / 128) x M.  A value that was not finite has q = -128 and reads as NaN."""
+    128 columns of a row; scales is ceil(k / 128) x M.  A value that was not finite has q = -128, its block the scale 255, and the
+    block reads as NaN."""
 
     __slots__ = ("q", "scales", "shape")
 
@@ -59,10 +60,11 @@ class PackedActivations:
 class LMOps:
     """The operators, with the scratch their kernels share: order the calls of one object (one stream, or events)."""
 
-    def __init__(self, workspace_limit: int = 2 << 30):
+    def __init__(self, workspace_limit: int = 2 << 30, widen: bool = True):
         """workspace_limit: bytes that a call of the vocabulary operators may take for what it keeps of the rows it works on
-        at a time (a longer batch is worked on in several passes)."""
-        self.workspace_limit = int(workspace_limit)
+        at a time (a longer batch is worked on in several passes).  widen: a weight gradient from a large checkpoint may take
+        room for the checkpoint in bf16, with which it is faster."""
+        self.workspace_limit, self.widen = int(workspace_limit), bool(widen)
         if not torch.cuda.is_available():
             raise RuntimeError("the language-model operators need a CUDA device (there is no CPU fallback)")
         self._lib = _E.load()
@@ -154,7 +156,7 @@ class LMOps:
             out = dy.new_empty((G, n, k), dtype=dtype)
         shape = (G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k)
         if isinstance(x, PackedActivations):
-            ws = self._scratch(self._lib.cocod_grouped_packed_workspace(M, k))
+            ws = self._scratch(self._lib.cocod_grouped_packed_workspace(G, M, n, k)) if self.widen else None
             self._call("cocod_grouped_weight_grad_packed", self._lib.cocod_grouped_weight_grad_packed, *shape, *self._rows(dy, "dy", M, n),
                        *self._rows(x.q, "x.q", M, k, torch.int8), x.scales.data_ptr(), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype],
                        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())

@@ -216,6 +216,7 @@ def pack_reference(x):
                 a = part[m, j].item()
                 if not math.isfinite(a):
                     q[m, 128 * b + j] = -128
+                    e[b, m] = 255
                 elif a != 0:
                     n = max(1, round(abs(a) * 2.0 ** -u))       # Python rounds half to even
                     if n * 2.0 ** u >= 2.0 ** 128:
@@ -241,8 +242,8 @@ def test_pack_is_its_definition(ops, M, k, kind):
     assert torch.equal(p.scales.long().cpu(), e)
     assert torch.equal(p.q.long().cpu(), q)
     y = ops.act_unpack(p)
-    unit = torch.exp2(e.double() - 127).T.repeat_interleave(128, 1)[:, :k]
-    want = torch.where(q == -128, float("nan"), q.double() * unit)
+    unit = torch.where(e == 255, float("nan"), torch.exp2(e.double() - 127)).T.repeat_interleave(128, 1)[:, :k]
+    want = q.double() * unit
     assert torch.equal(torch.nan_to_num(y.double().cpu(), nan=-1e30), torch.nan_to_num(want, nan=-1e30))
 
 
@@ -296,13 +297,36 @@ def test_weight_gradient_from_the_checkpoint(ops, sizes, n, k):
         assert_sum(ops.grouped_weight_grad(dy, p, off, out_dtype=dtype), want, size, max(sizes))
 
 
-def test_weight_gradient_from_the_checkpoint_keeps_groups_apart(ops):
+def test_weight_gradient_from_the_checkpoint_keeps_groups_apart(lm, ops):
     off, spans = offsets_of([70, 58, 200])
     x, dy = gaussian(1, 328, 256), gaussian(3, 328, 136)
     x[spans[1]] = float("nan")
     dy[spans[1]] = float("inf")
     dw = ops.grouped_weight_grad(dy, ops.act_pack(x), off)
     assert torch.isfinite(dw[0]).all() and torch.isfinite(dw[2]).all() and not torch.isfinite(dw[1]).any()
+
+
+@pytest.mark.parametrize("sizes,n,k", [([300, 0, 213], 136, 1000), ([2500, 1596], 512, 1032), ([20000], 256, 264)])
+def test_both_ways_to_read_a_checkpoint_give_the_same_bits(lm, sizes, n, k):
+    """Turned into bf16 inside the product, or by a kernel before it (long reductions, see the last shape)."""
+    off, spans = offsets_of(sizes)
+    x, dy = gaussian(1, sum(sizes), k).clamp(min=0), gaussian(3, sum(sizes), n)
+    x[5, 3] = float("nan")
+    o = lm.LMOps(widen=False)
+    p = o.act_pack(x)
+    wide = o.act_unpack(p)
+    for dtype in (torch.bfloat16, torch.float32):
+        inside = o.grouped_weight_grad(dy, p, off, out_dtype=dtype)
+        before = o.grouped_weight_grad(dy, wide, off, out_dtype=dtype)
+        o.widen = True
+        chosen = o.grouped_weight_grad(dy, p, off, out_dtype=dtype)
+        o.widen = False
+        same = torch.isfinite(before)
+        assert not same[0, :, 3].any() and torch.equal(same, torch.isfinite(inside)) and torch.equal(same, torch.isfinite(chosen))
+        assert torch.equal(inside[same], before[same]) and torch.equal(chosen[same], before[same])
+    assert o._lib.cocod_grouped_packed_workspace(4, 32768, 2048, 4096) == 32768 * 4096 * 2
+    assert o._lib.cocod_grouped_packed_workspace(16, 2048, 1024, 1024) == 0
+    o.destroy()
 
 
 # ------------------------------------------------------------------------------------------------------- vocabulary

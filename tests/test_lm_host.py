@@ -31,6 +31,7 @@ def test_calls_without_a_handle_are_refused(lib):
 
 
 def test_sizes_out_of_range_are_refused(lib):
+    assert lib.cocod_grouped_packed_workspace(0, 8, 8, 8) < 0
     for args in ((0, 8, 8, 8, 1, 0, 0), (1, -1, 8, 8, 1, 0, 0), (1, 8, 0, 8, 1, 0, 0), (1, 8, 8, 12, 1, 0, 0), (1, 8, 8, 8, 1, 2, 0), (1, 8, 8, 8, 1, 0, -1)):
         assert lib.cocod_vocab_workspace(*args) < 0
 
