@@ -127,23 +127,28 @@ class LMOps:
         offsets: G + 1 int32.  Rows behind offsets[G] are not written."""
         G, n, k = w.shape
         M = x.shape[0]
-        dtype = self._type(out, out_dtype, torch.bfloat16)
-        if out is None:
-            out = x.new_empty((M, n), dtype=dtype)
+        out, dtype, at, ld = self._result(x, M, n, out, out_dtype)
         self._call("cocod_grouped_forward", self._lib.cocod_grouped_forward, G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k,
-                   *self._rows(x, "x", M, k), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, n, dtype), _TYPES[dtype])
+                   *self._rows(x, "x", M, k), *self._groups(w, "w", G, n, k), at, ld, _TYPES[dtype])
         return out
 
     def grouped_input_grad(self, dy, w, offsets, out=None, out_dtype=None):
         """dx[m] = w[g]^T dy[m]: the gradient of grouped_forward's input.  dy: M x n bf16."""
         G, n, k = w.shape
         M = dy.shape[0]
-        dtype = self._type(out, out_dtype, torch.bfloat16)
-        if out is None:
-            out = dy.new_empty((M, k), dtype=dtype)
+        out, dtype, at, ld = self._result(dy, M, k, out, out_dtype)
         self._call("cocod_grouped_input_grad", self._lib.cocod_grouped_input_grad, G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k,
-                   *self._rows(dy, "dy", M, n), *self._groups(w, "w", G, n, k), *self._rows(out, "out", M, k, dtype), _TYPES[dtype])
+                   *self._rows(dy, "dy", M, n), *self._groups(w, "w", G, n, k), at, ld, _TYPES[dtype])
         return out
+
+    def _result(self, like, M, cols, out, out_dtype):
+        """(result, its type, address, row stride): a new M x cols matrix, or the caller's after a look."""
+        if out is None:
+            dtype = self._type(None, out_dtype, torch.bfloat16)
+            out = like.new_empty((M, cols), dtype=dtype)
+            return out, dtype, out.data_ptr(), cols
+        dtype = self._type(out, out_dtype, None)
+        return (out, dtype, *self._rows(out, "out", M, cols, dtype))
 
     def grouped_weight_grad(self, dy, x, offsets, out=None, out_dtype=None):
         """dw[g] = sum over the group's rows of dy[m] x[m]^T: the gradient of grouped_forward's weights, G x n x k, 0 for an
@@ -154,15 +159,17 @@ class LMOps:
         dtype = self._type(out, out_dtype, torch.float32)
         if out is None:
             out = dy.new_empty((G, n, k), dtype=dtype)
-        shape = (G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k)
+            result = out.data_ptr(), k, n * k
+        else:
+            result = self._groups(out, "out", G, n, k, dtype)
+        shape = (G, self._vector(offsets, "offsets", G + 1, torch.int32), M, n, k, *self._rows(dy, "dy", M, n))
         if isinstance(x, PackedActivations):
             ws = self._scratch(self._lib.cocod_grouped_packed_workspace(G, M, n, k)) if self.widen else None
-            self._call("cocod_grouped_weight_grad_packed", self._lib.cocod_grouped_weight_grad_packed, *shape, *self._rows(dy, "dy", M, n),
-                       *self._rows(x.q, "x.q", M, k, torch.int8), x.scales.data_ptr(), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype],
+            self._call("cocod_grouped_weight_grad_packed", self._lib.cocod_grouped_weight_grad_packed, *shape,
+                       *self._rows(x.q, "x.q", M, k, torch.int8), x.scales.data_ptr(), *result, _TYPES[dtype],
                        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
         else:
-            self._call("cocod_grouped_weight_grad", self._lib.cocod_grouped_weight_grad, *shape, *self._rows(dy, "dy", M, n),
-                       *self._rows(x, "x", M, k), *self._groups(out, "out", G, n, k, dtype), _TYPES[dtype])
+            self._call("cocod_grouped_weight_grad", self._lib.cocod_grouped_weight_grad, *shape, *self._rows(x, "x", M, k), *result, _TYPES[dtype])
         return out
 
     def _scratch(self, nbytes):
@@ -185,17 +192,23 @@ class LMOps:
         M, k = packed.shape
         if out is None:
             out = packed.q.new_empty((M, k), dtype=torch.bfloat16)
+            at, ld = out.data_ptr(), k
+        else:
+            at, ld = self._rows(out, "out", M, k, align=1)
         self._call("cocod_act_unpack", self._lib.cocod_act_unpack, M, k, *self._rows(packed.q, "packed.q", M, k, torch.int8),
-                   packed.scales.data_ptr(), *self._rows(out, "out", M, k, align=1))
+                   packed.scales.data_ptr(), at, ld)
         return out
 
     def act_relu_grad(self, dh, packed, out=None):
         """dz = dh where the kept activation is positive, 0 elsewhere (NaN where it was not finite).  out may be dh."""
         M, k = packed.shape
+        given = self._rows(dh, "dh", M, k, align=1)
         if out is None:
             out = dh.new_empty((M, k))
-        self._call("cocod_act_relu_grad", self._lib.cocod_act_relu_grad, M, k, *self._rows(dh, "dh", M, k, align=1),
-                   *self._rows(packed.q, "packed.q", M, k, torch.int8), *self._rows(out, "out", M, k, align=1))
+            at, ld = out.data_ptr(), k
+        else:
+            at, ld = self._rows(out, "out", M, k, align=1)
+        self._call("cocod_act_relu_grad", self._lib.cocod_act_relu_grad, M, k, *given, *self._rows(packed.q, "packed.q", M, k, torch.int8), at, ld)
         return out
 
     # ------------------------------------------------------------------------------------------ vocabulary
@@ -227,9 +240,12 @@ class LMOps:
         dx = x.new_empty((M, D))
         if dw is None:
             dw = x.new_empty((G, V, D), dtype=dtype)
+            result = dw.data_ptr(), D, V * D
+        else:
+            result = self._groups(dw, "dw", G, V, D, dtype)
         ws = self._scratch(self._lib.cocod_vocab_workspace(G, M, V, D, 1, _TYPES[dtype], self.workspace_limit))
         self._call("cocod_vocab_loss_grad", self._lib.cocod_vocab_loss_grad, *args, dx.data_ptr(), D,
-                   *self._groups(dw, "dw", G, V, D, dtype), _TYPES[dtype], ws.data_ptr(), ws.numel())
+                   *result, _TYPES[dtype], ws.data_ptr(), ws.numel())
         return loss, row_loss, dx, dw
 
     # ------------------------------------------------------------------------------------------ the rest
