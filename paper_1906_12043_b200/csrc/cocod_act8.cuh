@@ -19,31 +19,62 @@ using namespace cocod::gemm;
 constexpr int ACT_BLOCK = 128;         // columns that share a power of two
 constexpr int ACT_ROWS = 64;           // rows of a CTA of 256 threads
 
-// Eight bf16 of a row, starting at column c of k; what lies behind the row's end is 0.
-__device__ __forceinline__ uint4 load8(const __nv_bfloat16 *row, long long c, long long k, bool vec)
+// Eight bf16 of a row, starting at column c of k; what lies behind the row's end is 0.  A row may start at any even address (an odd
+// number of columns, a view): the widest accesses that the address allows, at worst one value, three pairs and one value.
+__device__ __forceinline__ uint4 load8(const __nv_bfloat16 *row, long long c, long long k)
 {
-    if (vec && c + 8 <= k) return *reinterpret_cast<const uint4 *>(row + c);
-    const unsigned short *r = reinterpret_cast<const unsigned short *>(row);
-    uint32_t v[4];
+    const unsigned short *r = reinterpret_cast<const unsigned short *>(row) + c;
+    const unsigned at = (unsigned)reinterpret_cast<uintptr_t>(r);
+    uint4 v;
+    if (c + 8 > k) {
+        uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = c + 2 * j < k ? r[c + 2 * j] : 0, hi = c + 2 * j + 1 < k ? r[c + 2 * j + 1] : 0;
-        v[j] = lo | hi << 16;
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = c + 2 * j < k ? r[2 * j] : 0, hi = c + 2 * j + 1 < k ? r[2 * j + 1] : 0;
+            w[j] = lo | hi << 16;
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if ((at & 15) == 0) {
+        v = *reinterpret_cast<const uint4 *>(r);
+    } else if ((at & 7) == 0) {
+        const uint2 a = *reinterpret_cast<const uint2 *>(r), b = *reinterpret_cast<const uint2 *>(r + 4);
+        v = make_uint4(a.x, a.y, b.x, b.y);
+    } else if ((at & 3) == 0) {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(r);
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(r + 1);
+        const uint32_t first = r[0], a = w[0], b = w[1], d = w[2], last = r[7];
+        v = make_uint4(first | a << 16, __funnelshift_l(a, b, 16), __funnelshift_l(b, d, 16), d >> 16 | last << 16);
     }
-    return make_uint4(v[0], v[1], v[2], v[3]);
+    return v;
 }
-__device__ __forceinline__ void store8(__nv_bfloat16 *row, long long c, long long k, bool vec, uint4 x)
+__device__ __forceinline__ void store8(__nv_bfloat16 *row, long long c, long long k, uint4 x)
 {
-    if (vec && c + 8 <= k) {
-        *reinterpret_cast<uint4 *>(row + c) = x;
-        return;
-    }
-    unsigned short *r = reinterpret_cast<unsigned short *>(row);
-    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+    unsigned short *r = reinterpret_cast<unsigned short *>(row) + c;
+    const unsigned at = (unsigned)reinterpret_cast<uintptr_t>(r);
+    if (c + 8 > k) {
+        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (c + 2 * j < k) r[c + 2 * j] = (unsigned short)v[j];
-        if (c + 2 * j + 1 < k) r[c + 2 * j + 1] = (unsigned short)(v[j] >> 16);
+        for (int j = 0; j < 4; ++j) {
+            if (c + 2 * j < k) r[2 * j] = (unsigned short)v[j];
+            if (c + 2 * j + 1 < k) r[2 * j + 1] = (unsigned short)(v[j] >> 16);
+        }
+    } else if ((at & 15) == 0) {
+        *reinterpret_cast<uint4 *>(r) = x;
+    } else if ((at & 7) == 0) {
+        *reinterpret_cast<uint2 *>(r) = make_uint2(x.x, x.y);
+        *reinterpret_cast<uint2 *>(r + 4) = make_uint2(x.z, x.w);
+    } else if ((at & 3) == 0) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(r);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    } else {
+        uint32_t *w = reinterpret_cast<uint32_t *>(r + 1);
+        r[0] = (unsigned short)x.x;
+        w[0] = __funnelshift_l(x.x, x.y, 16);
+        w[1] = __funnelshift_l(x.y, x.z, 16);
+        w[2] = __funnelshift_l(x.z, x.w, 16);
+        r[7] = (unsigned short)(x.w >> 16);
     }
 }
 
@@ -58,7 +89,7 @@ __device__ __forceinline__ int block_exponent(uint32_t amax)
 __device__ __forceinline__ float power_of_two(int biased) { return __uint_as_float((uint32_t)biased << 23); }
 
 __global__ void __launch_bounds__(256)
-act_pack(const __nv_bfloat16 *x, long long ldx, int8_t *q, long long ldq, uint8_t *scales, long long M, long long k, int vec)
+act_pack(const __nv_bfloat16 *x, long long ldx, int8_t *q, long long ldq, uint8_t *scales, long long M, long long k)
 {
     __shared__ uint8_t exps[ACT_ROWS];
     pdl_launch_dependents();
@@ -69,7 +100,7 @@ act_pack(const __nv_bfloat16 *x, long long ldx, int8_t *q, long long ldq, uint8_
     for (int h = 0; h < 2; ++h) {
         const long long m = (long long)blockIdx.x * ACT_ROWS + h * 32 + (threadIdx.x >> 3);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) in[h][p] = m < M ? load8(x + m * ldx, c + 64 * p, k, vec) : make_uint4(0, 0, 0, 0);
+        for (int p = 0; p < 2; ++p) in[h][p] = m < M ? load8(x + m * ldx, c + 64 * p, k) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -158,7 +189,7 @@ __device__ __forceinline__ __nv_bfloat162 unit_of(uint32_t scale)
 }
 
 __global__ void __launch_bounds__(256)
-act_unpack(const int8_t *q, long long ldq, const uint8_t *scales, __nv_bfloat16 *y, long long ldy, long long M, long long k, int vec)
+act_unpack(const int8_t *q, long long ldq, const uint8_t *scales, __nv_bfloat16 *y, long long ldy, long long M, long long k)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -183,14 +214,14 @@ act_unpack(const int8_t *q, long long ldq, const uint8_t *scales, __nv_bfloat16 
             uint4 v;
             widen4(b[h][p].x, unit, v.x, v.y);
             widen4(b[h][p].y, unit, v.z, v.w);
-            if (c + 64 * p < k) store8(y + m * ldy, c + 64 * p, k, vec, v);
+            if (c + 64 * p < k) store8(y + m * ldy, c + 64 * p, k, v);
         }
     }
 }
 
 __global__ void __launch_bounds__(256)
 act_relu_grad(const __nv_bfloat16 *dh, long long lddh, const int8_t *q, long long ldq, __nv_bfloat16 *dz, long long lddz, long long M,
-              long long k, int vec)
+              long long k)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -204,7 +235,7 @@ act_relu_grad(const __nv_bfloat16 *dh, long long lddh, const int8_t *q, long lon
         for (int p = 0; p < 2; ++p) {
             const bool there = m < M && c + 64 * p < k;
             b[h][p] = there ? *reinterpret_cast<const uint2 *>(q + m * ldq + c + 64 * p) : make_uint2(0, 0);
-            in[h][p] = there ? load8(dh + m * lddh, c + 64 * p, k, vec) : make_uint4(0, 0, 0, 0);
+            in[h][p] = there ? load8(dh + m * lddh, c + 64 * p, k) : make_uint4(0, 0, 0, 0);
         }
     }
 #pragma unroll
@@ -225,7 +256,7 @@ act_relu_grad(const __nv_bfloat16 *dh, long long lddh, const int8_t *q, long lon
                     v[2 * j + 1] |= __byte_perm(bad, 0, 0x3322) & 0x7fff7fffu;
                 }
             }
-            if (c + 64 * p < k) store8(dz + m * lddz, c + 64 * p, k, vec, make_uint4(v[0], v[1], v[2], v[3]));
+            if (c + 64 * p < k) store8(dz + m * lddz, c + 64 * p, k, make_uint4(v[0], v[1], v[2], v[3]));
         }
     }
 }

@@ -497,7 +497,7 @@ int cocod_act_pack(cocod_lm_handle *h, int64_t M, int64_t k, const void *x, int6
     if (M == 0) return COCOD_OK;
     const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
     TRY_CUDA(launch_dependent(true, act_pack, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(x), (long long)ldx, q,
-                              (long long)ldq, scales, (long long)M, (long long)k, (int)(aligned16(x) && ldx % 8 == 0)));
+                              (long long)ldq, scales, (long long)M, (long long)k));
     return COCOD_OK;
 }
 
@@ -508,7 +508,7 @@ int cocod_act_unpack(cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, 
     if (M == 0) return COCOD_OK;
     const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
     TRY_CUDA(launch_dependent(true, act_unpack, grid, dim3(256), 0, (cudaStream_t)stream, q, (long long)ldq, scales, static_cast<bf16 *>(y),
-                              (long long)ldy, (long long)M, (long long)k, (int)(aligned16(y) && ldy % 8 == 0)));
+                              (long long)ldy, (long long)M, (long long)k));
     return COCOD_OK;
 }
 
@@ -519,8 +519,7 @@ int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh
     if (M == 0) return COCOD_OK;
     const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
     TRY_CUDA(launch_dependent(true, act_relu_grad, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(dh), (long long)lddh, q,
-                              (long long)ldq, static_cast<bf16 *>(dz), (long long)lddz, (long long)M, (long long)k,
-                              (int)(aligned16(dh) && aligned16(dz) && lddh % 8 == 0 && lddz % 8 == 0)));
+                              (long long)ldq, static_cast<bf16 *>(dz), (long long)lddz, (long long)M, (long long)k));
     return COCOD_OK;
 }
 
