@@ -239,8 +239,10 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, i
     Matrix a_rows = A, b_rows = B;
     if (M == 0) a_rows.data = b_rows.data = h->group_maps;      // nothing is read
     CUtensorMap a, b, o;
-    if (!encode(&a, a_rows, rows, std::max<int64_t>(M, 1), 1, 64) || !encode(&b, b_rows, cols, std::max<int64_t>(M, 1), 1, 64) ||
-        !encode(&o, out, cols, rows, (uint64_t)G, 32))
+    if (!encode(&o, out, cols, rows, (uint64_t)G, 32)) return COCOD_ERR_CUDA;
+    a = b = o;                             // (the kernel takes the groups' maps, made of these two; a checkpoint has one for the whole batch)
+    if ((!maps_ready && !encode(&a, a_rows, rows, std::max<int64_t>(M, 1), 1, 64)) ||
+        ((!maps_ready || scales) && !encode(&b, b_rows, cols, std::max<int64_t>(M, 1), 1, 64)))
         return COCOD_ERR_CUDA;
     GroupedParams p{};
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;

@@ -23,7 +23,7 @@ BF16, F32 = 0, 1
 BLOCK = 128                      # columns that share a scale in an 8-bit checkpoint
 MAX_GROUPS = 1024
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
-_SIZES = {torch.bfloat16: 2, torch.float32: 4, torch.int8: 1}
+_SIZES = {torch.bfloat16: 2, torch.float32: 4}
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -37,12 +37,16 @@ class PackedActivations:
     128 columns of a row; scales is ceil(k / 128) x M.  A value that was not finite has q = -128, its block the scale 255, and the
     block reads as NaN."""
 
-    __slots__ = ("q", "scales", "shape")
+    __slots__ = ("shape", "_buffer", "_q", "_scales", "_at", "_ld", "_scales_at")
 
-    def __init__(self, M: int, k: int, device):
-        self.q = torch.empty((M, _round_up(k, 16)), dtype=torch.int8, device=device)[:, :k]
-        self.scales = torch.empty((-(-k // BLOCK), M), dtype=torch.uint8, device=device)
-        self.shape = (M, k)
+    def __init__(self, M: int, k: int, like):
+        """Room for M x k values on the device of `like`: one buffer, the whole numbers' rows first."""
+        ld = _round_up(k, 16)
+        self.shape, self._ld = (M, k), ld
+        self._buffer = like.new_empty(M * ld + -(-k // BLOCK) * M, dtype=torch.uint8)
+        self._at = self._buffer.data_ptr()
+        self._scales_at = self._at + M * ld
+        self._q = self._scales = None
 
     @classmethod
     def from_parts(cls, q, scales):
@@ -50,11 +54,28 @@ class PackedActivations:
         M, k = q.shape
         if q.dtype != torch.int8 or scales.dtype != torch.uint8 or tuple(scales.shape) != (-(-k // BLOCK), M):
             raise ValueError("q: M x k int8 and scales: ceil(k / 128) x M uint8 are needed")
-        if not scales.is_contiguous() or (q.numel() and (q.stride(1) != 1 or (M > 1 and q.stride(0) % 16) or q.data_ptr() % 16)):
-            raise ValueError("q needs 16-byte aligned rows, scales has to be contiguous")
+        if not scales.is_contiguous() or (q.numel() and (q.stride(1) != 1 or (M > 1 and (q.stride(0) % 16 or q.stride(0) < k)) or q.data_ptr() % 16)) \
+                or q.device != scales.device:
+            raise ValueError("q needs 16-byte aligned rows, scales has to be contiguous and on the same device")
         self = cls.__new__(cls)
-        self.q, self.scales, self.shape = q, scales, (M, k)
+        self.shape, self._ld = (M, k), q.stride(0) if M > 1 else _round_up(k, 16)
+        self._buffer, self._q, self._scales = q, q, scales
+        self._at, self._scales_at = q.data_ptr(), scales.data_ptr()
         return self
+
+    @property
+    def q(self):
+        if self._q is None:
+            M, k = self.shape
+            self._q = self._buffer[:M * self._ld].view(torch.int8).view(M, self._ld)[:, :k]
+        return self._q
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            M, k = self.shape
+            self._scales = self._buffer[M * self._ld:].view(-(-k // BLOCK), M)
+        return self._scales
 
 
 class LMOps:
@@ -166,7 +187,7 @@ class LMOps:
         if isinstance(x, PackedActivations):
             ws = self._scratch(self._lib.cocod_grouped_packed_workspace(G, M, n, k)) if self.widen else None
             self._call("cocod_grouped_weight_grad_packed", self._lib.cocod_grouped_weight_grad_packed, *shape,
-                       *self._rows(x.q, "x.q", M, k, torch.int8), x.scales.data_ptr(), *result, _TYPES[dtype],
+                       *self._kept(x, M, k), x._scales_at, *result, _TYPES[dtype],
                        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
         else:
             self._call("cocod_grouped_weight_grad", self._lib.cocod_grouped_weight_grad, *shape, *self._rows(x, "x", M, k), *result, _TYPES[dtype])
@@ -182,21 +203,25 @@ class LMOps:
         """The 8-bit form of x (M x k bf16)."""
         M, k = x.shape
         if out is None:
-            out = PackedActivations(M, k, x.device)
-        self._call("cocod_act_pack", self._lib.cocod_act_pack, M, k, *self._rows(x, "x", M, k, align=1),
-                   *self._rows(out.q, "out.q", M, k, torch.int8), out.scales.data_ptr())
+            out = PackedActivations(M, k, x)
+        self._call("cocod_act_pack", self._lib.cocod_act_pack, M, k, *self._rows(x, "x", M, k, align=1), *self._kept(out, M, k), out._scales_at)
         return out
+
+    def _kept(self, packed, M, k):
+        """(address, row stride) of a checkpoint's whole numbers."""
+        if packed.shape == (M, k) and packed._buffer.get_device() == self._device:
+            return packed._at, packed._ld
+        raise ValueError(f"checkpoint: need {M} x {k} on cuda:{self._device}, got {packed.shape} on {packed._buffer.device}")
 
     def act_unpack(self, packed, out=None):
         """The bf16 values that a checkpoint stands for."""
         M, k = packed.shape
         if out is None:
-            out = packed.q.new_empty((M, k), dtype=torch.bfloat16)
+            out = packed._buffer.new_empty((M, k), dtype=torch.bfloat16)
             at, ld = out.data_ptr(), k
         else:
             at, ld = self._rows(out, "out", M, k, align=1)
-        self._call("cocod_act_unpack", self._lib.cocod_act_unpack, M, k, *self._rows(packed.q, "packed.q", M, k, torch.int8),
-                   packed.scales.data_ptr(), at, ld)
+        self._call("cocod_act_unpack", self._lib.cocod_act_unpack, M, k, *self._kept(packed, M, k), packed._scales_at, at, ld)
         return out
 
     def act_relu_grad(self, dh, packed, out=None):
@@ -208,7 +233,7 @@ class LMOps:
             at, ld = out.data_ptr(), k
         else:
             at, ld = self._rows(out, "out", M, k, align=1)
-        self._call("cocod_act_relu_grad", self._lib.cocod_act_relu_grad, M, k, *given, *self._rows(packed.q, "packed.q", M, k, torch.int8), at, ld)
+        self._call("cocod_act_relu_grad", self._lib.cocod_act_relu_grad, M, k, *given, *self._kept(packed, M, k), at, ld)
         return out
 
     # ------------------------------------------------------------------------------------------ vocabulary
