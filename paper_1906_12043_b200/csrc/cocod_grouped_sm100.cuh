@@ -269,6 +269,7 @@ template <int TM, int TN, bool WG> struct Walker {
     __device__ Walker(const GroupedParams &params, int lane_, int clusters) : p(params), lane(lane_)
     {
         int tiles = 0;
+        bool loaded = false;
         if (WG) {
             for (int g0 = 0; g0 < p.groups; g0 += 32) {
                 if (g0 + lane < p.groups) group_range(p, g0 + lane, lo, hi);
@@ -283,6 +284,7 @@ template <int TM, int TN, bool WG> struct Walker {
             }
             gb = 0;
             whole = tiles;
+            loaded = p.groups <= 32;
         }
         if (p.max_parts > 1) {
             const int rest = tiles % clusters;
@@ -292,7 +294,7 @@ template <int TM, int TN, bool WG> struct Walker {
                 whole = tiles - rest;
             }
         }
-        if (!WG) load();
+        if (!WG && !loaded) load();
     }
     __device__ void load()
     {
@@ -817,10 +819,15 @@ join_parts(const GroupedParams p, const float *scratch, int clusters)
     if (t.m0 + row >= t.m1 || t.n0 + c >= p.n) return;
     const float *src = scratch + (long long)t.slot * (TM * TN) + row * TN + c;
     float4 s = *reinterpret_cast<const float4 *>(src);
-#pragma unroll 16
-    for (int k = 1; k < walk.parts; ++k) {
-        const float4 v = *reinterpret_cast<const float4 *>(src + (long long)k * (TM * TN));
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    for (int k0 = 1; k0 < walk.parts; k0 += 8) {          // eight loads under way together
+        float4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = k0 + k < walk.parts ? *reinterpret_cast<const float4 *>(src + (long long)(k0 + k) * (TM * TN)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            s.x += v[k].x; s.y += v[k].y; s.z += v[k].z; s.w += v[k].w;
+        }
     }
     const long long at = (WG ? t.g * p.out_stride : 0) + (t.m0 + row) * p.ld_out + t.n0 + c;
     if (OUT == OUT_BF16) {

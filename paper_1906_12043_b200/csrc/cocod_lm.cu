@@ -261,7 +261,7 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, i
 // ------------------------------------------------------------------------------------------ vocabulary
 // How a call's workspace is laid out when `at_once` rows are taken together.
 struct VocabLayout {
-    int64_t label, own, ref, share, any;       // whole batch: byte offsets
+    int64_t label, group, own, ref, share, any;       // whole batch: byte offsets
     int64_t rho, redo, sums, u, hs;            // rows of one pass
     int64_t total32;                           // fp32 gradient of the weights, if it is summed over passes and wanted in bf16
     int64_t bytes, ldu, n_sums;
@@ -272,6 +272,7 @@ VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int 
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t here = at; at += ceil_div(bytes, 256) * 256; return here; };
     l.label = take(4 * M);
+    l.group = take(4 * M);
     l.own = take(4 * M);
     l.ref = take(4 * M);
     l.share = take(4 * G);
@@ -317,7 +318,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
     v.offsets = offsets; v.groups = G; v.total = (int)M; v.vocab = (int)V; v.width = (int)D; v.labels = labels; v.row_weight = row_weight;
     v.h = static_cast<const bf16 *>(x.data); v.ldh = x.ld;
     v.w = static_cast<const bf16 *>(w.data); v.ldw = w.ld; v.w_stride = w.stride;
-    v.label = reinterpret_cast<int *>(ws + l.label); v.own = reinterpret_cast<float *>(ws + l.own);
+    v.label = reinterpret_cast<int *>(ws + l.label); v.group = reinterpret_cast<int *>(ws + l.group); v.own = reinterpret_cast<float *>(ws + l.own);
     v.ref = reinterpret_cast<float *>(ws + l.ref); v.share = reinterpret_cast<float *>(ws + l.share);
     v.redo_any = reinterpret_cast<int *>(ws + l.any);
     v.error_flag = h->flag;

@@ -31,6 +31,7 @@ struct VocabRows {
     const __nv_bfloat16 *w;            // [groups][vocab][ldw]
     long long ldw, w_stride;
     int *label;                        // [total]: negative where the row takes no part
+    int *group;                        // [total]: the row's group
     float *own;                        // [total]: the label's logit
     float *ref;                        // [total]: c_r
     float *share;                      // [groups]: 1 / rows with a label
@@ -38,15 +39,16 @@ struct VocabRows {
     int *error_flag;
 };
 
-__device__ __forceinline__ int group_of(const int *offsets, int groups, int r)      // -1: in no group
+// The group of row r, -1: in none (one warp, 32 groups at a time).
+__device__ __forceinline__ int group_of(const int *offsets, int groups, int r)
 {
-    if (r < offsets[0] || r >= offsets[groups]) return -1;
-    int lo = 0, hi = groups;           // offsets[lo] <= r < offsets[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (offsets[mid] <= r) lo = mid; else hi = mid;
+    const int lane = threadIdx.x & 31;
+    for (int g0 = 0; g0 < groups; g0 += 32) {
+        const int g = g0 + lane;
+        const uint32_t hit = __ballot_sync(0xffffffffu, g < groups && offsets[g] <= r && r < offsets[g + 1]);
+        if (hit) return g0 + __ffs(hit) - 1;
     }
-    return lo;
+    return -1;
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -93,8 +95,8 @@ vocab_begin(const __grid_constant__ CUtensorMap whole_u, const __grid_constant__
     }
     const long long r = window.row0 + (long long)blockIdx.x * 8 + warp;
     if (r >= window.row0 + window.rows) return;
-    const int g = group_of(p.offsets, p.groups, (int)r);
     int t = p.labels[r];
+    const int g = group_of(p.offsets, p.groups, (int)r);
     if (t >= p.vocab) {
         if (lane == 0 && p.error_flag != nullptr) atomicExch(p.error_flag, ERR_LABEL);
         t = -1;
@@ -118,6 +120,7 @@ vocab_begin(const __grid_constant__ CUtensorMap whole_u, const __grid_constant__
     s = warp_sum(s);
     if (lane == 0) {
         p.label[r] = t < 0 ? -1 : t;
+        p.group[r] = max(g, 0);
         p.own[r] = s;
         p.ref[r] = s;
     }
@@ -188,9 +191,20 @@ vocab_finish(const FinishParams p)
         t = p.v.label[p.row0 + row];
         own = p.v.own[p.row0 + row];
         ref = p.v.ref[p.row0 + row];
-        const int g = group_of(p.v.offsets, p.v.groups, p.row0 + row);
-        if (p.rho != nullptr && g >= 0) share = p.v.row_weight != nullptr ? p.v.row_weight[p.row0 + row] : p.v.share[g];
+        if (p.rho != nullptr) share = p.v.row_weight != nullptr ? p.v.row_weight[p.row0 + row] : p.v.share[p.v.group[p.row0 + row]];
     }
+    // The first values of h are under way before the sums are known.
+    const int vecs = p.v.width / 8, rows = min(FINISH_ROWS, p.rows - first), all = p.rho != nullptr ? rows * vecs : 0;
+    constexpr int BATCH = 4, THREADS = 32 * FINISH_WARPS;
+    uint4 x[BATCH];
+    auto fetch = [&](int i0) {
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const int i = i0 + b * THREADS, rr = i / vecs;
+            if (i < all) x[b] = reinterpret_cast<const uint4 *>(p.v.h + (long long)(p.row0 + first + rr) * p.v.ldh)[i - rr * vecs];
+        }
+    };
+    fetch(threadIdx.x);
     if (row < p.rows) {
 #pragma unroll 8
         for (int i = warp; i < p.n_sums; i += FINISH_WARPS) {
@@ -248,20 +262,23 @@ vocab_finish(const FinishParams p)
     }
     if (p.rho == nullptr) return;
     __syncthreads();
-    const int vecs = p.v.width / 8, rows = min(FINISH_ROWS, p.rows - first);
-    for (int i = threadIdx.x; i < rows * vecs; i += 32 * FINISH_WARPS) {
-        const int rr = i / vecs, c = i - rr * vecs;
-        const float f = factor[rr];
-        uint4 o = make_uint4(0, 0, 0, 0);
-        if (f != 0.0f) {               // (a row that takes no part is 0 whatever it holds)
-            const uint4 x = reinterpret_cast<const uint4 *>(p.v.h + (long long)(p.row0 + first + rr) * p.v.ldh)[c];
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-            uint32_t os[4];
+    for (int i0 = threadIdx.x; i0 < all; i0 += BATCH * THREADS) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) os[j] = pack_bf16x2(__uint_as_float(xs[j] << 16) * f, __uint_as_float(xs[j] & 0xffff0000u) * f);
-            o = make_uint4(os[0], os[1], os[2], os[3]);
+        for (int b = 0; b < BATCH; ++b) {
+            const int i = i0 + b * THREADS, rr = i / vecs;
+            if (i >= all) break;
+            const float f = factor[rr];
+            uint4 o = make_uint4(0, 0, 0, 0);
+            if (f != 0.0f) {           // (a row that takes no part is 0 whatever it holds)
+                const uint32_t xs[4] = {x[b].x, x[b].y, x[b].z, x[b].w};
+                uint32_t os[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) os[j] = pack_bf16x2(__uint_as_float(xs[j] << 16) * f, __uint_as_float(xs[j] & 0xffff0000u) * f);
+                o = make_uint4(os[0], os[1], os[2], os[3]);
+            }
+            reinterpret_cast<uint4 *>(p.hs + (long long)(first + rr) * p.v.width)[i - rr * vecs] = o;
         }
-        reinterpret_cast<uint4 *>(p.hs + (long long)(first + rr) * p.v.width)[c] = o;
+        fetch(i0 + BATCH * THREADS);
     }
 }
 
