@@ -818,16 +818,18 @@ join_parts(const GroupedParams p, const float *scratch, int clusters)
     const int i = blockIdx.y * 256 + threadIdx.x, row = i / QUADS, c = (i % QUADS) * 4;
     if (t.m0 + row >= t.m1 || t.n0 + c >= p.n) return;
     const float *src = scratch + (long long)t.slot * (TM * TN) + row * TN + c;
-    float4 s = *reinterpret_cast<const float4 *>(src);
-    for (int k0 = 1; k0 < walk.parts; k0 += 8) {          // eight loads under way together
-        float4 v[8];
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    constexpr int AT_ONCE = 24;                           // loads under way together: most tiles have no more parts (a round trip takes 1 us)
+    for (int k0 = 0; k0 < walk.parts; k0 += AT_ONCE) {
+        float4 v[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = k0 + k < walk.parts ? *reinterpret_cast<const float4 *>(src + (long long)(k0 + k) * (TM * TN)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (k0 + k < walk.parts) v[k] = *reinterpret_cast<const float4 *>(src + (long long)(k0 + k) * (TM * TN));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            s.x += v[k].x; s.y += v[k].y; s.z += v[k].z; s.w += v[k].w;
-        }
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (k0 + k < walk.parts) {
+                s.x += v[k].x; s.y += v[k].y; s.z += v[k].z; s.w += v[k].w;
+            }
     }
     const long long at = (WG ? t.g * p.out_stride : 0) + (t.m0 + row) * p.ld_out + t.n0 + c;
     if (OUT == OUT_BF16) {
