@@ -539,6 +539,57 @@ def test_vocabulary_into_the_workers_gradients(ops):
     assert (grads[:, :64] == 3).all() and (grads[:, 64 + V * D:] == 3).all()
 
 
+# ------------------------------------------------------------------------------------------------------- beyond 2^31 values
+def test_checkpoint_beyond_32_bits(ops):
+    M, k = 70001, 32768
+    x = torch.empty(M, k, device="cuda", dtype=torch.bfloat16)
+    x[:64], x[-64:] = gaussian(1, 64, k), gaussian(2, 64, k)
+    p = ops.act_pack(x)
+    for rows in (slice(0, 64), slice(M - 64, M)):
+        alone = ops.act_pack(x[rows].clone())
+        assert torch.equal(alone.q, p.q[rows]) and torch.equal(alone.scales, p.scales[:, rows])
+    y = ops.act_unpack(p)
+    assert torch.equal(y[-64:], ops.act_unpack(ops.act_pack(x[-64:].clone())))
+    del y
+    z = ops.act_relu_grad(x, p, out=x)
+    assert torch.equal(z[-64:], torch.where(p.q[-64:] > 0, z[-64:], torch.zeros_like(z[-64:]))) and (z[-64:] > 0).any()
+
+
+def test_products_beyond_32_bits(ops):
+    M, n, k = 66001, 33024, 16
+    off, spans = offsets_of([30000, 36001])
+    x, w = gaussian(1, M, k), gaussian(2, 2, n, k)
+    y = ops.grouped_forward(x, w, off)
+    for rows, g in ((slice(29900, 30000), 0), (slice(30000, 30100), 1), (slice(M - 100, M), 1)):
+        want, size = x[rows].double() @ w[g].double().T, x[rows].double().abs() @ w[g].double().abs().T
+        assert_sum(y[rows], want, size, k)
+    dw = ops.grouped_weight_grad(y, x, off)
+    want, size = y[30000:, -64:].double().T @ x[30000:].double(), y[30000:, -64:].double().abs().T @ x[30000:].double().abs()
+    assert_sum(dw[1, -64:], want, size, 36001)
+
+
+def test_vocabulary_beyond_32_bits(lm):
+    M, V, D = 17001, 131073, 16
+    off, spans = offsets_of([M])
+    h, w = gaussian(1, M, D), gaussian(2, 1, V, D, scale=0.5)
+    labels = torch.randint(0, V, (M,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    o = lm.LMOps(workspace_limit=16 << 30)
+    loss, row, dx, dw = o.vocab_loss_grad(h, w, labels, off)
+    o.check()
+    last = slice(M - 50, M)
+    logits = h[last].double() @ w[0].double().T
+    own = logits.gather(1, labels[last].long()[:, None])[:, 0]
+    want = torch.logsumexp(logits, 1) - own
+    d = (D / 16 + 8) * 2.0 ** -23 * float(h.float().norm(dim=1).max() * w.float().norm(dim=2).max())
+    assert ((row[last].double() - want).abs() <= 2 * d + 2.0 ** -20 * (1 + want)).all()
+    p = torch.softmax(logits, 1)
+    p[torch.arange(50, device="cuda"), labels[last].long()] -= 1
+    p /= M
+    near = p.abs() @ w[0].double().abs()
+    assert ((dx[last].double() - p @ w[0].double()).abs() <= (2.0 ** -8 * 1.02 + 2 * d + (V / 16 + 40) * 2.0 ** -23) * near + 2.0 ** -8 * near + 1e-38).all()
+    o.destroy()
+
+
 # ------------------------------------------------------------------------------------------------------- refusals
 def test_refusals(lm, ops):
     from paper_1906_12043_b200.engine import CocodError, ERR_INVALID, ERR_TIMEOUT
