@@ -46,12 +46,12 @@ enum Operand { B_K = 0, B_MN = 1, B_Q8 = 2 };                       // B: reduct
 constexpr int EPI_WARPS = 8, CONV_WARPS = 8;
 __host__ __device__ constexpr int grouped_threads(int b) { return 128 + 32 * EPI_WARPS + (b == B_Q8 ? 32 * CONV_WARPS : 0); }
 constexpr int Q_BYTES = 64 * 128;                                   // 8-bit values of a block of the reduction
-__host__ __device__ constexpr int ring(int b) { return b == B_Q8 ? 4 : 5; }                  // stages
+__host__ __device__ constexpr int ring(int b) { return b == B_Q8 ? 4 : 6; }                  // stages
 __host__ __device__ constexpr int stage_bytes(int b) { return STAGE_BYTES + (b == B_Q8 ? Q_BYTES : 0); }
-constexpr int OUT_BYTES = 2 * 4096;                                 // staging of an epilogue warp: twice 32 rows of 128 bytes
+constexpr int OUT_BYTES = 4096;                                     // staging of an epilogue warp: 32 rows of 128 bytes
 constexpr int AHEAD = 4;                                            // tiles that the scheduler may be ahead
-constexpr int GROUPED_SMEM = 5 * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 1024;
-static_assert(ring(B_Q8) * stage_bytes(B_Q8) <= 5 * STAGE_BYTES, "the stages with 8-bit values take the same room");
+constexpr int GROUPED_SMEM = 6 * STAGE_BYTES + EPI_WARPS * OUT_BYTES + 1024 + 1024;
+static_assert(ring(B_Q8) * stage_bytes(B_Q8) <= 6 * STAGE_BYTES, "the stages with 8-bit values take the same room");
 // Registers per thread: what a launch holds, and what the warps 0..3, the epilogue and the converting warps keep of it.
 __host__ __device__ constexpr int launch_registers(int b) { return b == B_Q8 ? 96 : 168; }
 __host__ __device__ constexpr int few_registers(int b) { return b == B_Q8 ? 48 : 64; }
@@ -483,49 +483,45 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         uint8_t *staging = outs + (warp - 4) * OUT_BYTES;
         constexpr int HALF = TN / 2, CHUNK = is_f32(OUT) ? 32 : 64, CHUNKS = HALF / CHUNK;      // a chunk: 128 bytes of a row
-        constexpr int ES = is_f32(OUT) ? 4 : 2, PER = 16 / ES, AT_ONCE = CHUNKS < 2 ? 1 : 2;
+        constexpr int ES = is_f32(OUT) ? 4 : 2, PER = 16 / ES;
         Tile t{};
         unsigned ai = 0;
-        // Up to two chunks at a time go through the warp's staging: one wait for the store engine's reads, one fence.
+        // A chunk at a time goes through the warp's staging.  (Room for two saved waits and cost a stage of the ring: 1 to 5 % slower.)
         auto staging_free = [&]() {
             if (lane == 0) tma_store_wait_read<0>();
             __syncwarp();
         };
-        auto stage_f32 = [&](const uint32_t (&r)[32], int h) {
+        auto stage_f32 = [&](const uint32_t (&r)[32]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                *reinterpret_cast<uint4 *>(staging + h * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                *reinterpret_cast<uint4 *>(staging + lane * 128 + ((j ^ (lane & 7)) << 4)) =
                     make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
         };
-        auto stage_bf16 = [&](const uint32_t (&r)[64], int h) {
+        auto stage_bf16 = [&](const uint32_t (&r)[64]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                *reinterpret_cast<uint4 *>(staging + h * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                *reinterpret_cast<uint4 *>(staging + lane * 128 + ((j ^ (lane & 7)) << 4)) =
                     make_uint4(pack_bf16x2(__uint_as_float(r[8 * j]), __uint_as_float(r[8 * j + 1])), pack_bf16x2(__uint_as_float(r[8 * j + 2]), __uint_as_float(r[8 * j + 3])),
                                pack_bf16x2(__uint_as_float(r[8 * j + 4]), __uint_as_float(r[8 * j + 5])), pack_bf16x2(__uint_as_float(r[8 * j + 6]), __uint_as_float(r[8 * j + 7])));
         };
-        // The staged chunks to out: row m, column col.
+        // The staged chunk to out: row m, column col.
         auto store = [&](int col, int m, int valid) {
             if (WG || valid >= 32) {
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-#pragma unroll
-                    for (int h = 0; h < AT_ONCE; ++h) {
-                        if (col + h * CHUNK >= p.n) break;
-                        if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, t.g);
-                        else tma_store_3d(&map_out, smem_u32(staging) + h * 4096, col + h * CHUNK, m, WG ? t.g : 0);
-                    }
+                    if (OUT == OUT_ADD_F32) tma_add_3d(&map_out, smem_u32(staging), col, m, t.g);
+                    else tma_store_3d(&map_out, smem_u32(staging), col, m, WG ? t.g : 0);
                     tma_store_commit();
                 }
             } else {
                 __syncwarp();
                 uint8_t *dst = static_cast<uint8_t *>(p.out) + ((long long)m * p.ld_out + col) * ES;
 #pragma unroll
-                for (int q = 0; q < 8 * AT_ONCE; ++q) {
-                    const int row = (q & 7) * 4 + (lane >> 3), piece = lane & 7, c = (q >> 3) * CHUNK + piece * PER;
-                    const uint4 v = *reinterpret_cast<const uint4 *>(staging + (q >> 3) * 4096 + row * 128 + ((piece ^ (row & 7)) << 4));
-                    if (row < valid && col + c < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + c * ES) = v;
+                for (int q = 0; q < 8; ++q) {
+                    const int row = q * 4 + (lane >> 3), piece = lane & 7;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(staging + row * 128 + ((piece ^ (row & 7)) << 4));
+                    if (row < valid && col + piece * PER < p.n) *reinterpret_cast<uint4 *>(dst + (long long)row * p.ld_out * ES + piece * 16) = v;
                 }
                 __syncwarp();
             }
@@ -587,16 +583,13 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             }
             if (!is_vocab(OUT) && t.slot >= 0) {         // a part: fp32, in the scratch
 #pragma unroll
-                for (int c = 0; c < HALF; c += 64) {
+                for (int c = 0; c < HALF; c += 32) {
                     staging_free();
-                    stage_f32(*reinterpret_cast<const uint32_t (*)[32]>(&acc[c]), 0);
-                    stage_f32(*reinterpret_cast<const uint32_t (*)[32]>(&acc[c + 32]), 1);
+                    stage_f32(*reinterpret_cast<const uint32_t (*)[32]>(&acc[c]));
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            tma_store_3d(&map_parts, smem_u32(staging) + h * 4096, half * HALF + c + h * 32, t.slot * TM + (int)rank * 128 + quarter * 32, 0);
+                        tma_store_3d(&map_parts, smem_u32(staging), half * HALF + c, t.slot * TM + (int)rank * 128 + quarter * 32, 0);
                         tma_store_commit();
                     }
                 }
@@ -624,13 +617,11 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     }
                     sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
                 }
-                if (OUT == OUT_VOCAB_SUMS) continue;
-                const int h = c % AT_ONCE;
-                if (col - h * CHUNK >= p.n) continue;
-                if (h == 0) staging_free();
-                if constexpr (is_f32(OUT)) stage_f32(r, h);
-                else stage_bf16(r, h);
-                if (h == AT_ONCE - 1) store(col - h * CHUNK, m, valid);
+                if (OUT == OUT_VOCAB_SUMS || col >= p.n) continue;
+                staging_free();
+                if constexpr (is_f32(OUT)) stage_f32(r);
+                else stage_bf16(r);
+                store(col, m, valid);
             }
             if (is_vocab(OUT) && col0 < p.n && lane < valid) p.sums[(long long)(col0 / HALF) * p.ld_sums + m + lane] = make_float2(sum, most);
         }
