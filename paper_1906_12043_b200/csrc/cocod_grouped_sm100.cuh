@@ -807,7 +807,7 @@ join_parts(const GroupedParams p, const float *scratch, int clusters)
     if ((int)blockIdx.x >= walk.cut || !walk.find(walk.whole + blockIdx.x * walk.parts, t)) return;
     constexpr int QUADS = TN / 4;
     const int i = blockIdx.y * 256 + threadIdx.x, row = i / QUADS, c = (i % QUADS) * 4;
-    if (t.m0 + row >= t.m1 || t.n0 + c >= p.n) return;
+    if (t.m0 + row >= (WG ? p.kdim : t.m1) || t.n0 + c >= p.n) return;
     const float *src = scratch + (long long)t.slot * (TM * TN) + row * TN + c;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     constexpr int AT_ONCE = 24;                           // loads under way together: most tiles have no more parts (a round trip takes 1 us)

@@ -119,6 +119,44 @@ def test_views_of_the_workers_state(ops, sizes, n, k):
     assert_sum(ops.grouped_input_grad(dy, w, off), dx, dxa, n)
 
 
+@pytest.mark.parametrize("sizes,n,k", [([6294, 100, 6294], 592, 392), ([20000], 136, 72), ([3000, 9000], 264, 520), ([40, 0, 12000], 200, 1032)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_long_reductions_with_few_results(ops, sizes, n, k, dtype):
+    """Tiles whose reduction is cut into parts, at widths that end inside a tile: every group's matrix is complete and nothing beside it is
+    written."""
+    off, spans = offsets_of(sizes)
+    M, G = sum(sizes), len(sizes)
+    P = n * k + 512
+    x, dy = gaussian(1, M, k), gaussian(3, M, n)
+    want = torch.stack([dy[s].double().T @ x[s].double() for s in spans])
+    size = torch.stack([dy[s].double().abs().T @ x[s].double().abs() for s in spans])
+    grads = torch.full((G + 1, P), 7.0, device="cuda", dtype=dtype)
+    out = torch.as_strided(grads, (G, n, k), (P, k, 1), 256)
+    for a in (x, ops.act_pack(x)):
+        grads.fill_(7.0)
+        got = ops.grouped_weight_grad(dy, a, off, out=out)
+        if a is x:
+            assert_sum(got, want, size, max(sizes))
+        else:
+            kept = ops.act_unpack(a)
+            assert_sum(got, torch.stack([dy[s].double().T @ kept[s].double() for s in spans]), size * 1.02 + 1e-3, max(sizes))
+        assert (grads[0, :256] == 7).all() and (grads[G] == 7).all() and (grads[:G, 256 + n * k:] == 7).all()
+        assert (grads[1:G, :256] == 7).all()
+    # and the rows form: a deep product with few rows
+    w = gaussian(2, G, 264, M // 8 * 8, scale=0.02)
+    few, few_spans = offsets_of([3, 30] + [5] * (G - 2) if G > 1 else [37])
+    r = int(few[-1])
+    deep = gaussian(4, r, w.shape[2])
+    y = torch.full((r + 2, 272), 7.0, device="cuda", dtype=dtype)
+    ops.grouped_forward(deep, w, few, out=y[1:-1, :264])
+    yw = torch.cat([deep[s].double() @ w[g].double().T for g, s in enumerate(few_spans)])
+    ya = torch.cat([deep[s].double().abs() @ w[g].double().abs().T for g, s in enumerate(few_spans)])
+    assert_sum(y[1:-1, :264], yw, ya, w.shape[2])
+    assert (y[0] == 7).all() and (y[-1] == 7).all() and (y[:, 264:] == 7).all()
+    dx = ops.grouped_input_grad(gaussian(5, r, 264), gaussian(6, G, 264, 4096, scale=0.1), few)
+    assert torch.isfinite(dx.float()).all()
+
+
 def test_other_groups_values_never_leak(ops):
     """NaN and infinities in one group's rows and weights stay in that group's results."""
     sizes = [130, 61, 7, 300]
