@@ -577,6 +577,34 @@ def test_vocabulary_into_the_workers_gradients(ops):
     assert (grads[:, :64] == 3).all() and (grads[:, 64 + V * D:] == 3).all()
 
 
+# ------------------------------------------------------------------------------------------------------- drawn shapes
+@pytest.mark.parametrize("seed", range(40))
+def test_drawn_shapes(lm, ops, seed):
+    """Sizes, divisions and types by chance; groups without rows anywhere."""
+    import random
+    r = random.Random(seed)
+    G, M = r.choice([1, 2, 3, 7, 33]), r.choice([1, 5, 64, 300, 1500, 6000])
+    n, k = 8 * r.choice([1, 3, 16, 33, 75, 130]), 8 * r.choice([1, 2, 9, 32, 49, 128])
+    cuts = sorted(r.choice([0, M, r.randint(0, M)]) for _ in range(G - 1))
+    sizes = [b - a for a, b in zip([0] + cuts, cuts + [M])]
+    off, spans = offsets_of(sizes)
+    dtype = r.choice([torch.bfloat16, torch.float32])
+    x, w, dy = gaussian(seed, M, k), gaussian(seed + 1, G, n, k, scale=k ** -0.5), gaussian(seed + 2, M, n)
+    (y, ya), (dx, dxa), (dw, dwa) = products(x, w, dy, spans)
+    assert_sum(ops.grouped_forward(x, w, off, out_dtype=dtype), y, ya, k)
+    assert_sum(ops.grouped_input_grad(dy, w, off, out_dtype=dtype), dx, dxa, n)
+    assert_sum(ops.grouped_weight_grad(dy, x, off, out_dtype=dtype), dw, dwa, M)
+    p = ops.act_pack(x)
+    kept = ops.act_unpack(p)
+    (_, _), (_, _), (dw, dwa) = products(kept, w, dy, spans)
+    assert_sum(ops.grouped_weight_grad(dy, p, off, out_dtype=dtype), dw, dwa, M)
+    V = r.choice([3, 127, 1000, 4097])
+    w = gaussian(seed + 1, G, V, k, scale=2 * k ** -0.5)
+    labels = torch.randint(-1, V, (M,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32).cuda()
+    check_vocab(ops.vocab_loss_grad(x, w, labels, off, dw_dtype=dtype), x, w, labels, spans)
+    ops.check()
+
+
 # ------------------------------------------------------------------------------------------------------- beyond 2^31 values
 def test_checkpoint_beyond_32_bits(ops):
     M, k = 70001, 32768
