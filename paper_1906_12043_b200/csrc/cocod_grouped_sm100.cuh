@@ -8,8 +8,8 @@
 // One persistent, warp-specialised kernel serves all forms:
 //   * A tile is 256 x 256, computed by a PAIR of CTAs (cta_group::2): each holds 128 rows of A and 128 columns of B per
 //     64-deep block of the reduction (32 KB a stage, six stages), so a pair moves 64 bytes per SM and clock for tensor
-//     cores that need 512 clocks for the block; a single CTA with a tile of its own would need half as much again from
-//     L2.  Problems with few tiles use 128 x 128 tiles and single CTAs (CG = 1): more SMs take part.
+//     cores that need 512 clocks for the block.  Problems with few tiles use 128 x 128 tiles and single CTAs (CG = 1): twice
+//     the bytes for a product, but more SMs take part.
 //   * Two accumulators in tensor memory: the epilogue of a tile runs under the products of the next.
 //   * Warps: 0 producer (TMA), 1 issuer of tcgen05.mma (leading CTA of the pair only), 2 tensor memory, 3 scheduler, 4..11 epilogue.
 //     The scheduler reads the tile list (Walker) some tiles ahead and leaves them in shared memory; when every role found
@@ -26,12 +26,18 @@
 // the difference.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
 // with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
-// The weight gradient can take B as an 8-bit checkpoint (B_Q8): TMA brings the bytes, an idle warp their scales, and four more warps write
+// The weight gradient can take B as an 8-bit checkpoint (B_Q8): TMA brings the bytes, an idle warp their scales, and eight more warps write
 // the bf16 operand tile, exactly (a whole number times a power of two), with zeros behind the group's end.
 // The number of tiles is seldom a multiple of the CTA pairs.  The tiles of the last, incomplete wave (all of them when there are few)
 // are cut along the reduction into as many parts as keep every pair busy; a part leaves as fp32 in scratch, at most one per
 // pair, and join_parts adds the parts of a tile up in a fixed order.  5.2 waves of tiles take 5.2 and not 6 times a tile.
 // Every wait is bounded, as in cocod_gemm_sm100.cuh.
+//
+// What bounds it.  Large products: the GPU's power limit.  8192 x 65536 x 2048 back to back runs at 1.45 GHz and takes 1752 us
+// forward (1255 TFLOP/s), 1820 as an input gradient, 1768 as a weight gradient; all zeros, which switch less, run a fifth
+// faster.  A block of 64 takes a pair 589 clocks, its products 506.  Small ones: the launch, the pipeline's filling and the
+// last wave (24 rows in 4 groups, 512 x 512: 6.8 us, of which 3.5 are a kernel without tiles).  Few rows with much to write: DRAM (16 workers
+// of 16 to 128 rows, a 16777216-value gradient each: 125 us, 4.3 TB/s of writes).
 #pragma once
 #include "cocod_act8.cuh"
 #include "cocod_gemm_sm100.cuh"
@@ -656,8 +662,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint4 w;
-                        widen4(v[i][h].x, unit, w.x, w.y);
-                        widen4(v[i][h].y, unit, w.z, w.w);
+                        widen4(v[i][h].x, unit, unit, w.x, w.y);
+                        widen4(v[i][h].y, unit, unit, w.z, w.w);
                         *reinterpret_cast<uint4 *>(db + (h ^ odd) * (BK * 128) + r * 128 + ((j ^ (r & 7)) << 4)) = w;
                     }
                 }

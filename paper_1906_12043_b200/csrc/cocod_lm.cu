@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 
 struct cocod_lm {                          // device addresses in the scratch that the caller lends
     CUtensorMap *group_maps = nullptr;     // two per group
@@ -489,9 +490,17 @@ int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets,
 
 static bool good_act(const cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, int64_t ldq)
 {
-    return h && M >= 0 && M <= MAX_DIM && k >= 1 && k <= 65535ll * ACT_BLOCK && (M == 0 || q) && aligned16(q) && ldq % 16 == 0 && ldq >= k &&
+    return h && M >= 0 && M <= MAX_DIM && k >= 1 && k <= 65535ll * ACT_BLOCK - 7 && (M == 0 || q) && aligned16(q) && ldq % 16 == 0 && ldq >= k &&
            ldq < (1ll << 36);
 }
+// Which form of the kernels below a call takes (cocod_act8.cuh): whether all rows start at multiples of so many bytes ...
+static bool rows_aligned(const void *p, int64_t ld, int64_t M, int bytes)
+{
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (M == 1 || ld * 2 % bytes == 0);
+}
+// ... and how many rows a thread takes: one while all CTAs find a place at the same time (8192 x 512: packed in 3.8 us, two rows 4.3;
+// 77 x 999: 2.1 and 2.8), two beyond that (32768 x 4095: 98 us, one row 104).
+static int act_rows_at_once(int64_t M, int64_t k) { return ceil_div(M, ACT_ROWS) * ceil_div(k, ACT_BLOCK) <= 8 * (int64_t)sm_count() ? 1 : 2; }
 static bool good_bf16(const void *p, int64_t ld, int64_t M, int64_t k)
 {
     return (M == 0 || p) && (reinterpret_cast<uintptr_t>(p) & 1u) == 0 && ld >= k && ld < (1ll << 36);
@@ -502,9 +511,15 @@ int cocod_act_pack(cocod_lm_handle *h, int64_t M, int64_t k, const void *x, int6
 {
     if (!good_act(h, M, k, q, ldq) || !good_bf16(x, ldx, M, k) || (M > 0 && !scales)) return COCOD_ERR_INVALID;
     if (M == 0) return COCOD_OK;
-    const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
-    TRY_CUDA(launch_dependent(true, act_pack, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(x), (long long)ldx, q,
-                              (long long)ldq, scales, (long long)M, (long long)k));
+    const int at_once = act_rows_at_once(M, k);
+    const dim3 grid((unsigned)ceil_div(M, at_once * ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
+    const auto kernels = rows_aligned(x, ldx, M, 16) ? std::make_pair(act_pack<16, 1>, act_pack<16, 2>)
+                       : rows_aligned(x, ldx, M, 8)  ? std::make_pair(act_pack<8, 1>, act_pack<8, 2>)
+                       : rows_aligned(x, ldx, M, 4)  ? std::make_pair(act_pack<4, 1>, act_pack<4, 2>)
+                                                     : std::make_pair(act_pack<2, 1>, act_pack<2, 2>);
+    const auto kernel = at_once == 1 ? kernels.first : kernels.second;
+    TRY_CUDA(launch_dependent(true, kernel, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(x), (long long)ldx, q,
+                              (long long)ldq, scales, (long long)M, (int)k));
     return COCOD_OK;
 }
 
@@ -513,9 +528,12 @@ int cocod_act_unpack(cocod_lm_handle *h, int64_t M, int64_t k, const int8_t *q, 
 {
     if (!good_act(h, M, k, q, ldq) || !good_bf16(y, ldy, M, k) || (M > 0 && !scales)) return COCOD_ERR_INVALID;
     if (M == 0) return COCOD_OK;
-    const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
-    TRY_CUDA(launch_dependent(true, act_unpack, grid, dim3(256), 0, (cudaStream_t)stream, q, (long long)ldq, scales, static_cast<bf16 *>(y),
-                              (long long)ldy, (long long)M, (long long)k));
+    const bool aligned = rows_aligned(y, ldy, M, 16);
+    const int at_once = act_rows_at_once(M, k);
+    const dim3 grid((unsigned)ceil_div(M, at_once * ACT_ROWS), (unsigned)ceil_div(aligned ? k : k + 7, ACT_BLOCK));     // (columns moved by up to 7)
+    const auto kernel = at_once == 1 ? (aligned ? act_unpack<true, 1> : act_unpack<false, 1>) : (aligned ? act_unpack<true, 2> : act_unpack<false, 2>);
+    TRY_CUDA(launch_dependent(true, kernel, grid, dim3(256), 0, (cudaStream_t)stream, q, (long long)ldq, scales, static_cast<bf16 *>(y),
+                              (long long)ldy, (long long)M, (int)k));
     return COCOD_OK;
 }
 
@@ -524,16 +542,23 @@ int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh
 {
     if (!good_act(h, M, k, q, ldq) || !good_bf16(dh, lddh, M, k) || !good_bf16(dz, lddz, M, k)) return COCOD_ERR_INVALID;
     if (M == 0) return COCOD_OK;
-    const dim3 grid((unsigned)ceil_div(M, ACT_ROWS), (unsigned)ceil_div(k, ACT_BLOCK));
-    TRY_CUDA(launch_dependent(true, act_relu_grad, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(dh), (long long)lddh, q,
-                              (long long)ldq, static_cast<bf16 *>(dz), (long long)lddz, (long long)M, (long long)k));
+    const bool aligned = rows_aligned(dh, lddh, M, 16) && rows_aligned(dz, lddz, M, 16);
+    const bool together = (reinterpret_cast<uintptr_t>(dh) - reinterpret_cast<uintptr_t>(dz)) % 16 == 0 && (M == 1 || (lddh - lddz) % 8 == 0);
+    const int at_once = act_rows_at_once(M, k);
+    const dim3 grid((unsigned)ceil_div(M, at_once * ACT_ROWS), (unsigned)ceil_div(aligned ? k : k + 7, ACT_BLOCK));
+    const auto kernels = aligned    ? std::make_pair(act_relu_grad<true, true, 1>, act_relu_grad<true, true, 2>)
+                         : together ? std::make_pair(act_relu_grad<false, true, 1>, act_relu_grad<false, true, 2>)
+                                    : std::make_pair(act_relu_grad<false, false, 1>, act_relu_grad<false, false, 2>);
+    const auto kernel = at_once == 1 ? kernels.first : kernels.second;
+    TRY_CUDA(launch_dependent(true, kernel, grid, dim3(256), 0, (cudaStream_t)stream, static_cast<const bf16 *>(dh), (long long)lddh, q,
+                              (long long)ldq, static_cast<bf16 *>(dz), (long long)lddz, (long long)M, (int)k));
     return COCOD_OK;
 }
 
 // Whether a checkpoint is better turned into bf16 once, by a kernel before the product, than inside it.  The conversion costs the
-// product about 0.18 us for every block of 64 of a tile's reduction (4 groups of 8192 rows, 2048 x 4096 results: 603 us against
-// 538 with the kernel before it, which takes 74); the kernel costs a launch and 3 bytes a value at 5.4 TB/s (16 groups of
-// 128 rows, 1024 x 1024 results: 25.2 us against 23.1 with the conversion inside).
+// product about 0.18 us for every block of 64 of a tile's reduction (4 groups of 8192 rows, 2048 x 4096 results: 490 us against
+// 435 with the kernel before it); the kernel costs a launch and 3 bytes a value at 5.4 TB/s (16 groups of 128 rows, 1024 x 1024
+// results: 29.0 us against 25.7 with the conversion inside).
 static bool widen_first(int G, int64_t M, int64_t n, int64_t k)
 {
     const int64_t depth = ceil_div(std::max<int64_t>(M, 1), G);

@@ -316,6 +316,48 @@ def test_relu_gate_from_the_checkpoint(ops, M, k):
     assert torch.equal(ops.act_unpack(p, out=torch.empty(M, k + 5, device="cuda", dtype=torch.bfloat16)[:, 2:2 + k]), ops.act_unpack(p))
 
 
+def inside(values, lead, behind, fill):
+    """A copy of values whose rows lie `lead` values into rows of `fill`, and the whole of it."""
+    M, k = values.shape
+    whole = torch.full((M + 2, lead + k + behind), fill, device="cuda", dtype=torch.bfloat16)
+    view = whole[1:-1, lead:lead + k]
+    view.copy_(values)
+    return view, whole
+
+
+@pytest.mark.parametrize("k", [1, 6, 7, 8, 9, 15, 17, 63, 64, 65, 121, 127, 128, 129, 250, 256, 1001])
+@pytest.mark.parametrize("behind", [0, 1, 2, 5, 8])
+def test_checkpoints_of_rows_at_any_address(ops, k, behind):
+    M = 70
+    scale = torch.exp2(torch.arange(-(-k // 128), device="cuda").repeat_interleave(128)[:k].float() * 3 - 4)   # another unit in every block
+    x = (gaussian(k, M, k).float() * scale).bfloat16()
+    x[3, k // 2], x[5, 0], x[7, k - 1] = float("inf"), float("nan"), 0.0
+    dh = gaussian(k + 1, M, k)
+    for lead in range(9):
+        base, other = inside(x, 8, -k % 8, 0.0)[0], (lead * 3 + 1) % 8
+        want = ops.act_pack(base)                                          # rows at multiples of 16 bytes
+        assert base.data_ptr() % 16 == 0 and base.stride(0) % 8 == 0
+        got = ops.act_pack(inside(x, lead, behind, float("nan"))[0])        # what surrounds the rows is not finite
+        assert torch.equal(got.q, want.q) and torch.equal(got.scales, want.scales)
+        plain = inside(x, 8, -k % 8, 0.0)[0]
+        ops.act_unpack(want, out=plain)
+        y, whole = inside(torch.zeros_like(x), lead, behind, 7.0)
+        ops.act_unpack(want, out=y)
+        assert torch.equal(torch.nan_to_num(y, nan=-3.0), torch.nan_to_num(plain, nan=-3.0))
+        y.fill_(7.0)
+        assert (whole == 7.0).all()                                        # nothing beside the rows was written
+        gate = torch.where(want.q > 0, dh, torch.zeros_like(dh))
+        gate[want.q == -128] = float("nan")
+        z, whole = inside(torch.zeros_like(x), lead, behind, 7.0)
+        ops.act_relu_grad(inside(dh, other, behind, float("nan"))[0], want, out=z)
+        assert torch.equal(torch.nan_to_num(z, nan=-3.0), torch.nan_to_num(gate, nan=-3.0))
+        z.copy_(dh)
+        ops.act_relu_grad(z, want, out=z)                                  # in place
+        assert torch.equal(torch.nan_to_num(z, nan=-3.0), torch.nan_to_num(gate, nan=-3.0))
+        z.fill_(7.0)
+        assert (whole == 7.0).all()
+
+
 def test_relu_gate_passes_on_what_was_not_finite(ops):
     x = torch.tensor([[1.0, float("inf"), float("nan"), -1.0]], device="cuda").bfloat16()
     dz = ops.act_relu_grad(torch.ones_like(x), ops.act_pack(x))
