@@ -21,7 +21,7 @@
  * Precision: bf16 operands, products and sums in fp32, one rounding at the end where the result is bf16.
  *
  * Same conventions as cocod.h: int return codes (COCOD_*), device pointers on the device current at create, one host
- * thread per handle, asynchronous on the given stream.  The calls on one handle use one scratch: order them
+ * thread per handle, asynchronous on the given stream.  The calls on one handle use scratch of the handle: order them
  * (one stream, or events).  Calls can be captured into a CUDA graph.
  * workspace: device memory lent for the call (until the stream has passed it), 256-byte aligned.
  */
@@ -42,11 +42,8 @@ enum { COCOD_BF16 = 0, COCOD_F32 = 1 };      /* type of a result */
 
 #define COCOD_LM_MAX_GROUPS 1024
 
-/* The kernels' scratch (flags, tensor maps, parts of sums) is lent by the caller: cocod_lm_scratch_bytes() bytes of device memory, about
- * 20 MB, 256-byte aligned, the first 256 bytes zero, valid until the handle is destroyed and its work is done.  Both calls
- * work on the host alone.  Errors: INVALID, OOM (no host memory), CUDA (no tensor-map encoder, no device). */
-int64_t cocod_lm_scratch_bytes(void);
-int cocod_lm_create(cocod_lm_handle **out, void *scratch, int64_t scratch_bytes);
+/* Allocates the kernels' scratch (tensor maps, flags, parts of sums), about 20 MB.  Errors: INVALID, OOM, CUDA. */
+int cocod_lm_create(cocod_lm_handle **out);
 int cocod_lm_destroy(cocod_lm_handle *h);
 
 /* Synchronise `stream` and report what the kernels of this handle met since the last check: COCOD_ERR_TIMEOUT (a kernel

@@ -11,11 +11,11 @@
 #include <new>
 #include <utility>
 
-struct cocod_lm {                          // device addresses in the scratch that the caller lends
-    CUtensorMap *group_maps = nullptr;     // two per group
-    int *order = nullptr;                  // the groups by size
-    float *parts = nullptr;                // parts of tiles, 256 x 256 for each pair of CTAs
-    int *flag = nullptr;                   // what the kernels met
+struct cocod_lm {
+    CUtensorMap *group_maps = nullptr;     // device: two per group
+    int *order = nullptr;                  // device: the groups by size
+    float *parts = nullptr;                // device: parts of tiles, 256 x 256 for each pair of CTAs
+    int *flag = nullptr;                   // device: what the kernels met
     long long launches = 0;
 };
 
@@ -396,18 +396,11 @@ bool good_shape(const cocod_lm *h, int G, const int32_t *offsets, int64_t M, int
     return h && G >= 1 && G <= COCOD_LM_MAX_GROUPS && offsets && (reinterpret_cast<uintptr_t>(offsets) & 3u) == 0 && M >= 0 && M <= MAX_DIM &&
            n >= 8 && n <= MAX_DIM && n % 8 == 0 && k >= 8 && k <= MAX_DIM && k % 8 == 0;
 }
-// Byte offsets in the scratch.
-struct Scratch {
-    int64_t maps, order, parts, bytes;
-};
-Scratch scratch_layout()
+void lm_free(cocod_lm *h)
 {
-    Scratch l{};
-    l.maps = 256;
-    l.order = l.maps + 2 * COCOD_LM_MAX_GROUPS * (int64_t)sizeof(CUtensorMap);
-    l.parts = l.order + COCOD_LM_MAX_GROUPS * (int64_t)sizeof(int);
-    l.bytes = l.parts + (sm_count() / 2 + 1) * (int64_t)(256 * 256 * sizeof(float));
-    return l;
+    void *ptrs[] = {h->group_maps, h->order, h->parts, h->flag};
+    for (void *p : ptrs) if (p) cudaFree(p);
+    delete h;
 }
 inline int size_of(int type) { return type == COCOD_BF16 ? 2 : type == COCOD_F32 ? 4 : 0; }
 
@@ -415,28 +408,31 @@ inline int size_of(int type) { return type == COCOD_BF16 ? 2 : type == COCOD_F32
 
 extern "C" {
 
-int64_t cocod_lm_scratch_bytes(void) { return scratch_layout().bytes; }
-
-int cocod_lm_create(cocod_lm_handle **out, void *scratch, int64_t scratch_bytes)
+int cocod_lm_create(cocod_lm_handle **out)
 {
-    if (!out || !scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u)) return COCOD_ERR_INVALID;
-    if (sm_count() < 2 || !get_encoder()) return COCOD_ERR_CUDA;
-    const Scratch l = scratch_layout();
-    if (scratch_bytes < l.bytes) return COCOD_ERR_INVALID;
+    if (!out) return COCOD_ERR_INVALID;
+    if (!get_encoder()) return COCOD_ERR_CUDA;
     cocod_lm *h = new (std::nothrow) cocod_lm();
     if (!h) return COCOD_ERR_OOM;
-    char *p = static_cast<char *>(scratch);
-    h->flag = reinterpret_cast<int *>(p);
-    h->group_maps = reinterpret_cast<CUtensorMap *>(p + l.maps);
-    h->order = reinterpret_cast<int *>(p + l.order);
-    h->parts = reinterpret_cast<float *>(p + l.parts);
+    cudaError_t e = cudaMalloc((void **)&h->group_maps, 2 * COCOD_LM_MAX_GROUPS * sizeof(CUtensorMap));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->order, COCOD_LM_MAX_GROUPS * sizeof(int));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->parts, (size_t)(sm_count() / 2 + 1) * 256 * 256 * sizeof(float));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
+    if (e == cudaSuccess) e = cudaMemset(h->flag, 0, 256);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        lm_free(h);
+        return e == cudaErrorMemoryAllocation ? COCOD_ERR_OOM : COCOD_ERR_CUDA;
+    }
     *out = h;
     return COCOD_OK;
 }
 
 int cocod_lm_destroy(cocod_lm_handle *h)
 {
-    delete h;
+    if (!h) return COCOD_OK;
+    cudaDeviceSynchronize();
+    lm_free(h);
     return COCOD_OK;
 }
 

@@ -68,8 +68,7 @@ SIGNATURES = {
     "cocod_kernel_merge": (_i, [_vp, _vp, _vp, _i, _i64, _vp]),
     "cocod_kernel_local_step_host_noalloc": (_i, [_vp, _vp, _vp, _vp, _i64, _f, _f, _f, _vp]),
     # include/cocod_lm.h (bound by lm.py)
-    "cocod_lm_scratch_bytes": (_i64, []),
-    "cocod_lm_create": (_i, [ctypes.POINTER(_vp), _vp, _i64]),
+    "cocod_lm_create": (_i, [ctypes.POINTER(_vp)]),
     "cocod_lm_destroy": (_i, [_vp]),
     "cocod_lm_check": (_i, [_vp, _vp]),
     "cocod_lm_launch_count": (_i64, [_vp]),

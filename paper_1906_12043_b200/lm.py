@@ -77,8 +77,7 @@ class PackedActivations:
 
 
 class LMOps:
-    """The operators, with the scratch their kernels share (20 MB): order the calls of one object (one stream, or events), and its
-    creation before them."""
+    """The operators, with the scratch their kernels share: order the calls of one object (one stream, or events)."""
 
     def __init__(self, workspace_limit: int = 2 << 30, widen: bool = True):
         """workspace_limit: bytes that a call of the vocabulary operators may take for what it keeps of the rows it works on
@@ -90,14 +89,12 @@ class LMOps:
         self._lib = _E.load()
         from . import _lm_binding
         self._b = _lm_binding
-        self._device = torch.cuda.current_device()
-        self._scratch = torch.empty(self._lib.cocod_lm_scratch_bytes(), dtype=torch.uint8, device=self._device)
-        self._scratch[:256].zero_()
         h = ctypes.c_void_p()
-        rc = self._lib.cocod_lm_create(ctypes.byref(h), self._scratch.data_ptr(), self._scratch.numel())
+        rc = self._lib.cocod_lm_create(ctypes.byref(h))
         if rc != _E.OK:
             raise _E.CocodError(rc, "cocod_lm_create")
         self._h = h.value
+        self._device = torch.cuda.current_device()
 
     @staticmethod
     def _checked(result, name):
@@ -194,9 +191,7 @@ class LMOps:
     def destroy(self):
         if getattr(self, "_h", 0):
             h, self._h = self._h, 0
-            torch.cuda.synchronize(self._device)          # (calls on any stream may still use the scratch)
             self._lib.cocod_lm_destroy(h)
-            self._scratch = None
 
     def __del__(self):
         try:

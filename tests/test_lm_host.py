@@ -1,6 +1,4 @@
 """The language-model operators' host side, without a GPU: refusals, and the sizes of workspaces."""
-import ctypes
-
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -15,11 +13,7 @@ def lib():
 
 def test_calls_without_a_handle_are_refused(lib):
     from paper_1906_12043_b200.engine import ERR_INVALID, OK
-    out = ctypes.c_void_p()
-    assert lib.cocod_lm_create(None, 256, 1 << 30) == ERR_INVALID
-    assert lib.cocod_lm_create(ctypes.byref(out), None, 1 << 30) == ERR_INVALID
-    assert lib.cocod_lm_create(ctypes.byref(out), 128, 1 << 30) == ERR_INVALID and not out.value
-    assert lib.cocod_lm_scratch_bytes() > 0
+    assert lib.cocod_lm_create(None) == ERR_INVALID
     assert lib.cocod_lm_destroy(None) == OK
     assert lib.cocod_lm_check(None, None) == ERR_INVALID
     assert lib.cocod_lm_launch_count(None) == -1
