@@ -285,7 +285,7 @@ VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int 
     if (grad) {
         l.rho = take(4 * at_once);
         l.u = take(2 * at_once * l.ldu);
-        l.hs = take(2 * at_once * D);
+        l.hs = take(2 * (at_once + 64) * D);   // (the last box of 64 rows that a group's product begins stays within the workspace, though its map ends before)
         if (at_once < M && dw_elem == 2) l.total32 = take(4 * G * V * D);
     }
     l.bytes = at;
