@@ -95,10 +95,13 @@ struct GroupedParams {
     void *out;                         // for the rows of a partial tile, and for join_parts
     long long ld_out, out_stride;      // elements; out_stride (weight form): between groups
     const float *row_scale;            // rows form, optional: factor of every row (0: the row is 0 whatever the product is)
+    const float *rest;                 // rows form with row_scale, optional: row r gets rest[r] B_g(., label[r]) added before the factor
+    const __nv_bfloat16 *rest_b;       // with rest: B, stored [reduction][n]
+    long long ld_b, b_stride;
     const CUtensorMap *group_maps;     // weight form: A and B of group g at 2 g and 2 g + 1
     const int *order;                  // weight form: the groups, those with the most rows first
     const uint8_t *scales;             // B_Q8: [ceil(n / 128)][total_rows], exponents + 127
-    // OUT_VOCAB, OUT_VOCAB_SUMS (rows counted from row0)
+    // OUT_VOCAB, OUT_VOCAB_SUMS (rows counted from row0; label: also with rest)
     const float *ref;                  // c_r
     const int *label;                  // t_r; negative: the row takes no part (u = 0)
     float2 *sums;                      // [half tiles][ld_sums]: {sum, max}
@@ -582,6 +585,22 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (t.kb0 == t.kb1) {
 #pragma unroll
                 for (int j = 0; j < HALF; ++j) acc[j] = 0u;
+            }
+            if (!WG && B == B_MN && OUT == OUT_BF16 && p.rest != nullptr && t.kb0 == 0 && lane < valid) {
+                const float rest = p.rest[m + lane];
+                if (rest != 0.0f) {
+                    const uint4 *b = reinterpret_cast<const uint4 *>(p.rest_b + t.g * p.b_stride + p.label[m + lane] * p.ld_b + col0);
+#pragma unroll
+                    for (int j = 0; j < HALF / 8; ++j) {
+                        const uint4 v = col0 + 8 * j < p.n ? b[j] : make_uint4(0, 0, 0, 0);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            acc[8 * j + 2 * e] = __float_as_uint(fmaf(rest, __uint_as_float(w[e] << 16), __uint_as_float(acc[8 * j + 2 * e])));
+                            acc[8 * j + 2 * e + 1] = __float_as_uint(fmaf(rest, __uint_as_float(w[e] & 0xffff0000u), __uint_as_float(acc[8 * j + 2 * e + 1])));
+                        }
+                    }
+                }
             }
             if (!WG && !is_vocab(OUT) && p.row_scale != nullptr) {
 #pragma unroll

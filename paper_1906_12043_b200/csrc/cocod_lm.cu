@@ -209,8 +209,9 @@ struct Window {
 };
 
 // rows form: out (M x cols) = A (M x depth) times B_g (cols x depth for FORWARD, depth x cols for INPUT_GRAD)
+// (row_scale, rest, label: see GroupedParams)
 int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window &win, int64_t cols, int64_t depth, const Matrix &A, const Matrix &B,
-             const Matrix &out, const float *row_scale, cudaStream_t s)
+             const Matrix &out, const float *row_scale, const float *rest, const int *label, cudaStream_t s)
 {
     const int64_t M = win.rows;
     if (M == 0) return COCOD_OK;
@@ -222,6 +223,7 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window
     GroupedParams p{};
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)depth;
     p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = cut.max_parts; p.row_scale = row_scale;
+    p.rest = rest; p.label = label; p.rest_b = static_cast<const bf16 *>(B.data); p.ld_b = B.ld; p.b_stride = B.stride;
     p.out = const_cast<void *>(out.data); p.ld_out = out.ld;
     p.error_flag = h->flag;
     if (form == FORWARD)
@@ -263,7 +265,7 @@ int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, i
 // How a call's workspace is laid out when `at_once` rows are taken together.
 struct VocabLayout {
     int64_t label, group, own, ref, share, any;       // whole batch: byte offsets
-    int64_t rho, redo, sums, u, hs;            // rows of one pass
+    int64_t rho, rest, redo, sums, u, hs;      // rows of one pass
     int64_t total32;                           // fp32 gradient of the weights, if it is summed over passes and wanted in bf16
     int64_t bytes, ldu, n_sums;
 };
@@ -284,6 +286,7 @@ VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int 
     l.ldu = ceil_div(V, 64) * 64;
     if (grad) {
         l.rho = take(4 * at_once);
+        l.rest = take(4 * at_once);
         l.u = take(2 * at_once * l.ldu);
         l.hs = take(2 * (at_once + 64) * D);   // (the last box of 64 rows that a group's product begins stays within the workspace, though its map ends before)
         if (at_once < M && dw_elem == 2) l.total32 = take(4 * G * V * D);
@@ -351,6 +354,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
         f.loss = row0 + win.rows >= M ? loss : nullptr;
         if (grad) {
             f.rho = reinterpret_cast<float *>(ws + l.rho);
+            f.rest = reinterpret_cast<float *>(ws + l.rest);
             f.u = reinterpret_cast<bf16 *>(ws + l.u); f.ldu = l.ldu;
             f.hs = reinterpret_cast<bf16 *>(ws + l.hs);
         }
@@ -367,7 +371,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
         }
         if (grad) {
             const Matrix dh{static_cast<const bf16 *>(grad->dh.data) + row0 * grad->dh.ld, grad->dh.ld, 0, 2};
-            if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, s)) return rc;
+            if (int rc = run_rows(h, INPUT_GRAD, G, offsets, win, D, V, u, w, dh, f.rho, f.rest, p.label, s)) return rc;
             const Matrix dst = several && dw_elem == 2 ? Matrix{ws + l.total32, D, V * D, 4} : grad->dw;
             if (int rc = run_weights(h, G, offsets, win, V, D, u, hs, nullptr, dst, several && row0 > 0, true, s)) return rc;
         }
@@ -458,7 +462,8 @@ int cocod_grouped_forward(cocod_lm_handle *h, int G, const int32_t *offsets, int
     if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(x, ldx, k, M, 2) ||
         !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(y, ldy, n, M, es))
         return COCOD_ERR_INVALID;
-    return run_rows(h, FORWARD, G, offsets, Window{0, M, M}, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, nullptr, (cudaStream_t)stream);
+    return run_rows(h, FORWARD, G, offsets, Window{0, M, M}, n, k, Matrix{x, ldx, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{y, ldy, 0, es}, nullptr, nullptr, nullptr,
+                    (cudaStream_t)stream);
 }
 
 int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy, int64_t lddy,
@@ -469,7 +474,8 @@ int cocod_grouped_input_grad(cocod_lm_handle *h, int G, const int32_t *offsets, 
     if (!good_shape(h, G, offsets, M, n, k) || !es || !good_rows(dy, lddy, n, M, 2) ||
         !good_groups(w, ldw, w_stride, n, k, G, 2) || !good_rows(dx, lddx, k, M, es))
         return COCOD_ERR_INVALID;
-    return run_rows(h, INPUT_GRAD, G, offsets, Window{0, M, M}, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, nullptr, (cudaStream_t)stream);
+    return run_rows(h, INPUT_GRAD, G, offsets, Window{0, M, M}, k, n, Matrix{dy, lddy, 0, 2}, Matrix{w, ldw, w_stride, 2}, Matrix{dx, lddx, 0, es}, nullptr, nullptr, nullptr,
+                    (cudaStream_t)stream);
 }
 
 int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t n, int64_t k, const void *dy, int64_t lddy,

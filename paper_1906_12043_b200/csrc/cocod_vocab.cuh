@@ -8,8 +8,9 @@
 // exponentials are written once, next to the sums, and read by the two products as they are; no pass over them between.
 // The label's own entry is the one whose value hangs on the sums; this file's vocab_finish puts it in.
 // u in bf16 has 8 bits everywhere: -S_r is formed from the sum, not as a difference from one.  A row's largest entry of
-// softmax - onehot is as a rule its label's: the factor that goes into h is rho_r S_r / bf16(S_r), so that the label's term of dw
-// carries one rounding (of rho h) and not two; the factor of dh stays rho_r.
+// softmax - onehot is as a rule its label's, so its rounding is made good.  In dw by the factor that goes into h, rho_r S_r / bf16(S_r): the
+// label's term carries one rounding (of rho h) and not two.  In dh by what the rounding left out, times the label's row of w, which
+// the product's epilogue adds in fp32 (37 rows of 256 over 8191 entries: error against 64 bits 0.0025 -> 0.0017, a bf16 result's own).
 // When loss_r > 50, exp(l - c_r) could leave bf16's range or rho_r fp32's: such a row is done again relative to its largest logit.
 #pragma once
 #include "cocod_grouped_sm100.cuh"
@@ -133,6 +134,7 @@ struct FinishParams {
     int n_sums, ld_sums;
     float *row_loss;                   // [total]
     float *rho;                        // [rows], nullptr: the loss alone is wanted
+    float *rest;                       // [rows]: -S less its rounding to bf16 (with rho)
     __nv_bfloat16 *u;                  // [rows][ldu]
     long long ldu;
     __nv_bfloat16 *hs;                 // [rows][width]: rho h
@@ -216,7 +218,7 @@ vocab_finish(const FinishParams p)
     part[warp][lane] = make_float2(s, most);
     __syncthreads();
     if (warp == 0) {
-        float rho = 0.0f, scale = 0.0f;
+        float rho = 0.0f, scale = 0.0f, rest = 0.0f;
         int again = 0;
         if (row < p.rows) {
             const int r = p.row0 + row;
@@ -240,11 +242,12 @@ vocab_finish(const FinishParams p)
                     const float kept = -__bfloat162float(entry);
                     p.u[row * p.ldu + t] = entry;
                     scale = kept > 0.0f && kept <= 3.0e38f ? rho * (s / kept) : rho;
+                    rest = kept - s;
                 }
             }
             p.row_loss[r] = loss;
             if (!p.second) p.redo[row] = again;
-            if (p.rho != nullptr) p.rho[row] = rho;
+            if (p.rho != nullptr) p.rho[row] = rho, p.rest[row] = rest;
         }
         factor[lane] = scale;
     }

@@ -1,0 +1,64 @@
+"""The language-model operators where they are easily wrong: what lies beside a checkpoint, very long and very wide products, the
+vocabulary's largest term, streams and repeated calls.
+
+Tolerances are derived beside each test.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lm():
+    from paper_1906_12043_b200 import build, lm
+    build.build()
+    return lm
+
+
+@pytest.fixture(scope="module")
+def ops(lm):
+    o = lm.LMOps()
+    yield o
+    o.check()
+    o.destroy()
+
+
+def offsets_of(sizes):
+    o = [0]
+    for s in sizes:
+        o.append(o[-1] + s)
+    return torch.tensor(o, dtype=torch.int32, device="cuda"), [slice(a, b) for a, b in zip(o, o[1:])]
+
+
+def gaussian(seed, *shape, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).bfloat16()
+
+
+def half_unit(x):
+    """Half a unit in the last place of bf16 (8 significant bits) at the values x."""
+    return torch.exp2(torch.frexp(x)[1].double() - 9)
+
+
+# ------------------------------------------------------------------------------------------------------- vocabulary
+@pytest.mark.parametrize("sizes,V,D", [([37], 8191, 256), ([300, 0, 77], 1000, 264), ([1], 50, 8)])
+def test_the_label_s_term_of_dx_is_rounded_once(ops, sizes, V, D):
+    """All rows have the same label, whose row of w is the only one that is not 0, so that dx is that one term, a (softmax - 1) w: its sum is in
+    fp32 and the result rounds it once.  A logit is off by at most (D / 16 + 8) * 2^-23 |h| |w| < 2^-13 for |h| |w| <= 2^5 here, and the
+    term by no more than that much of itself (d (1 - softmax) / (1 - softmax) = softmax)."""
+    off, spans = offsets_of(sizes)
+    M, G = sum(sizes), len(sizes)
+    h = gaussian(1, M, D)
+    w = torch.zeros(G, V, D, device="cuda", dtype=torch.bfloat16)
+    w[:, V // 3] = gaussian(2, G, D, scale=D ** -0.5)
+    labels = torch.full((M,), V // 3, dtype=torch.int32, device="cuda")
+    assert float(h.float().norm(dim=1).max() * w.float().norm(dim=2).max()) <= 32
+    for dtype in (torch.bfloat16, torch.float32):
+        dx = ops.vocab_loss_grad(h, w, labels, off, dw_dtype=dtype)[2].double()
+        for g, s in enumerate(spans):
+            l = h[s].double() @ w[g].double().T
+            want = ((torch.softmax(l, 1)[:, V // 3] - 1) / max(1, sizes[g]))[:, None] * w[g, V // 3].double()
+            assert ((dx[s] - want).abs() <= half_unit(want) + 2.0 ** -13 * want.abs()).all()
+    ops.check()
