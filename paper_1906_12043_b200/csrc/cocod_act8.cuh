@@ -101,22 +101,39 @@ __device__ __forceinline__ int lead(const __nv_bfloat16 *row)
 {
     return ALIGNED ? 0 : (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 7;
 }
-// The 8-bit values of columns c - s .. c - s + 7 (c a multiple of 8, 0 <= s < 8; rows of q are 16-byte aligned and as long as
-// their distance): the words that hold them, and how they come out of those.
+// Four 8-bit values from column `at` (a multiple of 4) on.  Rows of q are 16-byte aligned, but what lies behind their last column need not
+// belong to the checkpoint (a view, the end of a buffer): the values of a word that the row does not fill go one by one.
+__device__ __forceinline__ uint32_t word_q(const int8_t *row, int at, int k)
+{
+    if (at >= 0 && at + 4 <= k) return *reinterpret_cast<const uint32_t *>(row + at);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (at >= 0 && at + i < k) w |= (uint32_t)(uint8_t)row[at + i] << (8 * i);
+    return w;
+}
+__device__ __forceinline__ void store8_q(int8_t *row, int c, int k, uint2 x)
+{
+    if (c + 8 <= k) {
+        *reinterpret_cast<uint2 *>(row + c) = x;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+        if (c + j < k) row[c + j] = (int8_t)((j < 4 ? x.x : x.y) >> (8 * (j & 3)));
+}
+// The 8-bit values of columns c - s .. c - s + 7 (c a multiple of 8, 0 <= s < 8): the words that hold them, and how they come out of those.
 template <bool ALIGNED>
 __device__ __forceinline__ void begin_q(uint32_t (&w)[3], const int8_t *row, int c, int k, int s)
 {
     w[2] = 0;
     if (ALIGNED) {
-        const uint2 v = c < k ? *reinterpret_cast<const uint2 *>(row + c) : make_uint2(0, 0);
+        const uint2 v = c + 8 <= k ? *reinterpret_cast<const uint2 *>(row + c) : make_uint2(word_q(row, c, k), word_q(row, c + 4, k));
         w[0] = v.x, w[1] = v.y;
     } else {
         const int from = (c - s) & ~3;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            const int at = from + 4 * i;
-            w[i] = at >= 0 && at < k ? *reinterpret_cast<const uint32_t *>(row + at) : 0;
-        }
+        for (int i = 0; i < 3; ++i) w[i] = word_q(row, from + 4 * i, k);
     }
 }
 template <bool ALIGNED>
@@ -209,8 +226,8 @@ act_pack(const __nv_bfloat16 *x, long long ldx, int8_t *q, long long ldq, uint8_
         }
         if (m < M) {
             int8_t *row = q + m * ldq;
-            if (c < k) *reinterpret_cast<uint2 *>(row + c) = make_uint2(packed[0], packed[1]);
-            if (c + 64 < k) *reinterpret_cast<uint2 *>(row + c + 64) = make_uint2(packed[2], packed[3]);
+            store8_q(row, c, k, make_uint2(packed[0], packed[1]));
+            store8_q(row, c + 64, k, make_uint2(packed[2], packed[3]));
         }
         const uint32_t finite = __ballot_sync(0xffffffffu, plain) >> (threadIdx.x & 24) & 0xffu;      // of the eight threads of this block
         if ((threadIdx.x & 7) == 0) exps[h * 32 + (threadIdx.x >> 3)] = finite == 0xffu ? (uint8_t)biased : 255;

@@ -62,3 +62,38 @@ def test_the_label_s_term_of_dx_is_rounded_once(ops, sizes, V, D):
             want = ((torch.softmax(l, 1)[:, V // 3] - 1) / max(1, sizes[g]))[:, None] * w[g, V // 3].double()
             assert ((dx[s] - want).abs() <= half_unit(want) + 2.0 ** -13 * want.abs()).all()
     ops.check()
+
+
+# ------------------------------------------------------------------------------------------------------- checkpoints
+@pytest.mark.parametrize("M,k", [(1, 1), (1, 7), (1, 1001), (3, 9), (33, 100), (70, 129), (40, 263), (5, 520)])
+def test_a_checkpoint_in_a_view_leaves_its_surroundings(lm, ops, M, k):
+    """q as columns of a wider buffer, and one that ends with its last value and has its scales right behind: neither is written nor used
+    beyond the k values of a row, and what is read from it is what an own checkpoint gives."""
+    x = gaussian(1, M, k)
+    own = ops.act_pack(x)
+    wide = torch.full((M, -(-k // 16) * 16 + 32), 77, device="cuda", dtype=torch.int8)
+    blocks = -(-k // 128)
+    at = (M - 1) * (-(-k // 16) * 16) + k
+    flat = torch.full((at + blocks * M + 64,), 77, device="cuda", dtype=torch.int8)
+    views = [(wide[:, 16:16 + k], torch.full((blocks, M), 77, device="cuda", dtype=torch.uint8)),
+             (torch.as_strided(flat, (M, k), (-(-k // 16) * 16, 1)), flat[at:at + blocks * M].view(torch.uint8).view(blocks, M))]
+    dh = gaussian(2, M, k + 1)
+    for q, scales in views:
+        p = lm.PackedActivations.from_parts(q, scales)
+        for _ in range(3):
+            assert ops.act_pack(x, out=p) is p
+            assert torch.equal(q, own.q) and torch.equal(scales, own.scales)
+        assert torch.equal(ops.act_unpack(p), ops.act_unpack(own))
+        for d in (dh[:, :k], dh[:, 1:]):
+            assert torch.equal(ops.act_relu_grad(d, p), ops.act_relu_grad(d, own))
+            other = torch.empty(M, k + 1, device="cuda", dtype=torch.bfloat16)[:, 1:]
+            assert torch.equal(ops.act_relu_grad(d, p, out=other), ops.act_relu_grad(d, own))
+            assert torch.equal(ops.act_unpack(p, out=other), ops.act_unpack(own))
+        if k % 8 == 0:
+            off, _ = offsets_of([M])
+            assert torch.equal(ops.grouped_weight_grad(gaussian(3, M, 16), p, off), ops.grouped_weight_grad(gaussian(3, M, 16), own, off))
+    assert (wide[:, :16] == 77).all() and (wide[:, 16 + k:] == 77).all() and (flat[at + blocks * M:] == 77).all()
+    gaps = torch.ones(at, dtype=torch.bool, device="cuda")
+    torch.as_strided(gaps, (M, k), (-(-k // 16) * 16, 1)).fill_(False)
+    assert (flat[:at][gaps] == 77).all()
+    ops.check()
