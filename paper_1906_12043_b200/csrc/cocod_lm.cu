@@ -128,10 +128,11 @@ Cut choose_cut(Form form, int64_t groups, int64_t rows, int64_t cols, int64_t de
         const int64_t tiles = std::max<int64_t>(1, (int64_t)(likely * col_tiles)), full = tiles / slots, rest = tiles % slots;
         const double busy = std::min(1.0, (double)tiles / slots);
         const double block = pair ? std::max(0.33, 0.40 * busy) : std::max(0.28, 0.34 * busy), tile = pair ? 2.0 : 1.5;
-        // A's tile rows of a band stay in L2 while B passes by; where all of B fits, or A's do not, eight are enough
-        const int64_t row_bytes = t * depth * 2;
+        // A's tile rows of a band stay in L2 while B passes by; where all of B fits, or A's do not, eight are enough.  Never more
+        // than there are: the kernel counts a band's tiles in 32 bits, which hold all tiles of a matrix.
+        const int64_t row_bytes = t * depth * 2, tile_rows = std::max<int64_t>(1, ceil_div(rows, t));
         const bool b_fits = cols * depth * 2 <= (40 << 20);
-        const int band = (int)std::max<int64_t>(8, std::min<int64_t>(b_fits ? 8 : (40 << 20) / std::max<int64_t>(row_bytes, 1), 1 << 16));
+        const int band = (int)std::min(tile_rows, std::max<int64_t>(8, b_fits ? 8 : (40 << 20) / std::max<int64_t>(row_bytes, 1)));
         // (joining takes about 0.09 us for each part: more parts than this cost more than they save)
         const int64_t sensible = (int64_t)std::sqrt(blocks * (pair ? 0.33 : 0.28) / 0.09) + 1, bound = std::min(blocks / 4, std::max<int64_t>(sensible, 2));
         const int64_t most_parts = rest > 0 && parts_allowed ? std::min(slots / rest, bound) : 1;
@@ -340,7 +341,8 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
             return COCOD_ERR_CUDA;
         GroupedParams p{};
         p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.row0 = (int)row0; p.rows = (int)win.rows; p.n = (int)V; p.kdim = (int)D;
-        p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = 1;
+        p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.max_parts = 1;
+        p.band = (int)std::min<int64_t>(cut.band, ceil_div(rows, cut.pair ? 256 : 128));
         p.out = ws + l.u; p.ld_out = l.ldu; p.error_flag = h->flag;
         p.ref = v.ref + row0; p.label = v.label + row0; p.sums = reinterpret_cast<float2 *>(ws + l.sums); p.ld_sums = (int)win.rows;
         const int row_blocks = (int)ceil_div(win.rows, 8);

@@ -97,3 +97,19 @@ def test_a_checkpoint_in_a_view_leaves_its_surroundings(lm, ops, M, k):
     torch.as_strided(gaps, (M, k), (-(-k // 16) * 16, 1)).fill_(False)
     assert (flat[:at][gaps] == 77).all()
     ops.check()
+
+
+# ------------------------------------------------------------------------------------------------------- products
+@pytest.mark.parametrize("rows", [1, 2])
+def test_weight_gradient_of_few_rows_into_very_wide_ones(ops, rows):
+    """8 x 2^25 results from one or two rows: as many tile columns as a band of 65536 tile rows would overflow 32 bits with.  Each result is at
+    most two products of bf16, exact in fp32, and their sum, which the tensor cores cut off by at most 2^-22 of the products' magnitude."""
+    n, k = 8, 1 << 25
+    off, _ = offsets_of([rows])
+    dy, x = gaussian(1, rows, n), gaussian(2, rows, k)
+    dw = ops.grouped_weight_grad(dy, x, off, out=torch.full((1, n, k), 7.0, device="cuda"))
+    ops.check()
+    for at in range(0, k, 1 << 23):
+        part = slice(at, at + (1 << 23))
+        want = dy.double().T @ x[:, part].double()
+        assert ((dw[0, :, part].double() - want).abs() <= 2.0 ** -22 * (dy.double().abs().T @ x[:, part].double().abs())).all()
