@@ -255,6 +255,7 @@ vocab_finish(const FinishParams p)
         __shared__ int last;
         if (warp == 0) {
             __threadfence();
+            __syncwarp();              // every lane's loss is out before the block counts as through
             if (lane == 0) last = atomicAdd(p.v.redo_any + 1, 1) == (int)gridDim.x - 1;
         }
         __syncthreads();

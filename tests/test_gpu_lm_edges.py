@@ -113,3 +113,23 @@ def test_weight_gradient_of_few_rows_into_very_wide_ones(ops, rows):
         part = slice(at, at + (1 << 23))
         want = dy.double().T @ x[:, part].double()
         assert ((dw[0, :, part].double() - want).abs() <= 2.0 ** -22 * (dy.double().abs().T @ x[:, part].double().abs())).all()
+
+
+# ------------------------------------------------------------------------------------------------------- vocabulary, second pass
+def test_means_after_a_second_pass_hold_every_row(ops):
+    """Losses above 50 in rows of every block of 32, so that the rows are done again and the blocks that end last add the losses up: the means are
+    those of the losses that are returned (sums of n positive fp32 values in any order: within n * 2^-23 of themselves), every time."""
+    sizes, V, D = [700, 0, 1500, 333], 300, 16
+    off, spans = offsets_of(sizes)
+    h, w = gaussian(1, sum(sizes), D), gaussian(2, len(sizes), V, D)
+    h[::7] *= 40
+    labels = torch.randint(0, V, (sum(sizes),), generator=torch.Generator().manual_seed(3)).int().cuda()
+    first = ops.vocab_loss(h, w, labels, off)
+    assert (first[1].view(-1)[::7] > 50).any()
+    for _ in range(200):
+        loss, row = ops.vocab_loss(h, w, labels, off)
+        assert torch.equal(row, first[1]) and torch.equal(loss, first[0])
+    for g, s in enumerate(spans):
+        want = first[1][s].double().sum() / max(1, sizes[g])
+        assert abs(float(first[0][g] - want)) <= 2.0 ** -23 * max(sizes) * float(want)
+    ops.check()
