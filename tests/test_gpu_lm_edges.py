@@ -133,3 +133,18 @@ def test_means_after_a_second_pass_hold_every_row(ops):
         want = first[1][s].double().sum() / max(1, sizes[g])
         assert abs(float(first[0][g] - want)) <= 2.0 ** -23 * max(sizes) * float(want)
     ops.check()
+
+
+@pytest.mark.parametrize("sizes,n,k", [([2500, 1596], 512, 1032), ([300, 0, 213, 4000], 1024, 520)])
+def test_checkpoints_turned_inside_the_product_always_give_the_same_bits(lm, sizes, n, k):
+    """Operand tiles that converting warps write, in single thread blocks and in pairs: every repetition gives what the checkpoint in bf16 gives."""
+    o = lm.LMOps(widen=False)
+    off, _ = offsets_of(sizes)
+    x, dy = gaussian(1, sum(sizes), k).relu(), gaussian(2, sum(sizes), n)
+    p = o.act_pack(x)
+    for dtype in (torch.bfloat16, torch.float32):
+        want = o.grouped_weight_grad(dy, o.act_unpack(p), off, out_dtype=dtype)
+        for _ in range(150):
+            assert torch.equal(o.grouped_weight_grad(dy, p, off, out_dtype=dtype), want)
+    o.check()
+    o.destroy()
