@@ -425,6 +425,7 @@ int cocod_lm_create(cocod_lm_handle **out)
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->parts, (size_t)(sm_count() / 2 + 1) * 256 * 256 * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
     if (e == cudaSuccess) e = cudaMemset(h->flag, 0, 256);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);      // (calls come on any stream, and memset need not have ended)
     if (e != cudaSuccess) {
         cudaGetLastError();
         lm_free(h);

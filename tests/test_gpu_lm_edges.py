@@ -148,3 +148,24 @@ def test_checkpoints_turned_inside_the_product_always_give_the_same_bits(lm, siz
             assert torch.equal(o.grouped_weight_grad(dy, p, off, out_dtype=dtype), want)
     o.check()
     o.destroy()
+
+
+# ------------------------------------------------------------------------------------------------------- streams
+def test_a_report_outlives_the_creation_on_a_busy_stream(lm):
+    """Operators made while the default stream is busy, and used at once on a stream of their own: what the first call reports stands."""
+    from paper_1906_12043_b200.engine import CocodError, ERR_INVALID
+    x, w = gaussian(1, 64, 64), gaussian(2, 2, 64, 64)
+    bad = torch.tensor([0, 40, 30], dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    lm.LMOps().grouped_forward(x, w, bad)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)                         # about 0.2 s
+    o = lm.LMOps()
+    with torch.cuda.stream(side):
+        o.grouped_forward(x, w, bad)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), pytest.raises(CocodError) as e:
+        o.check()
+    assert e.value.code == ERR_INVALID
+    o.check()
+    o.destroy()
