@@ -61,6 +61,10 @@ class PackedActivations:
         self._at, self._scales_at = q.data_ptr(), scales.data_ptr()
         return self
 
+    def __reduce__(self):
+        """Copies and pickles hold tensors of their own, and the addresses of those."""
+        return PackedActivations.from_parts, (self.q, self.scales)
+
     @property
     def q(self):
         if self._q is None:
