@@ -23,7 +23,7 @@
 // nearest, to sums that it holds in registers (half a tile row per thread; the epilogue warps take the registers that the
 // others give up).  8192 x 8192 x 8192 in fp32: 774 us without, 788 in parts of 1024, 823 in parts of 512 (the epilogue's
 // reads of tensor memory hold the products up for about 400 clocks a part); error 7e-7 at 768, 1.0e-6 at 1024.  A bf16 result does not show
-// the difference.
+// the difference below some 100000 products (1e-4 at that rate): its parts are of 32768, which cost nothing.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
 // with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
 // The weight gradient can take B as an 8-bit checkpoint (B_Q8): TMA brings the bytes, an idle warp their scales, and eight more warps write
@@ -80,7 +80,7 @@ enum Out {
 __host__ __device__ constexpr bool is_f32(int out) { return out == OUT_F32 || out == OUT_ADD_F32; }
 __host__ __device__ constexpr bool is_vocab(int out) { return out == OUT_VOCAB || out == OUT_VOCAB_SUMS; }
 // Blocks of 64 that the tensor cores sum at a time.
-__host__ __device__ constexpr int part_blocks(int out) { return is_f32(out) ? 12 : is_vocab(out) ? 32 : 1 << 24; }
+__host__ __device__ constexpr int part_blocks(int out) { return is_f32(out) ? 12 : is_vocab(out) ? 32 : 512; }
 
 struct GroupedParams {
     const int *offsets;                // [groups + 1], device

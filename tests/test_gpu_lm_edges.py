@@ -169,3 +169,17 @@ def test_a_report_outlives_the_creation_on_a_busy_stream(lm):
     assert e.value.code == ERR_INVALID
     o.check()
     o.destroy()
+
+
+def test_long_sums_of_positive_products_do_not_shrink(ops):
+    """bf16 results of 2^19 positive products each, in tiles that are not cut.  The tensor cores add in parts of 32768 products: each of a part's
+    2048 steps cuts off at most a unit in the last place of the running sum, 2^-23 of it, and that is half of the part's on average, so
+    that a result is too small by at most 2^-13 of itself.  The mean over 4096 results shows it: their roundings (at most 2^-8, of
+    either sign) leave 5 * 2^-8 / sqrt(12) / 64 < 2^-13 of it."""
+    M, n, k = 2304, 2304, 1 << 19
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w = ((torch.rand(M, k, generator=g, device="cuda") + 0.5).bfloat16() for _ in range(2))
+    y = ops.grouped_forward(x, w[None], torch.tensor([0, M], dtype=torch.int32, device="cuda"))
+    ops.check()
+    want = x[:64].double() @ w[:64].double().T
+    assert abs(float((y[:64, :64].double() / want - 1).mean())) <= 2.0 ** -12
