@@ -24,6 +24,9 @@
  * thread per handle, asynchronous on the given stream.  The calls on one handle use scratch of the handle: order them
  * (one stream, or events).  Calls can be captured into a CUDA graph.
  * workspace: device memory lent for the call (until the stream has passed it), 256-byte aligned.
+ *
+ * An earlier form of the weight gradients (tensor maps modified on the device, scratch recycled between handles) once ended in an illegal
+ * address whose cause was not found.  Neither is left: copies go through maps of whole matrices only, made on the host.
  */
 #ifndef COCOD_LM_H
 #define COCOD_LM_H
@@ -42,7 +45,7 @@ enum { COCOD_BF16 = 0, COCOD_F32 = 1 };      /* type of a result */
 
 #define COCOD_LM_MAX_GROUPS 1024
 
-/* Allocates the kernels' scratch (tensor maps, flags, parts of sums), about 20 MB.  Errors: INVALID, OOM, CUDA. */
+/* Allocates the kernels' scratch (flags, parts of sums), about 20 MB.  Errors: INVALID, OOM, CUDA. */
 int cocod_lm_create(cocod_lm_handle **out);
 int cocod_lm_destroy(cocod_lm_handle *h);
 

@@ -25,9 +25,11 @@
 // reads of tensor memory hold the products up for about 400 clocks a part); error 7e-7 at 768, 1.0e-6 at 1024.  A bf16 result does not show
 // the difference below some 100000 products (1e-4 at that rate): its parts are of 32768, which cost nothing.
 // Reductions end where the matrices do: TMA fills what lies outside with zeros.  In the weight form the reduction ends
-// with the group, so every group has tensor maps of its own (group_maps) whose last row is the group's last row.
-// The weight gradient can take B as an 8-bit checkpoint (B_Q8): TMA brings the bytes, an idle warp their scales, and eight more warps write
-// the bf16 operand tile, exactly (a whole number times a power of two), with zeros behind the group's end.
+// with the group, and behind its last row lie the next group's, which may hold anything: where a group's last block of 64 rows
+// holds some, its copies complete at a barrier of their own CTA (rfull), warp 2 overwrites those rows with zeros as far as the last step of 16
+// products reaches that the issuer takes of the block, and hands it on (rready).
+// The weight gradient can take B as an 8-bit checkpoint (B_Q8): TMA brings the bytes, warp 2 their scales, and eight more warps write
+// the bf16 operand tile, exactly (a whole number times a power of two), with zeros behind the group's end (and zeros into A there).
 // The number of tiles is seldom a multiple of the CTA pairs.  The tiles of the last, incomplete wave (all of them when there are few)
 // are cut along the reduction into as many parts as keep every pair busy; a part leaves as fp32 in scratch, at most one per
 // pair, and join_parts adds the parts of a tile up in a fixed order.  5.2 waves of tiles take 5.2 and not 6 times a tile.
@@ -98,8 +100,7 @@ struct GroupedParams {
     const float *rest;                 // rows form with row_scale, optional: row r gets rest[r] B_g(., label[r]) added before the factor
     const __nv_bfloat16 *rest_b;       // with rest: B, stored [reduction][n]
     long long ld_b, b_stride;
-    const CUtensorMap *group_maps;     // weight form: A and B of group g at 2 g and 2 g + 1
-    const int *order;                  // weight form: the groups, those with the most rows first
+    const int *order;                  // weight form: the groups, those with the most rows first; nullptr: a warp finds it (up to 32)
     const uint8_t *scales;             // B_Q8: [ceil(n / 128)][total_rows], exponents + 127
     // OUT_VOCAB, OUT_VOCAB_SUMS (rows counted from row0; label: also with rest)
     const float *ref;                  // c_r
@@ -162,10 +163,6 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void acquire_map(const CUtensorMap *map)
-{
-    asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(map) : "memory");
 }
 // A tile load of one CTA of a pair; its bytes are counted at `bar` (a shared::cluster address: the leading CTA's barrier).
 template <int CG>
@@ -253,24 +250,11 @@ __device__ __forceinline__ void group_range(const GroupedParams &p, int g, int &
     hi = min(max(p.offsets[g + 1] - p.row0, lo), p.rows);
 }
 
-// The tensor map of group g's rows (the weight form reduces over them): the map of the whole matrix with the first row moved to
-// the group's first and the number of rows set to the group's.  One warp; `map` is scratch in shared memory.
-__device__ __forceinline__ void write_group_map(const CUtensorMap &whole, const char *base, long long ld_bytes, const GroupedParams &p, int g,
-                                                CUtensorMap *dst, CUtensorMap &map)
+// Weight form: the end of the tile's blocks that hold rows of its group alone.  The next one, if it is in the tile, holds rows of the next
+// group too (behind the batch's last row TMA writes zeros).
+__device__ __forceinline__ int plain_blocks(const GroupedParams &p, const Tile &t)
 {
-    const int lane = threadIdx.x & 31;
-    int lo, hi;
-    group_range(p, g, lo, hi);
-    reinterpret_cast<uint32_t *>(&map)[lane] = reinterpret_cast<const uint32_t *>(&whole)[lane];
-    __syncwarp();
-    if (lane == 0) {
-        asm volatile("tensormap.replace.tile.global_address.shared::cta.b1024.b64 [%0], %1;"
-                     ::"r"(smem_u32(&map)), "l"(reinterpret_cast<uint64_t>(base + lo * ld_bytes)) : "memory");
-        asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(smem_u32(&map)), "r"(max(hi - lo, 1)) : "memory");
-    }
-    __syncwarp();
-    asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;"
-                 ::"l"(dst), "r"(smem_u32(&map)) : "memory");
+    return t.m1 < p.rows ? min(t.kb1, (t.m1 - t.lo) / BK) : t.kb1;
 }
 
 // The place of group g when the groups are ordered by their rows, most first (one warp).
@@ -301,7 +285,7 @@ __device__ __forceinline__ void in_band(int i, int high, int tiles_m, int tiles_
 // fill; 32 groups are looked at together, one per lane.
 template <int TM, int TN, bool WG> struct Walker {
     const GroupedParams &p;
-    int lane, gb = 0, base = 0, lo = 0, hi = 0, cnt = 0, incl = 0, total = 0;
+    int lane, gb = 0, base = 0, lo = 0, hi = 0, cnt = 0, incl = 0, total = 0, rank = 0;
     int whole = 0x7fffffff, cut = 0, parts = 1;
     __device__ Walker(const GroupedParams &params, int lane_, int clusters) : p(params), lane(lane_)
     {
@@ -314,6 +298,13 @@ template <int TM, int TN, bool WG> struct Walker {
             }
             tiles *= (p.kdim + TM - 1) / TM * p.tiles_n;
             whole = tiles;
+            if (p.order == nullptr) {                     // (group_rank with a group in each lane)
+                const int mine = lane < p.groups ? hi - lo : -1;
+                for (int j = 0; j < p.groups; ++j) {
+                    const int rows = __shfl_sync(0xffffffffu, mine, j);
+                    rank += rows > mine || (rows == mine && j < lane);
+                }
+            }
         } else if (p.max_parts > 1) {
             for (gb = 0; gb < p.groups; gb += 32) {
                 load();
@@ -370,7 +361,7 @@ template <int TM, int TN, bool WG> struct Walker {
             tiles_m = (p.kdim + TM - 1) / TM;
             const int per = tiles_m * p.tiles_n, at = t / per;
             if (at >= p.groups) return false;
-            tile.g = p.order[at];
+            tile.g = p.order != nullptr ? p.order[at] : __ffs(__ballot_sync(0xffffffffu, lane < p.groups && rank == at)) - 1;
             t -= at * per;
             group_range(p, tile.g, lo, hi);
         } else {
@@ -414,6 +405,16 @@ template <int TM> __device__ __forceinline__ bool redo_tile(const GroupedParams 
     return __any_sync(0xffffffffu, any);
 }
 
+// Zeros into rows `first` .. end - 1 of each of BOXES boxes of 64 rows of 128 bytes, by `threads` threads.
+template <int BOXES> __device__ __forceinline__ void zero_rows(uint8_t *boxes, int first, int end, int thread, int threads)
+{
+    const int pieces = (end - first) * 8;                      // of 16 bytes, in a box
+    for (int i = thread; i < BOXES * pieces; i += threads) {
+        const int box = i / pieces;
+        *reinterpret_cast<uint4 *>(boxes + box * (BK * 128) + first * 128 + (i - box * pieces) * 16) = make_uint4(0, 0, 0, 0);
+    }
+}
+
 __device__ __forceinline__ float exp2_approx(float x)
 {
     float y;
@@ -444,10 +445,11 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     Tile *tiles = reinterpret_cast<Tile *>(bars + 2 * RING + 4 + 2 * AHEAD);
     uint64_t *bbars = reinterpret_cast<uint64_t *>(tiles + AHEAD);
     const uint32_t bfull0 = smem_u32(bbars), qfull0 = smem_u32(bbars + RING);      // B_Q8: the bf16 tile is written; bytes and scales are there
+    const uint32_t rready0 = bfull0, rfull0 = qfull0;                              // else, weight form: the block is mended; its copies are there
     uint8_t *unit_bytes = reinterpret_cast<uint8_t *>(bbars + 2 * RING);           // B_Q8: scales of the 64 rows of every stage
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(unit_bytes + 64 * RING);
     volatile int *abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    uint32_t *words = tmem_slot + 2;                                               // B_Q8, pairs: where the other CTA's signals go
+    uint32_t *words = tmem_slot + 2;                                               // weight form, pairs: where the other CTA's signals go
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cta_rank<CG>();
     const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
@@ -466,8 +468,8 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         for (int s = 0; s < RING; ++s) {
             mbar_init(full0 + 8 * s, 1);
             mbar_init(empty0 + 8 * s, 1);
-            mbar_init(bfull0 + 8 * s, CONV_WARPS);                 // (and the signals of the other CTA of a pair)
-            mbar_init(qfull0 + 8 * s, 2);
+            mbar_init(bfull0 + 8 * s, QB ? CONV_WARPS : 1);        // (and the signals of the other CTA of a pair)
+            mbar_init(qfull0 + 8 * s, QB ? 2 : 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(accf0 + 8 * s, 1);
@@ -475,7 +477,7 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         }
         for (int s = 0; s < AHEAD; ++s) {
             mbar_init(tilef0 + 8 * s, 1);
-            mbar_init(tilee0 + 8 * s, 1 + (rank == 0 ? 1 : 0) + EPI_WARPS + (QB ? CONV_WARPS + 1 : 0));      // producer, issuer, epilogue, converters, scales
+            mbar_init(tilee0 + 8 * s, 1 + (rank == 0 ? 1 : 0) + EPI_WARPS + (WG ? 1 : 0) + (QB ? CONV_WARPS : 0));      // producer, issuer, epilogue, warp 2, converters
         }
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -689,10 +691,12 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         Tile t;
         unsigned it = 0;
         while (next_tile_warp(t)) {
+            const int plain = plain_blocks(p, t);
             for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
                 const unsigned s = it % RING;
                 if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * s, (it / RING) & 1, abort, limit))) { failed = 6; break; }
                 uint8_t *db = smem + s * STAGE + A_BYTES;
+                if (kb == plain) zero_rows<2>(smem + s * STAGE, t.m1 - t.lo - kb * BK, BK, threadIdx.x - 32 * (4 + EPI_WARPS), 32 * CONV_WARPS);
                 const uint8_t *q = db + B_BYTES;
                 uint2 v[MINE][2];
                 uint32_t scale[MINE];
@@ -731,37 +735,46 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             // ---- producer (one thread: a warp's own synchronisation at every tile cost the ring 300 clocks)
             Tile t;
             unsigned it = 0;
-            int last_g = -1;
             while (lane == 0 && !failed && next_tile(t)) {
                 if (p.debug_no_loads) continue;
-                const CUtensorMap *ma = WG ? p.group_maps + 2 * t.g : &map_a, *mb = WG && !QB ? ma + 1 : &map_b;
-                if (WG && t.g != last_g) {
-                    acquire_map(ma);
-                    if (!QB) acquire_map(mb);
-                    last_g = t.g;
-                }
-                const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g;
-                for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+                const int m0 = t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128, zb = WG ? 0 : t.g, r0 = WG ? t.lo : 0, plain = WG ? plain_blocks(p, t) : t.kb1;
+                for (int kb = t.kb0; kb < plain; ++kb, ++it) {
                     const unsigned s = it % RING, use = it / RING;
                     if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
                     if (rank == 0) mbar_expect_tx(full0 + 8 * s, CG * (QB ? A_BYTES : STAGE_BYTES));
                     const uint32_t bar = CG == 1 ? full0 + 8 * s : map_to_rank(full0 + 8 * s, 0);
                     const uint32_t da = smem_base + s * STAGE, db = da + A_BYTES;
                     if (A_MN) {
-                        load_tile<CG>(da, ma, bar, m0, kb * BK, 0);
-                        load_tile<CG>(da + BK * 128, ma, bar, m0 + 64, kb * BK, 0);
+                        load_tile<CG>(da, &map_a, bar, m0, r0 + kb * BK, 0);
+                        load_tile<CG>(da + BK * 128, &map_a, bar, m0 + 64, r0 + kb * BK, 0);
                     } else {
-                        load_tile<CG>(da, ma, bar, kb * BK, m0, 0);
+                        load_tile<CG>(da, &map_a, bar, kb * BK, m0, 0);
                     }
                     if (QB) {
                         mbar_expect_tx(qfull0 + 8 * s, Q_BYTES);
-                        tma_load_3d(db + B_BYTES, &map_b, qfull0 + 8 * s, n0, t.lo + kb * BK, 0);
+                        tma_load_3d(db + B_BYTES, &map_b, qfull0 + 8 * s, n0, r0 + kb * BK, 0);
                     } else if (B == B_MN) {
-                        load_tile<CG>(db, mb, bar, n0, kb * BK, zb);
-                        load_tile<CG>(db + BK * 128, mb, bar, n0 + 64, kb * BK, zb);
+                        load_tile<CG>(db, &map_b, bar, n0, r0 + kb * BK, zb);
+                        load_tile<CG>(db + BK * 128, &map_b, bar, n0 + 64, r0 + kb * BK, zb);
                     } else {
-                        load_tile<CG>(db, mb, bar, kb * BK, n0, zb);
+                        load_tile<CG>(db, &map_b, bar, kb * BK, n0, zb);
                     }
+                }
+                if (WG && plain < t.kb1 && !failed) {          // a block shared with the next group: this CTA's barrier counts the bytes, `full` keeps step
+                    const unsigned s = it % RING, use = it / RING;
+                    if (use > 0 && !mbar_wait(empty0 + 8 * s, (use - 1) & 1, abort, limit)) { failed = 1; break; }
+                    const uint32_t own = qfull0 + 8 * s, da = smem_base + s * STAGE, db = da + A_BYTES;
+                    if (rank == 0) mbar_arrive_local(full0 + 8 * s);
+                    mbar_expect_tx(own, QB ? A_BYTES + Q_BYTES : STAGE_BYTES);
+                    tma_load_3d(da, &map_a, own, m0, r0 + plain * BK, 0);
+                    tma_load_3d(da + BK * 128, &map_a, own, m0 + 64, r0 + plain * BK, 0);
+                    if (QB) {
+                        tma_load_3d(db + B_BYTES, &map_b, own, n0, r0 + plain * BK, 0);
+                    } else {
+                        tma_load_3d(db, &map_b, own, n0, r0 + plain * BK, 0);
+                        tma_load_3d(db + BK * 128, &map_b, own, n0 + 64, r0 + plain * BK, 0);
+                    }
+                    ++it;
                 }
             }
         } else if (warp == 1 && rank == 0) {
@@ -769,14 +782,15 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             constexpr uint32_t idesc = grouped_idesc<CG, TN, A_MN, B != B_K>();
             constexpr uint32_t a_step = A_MN ? 2048u : 32u, b_step = B != B_K ? 2048u : 32u;
             Tile t;
-            unsigned it = 0, ai = 0;
+            unsigned it = 0, ai = 0, mended = 0;               // mended: phases of rready, a bit for each stage
             while (lane == 0 && !failed && next_tile(t)) {
+                const int plain = WG && !QB ? plain_blocks(p, t) : t.kb1;
                 for (int k0 = t.kb0; k0 < t.kb1; ++ai) {
                     const int k1 = min(k0 + part_blocks(OUT), t.kb1);
                     const unsigned a = ai & 1, use = ai >> 1;
                     if (use > 0 && !mbar_wait(acce0 + 8 * a, (use - 1) & 1, abort, limit)) { failed = 2; break; }
                     tc_fence_after();
-                    for (int kb = k0; kb < k1; ++kb, ++it) {
+                    for (int kb = k0; kb < min(k1, plain); ++kb, ++it) {
                         const unsigned s = it % RING;
                         if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
                         if (QB && !mbar_wait_operand(bfull0 + 8 * s, (it / RING) & 1, abort, limit)) { failed = 2; break; }
@@ -787,6 +801,19 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                             umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B != B_K), idesc,
                                        (kb > k0 || k > 0) ? 1u : 0u);
                         umma_commit_g<CG>(empty0 + 8 * s);
+                    }
+                    if (WG && !QB && plain < k1 && !failed) {
+                        const unsigned s = it % RING;
+                        if (!mbar_wait(full0 + 8 * s, (it / RING) & 1, abort, limit) || !mbar_wait_operand(rready0 + 8 * s, (mended >> s) & 1, abort, limit)) { failed = 2; break; }
+                        mended ^= 1u << s;
+                        tc_fence_after();
+                        const uint32_t da = smem_base + s * STAGE, db = da + A_BYTES;
+                        const int steps = (t.m1 - t.lo - plain * BK + UMMA_K - 1) / UMMA_K;
+                        for (int k = 0; k < steps; ++k)
+                            umma_g<CG>(tmem_base + a * TN, smem_desc(da + k * a_step, A_MN), smem_desc(db + k * b_step, B != B_K), idesc,
+                                       (plain > k0 || k > 0) ? 1u : 0u);
+                        umma_commit_g<CG>(empty0 + 8 * s);
+                        ++it;
                     }
                     if (failed) break;
                     umma_commit_g<CG>(accf0 + 8 * a);
@@ -811,6 +838,27 @@ grouped_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     if (lane == 0) mbar_arrive_local(qfull0 + 8 * s);
                 }
                 if (failed) break;
+            }
+        } else if (WG && !QB && warp == 2) {
+            // ---- the last blocks of groups: zeros behind the group's end
+            Tile t;
+            unsigned it = 0, there = 0;                        // there: phases of rfull, a bit for each stage
+            while (next_tile_warp(t)) {
+                it += t.kb1 - t.kb0;
+                const int plain = plain_blocks(p, t);
+                if (plain >= t.kb1) continue;
+                const unsigned s = (it - 1) % RING;
+                if (!__all_sync(0xffffffffu, mbar_wait(rfull0 + 8 * s, (there >> s) & 1, abort, limit))) { failed = 8; break; }
+                there ^= 1u << s;
+                const int rows = t.m1 - t.lo - plain * BK;     // (the issuer takes only the steps of 16 that hold some)
+                zero_rows<4>(smem + s * STAGE, rows, (rows + UMMA_K - 1) / UMMA_K * UMMA_K, lane, 32);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (rank == 1) signal_operand(map_to_rank(smem_u32(words), 0), map_to_rank(rready0 + 8 * s, 0));
+                    else if (CG == 2) mbar_expect_tx(rready0 + 8 * s, SIGNAL_BYTES);
+                    else mbar_arrive_local(rready0 + 8 * s);
+                }
             }
         } else if (warp == 3) {
             // ---- scheduler

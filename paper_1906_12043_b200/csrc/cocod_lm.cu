@@ -12,7 +12,6 @@
 #include <utility>
 
 struct cocod_lm {
-    CUtensorMap *group_maps = nullptr;     // device: two per group
     int *order = nullptr;                  // device: the groups by size
     float *parts = nullptr;                // device: parts of tiles, 256 x 256 for each pair of CTAs
     int *flag = nullptr;                   // device: what the kernels met
@@ -63,23 +62,18 @@ bool encode(CUtensorMap *m, const Matrix &x, uint64_t cols, uint64_t rows, uint6
 }
 
 // ------------------------------------------------------------------------------------------ small kernels
-// Block 2 g + i: the tensor map of group g's rows of A (i = 0) or B; and the group's place by size.
-__global__ void __launch_bounds__(32)
-make_group_maps(const __grid_constant__ CUtensorMap whole_a, const __grid_constant__ CUtensorMap whole_b, const char *a, long long lda_bytes,
-                const char *b, long long ldb_bytes, const GroupedParams p, CUtensorMap *maps, int *order)
+// The groups by size, a warp for each.
+__global__ void __launch_bounds__(256)
+order_groups(const GroupedParams p, int *order)
 {
-    __shared__ __align__(128) CUtensorMap map;
     pdl_launch_dependents();
     pdl_wait();
-    const int g = blockIdx.x >> 1;
-    if (blockIdx.x & 1) {
-        write_group_map(whole_b, b, ldb_bytes, p, g, maps + 2 * g + 1, map);
-    } else {
-        write_group_map(whole_a, a, lda_bytes, p, g, maps + 2 * g, map);
-        const int rank = group_rank(p, g);
-        if (threadIdx.x == 0) order[rank] = g;
-    }
+    const int g = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (g >= p.groups) return;
+    const int rank = group_rank(p, g);
+    if ((threadIdx.x & 31) == 0) order[rank] = g;
 }
+constexpr int WARP_GROUPS = 32;            // so many groups the product's warps order themselves
 
 // out = bf16(sums), for `rows` rows of n columns (n a multiple of 4); row r of the result is row r % per_group of group r / per_group.
 __global__ void __launch_bounds__(256)
@@ -233,29 +227,25 @@ int run_rows(cocod_lm *h, Form form, int G, const int32_t *offsets, const Window
 }
 
 // weight form: out_g (rows x cols) = sum over the group's rows m of A[m][.]^T B[m][.]
-// (scales: B is an 8-bit checkpoint;  add: added to what out, fp32, holds;  maps_ready: a kernel before this one has
-// written the groups' maps and order)
+// (scales: B is an 8-bit checkpoint;  add: added to what out, fp32, holds;  ordered: a kernel before this one has
+// written the groups' order, where there are more than WARP_GROUPS)
 int run_weights(cocod_lm *h, int G, const int32_t *offsets, const Window &win, int64_t rows, int64_t cols, const Matrix &A, const Matrix &B,
-                const uint8_t *scales, const Matrix &out, bool add, bool maps_ready, cudaStream_t s)
+                const uint8_t *scales, const Matrix &out, bool add, bool ordered, cudaStream_t s)
 {
     const int64_t M = win.rows;
     const Cut cut = choose_cut(WEIGHT_GRAD, G, rows, cols, ceil_div(std::max<int64_t>(M, 1), G), true);
     Matrix a_rows = A, b_rows = B;
-    if (M == 0) a_rows.data = b_rows.data = h->group_maps;      // nothing is read
+    if (M == 0) a_rows.data = b_rows.data = h->parts;           // nothing is read
     CUtensorMap a, b, o;
-    if (!encode(&o, out, cols, rows, (uint64_t)G, 32)) return COCOD_ERR_CUDA;
-    a = b = o;                             // (the kernel takes the groups' maps, made of these two; a checkpoint has one for the whole batch)
-    if ((!maps_ready && !encode(&a, a_rows, rows, std::max<int64_t>(M, 1), 1, 64)) ||
-        ((!maps_ready || scales) && !encode(&b, b_rows, cols, std::max<int64_t>(M, 1), 1, 64)))
+    if (!encode(&o, out, cols, rows, (uint64_t)G, 32) || !encode(&a, a_rows, rows, std::max<int64_t>(M, 1), 1, 64) ||
+        !encode(&b, b_rows, cols, std::max<int64_t>(M, 1), 1, 64))
         return COCOD_ERR_CUDA;
     GroupedParams p{};
     p.offsets = offsets; p.groups = G; p.total_rows = (int)win.total; p.row0 = (int)win.row0; p.rows = (int)M; p.n = (int)cols; p.kdim = (int)rows;
     p.tiles_n = (int)ceil_div(cols, cut.pair ? 256 : 128); p.band = cut.band; p.max_parts = cut.max_parts;
     p.out = const_cast<void *>(out.data); p.ld_out = out.ld; p.out_stride = out.stride;
-    p.group_maps = h->group_maps; p.order = h->order; p.scales = scales; p.error_flag = h->flag;
-    if (!maps_ready)                       // (a checkpoint needs none: what lies behind its group becomes zeros in the conversion)
-        TRY_CUDA(launch_dependent(true, make_group_maps, dim3(2 * G), dim3(32), 0, s, a, scales ? a : b, static_cast<const char *>(A.data),
-                                  (long long)A.ld * 2, static_cast<const char *>(scales ? A.data : B.data), (long long)(scales ? A.ld : B.ld) * 2, p, h->group_maps, h->order));
+    p.order = G > WARP_GROUPS ? h->order : nullptr; p.scales = scales; p.error_flag = h->flag;
+    if (G > WARP_GROUPS && !ordered) TRY_CUDA(launch_dependent(true, order_groups, dim3((unsigned)ceil_div(G, 8)), dim3(256), 0, s, p, h->order));
     if (scales)
         return out.elem == 2 ? launch_form<true, B_Q8, OUT_BF16>(h, cut, a, b, o, p, s) : launch_form<true, B_Q8, OUT_F32>(h, cut, a, b, o, p, s);
     if (add) return launch_form<true, B_MN, OUT_ADD_F32>(h, cut, a, b, o, p, s);
@@ -289,7 +279,7 @@ VocabLayout vocab_layout(int G, int64_t M, int64_t V, int64_t D, bool grad, int 
         l.rho = take(4 * at_once);
         l.rest = take(4 * at_once);
         l.u = take(2 * at_once * l.ldu);
-        l.hs = take(2 * (at_once + 64) * D);   // (the last box of 64 rows that a group's product begins stays within the workspace, though its map ends before)
+        l.hs = take(2 * at_once * D);
         if (at_once < M && dw_elem == 2) l.total32 = take(4 * G * V * D);
     }
     l.bytes = at;
@@ -333,12 +323,10 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
     do {                                   // (no rows at all: one pass, for the results' zeros)
         const Window win{row0, std::min(at_once, M - row0), M};
         const int64_t rows = std::max<int64_t>(win.rows, 1);
-        const Matrix hx{M ? static_cast<const bf16 *>(x.data) + row0 * x.ld : (const void *)h->group_maps, M ? x.ld : D, 0, 2};
-        const Matrix u{grad ? ws + l.u : (char *)h->group_maps, l.ldu, 0, 2}, hs{grad ? ws + l.hs : (char *)h->group_maps, D, 0, 2};
-        CUtensorMap a, b, o, u_rows, hs_rows;
-        if (!encode(&a, hx, D, rows, 1, 128) || !encode(&b, w, D, V, G, 128) || !encode(&o, grad ? u : hx, grad ? V : D, rows, 1, 32) ||
-            !encode(&u_rows, u, V, rows, 1, 64) || !encode(&hs_rows, hs, D, rows, 1, 64))
-            return COCOD_ERR_CUDA;
+        const Matrix hx{M ? static_cast<const bf16 *>(x.data) + row0 * x.ld : (const void *)h->parts, M ? x.ld : D, 0, 2};
+        const Matrix u{ws + l.u, l.ldu, 0, 2}, hs{ws + l.hs, D, 0, 2};
+        CUtensorMap a, b, o;
+        if (!encode(&a, hx, D, rows, 1, 128) || !encode(&b, w, D, V, G, 128) || !encode(&o, grad ? u : hx, grad ? V : D, rows, 1, 32)) return COCOD_ERR_CUDA;
         GroupedParams p{};
         p.offsets = offsets; p.groups = G; p.total_rows = (int)M; p.row0 = (int)row0; p.rows = (int)win.rows; p.n = (int)V; p.kdim = (int)D;
         p.tiles_n = (int)ceil_div(V, cut.pair ? 256 : 128); p.max_parts = 1;
@@ -346,9 +334,7 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
         p.out = ws + l.u; p.ld_out = l.ldu; p.error_flag = h->flag;
         p.ref = v.ref + row0; p.label = v.label + row0; p.sums = reinterpret_cast<float2 *>(ws + l.sums); p.ld_sums = (int)win.rows;
         const int row_blocks = (int)ceil_div(win.rows, 8);
-        TRY_CUDA(launch_dependent(true, vocab_begin, dim3(row_blocks + G), dim3(256), 0, s, u_rows, hs_rows, static_cast<const char *>(u.data),
-                                  (long long)u.ld * 2, static_cast<const char *>(hs.data), (long long)hs.ld * 2, p,
-                                  grad ? h->group_maps : (CUtensorMap *)nullptr, h->order, v, row_blocks));
+        TRY_CUDA(launch_dependent(true, vocab_begin, dim3(row_blocks + G), dim3(256), 0, s, p, grad && G > WARP_GROUPS ? h->order : (int *)nullptr, v, row_blocks));
         FinishParams f{};
         f.v = v; f.row0 = (int)row0; f.rows = (int)win.rows; f.sums = p.sums; f.ld_sums = p.ld_sums;
         f.n_sums = (int)ceil_div(V, cut.pair ? 128 : 64);
@@ -404,7 +390,7 @@ bool good_shape(const cocod_lm *h, int G, const int32_t *offsets, int64_t M, int
 }
 void lm_free(cocod_lm *h)
 {
-    void *ptrs[] = {h->group_maps, h->order, h->parts, h->flag};
+    void *ptrs[] = {h->order, h->parts, h->flag};
     for (void *p : ptrs) if (p) cudaFree(p);
     delete h;
 }
@@ -420,8 +406,7 @@ int cocod_lm_create(cocod_lm_handle **out)
     if (!get_encoder()) return COCOD_ERR_CUDA;
     cocod_lm *h = new (std::nothrow) cocod_lm();
     if (!h) return COCOD_ERR_OOM;
-    cudaError_t e = cudaMalloc((void **)&h->group_maps, 2 * COCOD_LM_MAX_GROUPS * sizeof(CUtensorMap));
-    if (e == cudaSuccess) e = cudaMalloc((void **)&h->order, COCOD_LM_MAX_GROUPS * sizeof(int));
+    cudaError_t e = cudaMalloc((void **)&h->order, COCOD_LM_MAX_GROUPS * sizeof(int));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->parts, (size_t)(sm_count() / 2 + 1) * 256 * 256 * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
     if (e == cudaSuccess) e = cudaMemset(h->flag, 0, 256);

@@ -59,13 +59,11 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// One warp per row: the label's logit.  The last `groups` blocks count the rows of a group that have a label, and, where the
-// gradient is wanted (maps != nullptr), write the tensor maps of the group's rows of u and of rho h and its place by size.
+// One warp per row: the label's logit.  The last `groups` blocks count the rows of a group that have a label, and, where it is
+// wanted, write the group's place by size.
 __global__ void __launch_bounds__(256)
-vocab_begin(const __grid_constant__ CUtensorMap whole_u, const __grid_constant__ CUtensorMap whole_hs, const char *u, long long ldu_bytes,
-            const char *hs, long long ldhs_bytes, const GroupedParams window, CUtensorMap *maps, int *order, const VocabRows p, int row_blocks)
+vocab_begin(const GroupedParams window, int *order, const VocabRows p, int row_blocks)
 {
-    __shared__ __align__(128) CUtensorMap map[2];
     __shared__ int part[8];
     pdl_launch_dependents();
     pdl_wait();
@@ -73,12 +71,10 @@ vocab_begin(const __grid_constant__ CUtensorMap whole_u, const __grid_constant__
     if ((int)blockIdx.x >= row_blocks) {
         const int g = blockIdx.x - row_blocks;
         if (g == 0 && threadIdx.x < 2) p.redo_any[threadIdx.x] = 0;
-        if (maps != nullptr && warp == 5) {
+        if (order != nullptr && warp == 5) {
             const int rank = group_rank(window, g);
             if (lane == 0) order[rank] = g;
         }
-        if (maps != nullptr && warp == 6) write_group_map(whole_u, u, ldu_bytes, window, g, maps + 2 * g, map[0]);
-        if (maps != nullptr && warp == 7) write_group_map(whole_hs, hs, ldhs_bytes, window, g, maps + 2 * g + 1, map[1]);
         const int lo = min(max(p.offsets[g], 0), p.total), hi = min(max(p.offsets[g + 1], lo), p.total);
         int n = 0;
         for (int r = lo + threadIdx.x; r < hi; r += 256) {

@@ -183,3 +183,34 @@ def test_long_sums_of_positive_products_do_not_shrink(ops):
     ops.check()
     want = x[:64].double() @ w[:64].double().T
     assert abs(float((y[:64, :64].double() / want - 1).mean())) <= 2.0 ** -12
+
+
+@pytest.mark.parametrize("n,k", [(24, 40), (136, 264), (1024, 1032)])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("few", [True, False])
+def test_every_remainder_of_a_group_beside_rows_that_are_not_finite(lm, n, k, packed, few):
+    """Groups of every length modulo 64, each followed by one whose rows are NaN and infinite: nothing of those comes in, and they are NaN.
+    fp32 results of up to 200 products: 13 steps that cut off at most 2^-23 of the sum of magnitudes, and as much again for the joining of parts."""
+    lengths = [1, 15, 16, 17, 31, 47, 48, 49, 63, 64, 65, 127, 129, 177, 200] if few else list(range(1, 66)) + [100, 190]
+    sizes = [s for length in lengths for s in (length, 1 + length % 5)][:32 if few else None]
+    off, spans = offsets_of(sizes)
+    M, G = sum(sizes), len(sizes)
+    assert (G > 32) != few
+    x, dy = gaussian(1, M, k), gaussian(2, M, n)
+    for s in spans[1::2]:
+        x[s], dy[s] = float("nan"), float("inf")
+    o = lm.LMOps(widen=False)
+    a = o.act_pack(x) if packed else x
+    if packed:
+        x = o.act_unpack(a)
+    for dtype in (torch.float32, torch.bfloat16):
+        dw = o.grouped_weight_grad(dy, a, off, out_dtype=dtype)
+        for g, s in enumerate(spans):
+            if g % 2:
+                assert torch.isnan(dw[g]).all()
+                continue
+            want, size = dy[s].double().T @ x[s].double(), dy[s].double().abs().T @ x[s].double().abs()
+            bound = 26 * 2.0 ** -23 * size + (half_unit(want) * 1.01 if dtype == torch.bfloat16 else 0)
+            assert ((dw[g].double() - want).abs() <= bound).all()
+    o.check()
+    o.destroy()
