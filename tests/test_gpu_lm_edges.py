@@ -214,3 +214,40 @@ def test_every_remainder_of_a_group_beside_rows_that_are_not_finite(lm, n, k, pa
             assert ((dw[g].double() - want).abs() <= bound).all()
     o.check()
     o.destroy()
+
+
+# ------------------------------------------------------------------------------------------------------- beyond 2^31 values
+def test_open_gates_beyond_32_bits_pass_their_values(ops):
+    M, k = 70001, 32768
+    x = torch.empty(M, k, device="cuda", dtype=torch.bfloat16)
+    ends = [slice(0, 64), slice(M - 64, M)]
+    for i, rows in enumerate(ends):
+        x[rows] = gaussian(i, 64, k)
+    p = ops.act_pack(x)
+    for i, rows in enumerate(ends):
+        x[rows] = gaussian(i + 2, 64, k)
+    ops.act_relu_grad(x, p, out=x)
+    for i, rows in enumerate(ends):
+        assert torch.equal(x[rows], torch.where(gaussian(i, 64, k) > 0, gaussian(i + 2, 64, k), 0.0).bfloat16())
+    ops.check()
+
+
+def test_gradient_of_the_weights_beyond_32_bits(lm):
+    """dw of both ends of a vocabulary, over more than 2^31 exponentials.  A term carries three bf16 roundings (3 * 2^-8) and twice a logit's
+    error d (each step of 16 products cuts off at most 2^-23 of |h| |w|), the result one more; the sum of M terms M / 16 + 40 steps."""
+    M, V, D = 17001, 131073, 16
+    off, _ = offsets_of([M])
+    h, w = gaussian(1, M, D), gaussian(2, 1, V, D, scale=0.5)
+    labels = torch.randint(0, V, (M,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    labels[::9] = V - 3
+    o = lm.LMOps(workspace_limit=16 << 30)
+    dw = o.vocab_loss_grad(h, w, labels, off)[3][0].double()
+    o.check()
+    o.destroy()
+    lse = torch.cat([torch.logsumexp(part.double() @ w[0].double().T, 1) for part in h.split(1000)])
+    d = (D / 16 + 8) * 2.0 ** -23 * float(h.float().norm(dim=1).max() * w.float().norm(dim=2).max())
+    for at in (slice(0, 40), slice(V - 40, V)):
+        p = torch.exp(h.double() @ w[0, at].double().T - lse[:, None])
+        p -= (labels.long()[:, None] == torch.arange(V, device="cuda")[None, at]).double()
+        want, size = p.T @ h.double() / M, p.abs().T @ h.double().abs() / M
+        assert ((dw[at] - want).abs() <= (3 * 2.0 ** -8 * 1.02 + 2 * d + (M / 16 + 40) * 2.0 ** -23) * size + 2.0 ** -8 * want.abs()).all()
