@@ -15,6 +15,7 @@ struct cocod_lm {
     int *order = nullptr;                  // device: the groups by size
     float *parts = nullptr;                // device: parts of tiles, 256 x 256 for each pair of CTAs
     int *flag = nullptr;                   // device: what the kernels met
+    int device = -1;                       // the one current at creation
     long long launches = 0;
 };
 
@@ -406,6 +407,7 @@ int cocod_lm_create(cocod_lm_handle **out)
     if (!get_encoder()) return COCOD_ERR_CUDA;
     cocod_lm *h = new (std::nothrow) cocod_lm();
     if (!h) return COCOD_ERR_OOM;
+    h->device = current_device();
     cudaError_t e = cudaMalloc((void **)&h->order, COCOD_LM_MAX_GROUPS * sizeof(int));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->parts, (size_t)(sm_count() / 2 + 1) * 256 * 256 * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
@@ -423,7 +425,10 @@ int cocod_lm_create(cocod_lm_handle **out)
 int cocod_lm_destroy(cocod_lm_handle *h)
 {
     if (!h) return COCOD_OK;
+    const int now = current_device();      // (another one may be current: it is this one whose work has to end)
+    if (now != h->device) cudaSetDevice(h->device);
     cudaDeviceSynchronize();
+    if (now != h->device && now >= 0) cudaSetDevice(now);
     lm_free(h);
     return COCOD_OK;
 }

@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -83,6 +84,16 @@ int64_t whole(PyObject *o)
     return v;
 }
 
+// The operators' device; kernels are launched on the current one.
+int64_t device(PyObject *o)
+{
+    const int64_t dev = whole(o), now = c10::cuda::current_device();
+    if (dev != now)
+        throw std::invalid_argument("the current device is cuda:" + std::to_string(now) + ", these operators were made on cuda:" + std::to_string(dev) +
+                                    ": call them under torch.cuda.device(" + std::to_string(dev) + ")");
+    return dev;
+}
+
 // The result's type: the caller's choice (0 bf16, 1 fp32, -1 none), which has to be the type of a result that is given.
 at::ScalarType result_type(PyObject *out, int64_t code, at::ScalarType usual)
 {
@@ -133,7 +144,7 @@ inline cocod_lm_handle *handle(PyObject *o)
 template <bool FORWARD> PyObject *rows_product(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]);
+    const int64_t dev = device(a[1]);
     const char *name = FORWARD ? "x" : "dy";
     const Tensor &x = tensor(a[2], name, 2), &w = tensor(a[3], "w", 3), &off = tensor(a[4], "offsets", 1);
     const int64_t G = w.size(0), n = w.size(1), k = w.size(2), M = x.size(0), cols = FORWARD ? n : k;
@@ -168,7 +179,7 @@ Weights weights(PyObject *out, PyObject *code, const Tensor &like, const char *n
 PyObject *weight_grad(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]);
+    const int64_t dev = device(a[1]);
     const Tensor &dy = tensor(a[2], "dy", 2), &x = tensor(a[3], "x", 2), &off = tensor(a[4], "offsets", 1);
     const int64_t M = x.size(0), k = x.size(1), n = dy.size(1), G = off.size(0) - 1;
     const int32_t *offsets = static_cast<const int32_t *>(vector(off, "offsets", G + 1, at::kInt, dev));
@@ -183,7 +194,7 @@ PyObject *weight_grad(PyObject *const *a)
 PyObject *weight_grad_packed(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]), M = whole(a[3]), k = whole(a[4]);
+    const int64_t dev = device(a[1]), M = whole(a[3]), k = whole(a[4]);
     const Tensor &dy = tensor(a[2], "dy", 2), &off = tensor(a[8], "offsets", 1);
     const int64_t n = dy.size(1), G = off.size(0) - 1;
     const int32_t *offsets = static_cast<const int32_t *>(vector(off, "offsets", G + 1, at::kInt, dev));
@@ -204,7 +215,7 @@ PyObject *weight_grad_packed(PyObject *const *a)
 PyObject *act_pack_new(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]);
+    const int64_t dev = device(a[1]);
     const Tensor &x = tensor(a[2], "x", 2);
     const int64_t M = x.size(0), k = x.size(1), ld = (k + 15) / 16 * 16;
     const Matrix mx = rows(x, "x", M, k, at::kBFloat16, dev, 1);
@@ -215,7 +226,7 @@ PyObject *act_pack_new(PyObject *const *a)
 PyObject *act_pack_into(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]), M = whole(a[3]), k = whole(a[4]);
+    const int64_t dev = device(a[1]), M = whole(a[3]), k = whole(a[4]);
     const Matrix mx = rows(tensor(a[2], "x", 2), "x", M, k, at::kBFloat16, dev, 1);
     return PyLong_FromLong(cocod_act_pack(h, M, k, mx.data, mx.ld, static_cast<int8_t *>(PyLong_AsVoidPtr(a[5])), whole(a[6]),
                                           static_cast<uint8_t *>(PyLong_AsVoidPtr(a[7])), current(dev)));
@@ -225,7 +236,7 @@ PyObject *act_pack_into(PyObject *const *a)
 PyObject *act_unpack(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]), M = whole(a[3]), k = whole(a[4]);
+    const int64_t dev = device(a[1]), M = whole(a[3]), k = whole(a[4]);
     const Tensor out = a[8] == Py_None ? fresh(tensor(a[2], "checkpoint", -1), {M, k}, at::kBFloat16) : tensor(a[8], "out", 2);
     const Matrix mo = a[8] == Py_None ? Matrix{out.data_ptr(), k, 0} : rows(out, "out", M, k, at::kBFloat16, dev, 1);
     const int rc = cocod_act_unpack(h, M, k, static_cast<const int8_t *>(PyLong_AsVoidPtr(a[5])), whole(a[6]), static_cast<const uint8_t *>(PyLong_AsVoidPtr(a[7])),
@@ -237,7 +248,7 @@ PyObject *act_unpack(PyObject *const *a)
 PyObject *act_relu_grad(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]), M = whole(a[3]), k = whole(a[4]);
+    const int64_t dev = device(a[1]), M = whole(a[3]), k = whole(a[4]);
     const Tensor &dh = tensor(a[2], "dh", 2);
     const Matrix md = rows(dh, "dh", M, k, at::kBFloat16, dev, 1);
     const Tensor out = a[7] == Py_None ? fresh(dh, {M, k}, at::kBFloat16) : tensor(a[7], "out", 2);
@@ -250,7 +261,7 @@ PyObject *act_relu_grad(PyObject *const *a)
 template <bool GRAD> PyObject *vocab(PyObject *const *a)
 {
     cocod_lm_handle *h = handle(a[0]);
-    const int64_t dev = whole(a[1]), limit = whole(a[7]);
+    const int64_t dev = device(a[1]), limit = whole(a[7]);
     const Tensor &x = tensor(a[2], "x", 2), &w = tensor(a[3], "w", 3);
     const int64_t G = w.size(0), V = w.size(1), D = w.size(2), M = x.size(0);
     const Matrix mx = rows(x, "x", M, D, at::kBFloat16, dev, 16), mw = groups(w, "w", G, V, D, at::kBFloat16, dev);

@@ -251,3 +251,23 @@ def test_gradient_of_the_weights_beyond_32_bits(lm):
         p -= (labels.long()[:, None] == torch.arange(V, device="cuda")[None, at]).double()
         want, size = p.T @ h.double() / M, p.abs().T @ h.double().abs() / M
         assert ((dw[at] - want).abs() <= (3 * 2.0 ** -8 * 1.02 + 2 * d + (M / 16 + 40) * 2.0 ** -23) * size + 2.0 ** -8 * want.abs()).all()
+
+
+# ------------------------------------------------------------------------------------------------------- refusals
+def test_a_call_while_another_device_is_current_is_refused_by_name(lm):
+    """(As if the operators had been made on the next device: the box of these tests may have one.)"""
+    o = lm.LMOps()
+    here, other = torch.cuda.current_device(), torch.cuda.current_device() + 1
+    x, w, off = gaussian(1, 64, 64), gaussian(2, 1, 64, 64), torch.tensor([0, 64], dtype=torch.int32, device="cuda")
+    labels, p = torch.zeros(64, dtype=torch.int32, device="cuda"), o.act_pack(x)
+    o._device = other
+    o._here = lambda packed: None
+    for call in (lambda: o.grouped_forward(x, w, off), lambda: o.grouped_input_grad(x, w, off), lambda: o.grouped_weight_grad(x, x, off),
+                 lambda: o.grouped_weight_grad(x, p, off), lambda: o.act_pack(x), lambda: o.act_pack(x, out=p), lambda: o.act_unpack(p),
+                 lambda: o.act_relu_grad(x, p), lambda: o.vocab_loss(x, w, labels, off), lambda: o.vocab_loss_grad(x, w, labels, off)):
+        with pytest.raises(ValueError, match=f"current device is cuda:{here}.*made on cuda:{other}"):
+            call()
+    o._device = here
+    o.grouped_forward(x, w, off)
+    o.check()
+    o.destroy()
