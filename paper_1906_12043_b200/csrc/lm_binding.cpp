@@ -2,7 +2,8 @@
 // torch and makes the C call on torch's current stream.  Marshalling only.  The same in Python and ctypes took 5 to 8 us a
 // call, as long as the kernels of a small call themselves.
 //
-// Every function returns its result, or the library's error code as an int (the caller raises); a tensor that does not fit is a ValueError.
+// Every function returns its result, or the library's error code as an int (the caller raises); a tensor that does not fit is a ValueError,
+// and a result or scratch that torch has no room for its OutOfMemoryError.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -123,6 +124,11 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n)
         return F(args);
     } catch (const std::invalid_argument &e) {
         PyErr_SetString(PyExc_ValueError, e.what());
+    } catch (const c10::OutOfMemoryError &e) {
+        PyObject *torch = PyImport_ImportModule("torch"), *type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (type) PyErr_SetString(type, e.what_without_backtrace());
+        Py_XDECREF(type);
+        Py_XDECREF(torch);
     } catch (const std::exception &e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
     } catch (...) {

@@ -271,3 +271,11 @@ def test_a_call_while_another_device_is_current_is_refused_by_name(lm):
     o.grouped_forward(x, w, off)
     o.check()
     o.destroy()
+
+
+def test_no_room_for_a_result_is_torch_s_own_error(ops):
+    dy, off = gaussian(1, 8, 1 << 19), torch.tensor([0, 8], dtype=torch.int32, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):
+        ops.grouped_weight_grad(dy, dy, off)               # 2^38 fp32 values
+    assert torch.isfinite(ops.grouped_weight_grad(dy[:, :64], dy[:, :64], off)).all()
+    ops.check()

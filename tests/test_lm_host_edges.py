@@ -39,3 +39,13 @@ def test_workspaces_rise_with_their_limit_and_stay_within_it(G, M, V, D, grad, d
         assert got >= last and (got <= limit or got == least)
         assert limit < whole or got == whole
         last = got
+
+
+def test_the_binding_loads_and_refuses_without_a_gpu():
+    from paper_1906_12043_b200 import build
+    build.build()
+    from paper_1906_12043_b200 import _lm_binding
+    with pytest.raises(ValueError, match="destroyed"):
+        _lm_binding.act_pack_new(0, 0, torch.zeros(1, 1))
+    with pytest.raises(ValueError, match="number of arguments"):
+        _lm_binding.act_pack_new(0)
