@@ -11,12 +11,13 @@
  * Groups.  The rows of all groups (workers, whose mini-batches M_i may differ in size, Section 3.2; or experts) lie one
  * behind the other in one matrix: row m belongs to group g when offsets[g] <= m < offsets[g + 1].  offsets: device,
  * G + 1 int32, rising from 0 to M; groups may be empty.  The offsets are only read on the device.  Offsets that do not
- * rise from 0 to M never lead to an access outside the matrices; the next cocod_lm_check reports them (INVALID).
+ * rise from 0 to M never lead to an access outside the matrices; the next cocod_lm_check reports them (INVALID;
+ * a product without any rows looks at none).
  *
  * Matrices are row-major; a leading dimension (row stride) and a group stride are in elements, so that the weights may be
  * views of the engine's K x P bf16 copy (cocod_get_bf16_shadow) and the weight gradients views of the K x P fp32
  * gradients that cocod_local_step takes.  Every base address has to be a multiple of 16 bytes, and so has every stride;
- * n and k have to be multiples of 8 (INVALID otherwise).
+ * n and k have to be multiples of 8 (INVALID otherwise).  A result may not lie on an operand (but see act_relu_grad).
  *
  * Precision: bf16 operands, products and sums in fp32, one rounding at the end where the result is bf16.
  *

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -95,6 +96,18 @@ int64_t device(PyObject *o)
     return dev;
 }
 
+// A result that is given may not lie on an operand, which other thread blocks still read (seen where one begins at the other, or both are without
+// gaps; rows of one buffer beside one another are fine).
+void apart(const Tensor &out, const char *out_name, const Tensor &in, const char *name, bool same_is_fine = false)
+{
+    const bool begins = out.data_ptr() == in.data_ptr() && out.numel() > 0 && in.numel() > 0;
+    const at::MemOverlapStatus s = at::get_overlap_status(out, in);
+    const bool same = begins && out.sizes() == in.sizes() && out.strides() == in.strides();
+    if (same && same_is_fine) return;
+    if (begins || s == at::MemOverlapStatus::Full || s == at::MemOverlapStatus::Partial)
+        throw std::invalid_argument(std::string(out_name) + ": lies on " + name);
+}
+
 // The result's type: the caller's choice (0 bf16, 1 fp32, -1 none), which has to be the type of a result that is given.
 at::ScalarType result_type(PyObject *out, int64_t code, at::ScalarType usual)
 {
@@ -159,6 +172,7 @@ template <bool FORWARD> PyObject *rows_product(PyObject *const *a)
     const at::ScalarType type = result_type(a[5], whole(a[6]), at::kBFloat16);
     const Tensor out = a[5] == Py_None ? fresh(x, {M, cols}, type) : tensor(a[5], "out", 2);
     const Matrix mo = a[5] == Py_None ? Matrix{out.data_ptr(), cols, 0} : rows(out, "out", M, cols, type, dev, 16);
+    if (a[5] != Py_None) apart(out, "out", x, name), apart(out, "out", w, "w");
     const int rc = (FORWARD ? cocod_grouped_forward : cocod_grouped_input_grad)(h, (int)G, offsets, M, n, k, mx.data, mx.ld, mw.data, mw.ld, mw.stride,
                                                                                mo.data, mo.ld, type_code(type), current(dev));
     return rc == COCOD_OK && a[5] != Py_None ? given(a[5]) : code_or(rc, out);
@@ -191,6 +205,7 @@ PyObject *weight_grad(PyObject *const *a)
     const int32_t *offsets = static_cast<const int32_t *>(vector(off, "offsets", G + 1, at::kInt, dev));
     const Matrix md = rows(dy, "dy", M, n, at::kBFloat16, dev, 16), mx = rows(x, "x", M, k, at::kBFloat16, dev, 16);
     const Weights w = weights(a[5], a[6], dy, "out", G, n, k, at::kFloat, dev);
+    if (a[5] != Py_None) apart(w.t, "out", dy, "dy"), apart(w.t, "out", x, "x");
     const int rc = cocod_grouped_weight_grad(h, (int)G, offsets, M, n, k, md.data, md.ld, mx.data, mx.ld, w.m.data, w.m.ld, w.m.stride, type_code(w.type),
                                              current(dev));
     return rc == COCOD_OK && a[5] != Py_None ? given(a[5]) : code_or(rc, w.t);
@@ -206,6 +221,7 @@ PyObject *weight_grad_packed(PyObject *const *a)
     const int32_t *offsets = static_cast<const int32_t *>(vector(off, "offsets", G + 1, at::kInt, dev));
     const Matrix md = rows(dy, "dy", M, n, at::kBFloat16, dev, 16);
     const Weights w = weights(a[9], a[10], dy, "out", G, n, k, at::kFloat, dev);
+    if (a[9] != Py_None) apart(w.t, "out", dy, "dy");
     int64_t bytes = whole(a[11]) ? cocod_grouped_packed_workspace((int)G, M, n, k) : 0;
     Tensor scratch;
     if (bytes > 0) scratch = fresh(dy, {bytes}, at::kByte);
@@ -259,6 +275,7 @@ PyObject *act_relu_grad(PyObject *const *a)
     const Matrix md = rows(dh, "dh", M, k, at::kBFloat16, dev, 1);
     const Tensor out = a[7] == Py_None ? fresh(dh, {M, k}, at::kBFloat16) : tensor(a[7], "out", 2);
     const Matrix mo = a[7] == Py_None ? Matrix{out.data_ptr(), k, 0} : rows(out, "out", M, k, at::kBFloat16, dev, 1);
+    if (a[7] != Py_None) apart(out, "out", dh, "dh", true);
     const int rc = cocod_act_relu_grad(h, M, k, md.data, md.ld, static_cast<const int8_t *>(PyLong_AsVoidPtr(a[5])), whole(a[6]), mo.data, mo.ld, current(dev));
     return rc == COCOD_OK && a[7] != Py_None ? given(a[7]) : code_or(rc, out);
 }
@@ -276,6 +293,7 @@ template <bool GRAD> PyObject *vocab(PyObject *const *a)
     const float *weight = a[6] == Py_None ? nullptr : static_cast<const float *>(vector(tensor(a[6], "row_weights", 1), "row_weights", M, at::kFloat, dev));
     Weights dw{};
     if (GRAD) dw = weights(a[8], a[9], x, "dw", G, V, D, at::kBFloat16, dev);
+    if (GRAD && a[8] != Py_None) apart(dw.t, "dw", x, "x"), apart(dw.t, "dw", w, "w");
     const int64_t bytes = cocod_vocab_workspace((int)G, M, V, D, GRAD, GRAD ? type_code(dw.type) : COCOD_BF16, limit);
     if (bytes < 0) return PyLong_FromLong((long)bytes);
     const Tensor scratch = fresh(x, {bytes}, at::kByte), loss = fresh(x, {G}, at::kFloat), row_loss = fresh(x, {M}, at::kFloat);

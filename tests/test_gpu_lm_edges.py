@@ -279,3 +279,22 @@ def test_no_room_for_a_result_is_torch_s_own_error(ops):
         ops.grouped_weight_grad(dy, dy, off)               # 2^38 fp32 values
     assert torch.isfinite(ops.grouped_weight_grad(dy[:, :64], dy[:, :64], off)).all()
     ops.check()
+
+
+def test_results_on_top_of_operands_are_refused(ops):
+    x, w, off = gaussian(1, 64, 64), gaussian(2, 1, 64, 64), torch.tensor([0, 64], dtype=torch.int32, device="cuda")
+    labels = torch.zeros(64, dtype=torch.int32, device="cuda")
+    two = gaussian(3, 128, 64)
+    for call in (lambda: ops.grouped_forward(x, w, off, out=x), lambda: ops.grouped_forward(x, w, off, out=w[0]),
+                 lambda: ops.grouped_forward(two[:64], w, off, out=two[1:65]), lambda: ops.grouped_input_grad(x, w, off, out=x),
+                 lambda: ops.grouped_weight_grad(x, two[:64], off, out=x[None]), lambda: ops.grouped_weight_grad(two[:64], x, off, out=x[None]),
+                 lambda: ops.grouped_weight_grad(x, ops.act_pack(x), off, out=x[None]), lambda: ops.act_relu_grad(two[:64], ops.act_pack(x), out=two[1:65]),
+                 lambda: ops.vocab_loss_grad(x, w, labels, off, dw=w), lambda: ops.vocab_loss_grad(x, w, labels, off, dw=x[None])):
+        with pytest.raises(ValueError, match="lies on"):
+            call()
+    # beside one another in one buffer, and in place where that is meant
+    buffer = torch.cat([x, x], 1)
+    assert torch.equal(ops.grouped_forward(buffer[:, :64], w, off, out=buffer[:, 64:]), ops.grouped_forward(x, w, off))
+    want = ops.act_relu_grad(x, ops.act_pack(two[:64]))
+    assert torch.equal(ops.act_relu_grad(x, ops.act_pack(two[:64]), out=x.view(64, 64)), want)
+    ops.check()
