@@ -83,7 +83,8 @@ int cocod_grouped_weight_grad(cocod_lm_handle *h, int G, const int32_t *offsets,
  * stands for q * 2^e: within half a unit of x (within one for |x| < 2^e / 2: the sign of a value always survives, so that
  * the gate of a ReLU can be taken from it; and within one where e is 122: bf16 ends below 64 * 2^122, so |q| stops at 63), and exact in bf16.  q = -128 marks a value that was not finite; a block that holds
  * one has scale byte 255 and reads as NaN.
- *   q      : M x k int8, row stride ldq (a multiple of 16, >= k); what lies behind a row's k values is neither read nor written
+ *   q      : M x k int8, row stride ldq (a multiple of 16, >= k); what lies behind a row's k values is never written, and read at
+ *            most up to the next multiple of 8 bytes (whatever it holds)
  *   scales : ceil(k / 128) x M bytes, e + 127 (or 255)
  *
  * act_pack       x: M x k bf16 (any k and ldx, any 2-byte alignment; 16-byte aligned rows are faster)

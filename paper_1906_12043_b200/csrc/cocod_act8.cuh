@@ -101,39 +101,37 @@ __device__ __forceinline__ int lead(const __nv_bfloat16 *row)
 {
     return ALIGNED ? 0 : (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 7;
 }
-// Four 8-bit values from column `at` (a multiple of 4) on.  Rows of q are 16-byte aligned, but what lies behind their last column need not
-// belong to the checkpoint (a view, the end of a buffer): the values of a word that the row does not fill go one by one.
-__device__ __forceinline__ uint32_t word_q(const int8_t *row, int at, int k)
-{
-    if (at >= 0 && at + 4 <= k) return *reinterpret_cast<const uint32_t *>(row + at);
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-        if (at >= 0 && at + i < k) w |= (uint32_t)(uint8_t)row[at + i] << (8 * i);
-    return w;
-}
+// Eight 8-bit values to columns c .. c + 7, as far as they are in the row: what lies behind need not belong to the checkpoint (a view, the
+// end of a buffer).
 __device__ __forceinline__ void store8_q(int8_t *row, int c, int k, uint2 x)
 {
     if (c + 8 <= k) {
         *reinterpret_cast<uint2 *>(row + c) = x;
         return;
     }
-#pragma unroll
-    for (int j = 0; j < 7; ++j)
-        if (c + j < k) row[c + j] = (int8_t)((j < 4 ? x.x : x.y) >> (8 * (j & 3)));
+#pragma unroll 1
+    for (; c < k; ++c) {
+        row[c] = (int8_t)x.x;
+        x.x = __funnelshift_r(x.x, x.y, 8);
+        x.y >>= 8;
+    }
 }
-// The 8-bit values of columns c - s .. c - s + 7 (c a multiple of 8, 0 <= s < 8): the words that hold them, and how they come out of those.
+// The 8-bit values of columns c - s .. c - s + 7 (c a multiple of 8, 0 <= s < 8; rows of q are 16-byte aligned, and the words that hold a
+// row's last values may be read as a whole): the words that hold them, and how they come out of those.
 template <bool ALIGNED>
 __device__ __forceinline__ void begin_q(uint32_t (&w)[3], const int8_t *row, int c, int k, int s)
 {
     w[2] = 0;
     if (ALIGNED) {
-        const uint2 v = c + 8 <= k ? *reinterpret_cast<const uint2 *>(row + c) : make_uint2(word_q(row, c, k), word_q(row, c + 4, k));
+        const uint2 v = c < k ? *reinterpret_cast<const uint2 *>(row + c) : make_uint2(0, 0);
         w[0] = v.x, w[1] = v.y;
     } else {
         const int from = (c - s) & ~3;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) w[i] = word_q(row, from + 4 * i, k);
+        for (int i = 0; i < 3; ++i) {
+            const int at = from + 4 * i;
+            w[i] = at >= 0 && at < k ? *reinterpret_cast<const uint32_t *>(row + at) : 0;
+        }
     }
 }
 template <bool ALIGNED>
