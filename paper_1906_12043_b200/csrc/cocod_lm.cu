@@ -551,15 +551,15 @@ int cocod_act_relu_grad(cocod_lm_handle *h, int64_t M, int64_t k, const void *dh
 }
 
 // Whether a checkpoint is better turned into bf16 once, by a kernel before the product, than inside it.  The conversion costs the
-// product about 0.18 us for every block of 64 of a tile's reduction (4 groups of 8192 rows, 2048 x 4096 results: 490 us against
-// 435 with the kernel before it); the kernel costs a launch and 3 bytes a value at 5.4 TB/s (16 groups of 128 rows, 1024 x 1024
-// results: 29.0 us against 25.7 with the conversion inside).
+// product about 0.26 us for every block of 64 of a tile's reduction (4 groups of 8192 rows, 2048 x 4096 results: 523 us against
+// 399 with the kernel before it; 2048 rows, 2048 x 2048: 26.0 and 19.7); the kernel costs a launch and 3 bytes a value at 5.4 TB/s (16
+// groups of 128 rows, 1024 x 1024 results: 20.5 us against 18.8 with the conversion inside).
 static bool widen_first(int G, int64_t M, int64_t n, int64_t k)
 {
     const int64_t depth = ceil_div(std::max<int64_t>(M, 1), G);
     const Cut cut = choose_cut(WEIGHT_GRAD, G, n, k, depth, true);
     const double waves = std::ceil((double)cut.tiles / (cut.pair ? sm_count() / 2 : std::max(sm_count(), 1)));
-    return waves * ceil_div(depth, 64) * 0.18 > 4.0 + 3.0 * M * k / 5.4e6;
+    return waves * ceil_div(depth, 64) * 0.26 > 4.0 + 3.0 * M * k / 5.4e6;
 }
 
 int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k)
