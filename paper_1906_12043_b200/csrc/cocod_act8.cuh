@@ -3,8 +3,8 @@
 // All three kernels stream, and HBM bounds them while rows start at multiples of 16 bytes.  Eight threads make a block of 128 columns of a
 // row; a thread takes columns 8 j .. + 7 and 64 + 8 j .. + 7, so that each of its 16-byte accesses to bf16 rows lies beside its
 // neighbours', and one or two rows, whose loads are under way together.  A CTA takes 32 or 64 rows of 128 columns; the scales, stored column
-// block by column block, leave it side by side.  32768 rows of 4096: pack 79 us (5.1 TB/s; rounding and packing take about as many
-// issue slots as the loads leave), unpack 72 (5.6), gate 111 (6.1).  Rows of 4095: 98, 98 and 120 us, bound by the
+// block by column block, leave it side by side.  32768 rows of 4096: pack 76 us (5.3 TB/s; rounding and packing take about as many
+// issue slots as the loads leave), unpack 72 (5.6), gate 111 (6.1).  Rows of 4095: 100, 98 and 120 us, bound by the
 // instructions that shift the values; one by one at the widest access that each address allows they took 121, 143 and 186.
 #pragma once
 #include <cuda_bf16.h>
@@ -24,8 +24,8 @@ constexpr int ACT_ROWS = 32;           // rows that a CTA of 256 threads takes a
 // Rows of bf16 may start at any even address (an odd number of columns, a view).  Where all start at multiples of 16 bytes (ALIGNED),
 // a thread's eight values are one access.  Otherwise a kernel that writes bf16 gives a thread the eight columns that one aligned access
 // covers in its row (unpacking 32768 x 4092: 98 us; 106 with two accesses of 8 bytes).  What is read at another alignment comes in
-// accesses of 8 or 4 bytes where all rows allow them (A = 8, 4: packing 32768 x 4092 81 us, x 4094 81), else (A = 2) as two aligned
-// accesses of 16, the second of which the neighbour reads too, shifted into place (98 us; A = 2 for x 4092: 101).  A row's first
+// accesses of 8 or 4 bytes where all rows allow them (A = 8, 4: packing 32768 x 4092 79 us, x 4094 85), else (A = 2) as two aligned
+// accesses of 16, the second of which the neighbour reads too, shifted into place (100 us; A = 2 for x 4092: 101).  A row's first
 // and last values go one by one there, so that nothing outside the row is touched.
 struct Raw8 {
     uint4 a, b;

@@ -35,9 +35,9 @@
 // pair, and join_parts adds the parts of a tile up in a fixed order.  5.2 waves of tiles take 5.2 and not 6 times a tile.
 // Every wait is bounded, as in cocod_gemm_sm100.cuh.
 //
-// What bounds it.  Large products: the GPU's power limit.  8192 x 65536 x 2048 back to back runs at 1.45 GHz and takes 1752 us
-// forward (1255 TFLOP/s), 1820 as an input gradient, 1768 as a weight gradient; all zeros, which switch less, run a fifth
-// faster.  A block of 64 takes a pair 589 clocks, its products 506.  Small ones: the launch, the pipeline's filling and the
+// What bounds it.  Large products: the GPU's power limit.  8192 x 65536 x 2048 back to back takes 1650 us forward (1333 TFLOP/s; SM clock 1387
+// MHz in the median, 993 W, the power cap active in every sample; cuBLAS in the same process 1644), 1803 as an input gradient, 1702 as a
+// weight gradient.  All zeros, which switch less, take 1170 us at 1935 MHz: the same number of clocks.  Small ones: the launch, the pipeline's filling and the
 // last wave (24 rows in 4 groups, 512 x 512: 6.8 us, of which 3.5 are a kernel without tiles).  Few rows with much to write: DRAM (16 workers
 // of 16 to 128 rows, a 16777216-value gradient each: 125 us, 4.3 TB/s of writes).
 #pragma once
