@@ -411,8 +411,12 @@ int cocod_lm_create(cocod_lm_handle **out)
     cudaError_t e = cudaMalloc((void **)&h->order, COCOD_LM_MAX_GROUPS * sizeof(int));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->parts, (size_t)(sm_count() / 2 + 1) * 256 * 256 * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->flag, 256);
-    if (e == cudaSuccess) e = cudaMemset(h->flag, 0, 256);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);      // (calls come on any stream, and memset need not have ended)
+    // (calls come on any stream: the zeros have to be there, and need not wait for other work)
+    cudaStream_t s = nullptr;
+    if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaMemsetAsync(h->flag, 0, 256, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (s) cudaStreamDestroy(s);
     if (e != cudaSuccess) {
         cudaGetLastError();
         lm_free(h);
