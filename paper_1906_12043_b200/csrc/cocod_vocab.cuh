@@ -11,7 +11,8 @@
 // softmax - onehot is as a rule its label's, so its rounding is made good.  In dw by the factor that goes into h, rho_r S_r / bf16(S_r): the
 // label's term carries one rounding (of rho h) and not two.  In dh by what the rounding left out, times the label's row of w, which
 // the product's epilogue adds in fp32 (37 rows of 256 over 8191 entries: error against 64 bits 0.0024 -> 0.0016, a bf16 result's own).
-// When loss_r > 50, exp(l - c_r) could leave bf16's range or rho_r fp32's: such a row is done again relative to its largest logit.
+// When loss_r > 50, exp(l - c_r) could leave bf16's range or rho_r fp32's, and with a small a_r (1e-25, loss 45) rho_r is gone earlier: such a
+// row is done again relative to its largest logit.
 #pragma once
 #include "cocod_grouped_sm100.cuh"
 
@@ -20,6 +21,7 @@ namespace lm {
 
 constexpr int FINISH_ROWS = 32, FINISH_WARPS = 16;
 constexpr float SUM_LIMIT = 5.0e21f;         // about exp(50)
+constexpr float RHO_LIMIT = 1.0e-30f;        // a smaller factor of a large sum is left to the second pass: it would near the end of fp32
 
 struct VocabRows {
     const int *offsets;                // [groups + 1]
@@ -227,13 +229,13 @@ vocab_finish(const FinishParams p)
                 }
                 const float et = own == ref ? 1.0f : expf(own - ref);
                 loss = own == ref ? log1pf(s) : logf(s + et) + (ref - own);
-                if (!p.second && !(s <= SUM_LIMIT)) {
+                if (p.rho != nullptr) rho = share / (s + et);
+                if (!p.second && (!(s <= SUM_LIMIT) || (s > 1.0f && p.rho != nullptr && fabsf(rho) < RHO_LIMIT))) {
                     again = 1;
                     p.v.ref[r] = most;
                     *p.v.redo_any = 1;
                 }
                 if (p.rho != nullptr) {
-                    rho = share / (s + et);
                     const __nv_bfloat16 entry = __float2bfloat16_rn(-s);
                     const float kept = -__bfloat162float(entry);
                     p.u[row * p.ldu + t] = entry;

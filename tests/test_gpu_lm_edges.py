@@ -298,3 +298,30 @@ def test_results_on_top_of_operands_are_refused(ops):
     want = ops.act_relu_grad(x, ops.act_pack(two[:64]))
     assert torch.equal(ops.act_relu_grad(x, ops.act_pack(two[:64]), out=x.view(64, 64)), want)
     ops.check()
+
+
+@pytest.mark.parametrize("weight", [1e-25, -3e-20, 1e-3])
+def test_small_weights_of_rows_with_large_losses(ops, weight):
+    """Losses of 30 to 49, for which exp(loss) alone takes up half of fp32's range: dx and dw keep their size.  A term of dx is off by one bf16
+    rounding and twice a logit's error d (each of D / 16 + 8 steps cuts off at most 2^-23 of |h| |w|), of dw by three; the result by one more,
+    which is up to half of 2^-133, bf16's least unit, for results below 2^-126."""
+    M, V, D = 40, 500, 64
+    off, _ = offsets_of([M])
+    h, w = gaussian(1, M, D), gaussian(2, 1, V, D, scale=D ** -0.5)
+    labels = torch.randint(0, V - 1, (M,), generator=torch.Generator().manual_seed(3)).int().cuda()
+    h = (h.float() * torch.linspace(28, 44, M, device="cuda")[:, None] / (h.float() @ w[0, -1].float())[:, None]).bfloat16()
+    weights = torch.full((M,), weight, device="cuda")
+    for dtype in (torch.bfloat16, torch.float32):
+        loss, row, dx, dw = ops.vocab_loss_grad(h, w, labels, off, row_weights=weights, dw_dtype=dtype)
+        l = h.double() @ w[0].double().T
+        want = torch.logsumexp(l, 1) - l.gather(1, labels.long()[:, None])[:, 0]
+        assert float(want.max()) > 40
+        d = (D / 16 + 8) * 2.0 ** -23 * float(h.float().norm(dim=1).max() * w.float().norm(dim=2).max())
+        assert ((row.double() - want).abs() <= 2 * d + 2.0 ** -20 * (1 + want)).all()
+        p = torch.softmax(l, 1)
+        p[torch.arange(M, device="cuda"), labels.long()] -= 1
+        p *= weights.double()[:, None]
+        more = 2 * d + (V / 16 + 40) * 2.0 ** -23
+        for got, to, size, terms in ((dx, p @ w[0].double(), p.abs() @ w[0].double().abs(), 1), (dw[0], p.T @ h.double(), p.abs().T @ h.double().abs(), 3)):
+            assert ((got.double() - to).abs() <= (terms * 2.0 ** -8 * 1.02 + more) * size + 2.0 ** -8 * to.abs() + 2.0 ** -134).all()
+    ops.check()
