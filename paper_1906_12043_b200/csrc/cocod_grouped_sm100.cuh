@@ -11,7 +11,7 @@
 //     cores that need 512 clocks for the block.  Problems with few tiles use 128 x 128 tiles and single CTAs (CG = 1): twice
 //     the bytes for a product, but more SMs take part.
 //   * Two accumulators in tensor memory: the epilogue of a tile runs under the products of the next.
-//   * Warps: 0 producer (TMA), 1 issuer of tcgen05.mma (leading CTA of the pair only), 2 tensor memory, 3 scheduler, 4..11 epilogue.
+//   * Warps: 0 producer (TMA), 1 issuer of tcgen05.mma (leading CTA of the pair only), 2 tensor memory and groups' last blocks, 3 scheduler, 4..11 epilogue.
 //     The scheduler reads the tile list (Walker) some tiles ahead and leaves them in shared memory; when every role found
 //     its tiles itself, the producer's pause for it emptied the ring: 3000 clocks a tile.
 //   * An epilogue warp owns 32 rows of its CTA's tile and half of the columns, stages them in shared memory of its own

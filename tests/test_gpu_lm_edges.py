@@ -255,7 +255,7 @@ def test_gradient_of_the_weights_beyond_32_bits(lm):
 
 # ------------------------------------------------------------------------------------------------------- refusals
 def test_a_call_while_another_device_is_current_is_refused_by_name(lm):
-    """(As if the operators had been made on the next device: the box of these tests may have one.)"""
+    """(As if the operators had been made on the next device, which need not exist.)"""
     o = lm.LMOps()
     here, other = torch.cuda.current_device(), torch.cuda.current_device() + 1
     x, w, off = gaussian(1, 64, 64), gaussian(2, 1, 64, 64), torch.tensor([0, 64], dtype=torch.int32, device="cuda")
