@@ -120,7 +120,7 @@ int64_t cocod_grouped_packed_workspace(int G, int64_t M, int64_t n, int64_t k);
  * these passes in fp32.  cocod_vocab_workspace: the bytes for one pass over all rows, or, if that is more than `limit`,
  * for the most rows that stay within it (more than `limit` if not even the fewest do); less: COCOD_ERR_TOO_LARGE.
  * Precision: the exponentials and a_r x / sum are rounded to bf16 as operands of the gradients' products (a term of dx carries a
- * relative error of up to 2^-8, a term of dw up to 3 * 2^-8, also where dw is fp32); the losses are formed in fp32. */
+ * relative error of up to 2^-8, the label's none; a term of dw up to 3 * 2^-8, also where dw is fp32); the losses are formed in fp32. */
 int64_t cocod_vocab_workspace(int G, int64_t M, int64_t V, int64_t D, int with_grad, int dw_type, int64_t limit);
 int cocod_vocab_loss(cocod_lm_handle *h, int G, const int32_t *offsets, int64_t M, int64_t V, int64_t D, const void *x, int64_t ldx,
                      const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, float *loss,
