@@ -7,6 +7,8 @@
  *     cocod_grouped_*   products of rows with their own group's weights, forward and backward
  *     cocod_act_*       activations kept from the forward pass in 8 bits, and their use in the backward pass
  *     cocod_vocab_*     softmax cross-entropy over a large vocabulary, and its gradient
+ *     cocod_expert_*    tokens sorted by expert, the rows of the products, and back, with the gradients
+ *     cocod_token_*     log probabilities of given tokens, entropy, top alternatives (a router's choice among them), and the gradient
  *
  * Groups.  The rows of all groups (workers, whose mini-batches M_i may differ in size, Section 3.2; or experts) lie one
  * behind the other in one matrix: row m belongs to group g when offsets[g] <= m < offsets[g + 1].  offsets: device,
@@ -51,7 +53,8 @@ int cocod_lm_create(cocod_lm_handle **out);
 int cocod_lm_destroy(cocod_lm_handle *h);
 
 /* Synchronise `stream` and report what the kernels of this handle met since the last check: COCOD_ERR_TIMEOUT (a kernel
- * gave up a wait), COCOD_ERR_INVALID (offsets that do not rise from 0 to M, or a label beyond the vocabulary), COCOD_OK. */
+ * gave up a wait), COCOD_ERR_INVALID (offsets that do not rise from 0 to M, a label beyond the vocabulary, an expert beyond their
+ * count, or a place beyond the rows), COCOD_OK. */
 int cocod_lm_check(cocod_lm_handle *h, cocod_stream_t stream);
 
 /* Number of kernels launched by this handle so far. */
@@ -129,6 +132,55 @@ int cocod_vocab_loss_grad(cocod_lm_handle *h, int G, const int32_t *offsets, int
                           const void *w, int64_t ldw, int64_t w_stride, const int32_t *labels, const float *row_weights, float *loss,
                           float *row_loss, void *dx, int64_t lddx, void *dw, int64_t lddw, int64_t dw_stride, int dw_type,
                           void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Tokens sorted by expert and back.  Token t has k slots s = t k + j, slot s goes to expert experts[t][j]; N = T k.
+ *
+ * expert_sort      the slots in the order of their experts (stable: of one expert, in their own order).  order[r]: the slot of row r;
+ *                  place[s]: the row of slot s; counts[e]: the slots of expert e; offsets: E + 1 values, as the products by group take them.
+ *   A negative number is a slot that takes no part; one >= E too, and the next cocod_lm_check reports it.  Such slots' rows lie behind the last
+ *   expert's and count as its own in the offsets, which so rise from 0 to N always (counts[E - 1] leaves them out); place[s] is the
+ *   bitwise complement of the row there.
+ * expert_rows      rows[place[s]] = x[s / k]; zeros in the rows of slots that take no part
+ * expert_join      y[t] = sum_j weights[t][j] rows[place[t][j]] over the slots that take part, in fp32 in the order of j; weights NULL: the sum
+ *                  alone, which is the gradient of expert_rows
+ * expert_join_grad drows[place[s]] = weights[s] dy[s / k] (zeros in rows of slots that take no part), dweights[s] = <dy[s / k], rows[place[s]]>
+ *                  (0 there); a result may not lie on an operand
+ *   experts: T x k int32, row stride ld; order, place, weights, dweights: N values; k <= 32, E <= COCOD_LM_MAX_GROUPS, N < 2^31 - 1024
+ *   x, y, dy: T x D; rows, drows: N x D; type: COCOD_BF16 or COCOD_F32, any D, row stride and alignment (rows that start at multiples of 16 bytes
+ *   and hold a multiple of them are faster).  Rows that no place names are not written.  A place beyond the rows is
+ *   reported by cocod_lm_check and left out.
+ * workspace: cocod_expert_workspace bytes (4-byte aligned; may be 0); less: COCOD_ERR_TOO_LARGE. */
+#define COCOD_LM_MAX_CHOICES 32
+int64_t cocod_expert_workspace(int64_t T, int k, int E);
+int cocod_expert_sort(cocod_lm_handle *h, int64_t T, int k, int E, const int32_t *experts, int64_t ld, int32_t *offsets, int32_t *counts, int32_t *order,
+                      int32_t *place, void *workspace, int64_t workspace_bytes, cocod_stream_t stream);
+int cocod_expert_rows(cocod_lm_handle *h, int64_t T, int k, int64_t D, const void *x, int64_t ldx, const int32_t *place, void *rows, int64_t ld, int type,
+                      cocod_stream_t stream);
+int cocod_expert_join(cocod_lm_handle *h, int64_t T, int k, int64_t D, const void *rows, int64_t ld, int type, const int32_t *place, const float *weights, void *y,
+                      int64_t ldy, int out_type, cocod_stream_t stream);
+int cocod_expert_join_grad(cocod_lm_handle *h, int64_t T, int k, int64_t D, const void *dy, int64_t lddy, const void *rows, int64_t ld, const int32_t *place,
+                           const float *weights, void *drows, int64_t ld_drows, float *dweights, int type, cocod_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Log probabilities of given tokens.  logits: M x V (type COCOD_BF16 or COCOD_F32, any row stride and alignment); y = scale * logits, scale > 0;
+ *     log_sum[r] = log sum_v exp y[r][v],   log p = y - log_sum,   logp[r] = log p[r][tokens[r]],
+ *     entropy[r] = - sum_v p log p,   top_tokens[r][j]: the token with the j-th largest logit (of equal ones the lower first), top_logp: its log p.
+ * tokens: M int32, or NULL: no tokens, logp is not written.  A row whose token is negative takes no part whatever it holds: its results are 0, its
+ * top_tokens -1; so does one whose token is >= V, which the next cocod_lm_check reports.  top: 0 .. 32, at most V.
+ * A logit of -inf has probability 0.  A row of nothing else: log_sum and every log p are -inf, entropy and gradient 0.  A row with a NaN or
+ * +inf: NaN for logp, entropy, log_sum and top_logp; top_tokens orders NaN before all others.
+ *
+ * token_logprobs_grad   dlogits = scale * (given - p * (sum of given + d_entropy * (log p + entropy))), with `given` the sum of d_logp at the row's token
+ *   and d_top at its top_tokens (a repeated or negative one is allowed: added up, left out).  log_sum and entropy are those of the forward call.
+ *   d_logp, d_entropy, d_top: NULL where there are none (entropy is read only with d_entropy; top_tokens and d_top are M x top).  dlogits:
+ *   M x V of the logits' type; may be the logits themselves (same address and stride). */
+#define COCOD_LM_MAX_TOP 32
+int cocod_token_logprobs(cocod_lm_handle *h, int64_t M, int64_t V, const void *logits, int64_t ld, int type, const int32_t *tokens, float scale, int top,
+                         float *logp, float *entropy, float *log_sum, float *top_logp, int32_t *top_tokens, cocod_stream_t stream);
+int cocod_token_logprobs_grad(cocod_lm_handle *h, int64_t M, int64_t V, const void *logits, int64_t ld, int type, const int32_t *tokens, float scale, int top,
+                              const int32_t *top_tokens, const float *log_sum, const float *entropy, const float *d_logp, const float *d_entropy,
+                              const float *d_top, void *dlogits, int64_t ld_dlogits, cocod_stream_t stream);
 
 /* Self-test of the bounded waits of the product kernels: one launch (pairs of thread blocks when `pair` is not 0) whose
  * copies are never issued.  Every wait ends after at most 1.5 * wait_ms (1 .. 2000), COCOD_ERR_TIMEOUT is returned and the

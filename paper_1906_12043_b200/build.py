@@ -18,7 +18,7 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 TARGETS = {
-    "libcocod.so": ["cocod_engine.cu", "cocod_mlp.cu", "cocod_lm.cu"],
+    "libcocod.so": ["cocod_engine.cu", "cocod_mlp.cu", "cocod_lm.cu", "cocod_lm_rows.cu"],
     "libcocod_inputs.so": ["inputs_gen.cu"],
 }
 

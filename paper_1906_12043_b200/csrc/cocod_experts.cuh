@@ -1,0 +1,400 @@
+// Tokens sorted by expert and back: the rows that the products by group take, made from tokens and the experts chosen for them.
+//
+// Slot s = t k + j is the j-th choice of token t.  A stable counting sort puts the slots in the order of their experts; row r of the
+// sorted matrix belongs to slot order[r], and place[s] is the row of slot s, or its bitwise complement where the slot takes no
+// part.  Everything after the sort goes by token: a token's row is read once and written k times on the way there, its k
+// rows are read and summed in registers, in the order of the choices, on the way back.  No atomics on results: the same bits every time.
+//
+// What bounds them: the sort its launches, the others HBM (each row of either side is touched once).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cocod_grouped_sm100.cuh"
+
+namespace cocod {
+namespace lm {
+
+constexpr int ERR_EXPERT = 102;              // error_flag: an expert's number beyond their count
+constexpr int ERR_PLACE = 103;               // error_flag: a place beyond the rows
+
+// ------------------------------------------------------------------------------------------ the sort
+constexpr int SORT_WARPS = 16, SORT_THREADS = 32 * SORT_WARPS;
+
+struct ExpertSlots {
+    const int *experts;
+    long long ld;                            // row stride
+    int top, total, experts_n;               // slots of a token, all slots, experts
+    int *error_flag;
+};
+// The bucket of slot s: its expert, or the one behind the last for slots that take no part.
+__device__ __forceinline__ int bucket_of(const ExpertSlots &p, int s, bool tell)
+{
+    const long long at = p.ld == p.top ? (long long)s : (long long)(s / p.top) * p.ld + s % p.top;
+    int e = p.experts[at];
+    if (e >= p.experts_n && tell) atomicExch(p.error_flag, ERR_EXPERT);
+    return e < 0 || e >= p.experts_n ? p.experts_n : e;
+}
+
+// Thread block b counts slots b * span .. of each bucket into counts[b].
+static __global__ void __launch_bounds__(SORT_THREADS)
+expert_count(const ExpertSlots p, int span, int *counts)
+{
+    extern __shared__ int sums[];
+    pdl_launch_dependents();
+    const int buckets = p.experts_n + 1;
+    for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) sums[e] = 0;
+    pdl_wait();
+    __syncthreads();
+    const long long from = (long long)blockIdx.x * span, to = min(from + span, (long long)p.total);
+    for (long long s = from + threadIdx.x; s < to; s += SORT_THREADS) atomicAdd(&sums[bucket_of(p, (int)s, false)], 1);
+    __syncthreads();
+    for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) counts[(long long)blockIdx.x * buckets + e] = sums[e];
+}
+
+// Thread block b puts its slots into place.  A warp takes a stretch of them, 32 at a time; those of one bucket find each other
+// (match), so that a slot's row is: the bucket's first row + what blocks, warps and tiles before hold of the bucket + how many lanes
+// before it.  counts: of all blocks (expert_count), not looked at where there is only one block.
+static __global__ void __launch_bounds__(SORT_THREADS)
+expert_place(const ExpertSlots p, int span, const int *counts, int *offsets, int *per_expert, int *order, int *place)
+{
+    extern __shared__ int shared[];
+    pdl_launch_dependents();
+    const int buckets = p.experts_n + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int *mine = shared + warp * buckets, *all = shared + SORT_WARPS * buckets, *before = all + buckets;
+    for (int i = threadIdx.x; i < (SORT_WARPS + 2) * buckets; i += SORT_THREADS) shared[i] = 0;
+    pdl_wait();
+    __syncthreads();
+    const int stretch = span / SORT_WARPS;
+    const long long from = (long long)blockIdx.x * span + (long long)warp * stretch, to = min(from + stretch, (long long)p.total);
+    constexpr int AT_ONCE = 4;
+    for (long long s0 = from; s0 < to; s0 += 32 * AT_ONCE) {
+        int e[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) e[u] = s0 + 32 * u + lane < to ? bucket_of(p, (int)(s0 + 32 * u + lane), true) : -1;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const unsigned peers = __match_any_sync(~0u, e[u]);
+            if (e[u] >= 0 && lane == __ffs(peers) - 1) mine[e[u]] += __popc(peers);
+            __syncwarp();
+        }
+    }
+    if (gridDim.x > 1) {                     // (all threads add up the blocks' counts)
+        const int parts = max(1, SORT_THREADS / buckets), blocks = gridDim.x;
+        for (int i = threadIdx.x; i < parts * buckets; i += SORT_THREADS) {
+            const int e = i % buckets, part = i / buckets;
+            int sum = 0, early = 0;
+#pragma unroll 4
+            for (int b = part; b < blocks; b += parts) {
+                const int c = counts[(long long)b * buckets + e];
+                sum += c;
+                if (b < (int)blockIdx.x) early += c;
+            }
+            atomicAdd(&all[e], sum);
+            atomicAdd(&before[e], early);
+        }
+    }
+    __syncthreads();
+    if (gridDim.x == 1) {
+        for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) {
+            int sum = 0;
+            for (int w = 0; w < SORT_WARPS; ++w) sum += shared[w * buckets + e];
+            all[e] = sum;
+        }
+        __syncthreads();
+    }
+    if (warp == 0) {                         // the buckets' first rows
+        int carry = 0;
+        for (int e0 = 0; e0 < buckets; e0 += 32) {
+            const int e = e0 + lane, n = e < buckets ? all[e] : 0;
+            int sum = n;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int o = __shfl_up_sync(~0u, sum, d);
+                if (lane >= d) sum += o;
+            }
+            const int first = carry + sum - n;
+            if (e < buckets) before[e] += first;
+            if (blockIdx.x == 0 && e < p.experts_n) {
+                offsets[e] = first;
+                per_expert[e] = n;
+            }
+            carry += __shfl_sync(~0u, sum, 31);
+        }
+        if (blockIdx.x == 0 && lane == 0) offsets[p.experts_n] = p.total;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) {
+        int at = before[e];
+        for (int w = 0; w < SORT_WARPS; ++w) {
+            const int n = shared[w * buckets + e];
+            shared[w * buckets + e] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    for (long long s0 = from; s0 < to; s0 += 32 * AT_ONCE) {
+        int e[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) e[u] = s0 + 32 * u + lane < to ? bucket_of(p, (int)(s0 + 32 * u + lane), false) : -1;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const unsigned peers = __match_any_sync(~0u, e[u]);
+            const int s = (int)(s0 + 32 * u + lane);
+            const int row = e[u] >= 0 ? mine[e[u]] + __popc(peers & ((1u << lane) - 1)) : 0;
+            __syncwarp();
+            if (e[u] >= 0 && row < p.total) {        // (always, unless the numbers change while they are sorted)
+                if (lane == __ffs(peers) - 1) mine[e[u]] += __popc(peers);
+                order[row] = s;
+                place[s] = e[u] < p.experts_n ? row : ~row;
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ rows
+// A piece is what a thread moves at once: 16 bytes where all rows start at multiples of 16 and hold a whole number of them, else one value.
+template <typename T, bool WIDE> struct Piece;
+template <typename T> struct Piece<T, true> {
+    static constexpr int N = 16 / sizeof(T);
+    uint4 raw;
+};
+template <typename T> struct Piece<T, false> {
+    static constexpr int N = 1;
+    T raw;
+};
+template <typename T, bool WIDE>
+__device__ __forceinline__ Piece<T, WIDE> load_piece(const T *p)
+{
+    Piece<T, WIDE> r;
+    r.raw = *reinterpret_cast<const decltype(r.raw) *>(p);
+    return r;
+}
+template <typename T, bool WIDE>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, WIDE> &r) { *reinterpret_cast<decltype(r.raw) *>(p) = r.raw; }
+template <typename T, bool WIDE>
+__device__ __forceinline__ Piece<T, WIDE> zero_piece()
+{
+    Piece<T, WIDE> r;
+    memset(&r, 0, sizeof(r));
+    return r;
+}
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T, bool WIDE>
+__device__ __forceinline__ void widen(const Piece<T, WIDE> &r, float (&x)[Piece<T, WIDE>::N])
+{
+    if constexpr (!WIDE) {
+        x[0] = as_float(r.raw);
+    } else if constexpr (sizeof(T) == 4) {
+        x[0] = __uint_as_float(r.raw.x); x[1] = __uint_as_float(r.raw.y); x[2] = __uint_as_float(r.raw.z); x[3] = __uint_as_float(r.raw.w);
+    } else {
+        const uint32_t w[4] = {r.raw.x, r.raw.y, r.raw.z, r.raw.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+}
+// N values of fp32, rounded to T, to p (a multiple of N values' size where N > 1).
+template <typename T, int N>
+__device__ __forceinline__ void store_values(T *p, const float (&x)[N])
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (N == 1) *p = x[0];
+        else
+#pragma unroll
+            for (int i = 0; i < N; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    } else {
+        if constexpr (N == 1) *p = __float2bfloat16_rn(x[0]);
+        else if constexpr (N == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        else
+            *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    }
+}
+
+constexpr int MAX_CHOICES = 32;              // of a token: a lane holds the place of each
+
+struct ExpertRows {
+    const int *place;                        // T x top, contiguous
+    int tokens, top, rows;                   // rows = T * top
+    int pieces;                              // of a row
+    int *error_flag;
+};
+// Lane j's place, checked: whatever the tensor holds, nothing outside the rows is touched (row -1: nothing).
+struct Slot {
+    int row;
+    bool there;
+};
+__device__ __forceinline__ Slot slot_of(const ExpertRows &p, int token, int lane)
+{
+    Slot s{-1, false};
+    if (lane < p.top) {
+        const int at = p.place[(long long)token * p.top + lane];
+        s.there = at >= 0;
+        s.row = at >= 0 ? at : ~at;
+        if (s.row >= p.rows) {
+            atomicExch(p.error_flag, ERR_PLACE);
+            s = Slot{-1, false};
+        }
+    }
+    return s;
+}
+
+// A warp takes ROW_PIECES x 32 pieces of a token's row and writes them to its k rows (zeros for a slot that takes no part).
+constexpr int ROW_PIECES = 4;
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256)
+expert_rows(const ExpertRows p, const T *x, long long ldx, T *out, long long ld_out)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int N = Piece<T, WIDE>::N;
+    const int lane = threadIdx.x & 31, parts = (p.pieces + 32 * ROW_PIECES - 1) / (32 * ROW_PIECES);
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int token = (int)min(unit / parts, (long long)p.tokens);
+    if (token >= p.tokens) return;
+    const int first = (int)(unit - (long long)token * parts) * 32 * ROW_PIECES + lane;
+    const Slot s = slot_of(p, token, lane);
+    const T *row = x + (long long)token * ldx;
+    Piece<T, WIDE> v[ROW_PIECES];
+#pragma unroll
+    for (int i = 0; i < ROW_PIECES; ++i)
+        if (first + 32 * i < p.pieces) v[i] = load_piece<T, WIDE>(row + (long long)(first + 32 * i) * N);
+    for (int j = 0; j < p.top; ++j) {
+        const int r = __shfl_sync(~0u, s.row, j);
+        const bool there = __shfl_sync(~0u, (int)s.there, j);
+        if (r < 0) continue;
+        T *to = out + (long long)r * ld_out;
+#pragma unroll
+        for (int i = 0; i < ROW_PIECES; ++i)
+            if (first + 32 * i < p.pieces) store_piece<T, WIDE>(to + (long long)(first + 32 * i) * N, there ? v[i] : zero_piece<T, WIDE>());
+    }
+}
+
+// The way back: y[t] = sum_j w[t][j] rows[place[t][j]] (weights == nullptr: the plain sum), fp32 in the order of j.  A warp takes
+// JOIN_PIECES x 32 pieces; four rows' pieces are under way together.
+constexpr int JOIN_PIECES = 2;
+template <typename T, typename O, bool WIDE>
+__global__ void __launch_bounds__(256)
+expert_join(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int N = Piece<T, WIDE>::N;
+    const int lane = threadIdx.x & 31, parts = (p.pieces + 32 * JOIN_PIECES - 1) / (32 * JOIN_PIECES);
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int token = (int)min(unit / parts, (long long)p.tokens);
+    if (token >= p.tokens) return;
+    const int first = (int)(unit - (long long)token * parts) * 32 * JOIN_PIECES + lane;
+    const Slot s = slot_of(p, token, lane);
+    const float w = weights != nullptr && lane < p.top ? weights[(long long)token * p.top + lane] : 1.0f;
+    float sum[JOIN_PIECES][N];
+#pragma unroll
+    for (int i = 0; i < JOIN_PIECES; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[i][e] = 0.0f;
+    for (int j0 = 0; j0 < p.top; j0 += 4) {
+        Piece<T, WIDE> v[4][JOIN_PIECES];
+        bool there[4];
+        float f[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = min(j0 + u, 31), r = __shfl_sync(~0u, s.row, j);
+            there[u] = __shfl_sync(~0u, (int)s.there, j) && j0 + u < p.top;
+            f[u] = __shfl_sync(~0u, w, j);
+#pragma unroll
+            for (int i = 0; i < JOIN_PIECES; ++i)
+                if (there[u] && first + 32 * i < p.pieces) v[u][i] = load_piece<T, WIDE>(rows + (long long)r * ld + (long long)(first + 32 * i) * N);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (!there[u]) continue;
+#pragma unroll
+            for (int i = 0; i < JOIN_PIECES; ++i) {
+                float a[N];
+                widen<T, WIDE>(v[u][i], a);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[i][e] = fmaf(f[u], a[e], sum[i][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < JOIN_PIECES; ++i)
+        if (first + 32 * i < p.pieces) store_values<O, N>(y + (long long)token * ldy + (long long)(first + 32 * i) * N, sum[i]);
+}
+
+// The gradient of that: back[place[t][j]] = w[t][j] dy[t] (0 where the slot takes no part), dw[t][j] = <dy[t], rows[place[t][j]]>.
+// WARPS warps take a token; each sum runs over a thread's pieces, the lanes and the warps, always in the same order.
+template <typename T, bool WIDE, int WARPS>
+__global__ void __launch_bounds__(256)
+expert_join_grad(const ExpertRows p, const T *dy, long long lddy, const T *rows, long long ld, const float *weights, T *back, long long ld_back, float *dw)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int N = Piece<T, WIDE>::N;
+    __shared__ float part[8][MAX_CHOICES];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, of = warp % WARPS;
+    const int token = blockIdx.x * (8 / WARPS) + warp / WARPS;
+    if (token < p.tokens) {
+        const Slot s = slot_of(p, token, lane);
+        const float w = lane < p.top ? weights[(long long)token * p.top + lane] : 0.0f;
+        const T *d_row = dy + (long long)token * lddy;
+        for (int j0 = 0; j0 < p.top; j0 += 4) {
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, f[4];
+            int r[4];
+            bool there[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = min(j0 + u, 31);
+                r[u] = __shfl_sync(~0u, s.row, j);
+                if (j0 + u >= p.top) r[u] = -1;
+                there[u] = __shfl_sync(~0u, (int)s.there, j);
+                f[u] = __shfl_sync(~0u, w, j);
+            }
+            for (int c = of * 32 + lane; c < p.pieces; c += 32 * WARPS) {
+                const long long at = (long long)c * N;
+                const Piece<T, WIDE> d = load_piece<T, WIDE>(d_row + at);
+                Piece<T, WIDE> v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (r[u] >= 0 && there[u]) v[u] = load_piece<T, WIDE>(rows + (long long)r[u] * ld + at);
+                float g[N];
+                widen<T, WIDE>(d, g);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (r[u] < 0) continue;
+                    float out[N];
+                    if (there[u]) {
+                        float a[N];
+                        widen<T, WIDE>(v[u], a);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) sum[u] = fmaf(g[e], a[e], sum[u]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < N; ++e) out[e] = there[u] ? f[u] * g[e] : 0.0f;
+                    store_values<T, N>(back + (long long)r[u] * ld_back + at, out);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                for (int d = 16; d > 0; d /= 2) sum[u] += __shfl_xor_sync(~0u, sum[u], d);
+                if (lane == 0 && j0 + u < p.top) part[warp][j0 + u] = sum[u];
+            }
+        }
+    }
+    __syncthreads();
+    if (token < p.tokens && of == 0 && lane < p.top) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) sum += part[warp + i][lane];
+        dw[(long long)token * p.top + lane] = sum;
+    }
+}
+
+}  // namespace lm
+}  // namespace cocod

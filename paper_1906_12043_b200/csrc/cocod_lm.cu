@@ -4,41 +4,18 @@
 #include "cocod_act8.cuh"
 #include "cocod_grouped_sm100.cuh"
 #include "cocod_vocab.cuh"
-#include "cocod_host.h"
+#include "cocod_lm_internal.h"
 
 #include <algorithm>
 #include <cmath>
 #include <new>
 #include <utility>
 
-struct cocod_lm {
-    int *order = nullptr;                  // device: the groups by size
-    float *parts = nullptr;                // device: parts of tiles, 256 x 256 for each pair of CTAs
-    int *flag = nullptr;                   // device: what the kernels met
-    int device = -1;                       // the one current at creation
-    long long launches = 0;
-};
-
 namespace {
 
 using namespace cocod;
 using namespace cocod::lm;
 using bf16 = __nv_bfloat16;
-
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-int sm_count()
-{
-    static int count[MAX_DEVICES] = {};
-    const int dev = current_device();
-    if (dev < 0) return 0;
-    if (count[dev] == 0 && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-        cudaGetLastError();
-        count[dev] = 0;
-    }
-    return count[dev];
-}
 
 // A row-major matrix, or one per group.
 struct Matrix {
@@ -93,8 +70,6 @@ round_sums(const float *sums, bf16 *out, long long ld, long long group_stride, l
 }
 
 // ------------------------------------------------------------------------------------------ launching the products
-#define TRY_CUDA(call) do { if ((call) != cudaSuccess) { cudaGetLastError(); return COCOD_ERR_CUDA; } ++h->launches; } while (0)
-
 enum Form { FORWARD, INPUT_GRAD, WEIGHT_GRAD };
 
 // How a product is cut into tiles and parts.
@@ -374,7 +349,6 @@ int run_vocab(cocod_lm *h, int G, const int32_t *offsets, int64_t M, int64_t V, 
 }
 
 // ------------------------------------------------------------------------------------------ checks of arguments
-constexpr int64_t MAX_DIM = (1ll << 31) - 1024;
 bool good_rows(const void *p, int64_t ld, int64_t cols, int64_t M, int elem)
 {
     return (M == 0 || p != nullptr) && aligned16(p) && ld >= cols && (ld * elem) % 16 == 0 && ld < (1ll << 36);
@@ -395,7 +369,6 @@ void lm_free(cocod_lm *h)
     for (void *p : ptrs) if (p) cudaFree(p);
     delete h;
 }
-inline int size_of(int type) { return type == COCOD_BF16 ? 2 : type == COCOD_F32 ? 4 : 0; }
 
 }  // namespace
 
@@ -446,7 +419,7 @@ int cocod_lm_check(cocod_lm_handle *h, cocod_stream_t stream)
         return COCOD_ERR_CUDA;
     if (f == 0) return COCOD_OK;
     if (cudaMemsetAsync(h->flag, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return COCOD_ERR_CUDA;
-    return f == ERR_OFFSETS || f == ERR_LABEL ? COCOD_ERR_INVALID : COCOD_ERR_TIMEOUT;
+    return f >= ERR_OFFSETS && f < 200 ? COCOD_ERR_INVALID : COCOD_ERR_TIMEOUT;
 }
 
 int64_t cocod_lm_launch_count(const cocod_lm_handle *h) { return h ? h->launches : -1; }

@@ -311,6 +311,187 @@ template <bool GRAD> PyObject *vocab(PyObject *const *a)
                          a[8] == Py_None ? THPVariable_Wrap(dw.t) : given(a[8]));
 }
 
+// ------------------------------------------------------------------------------------------ experts
+// A tensor's type as the library names it: bf16 or fp32.
+at::ScalarType value_type(const Tensor &t, const char *name)
+{
+    const at::ScalarType type = t.scalar_type();
+    if (type != at::kBFloat16 && type != at::kFloat) refuse(name, "bfloat16 or float32", t);
+    return type;
+}
+// T x k values side by side.
+void *table(const Tensor &t, const char *name, int64_t T, int64_t k, at::ScalarType type, int64_t device)
+{
+    if (there(t, type, device) && t.dim() == 2 && t.size(0) == T && t.size(1) == k && t.is_contiguous()) return t.data_ptr();
+    refuse(name, std::to_string(T) + " x " + std::to_string(k) + " contiguous " + c10::toString(type) + place(device), t);
+}
+// A matrix whose rows may start anywhere.  `given` (None: a new one like `like`) or a new one, which has to lie apart from the operands.
+Matrix any_rows(const Tensor &t, const char *name, int64_t M, int64_t cols, at::ScalarType type, int64_t dev)
+{
+    if (there(t, type, dev) && t.dim() == 2 && t.size(0) == M && t.size(1) == cols && (cols <= 1 || t.stride(1) == 1)) {
+        const int64_t ld = M > 1 ? t.stride(0) : cols;
+        if (ld >= cols) return Matrix{t.data_ptr(), ld, 0};
+    }
+    refuse(name, std::to_string(M) + " x " + std::to_string(cols) + " " + c10::toString(type) + place(dev) + ", rows contiguous and not overlapping", t);
+}
+
+// (handle, device, experts, E): (offsets, counts, order, place, all four in one buffer)
+PyObject *expert_sort(PyObject *const *a)
+{
+    cocod_lm_handle *h = handle(a[0]);
+    const int64_t dev = device(a[1]), E = whole(a[3]);
+    const Tensor &e = tensor(a[2], "experts", 2);
+    const int64_t T = e.size(0), k = e.size(1);
+    const Matrix m = any_rows(e, "experts", T, k, at::kInt, dev);
+    if (E < 1 || E > COCOD_LM_MAX_GROUPS || k < 1 || k > COCOD_LM_MAX_CHOICES)
+        throw std::invalid_argument("experts: 1 to " + std::to_string(COCOD_LM_MAX_CHOICES) + " choices among 1 to " + std::to_string(COCOD_LM_MAX_GROUPS) + " experts");
+    const int64_t bytes = cocod_expert_workspace(T, (int)k, (int)E);
+    if (bytes < 0) return PyLong_FromLong((long)bytes);
+    const Tensor all = fresh(e, {2 * E + 1 + 2 * T * k + bytes / 4}, at::kInt);
+    int32_t *p = static_cast<int32_t *>(all.data_ptr());
+    const int64_t N = T * k;
+    const int rc = cocod_expert_sort(h, T, (int)k, (int)E, static_cast<const int32_t *>(m.data), m.ld, p, p + E + 1, p + 2 * E + 1, p + 2 * E + 1 + N,
+                                     p + 2 * E + 1 + 2 * N, bytes, current(dev));
+    if (rc != COCOD_OK) return PyLong_FromLong(rc);
+    const auto part = [&](int64_t from, at::IntArrayRef size, at::IntArrayRef strides) { return THPVariable_Wrap(all.as_strided(size, strides, from)); };
+    return Py_BuildValue("(NNNN)", part(0, {E + 1}, {1}), part(E + 1, {E}, {1}), part(2 * E + 1, {N}, {1}), part(2 * E + 1 + N, {T, k}, {k, 1}));
+}
+
+// (handle, device, x, place, out or None)
+PyObject *expert_rows(PyObject *const *a)
+{
+    cocod_lm_handle *h = handle(a[0]);
+    const int64_t dev = device(a[1]);
+    const Tensor &x = tensor(a[2], "x", 2), &at = tensor(a[3], "place", 2);
+    const int64_t T = x.size(0), D = x.size(1), k = at.size(1);
+    const at::ScalarType type = value_type(x, "x");
+    const Matrix m = any_rows(x, "x", T, D, type, dev);
+    const int32_t *places = static_cast<const int32_t *>(table(at, "place", T, k, at::kInt, dev));
+    const Tensor out = a[4] == Py_None ? fresh(x, {T * k, D}, type) : tensor(a[4], "out", 2);
+    const Matrix mo = any_rows(out, "out", T * k, D, type, dev);
+    if (a[4] != Py_None) apart(out, "out", x, "x");
+    const int rc = cocod_expert_rows(h, T, (int)k, D, m.data, m.ld, places, mo.data, mo.ld, type_code(type), current(dev));
+    return rc == COCOD_OK && a[4] != Py_None ? given(a[4]) : code_or(rc, out);
+}
+
+// (handle, device, rows, place, weights or None, out or None, type)
+PyObject *expert_join(PyObject *const *a)
+{
+    cocod_lm_handle *h = handle(a[0]);
+    const int64_t dev = device(a[1]);
+    const Tensor &x = tensor(a[2], "rows", 2), &at = tensor(a[3], "place", 2);
+    const int64_t T = at.size(0), k = at.size(1), D = x.size(1);
+    const at::ScalarType type = value_type(x, "rows"), out_type = result_type(a[5], whole(a[6]), type);
+    const Matrix m = any_rows(x, "rows", T * k, D, type, dev);
+    const int32_t *places = static_cast<const int32_t *>(table(at, "place", T, k, at::kInt, dev));
+    const float *w = a[4] == Py_None ? nullptr : static_cast<const float *>(table(tensor(a[4], "weights", 2), "weights", T, k, at::kFloat, dev));
+    const Tensor out = a[5] == Py_None ? fresh(x, {T, D}, out_type) : tensor(a[5], "out", 2);
+    const Matrix mo = any_rows(out, "out", T, D, out_type, dev);
+    if (a[5] != Py_None) apart(out, "out", x, "rows");
+    const int rc = cocod_expert_join(h, T, (int)k, D, m.data, m.ld, type_code(type), places, w, mo.data, mo.ld, type_code(out_type), current(dev));
+    return rc == COCOD_OK && a[5] != Py_None ? given(a[5]) : code_or(rc, out);
+}
+
+// (handle, device, dy, rows, place, weights, out or None): (the rows' gradient, the weights')
+PyObject *expert_join_grad(PyObject *const *a)
+{
+    cocod_lm_handle *h = handle(a[0]);
+    const int64_t dev = device(a[1]);
+    const Tensor &dy = tensor(a[2], "dy", 2), &x = tensor(a[3], "rows", 2), &at = tensor(a[4], "place", 2);
+    const int64_t T = at.size(0), k = at.size(1), D = x.size(1);
+    const at::ScalarType type = value_type(x, "rows");
+    const Matrix md = any_rows(dy, "dy", T, D, type, dev), m = any_rows(x, "rows", T * k, D, type, dev);
+    const int32_t *places = static_cast<const int32_t *>(table(at, "place", T, k, at::kInt, dev));
+    const float *w = static_cast<const float *>(table(tensor(a[5], "weights", 2), "weights", T, k, at::kFloat, dev));
+    const Tensor out = a[6] == Py_None ? fresh(x, {T * k, D}, type) : tensor(a[6], "out", 2), dw = fresh(x, {T, k}, at::kFloat);
+    const Matrix mo = any_rows(out, "out", T * k, D, type, dev);
+    if (a[6] != Py_None) apart(out, "out", dy, "dy"), apart(out, "out", x, "rows");
+    const int rc = cocod_expert_join_grad(h, T, (int)k, D, md.data, md.ld, m.data, m.ld, places, w, mo.data, mo.ld, static_cast<float *>(dw.data_ptr()),
+                                          type_code(type), current(dev));
+    if (rc != COCOD_OK) return PyLong_FromLong(rc);
+    return Py_BuildValue("(NN)", a[6] == Py_None ? THPVariable_Wrap(out) : given(a[6]), THPVariable_Wrap(dw));
+}
+
+// ------------------------------------------------------------------------------------------ log probabilities
+inline float number(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw std::runtime_error("");
+    return (float)v;
+}
+int64_t alternatives(PyObject *o, int64_t V)
+{
+    const int64_t top = whole(o);
+    if (top < 0 || top > COCOD_LM_MAX_TOP || top > V)
+        throw std::invalid_argument("top: 0 to " + std::to_string(COCOD_LM_MAX_TOP) + " alternatives, at most as many as there are tokens; got " + std::to_string(top));
+    return top;
+}
+const int32_t *given_tokens(PyObject *o, int64_t M, int64_t dev)
+{
+    return o == Py_None ? nullptr : static_cast<const int32_t *>(vector(tensor(o, "tokens", 1), "tokens", M, at::kInt, dev));
+}
+
+// (handle, device, logits, tokens or None, top, scale): (logp or None, entropy, log_sum, top_logp or None, top_tokens or None)
+PyObject *token_logprobs(PyObject *const *a)
+{
+    cocod_lm_handle *h = handle(a[0]);
+    const int64_t dev = device(a[1]);
+    const Tensor &x = tensor(a[2], "logits", 2);
+    const int64_t M = x.size(0), V = x.size(1), top = alternatives(a[4], V);
+    const at::ScalarType type = value_type(x, "logits");
+    const Matrix m = any_rows(x, "logits", M, V, type, dev);
+    const int32_t *tokens = given_tokens(a[3], M, dev);
+    const float scale = number(a[5]);
+    const Tensor all = fresh(x, {3, M}, at::kFloat);
+    float *p = static_cast<float *>(all.data_ptr());
+    Tensor top_logp, top_tokens;
+    if (top) top_logp = fresh(x, {M, top}, at::kFloat), top_tokens = fresh(x, {M, top}, at::kInt);
+    const int rc = cocod_token_logprobs(h, M, V, m.data, m.ld, type_code(type), tokens, scale, (int)top, p, p + M, p + 2 * M,
+                                        top ? static_cast<float *>(top_logp.data_ptr()) : nullptr, top ? static_cast<int32_t *>(top_tokens.data_ptr()) : nullptr, current(dev));
+    if (rc != COCOD_OK) return PyLong_FromLong(rc);
+    const auto part = [&](int64_t i) { return THPVariable_Wrap(all.as_strided({M}, {1}, i * M)); };
+    return Py_BuildValue("(NNNNN)", tokens ? part(0) : given(Py_None), part(1), part(2), top ? THPVariable_Wrap(top_logp) : given(Py_None),
+                         top ? THPVariable_Wrap(top_tokens) : given(Py_None));
+}
+
+// (handle, device, logits, tokens or None, scale, top_tokens or None, log_sum, entropy or None, d_logp or None, d_entropy or None, d_top or None,
+// out or None)
+PyObject *token_logprobs_grad(PyObject *const *a)
+{
+    cocod_lm_handle *h = handle(a[0]);
+    const int64_t dev = device(a[1]);
+    const Tensor &x = tensor(a[2], "logits", 2);
+    const int64_t M = x.size(0), V = x.size(1);
+    const at::ScalarType type = value_type(x, "logits");
+    const Matrix m = any_rows(x, "logits", M, V, type, dev);
+    const int32_t *tokens = given_tokens(a[3], M, dev);
+    const float scale = number(a[4]);
+    const auto row_values = [&](PyObject *o, const char *name) {
+        return o == Py_None ? nullptr : static_cast<const float *>(vector(tensor(o, name, 1), name, M, at::kFloat, dev));
+    };
+    if (a[8] != Py_None && !tokens) throw std::invalid_argument("d_logp: there are no tokens whose log probabilities it could belong to");
+    if (a[9] != Py_None && a[7] == Py_None) throw std::invalid_argument("d_entropy: the entropy is needed");
+    if (a[10] != Py_None && a[5] == Py_None) throw std::invalid_argument("d_top: the top tokens are needed");
+    const float *log_sum = row_values(a[6], "log_sum"), *entropy = row_values(a[7], "entropy"), *d_logp = row_values(a[8], "d_logp"),
+                *d_entropy = row_values(a[9], "d_entropy"), *d_top = nullptr;
+    if (!log_sum && M > 0) throw std::invalid_argument("log_sum: need a tensor");
+    const int32_t *top_tokens = nullptr;
+    int64_t top = 0;
+    if (a[10] != Py_None) {
+        const Tensor &t = tensor(a[5], "top_tokens", 2);
+        top = t.size(1);
+        if (top > COCOD_LM_MAX_TOP || top > V) refuse("top_tokens", "at most " + std::to_string(COCOD_LM_MAX_TOP) + " columns, and no more than tokens", t);
+        top_tokens = static_cast<const int32_t *>(table(t, "top_tokens", M, top, at::kInt, dev));
+        d_top = static_cast<const float *>(table(tensor(a[10], "d_top", 2), "d_top", M, top, at::kFloat, dev));
+    }
+    const Tensor out = a[11] == Py_None ? fresh(x, {M, V}, type) : tensor(a[11], "out", 2);
+    const Matrix mo = any_rows(out, "out", M, V, type, dev);
+    if (a[11] != Py_None) apart(out, "out", x, "logits", true);
+    const int rc = cocod_token_logprobs_grad(h, M, V, m.data, m.ld, type_code(type), tokens, scale, (int)top, top_tokens, log_sum, entropy, d_logp, d_entropy, d_top,
+                                             mo.data, mo.ld, current(dev));
+    return rc == COCOD_OK && a[11] != Py_None ? given(a[11]) : code_or(rc, out);
+}
+
 #define METHOD(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     METHOD("grouped_forward", rows_product<true>, 7),
@@ -323,6 +504,12 @@ PyMethodDef methods[] = {
     METHOD("act_relu_grad", act_relu_grad, 8),
     METHOD("vocab_loss", vocab<false>, 8),
     METHOD("vocab_loss_grad", vocab<true>, 10),
+    METHOD("expert_sort", expert_sort, 4),
+    METHOD("expert_rows", expert_rows, 5),
+    METHOD("expert_join", expert_join, 7),
+    METHOD("expert_join_grad", expert_join_grad, 7),
+    METHOD("token_logprobs", token_logprobs, 6),
+    METHOD("token_logprobs_grad", token_logprobs_grad, 12),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lm_binding", "Marshalling for the language-model operators (used by lm.py).", -1, methods,

@@ -85,6 +85,13 @@ SIGNATURES = {
     "cocod_vocab_loss_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp,
                                    _vp, _i64, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
     "cocod_grouped_wait_selftest": (_i, [_i, _i, _vp]),
+    "cocod_expert_workspace": (_i64, [_i64, _i, _i]),
+    "cocod_expert_sort": (_i, [_vp, _i64, _i, _i, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "cocod_expert_rows": (_i, [_vp, _i64, _i, _i64, _vp, _i64, _vp, _vp, _i64, _i, _vp]),
+    "cocod_expert_join": (_i, [_vp, _i64, _i, _i64, _vp, _i64, _i, _vp, _vp, _vp, _i64, _i, _vp]),
+    "cocod_expert_join_grad": (_i, [_vp, _i64, _i, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i, _vp]),
+    "cocod_token_logprobs": (_i, [_vp, _i64, _i64, _vp, _i64, _i, _vp, _f, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "cocod_token_logprobs_grad": (_i, [_vp, _i64, _i64, _vp, _i64, _i, _vp, _f, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
 }
 
 _lib = None

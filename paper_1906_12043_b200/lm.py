@@ -10,10 +10,15 @@ by the library's CUDA kernels.  torch is used for device memory and streams.  No
     kept = ops.act_pack(x)                               # 8 bits per value until the backward pass
     dz = ops.act_relu_grad(dh, kept)                     # dh where the kept activation is positive
     loss, row_loss, dx, dw = ops.vocab_loss_grad(x, w, labels, offsets)
+    plan = ops.expert_sort(experts, E)                   # tokens' choices of experts -> plan.offsets and the rows' order
+    xs = ops.expert_rows(x, plan)                        # the products' rows; expert_rows_grad: back, added up by token
+    y  = ops.expert_join(ys, plan, weights)              # back to the tokens, weighted; expert_join_grad: its gradients
+    r  = ops.token_logprobs(logits, tokens, top=5)       # log probabilities, entropy, alternatives; token_logprobs_grad: the logits' gradient
 """
 from __future__ import annotations
 
 import ctypes
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -78,6 +83,23 @@ class PackedActivations:
             M, k = self.shape
             self._scales = self._buffer[M * self._ld:].view(-(-k // BLOCK), M)
         return self._scales
+
+
+class ExpertPlan(NamedTuple):
+    """Slots (token t's j-th choice) in the order of their experts.  A slot that takes no part has the bitwise complement of its row in `place`; such
+    rows lie behind the last expert's, count as its own in `offsets`, and are zero."""
+    offsets: torch.Tensor          # E + 1: row offsets[e] is expert e's first, as the products by group take them
+    counts: torch.Tensor           # E: slots of each expert
+    order: torch.Tensor            # the slot (t * k + j) of each row
+    place: torch.Tensor            # T x k: the row of each slot
+
+
+class TokenLogprobs(NamedTuple):
+    logp: Optional[torch.Tensor]          # of the rows' tokens (None without tokens)
+    entropy: torch.Tensor
+    log_sum: torch.Tensor                 # log of the sum of exp(scale * logits)
+    top_logp: Optional[torch.Tensor]      # M x top (None without alternatives)
+    top_tokens: Optional[torch.Tensor]
 
 
 class LMOps:
@@ -181,9 +203,45 @@ class LMOps:
         return self._checked(self._b.vocab_loss_grad(self._h, self._device, x, w, labels, offsets, row_weights, self.workspace_limit, dw,
                                                      self._code(dw_dtype)), "cocod_vocab_loss_grad")
 
+    # ------------------------------------------------------------------------------------------ tokens by expert
+    def expert_sort(self, experts, E: int) -> ExpertPlan:
+        """The order of the rows in which `experts` (T x k int32: every token's choices; negative: none) lets the products by group take them; a
+        stable sort.  k <= 32, E <= 1024."""
+        return ExpertPlan(*self._checked(self._b.expert_sort(self._h, self._device, experts, E), "cocod_expert_sort"))
+
+    def expert_rows(self, x, plan: ExpertPlan, out=None):
+        """The T k rows for the products, in the plan's order, of x (T x D, bf16 or float32); zeros for slots that take no part."""
+        return self._checked(self._b.expert_rows(self._h, self._device, x, plan.place, out), "cocod_expert_rows")
+
+    def expert_rows_grad(self, drows, plan: ExpertPlan, out=None, out_dtype=None):
+        """The gradient of expert_rows' x: every token's rows added up.  drows: T k x D; the result's type is drows' unless out or out_dtype says."""
+        return self._checked(self._b.expert_join(self._h, self._device, drows, plan.place, None, out, self._code(out_dtype)), "cocod_expert_join")
+
+    def expert_join(self, rows, plan: ExpertPlan, weights, out=None, out_dtype=None):
+        """y[t] = sum of weights[t][j] rows[place[t][j]] over the token's slots that take part.  rows: T k x D, weights: T x k float32."""
+        if weights is None:
+            raise ValueError("weights: need a tensor (expert_rows_grad adds up without)")
+        return self._checked(self._b.expert_join(self._h, self._device, rows, plan.place, weights, out, self._code(out_dtype)), "cocod_expert_join")
+
+    def expert_join_grad(self, dy, rows, plan: ExpertPlan, weights, out=None):
+        """(drows, dweights): the gradients of expert_join's rows (T k x D; zeros where a slot takes no part) and weights (T x k float32)."""
+        return self._checked(self._b.expert_join_grad(self._h, self._device, dy, rows, plan.place, weights, out), "cocod_expert_join_grad")
+
+    # ------------------------------------------------------------------------------------------ log probabilities
+    def token_logprobs(self, logits, tokens=None, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
+        """Log probabilities under the softmax of scale * logits (M x V, bf16 or float32): of `tokens` (M int32; negative: the row takes no part, its
+        results are 0 and -1), with the entropy and the `top` most probable tokens (of equal ones the lower first; at most 32)."""
+        return TokenLogprobs(*self._checked(self._b.token_logprobs(self._h, self._device, logits, tokens, top, scale), "cocod_token_logprobs"))
+
+    def token_logprobs_grad(self, logits, tokens, known: TokenLogprobs, d_logp=None, d_entropy=None, d_top=None, scale: float = 1.0, out=None):
+        """The gradient of the logits, given those of logp and entropy (M float32) and of top_logp (M x top).  known: what token_logprobs
+        returned for these logits, tokens and scale.  out: the logits' type; may be the logits."""
+        return self._checked(self._b.token_logprobs_grad(self._h, self._device, logits, tokens, scale, known.top_tokens, known.log_sum, known.entropy,
+                                                         d_logp, d_entropy, d_top, out), "cocod_token_logprobs_grad")
+
     # ------------------------------------------------------------------------------------------ the rest
     def check(self):
-        """Synchronise the current stream; raise if a kernel gave up a wait or met offsets or labels out of range."""
+        """Synchronise the current stream; raise if a kernel gave up a wait or met offsets, labels, experts or places out of range."""
         rc = self._lib.cocod_lm_check(self._h, torch.cuda.current_stream(self._device).cuda_stream)
         if rc != _E.OK:
             raise _E.CocodError(rc, "cocod_lm_check")

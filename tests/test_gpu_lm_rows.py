@@ -1,0 +1,555 @@
+"""Tokens sorted by expert and back, and log probabilities of tokens (lm.LMOps), against plain implementations in 64 bits.
+
+Tolerances, derived before the first run:
+
+* the sort, the rows and the order of the alternatives are exact.
+* a sum of k products in fp32, rounded once each: k * 2^-24 * (sum of magnitudes), plus half a step of a bf16 result (2^-8, fp32 2^-24 of the value).
+* a dot product of D products: a thread adds at most D / 32 + 8 of them one after the other, then 5 + 3 joins: (D / 32 + 16) * 2^-24 * (sum of magnitudes).
+* log probabilities: t = (l - m) * scale * log2 e carries three roundings (2^-24 each, relative to |t|) and the exponential 2^-22, so that a term of the sum is off by
+  at most 2^-22 + 3 * 2^-24 * |t|, and terms of |t| > 24 are below 2^-24 of the sum: 2^-22 + 72 * 2^-24 = 19 * 2^-22 for each that counts.  The sums add at most
+  V / 128 + 64 terms one after the other.  With s = 19 * 2^-22 + (V / 128 + 64) * 2^-24, ln S1 is off by s, Z and log p by s + 2^-22 * (1 + |y| + |Z|), and the entropy by
+  s * (2 + ln V) (S2 / S1 is at most ln V, and each of its terms is off by at most s of itself).
+* the gradient: log p is off by a = 2^-22 * (1 + |y| + |Z|) + (the given log_sum's own error, none: the test gives it in fp32, 2^-24 |Z|), p by 2^-22 + a relative, so that a
+  term p * (A + g (log p + H)) is off by p * ((2^-21 + a) * (|A| + |g| |log p + H|) + |g| (a + 2^-23 H)), plus the result's rounding.  ex2.approx flushes results below 2^-126 to zero.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def lm():
+    from paper_1906_12043_b200 import build, lm
+    build.build()
+    return lm
+
+
+@pytest.fixture(scope="module")
+def ops(lm):
+    o = lm.LMOps()
+    yield o
+    o.check()
+    o.destroy()
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+def gaussian(seed, *shape, scale=1.0, dtype=torch.float32):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def choices(seed, T, k, E, absent=0.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    e = torch.randint(0, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    if absent:
+        e[torch.rand(T, k, generator=g, device="cuda") < absent] = -1
+    return e
+
+
+# ------------------------------------------------------------------------------------------------------- experts
+def plain_sort(experts, E):
+    flat = experts.reshape(-1).cpu().tolist()
+    rows = [[] for _ in range(E + 1)]
+    for s, e in enumerate(flat):
+        rows[e if 0 <= e < E else E].append(s)
+    order = [s for r in rows for s in r]
+    live = len(flat) - len(rows[E])
+    place = [0] * len(flat)
+    for r, s in enumerate(order):
+        place[s] = r if r < live else ~r
+    offsets = [0]
+    for r in rows[:-1]:
+        offsets.append(offsets[-1] + len(r))
+    offsets[-1] = len(flat)
+    return offsets, [len(r) for r in rows[:-1]], order, place
+
+
+SORTS = [(0, 2, 4), (1, 1, 1), (1, 8, 8), (3, 5, 7), (37, 2, 8), (1000, 1, 1000), (1024, 4, 64), (1025, 4, 1024), (1366, 3, 5), (4097, 1, 3), (9999, 7, 60), (40000, 8, 128),
+         (7000, 32, 1023)]
+
+
+@pytest.mark.parametrize("T,k,E", SORTS)
+@pytest.mark.parametrize("absent", [0.0, 0.3, 1.0])
+def test_slots_in_the_order_of_their_experts(ops, T, k, E, absent):
+    e = choices(T + k, T, k, E, absent)
+    plan = ops.expert_sort(e, E)
+    offsets, counts, order, place = plain_sort(e, E)
+    assert plan.offsets.tolist() == offsets and plan.counts.tolist() == counts
+    assert plan.order.tolist() == order and plan.place.reshape(-1).tolist() == place
+    assert plan.place.shape == (T, k)
+    ops.check()
+
+
+def test_one_expert_takes_all_and_views_of_choices(ops):
+    for T, k in ((5000, 4), (100, 2)):
+        wide = torch.full((T, k + 3), 5, dtype=torch.int32, device="cuda")
+        plan = ops.expert_sort(wide[:, 1:1 + k], 9)
+        assert plan.order.tolist() == list(range(T * k)) and plan.offsets.tolist() == [0] * 6 + [T * k] * 4
+        wide[:, 1:1 + k] = choices(1, T, k, 9)
+        got, want = ops.expert_sort(wide[:, 1:1 + k], 9), ops.expert_sort(wide[:, 1:1 + k].contiguous(), 9)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("T,k,E", [(33, 2, 8), (3000, 4, 16)])
+def test_a_number_beyond_the_experts_takes_no_part_and_is_reported(ops, lm, T, k, E):
+    from paper_1906_12043_b200.engine import CocodError
+    e = choices(2, T, k, E)
+    bad = e.clone()
+    bad[T // 2, 0] = E
+    plan = ops.expert_sort(bad, E)
+    with pytest.raises(CocodError):
+        ops.check()
+    ops.check()
+    offsets, counts, order, place = plain_sort(bad, E)
+    assert plan.offsets.tolist() == offsets and plan.counts.tolist() == counts and plan.order.tolist() == order and plan.place.reshape(-1).tolist() == place
+
+
+ROWS = [(1, 1, 1, 8), (5, 3, 4, 7), (17, 2, 8, 512), (100, 8, 16, 264), (64, 1, 2, 1), (333, 6, 60, 1032), (50, 32, 40, 96), (9, 2, 5, 9000), (700, 4, 9, 2047)]
+
+
+@pytest.mark.parametrize("T,k,E,D", ROWS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("absent", [0.0, 0.25])
+def test_there_and_back(ops, T, k, E, D, dtype, absent):
+    plan = ops.expert_sort(choices(T, T, k, E, absent), E)
+    there = plan.place >= 0
+    at = torch.where(there, plan.place, ~plan.place).long()
+    x, ys, dy = gaussian(1, T, D, dtype=dtype), gaussian(2, T * k, D, dtype=dtype), gaussian(3, T, D, dtype=dtype)
+    w = gaussian(4, T, k)
+    if not there.all():
+        ys[at[~there]] = float("nan")                       # what such rows hold is not looked at
+    rows = ops.expert_rows(x, plan)
+    want = torch.zeros_like(rows)
+    want[at[there]] = x[:, None].expand(T, k, D)[there]
+    assert torch.equal(rows, want)
+    wide = torch.where(there[..., None], ys.double()[at], 0.0)
+    for out_dtype in (torch.bfloat16, torch.float32):
+        for weights in (w, None):
+            got = ops.expert_rows_grad(ys, plan, out_dtype=out_dtype) if weights is None else ops.expert_join(ys, plan, w, out_dtype=out_dtype)
+            f = (torch.ones_like(w) if weights is None else w).double()[..., None]
+            y, size = (f * wide).sum(1), (f * wide).abs().sum(1)
+            assert got.dtype == out_dtype
+            assert ((got.double() - y).abs() <= half_step(out_dtype) * y.abs() + 1.01 * (k + 1) * 2.0 ** -24 * size).all()
+    drows, dw = ops.expert_join_grad(dy, ys, plan, w)
+    back = torch.zeros(T * k, D, dtype=torch.float64, device="cuda")
+    back[at[there]] = (w.double()[..., None] * dy.double()[:, None])[there]
+    # (a product of fp32 is rounded to fp32, then to the result's type)
+    assert ((drows.double() - back).abs() <= 1.01 * (half_step(dtype) + 2.0 ** -24) * back.abs()).all()
+    assert (drows[at[~there]] == 0).all()
+    products = wide * dy.double()[:, None]
+    assert ((dw.double() - products.sum(2)).abs() <= (D / 32 + 16) * 2.0 ** -24 * products.abs().sum(2)).all()
+    assert (dw[~there] == 0).all()
+    ops.check()
+
+
+def test_gradients_are_the_formulas(ops):
+    """Against autograd in 64 bits through the same gather and weighted sum."""
+    T, k, E, D = 40, 3, 6, 72
+    e = choices(9, T, k, E, 0.2)
+    plan = ops.expert_sort(e, E)
+    at, there = torch.where(plan.place >= 0, plan.place, ~plan.place).long(), plan.place >= 0
+    x, w, dy, mix = gaussian(1, T, D), gaussian(2, T, k), gaussian(3, T, D), gaussian(4, T * k, D)
+    xd, wd = x.double().requires_grad_(True), w.double().requires_grad_(True)
+    rows = torch.zeros(T * k, D, dtype=torch.float64, device="cuda").index_put((at[there],), xd[:, None].expand(T, k, D)[there])
+    hidden = rows * mix.double()
+    y = (torch.where(there[..., None], hidden[at], 0.0) * wd[..., None]).sum(1)
+    y.backward(dy.double())
+    h = ops.expert_rows(x, plan) * mix
+    dh, dw = ops.expert_join_grad(dy, h, plan, w)
+    dx = ops.expert_rows_grad(dh * mix, plan)
+    assert ((dx.double() - xd.grad).abs() <= 16 * 2.0 ** -24 * (xd.grad.abs() + 8)).all()
+    assert ((dw.double() - wd.grad).abs() <= 64 * 2.0 ** -24 * 64).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lead", [0, 1, 8])
+def test_views_and_their_surroundings(ops, dtype, lead):
+    """Rows of a larger matrix, at any alignment; nothing beside them is written."""
+    T, k, E, D = 90, 3, 7, 136
+    plan = ops.expert_sort(choices(5, T, k, E, 0.1), E)
+    w = gaussian(4, T, k)
+
+    def inside(t):
+        whole = torch.full((t.shape[0] + 2, t.shape[1] + 24), 7.0, dtype=t.dtype, device="cuda")
+        view = whole[1:-1, lead:lead + t.shape[1]]
+        view.copy_(t)
+        return view, whole
+
+    def untouched(view, whole):
+        w2 = whole.clone()
+        w2[1:-1, lead:lead + view.shape[1]] = 7
+        return (w2 == 7).all()
+
+    x, ys, dy = gaussian(1, T, D, dtype=dtype), gaussian(2, T * k, D, dtype=dtype), gaussian(3, T, D, dtype=dtype)
+    out, whole = inside(torch.zeros(T * k, D, dtype=dtype, device="cuda"))
+    assert ops.expert_rows(inside(x)[0], plan, out=out) is out
+    assert torch.equal(out, ops.expert_rows(x, plan)) and untouched(out, whole)
+    y, whole = inside(torch.zeros(T, D, dtype=dtype, device="cuda"))
+    ops.expert_join(inside(ys)[0], plan, w, out=y)
+    assert torch.equal(y, ops.expert_join(ys, plan, w)) and untouched(y, whole)
+    d, whole = inside(torch.zeros(T * k, D, dtype=dtype, device="cuda"))
+    _, dw = ops.expert_join_grad(inside(dy)[0], inside(ys)[0], plan, w, out=d)
+    want, dw2 = ops.expert_join_grad(dy, ys, plan, w)
+    assert torch.equal(d, want) and untouched(d, whole)
+    products = ys.double().abs()[torch.where(plan.place >= 0, plan.place, ~plan.place).long()] * dy.double().abs()[:, None]
+    assert ((dw - dw2).abs().double() <= 2 * (D + 16) * 2.0 ** -24 * products.sum(2)).all()
+
+
+def test_a_place_beyond_the_rows_is_left_out_and_reported(ops, lm):
+    from paper_1906_12043_b200.engine import CocodError
+    T, k, E, D = 20, 2, 4, 64
+    plan = ops.expert_sort(choices(5, T, k, E), E)
+    x, ys = gaussian(1, T, D, dtype=torch.bfloat16), gaussian(2, T * k, D, dtype=torch.bfloat16)
+    for bad_row in (T * k, 2 ** 31 - 1, -1 - T * k, -2 ** 31):
+        place = plan.place.clone()
+        place[3, 1] = bad_row
+        bad = plan._replace(place=place)
+        out = torch.full((T * k, D), 7.0, dtype=torch.bfloat16, device="cuda")
+        ops.expert_rows(x, bad, out=out)
+        want = ops.expert_rows(x, plan)
+        want[plan.place[3, 1].long()] = 7
+        assert torch.equal(out, want)
+        with pytest.raises(CocodError):
+            ops.check()
+        y = ops.expert_rows_grad(ys, bad, out_dtype=torch.float32)
+        assert torch.equal(y[3], ys[plan.place[3, 0].long()].float())
+        with pytest.raises(CocodError):
+            ops.check()
+
+
+def test_more_than_2_to_the_31_values(ops):
+    T, k, E, D = 70000, 4, 8, 8192                              # 2.3e9 values of rows
+    plan = ops.expert_sort(choices(6, T, k, E), E)
+    x = gaussian(1, T, 64, dtype=torch.bfloat16).repeat(1, D // 64)
+    rows = ops.expert_rows(x, plan)
+    token = plan.order.long() // k
+    for a in range(0, T * k, 20000):
+        assert torch.equal(rows[a:a + 20000], x[token[a:a + 20000]])
+    y = ops.expert_rows_grad(rows, plan)
+    assert torch.equal(y, x * 4)
+    ops.check()
+
+
+def test_refusals(ops, lm):
+    T, k, E, D = 8, 2, 4, 16
+    e = choices(1, T, k, E)
+    plan = ops.expert_sort(e, E)
+    x, ys, w = gaussian(1, T, D), gaussian(2, T * k, D), gaussian(3, T, k)
+    for bad in (e.long(), e.cpu(), e.t(), e[0], torch.zeros(T, 33, dtype=torch.int32, device="cuda"), torch.zeros(T, 0, dtype=torch.int32, device="cuda")):
+        with pytest.raises(ValueError):
+            ops.expert_sort(bad, E)
+    for bad in (0, -1, 1025):
+        with pytest.raises(ValueError):
+            ops.expert_sort(e, bad)
+    for call in (lambda: ops.expert_rows(x[:-1], plan), lambda: ops.expert_rows(x.half(), plan), lambda: ops.expert_rows(x.t(), plan),
+                 lambda: ops.expert_rows(x, plan, out=ys[:-1]), lambda: ops.expert_rows(x, plan, out=ys.bfloat16()), lambda: ops.expert_rows(x.cpu(), plan),
+                 lambda: ops.expert_join(ys, plan, w.double()), lambda: ops.expert_join(ys, plan, w[:, :1]), lambda: ops.expert_join(ys, plan, None),
+                 lambda: ops.expert_join(ys[1:], plan, w), lambda: ops.expert_join(ys, plan, w, out=ys[:T]), lambda: ops.expert_join(ys, plan, w, out_dtype=torch.float16),
+                 lambda: ops.expert_join_grad(x, ys, plan, w, out=ys), lambda: ops.expert_join_grad(x.bfloat16(), ys, plan, w),
+                 lambda: ops.expert_join_grad(x, ys, plan, w.t()), lambda: ops.expert_rows(x, plan._replace(place=plan.place.long())),
+                 lambda: ops.token_logprobs(ys, top=33), lambda: ops.token_logprobs(ys, top=17), lambda: ops.token_logprobs(ys, top=-1), lambda: ops.token_logprobs(ys.half()),
+                 lambda: ops.token_logprobs(ys, plan.order.long()), lambda: ops.token_logprobs(ys, plan.order[1:]), lambda: ops.token_logprobs(ys.t())):
+        with pytest.raises(ValueError):
+            call()
+    from paper_1906_12043_b200.engine import CocodError
+    for bad in (0.0, -1.0, float("nan"), INF):
+        with pytest.raises(CocodError):
+            ops.token_logprobs(ys, scale=bad)
+    t = plan.order % D
+    known = ops.token_logprobs(ys, t, top=3)
+    g = gaussian(1, T * k)
+    for call in (lambda: ops.token_logprobs_grad(ys, None, known, g), lambda: ops.token_logprobs_grad(ys, t, known, g[1:]), lambda: ops.token_logprobs_grad(ys, t, known, g.double()),
+                 lambda: ops.token_logprobs_grad(ys, t, known, g, d_top=gaussian(1, T * k, 2)), lambda: ops.token_logprobs_grad(ys, t, known._replace(top_tokens=None), d_top=gaussian(1, T * k, 3)),
+                 lambda: ops.token_logprobs_grad(ys, t, known._replace(entropy=None), d_entropy=g), lambda: ops.token_logprobs_grad(ys, t, known._replace(log_sum=None), g),
+                 lambda: ops.token_logprobs_grad(ys, t, known, g, out=ys.bfloat16()), lambda: ops.token_logprobs_grad(ys[1:], t[1:], known, g[1:])):
+        with pytest.raises(ValueError):
+            call()
+    ops.check()
+
+
+# ------------------------------------------------------------------------------------------------------- log probabilities
+def plain_logprobs(logits, tokens, top, scale):
+    x = logits.double()
+    y = x * scale
+    most = y.amax(1, keepdim=True)
+    dead = most[:, 0] == -INF
+    t = y - torch.where(dead[:, None], 0.0, most)            # (relative to the largest: a row of the type's lowest value has a distribution, too)
+    log_sum = torch.logsumexp(t, 1)
+    z = log_sum + most[:, 0]
+    lp = torch.where(dead[:, None], torch.full_like(y, -INF), t - log_sum[:, None])
+    p = lp.exp()
+    h = -torch.where(p > 0, p * lp, torch.where(p.isnan(), p, 0.0)).sum(1)
+    best = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :top]
+    got = [None if tokens is None else lp.gather(1, tokens.clamp(min=0).long()[:, None])[:, 0], h, z, lp.gather(1, best), best]
+    if tokens is not None:
+        out = tokens < 0
+        for a, fill in zip(got, (0, 0, 0, 0, -1)):
+            a[out] = fill
+    return got
+
+
+def assert_logprobs(got, logits, tokens, top, scale):
+    want = plain_logprobs(logits, tokens, top, scale)
+    V = logits.shape[1]
+    s = 19 * 2.0 ** -22 + (V / 128 + 64) * 2.0 ** -24
+    z, finite = want[2], want[2].isfinite()
+    most = (logits.double() * scale).masked_fill(~(logits.abs() < 1e30), 0).abs().amax(1)
+
+    def close(a, b, bound, name):
+        assert a.shape == b.shape, name
+        same = (a.double() == b) | (a.isnan() & b.isnan())
+        near = ((a.double() - b).abs() <= bound) & b.isfinite()
+        assert (same | near).all(), f"{name}: worst {((a.double() - b).abs() / bound)[b.isfinite()].max()} of the bound"
+
+    step = s + 2.0 ** -22 * (1 + torch.where(finite, z.abs(), 0.0))
+    if tokens is not None:
+        own = torch.where(want[0].isfinite(), want[0].abs(), 0.0)
+        close(got.logp, want[0], step + 2.0 ** -22 * (own + 2 * most), "logp")
+    close(got.entropy, want[1], s * (2 + math.log(V)) + 2.0 ** -23, "entropy")
+    close(got.log_sum, z, step + 2.0 ** -23 * most, "log_sum")
+    if top:
+        assert torch.equal(got.top_tokens.long(), want[4])
+        lp = torch.where(want[3].isfinite(), want[3].abs(), 0.0)
+        close(got.top_logp, want[3], (step + 2.0 ** -22 * 2 * most)[:, None] + 2.0 ** -22 * lp, "top_logp")
+
+
+LOGITS = [(1, 1, 1), (3, 2, 2), (5, 7, 3), (64, 31, 31), (17, 32, 32), (100, 64, 4), (33, 100, 20), (9, 257, 8), (21, 513, 32), (12, 1000, 5), (8, 1024, 32), (7, 1025, 32), (40, 1033, 20),
+          (5, 2048, 32), (300, 4097, 3), (1, 8191, 32), (4, 50001, 20), (2, 131072, 32), (150, 33333, 1), (600, 5000, 0)]
+
+
+@pytest.mark.parametrize("M,V,top", LOGITS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["plain", "masked", "far apart", "equal"])
+def test_log_probabilities(ops, M, V, top, dtype, kind):
+    x = gaussian(M + V, M, V, scale=2.0, dtype=dtype)
+    scale = 1.0
+    g = torch.Generator(device="cuda").manual_seed(V)
+    if kind == "masked":                                    # all but few, or nothing at all
+        keep = torch.rand(M, V, generator=g, device="cuda") < torch.rand(M, 1, generator=g, device="cuda") * 0.5
+        x = x.masked_fill(~keep, -INF)
+        x[::5] = x[::5].masked_fill(x[::5] == -INF, torch.finfo(dtype).min)
+        x[M // 2] = -INF
+        x[M // 3, :] = -INF
+        x[M // 3, V // 2] = -3.0
+    elif kind == "far apart":
+        x, scale = x * 40, 0.7
+    elif kind == "equal":
+        x = (x / 3).round() * 0.0 + torch.randint(0, 2, (M, V), generator=g, device="cuda").to(dtype) * (torch.arange(M, device="cuda") % 3 == 0)[:, None]
+        x[1::2] = -x[1::2]                                  # zeros of either sign
+    tokens = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    tokens[::7] = -1 if M > 7 else tokens[::7]
+    assert_logprobs(ops.token_logprobs(x, tokens, top=top, scale=scale), x, tokens, top, scale)
+    alone = ops.token_logprobs(x, top=top, scale=scale)
+    assert alone.logp is None
+    assert_logprobs(alone, x, None, top, scale)
+    ops.check()
+
+
+@pytest.mark.parametrize("V", [40, 3000, 20000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_alternatives_where_the_bound_is_of_no_use(ops, V, dtype):
+    """Rows made so that few threads hold all large values, in every order, and rows with hundreds of values above all others."""
+    M, top = 12, min(V, 32)
+    x = torch.zeros(M, V, device="cuda")
+    i = torch.arange(V, device="cuda")
+    x[0], x[1] = i, -i.float()
+    x[2] = (i % 8 == 3) * 5.0
+    x[3] = (i % 512 == 17) * 5.0 + (i % 7) * 0.01
+    x[4] = (i // 8 % 512 < 3) * (i % 200).float()
+    x[5] = (i // 8 % 512 < 2) * 4.0
+    x[6, -3:] = 1
+    x[7, :3] = 1
+    x[8] = (i // 4 % 512 < 5) * (1 + i.float() / V)
+    x[9] = i // (V // 2)
+    x[10] = -INF
+    x[10, V // 3:V // 3 + 5] = i[:5].float()
+    x[11] = torch.where(i % 64 < 20, 3.0, -INF)
+    x = x.to(dtype)
+    assert_logprobs(ops.token_logprobs(x, top=top), x, None, top, 1.0)
+    wide = torch.full((M, V + 5), 99.0, dtype=dtype, device="cuda")
+    for lead in range(6):                                   # any alignment: what lies beside the rows is not looked at
+        wide.fill_(99.0)
+        v = wide[:, lead:lead + V] if lead < 6 else wide
+        v.copy_(x)
+        a, b = ops.token_logprobs(v, top=top), ops.token_logprobs(x, top=top)
+        assert torch.equal(a.top_tokens, b.top_tokens)
+        assert_logprobs(a, x, None, top, 1.0)
+
+
+@pytest.mark.parametrize("V", [50, 1500, 40000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_values_that_are_not_finite(ops, V, dtype):
+    x = gaussian(1, 6, V, dtype=dtype)
+    x[0, 7], x[1, V - 1], x[2, 0], x[2, 3], x[3, 5] = float("nan"), INF, INF, float("nan"), -float("nan")
+    t = torch.full((6,), 9, dtype=torch.int32, device="cuda")
+    t[3] = -1
+    r = ops.token_logprobs(x, t, top=4)
+    assert r.logp[:3].isnan().all() and r.entropy[:3].isnan().all() and r.log_sum[:3].isnan().all() and r.top_logp[:3].isnan().all()
+    assert r.top_tokens[0, 0] == 7 and r.top_tokens[1, 0] == V - 1 and r.top_tokens[2, :2].tolist() == [3, 0]
+    assert (r.top_tokens[3] == -1).all() and r.logp[3] == 0 and r.entropy[3] == 0 and r.log_sum[3] == 0 and (r.top_logp[3] == 0).all()
+    assert r.logp[4:].isfinite().all() and r.entropy[4:].isfinite().all()
+    d = ops.token_logprobs_grad(x, t, r, torch.ones(6, device="cuda"), torch.ones(6, device="cuda"))
+    assert d[:3].isnan().any(1).all() and (d[3] == 0).all() and d[4:].isfinite().all()
+
+
+def test_a_token_beyond_the_vocabulary_takes_no_part_and_is_reported(ops):
+    from paper_1906_12043_b200.engine import CocodError
+    for V in (60, 5000):
+        x = gaussian(1, 3, V)
+        t = torch.tensor([1, V, 2], dtype=torch.int32, device="cuda")
+        r = ops.token_logprobs(x, t, top=2)
+        with pytest.raises(CocodError):
+            ops.check()
+        assert r.logp[1] == 0 and (r.top_tokens[1] == -1).all() and r.logp[0] != 0
+        d = ops.token_logprobs_grad(x, t, r, torch.ones(3, device="cuda"))
+        assert (d[1] == 0).all() and d[0].any()
+        with pytest.raises(CocodError):
+            ops.check()
+        known = r._replace(top_tokens=torch.tensor([[1, 2], [-1, -1], [5, V]], dtype=torch.int32, device="cuda"))
+        g = torch.ones(3, 2, device="cuda")
+        d = ops.token_logprobs_grad(x, None, known, d_top=g)
+        with pytest.raises(CocodError):
+            ops.check()
+        assert (d[2].double().sum().abs() <= 1e-5) and d[2, 5] > 0
+
+
+def plain_gradient(x, tokens, r, d_logp, d_entropy, d_top, scale):
+    """(gradient, bound on the error of a result in fp32)"""
+    z, h = r.log_sum.double()[:, None], r.entropy.double()[:, None]
+    y = x.double() * scale
+    dead = (z == -INF) | (tokens < 0)[:, None]
+    lp = torch.where(dead, 0.0, y - z)
+    p = lp.exp()
+    given = torch.zeros_like(y)
+    given.scatter_add_(1, tokens.clamp(min=0).long()[:, None], d_logp.double()[:, None])
+    if d_top is not None:
+        given.scatter_add_(1, r.top_tokens.clamp(min=0).long(), torch.where(r.top_tokens >= 0, d_top.double(), 0.0))
+    every = given.sum(1, keepdim=True)
+    size = d_logp.double().abs()[:, None] + (0 if d_top is None else d_top.double().abs().sum(1, keepdim=True))
+    g = d_entropy.double()[:, None]
+    inner = torch.where(p > 0, lp + h, 0.0)
+    d = given - torch.where(p > 0, p * (every + g * inner), 0.0)
+    a = 2.0 ** -22 * (1 + torch.where(y.isfinite(), y.abs(), 0.0) + z.abs())
+    bound = p * ((2.0 ** -21 + a) * (size + g.abs() * inner.abs()) + g.abs() * (a + 2.0 ** -23 * (h + inner.abs()))) + 36 * 2.0 ** -24 * size * (given != 0) + 2.0 ** -100
+    return torch.where(dead, 0.0, scale * d), torch.where(dead, 0.0, scale * (bound + 2.0 ** -23 * d.abs()))
+
+
+@pytest.mark.parametrize("M,V,top", [(1, 1, 0), (3, 2, 2), (50, 64, 4), (9, 999, 0), (20, 1000, 8), (37, 8191, 0), (5, 50001, 20), (3, 131072, 32), (200, 4100, 1)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("masked", [False, True])
+def test_gradient(ops, M, V, top, dtype, masked):
+    x = gaussian(V, M, V, scale=2.0, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(M)
+    tokens = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    if masked:
+        x = x.masked_fill(torch.rand(M, V, generator=g, device="cuda") < 0.4, -INF)
+        x[M // 2] = -INF
+        if M > 2:
+            tokens[0] = -1
+    scale = 1.0 if M % 2 else 0.6
+    r = ops.token_logprobs(x, tokens, top=top, scale=scale)
+    d_logp, d_entropy = gaussian(1, M), gaussian(2, M)
+    d_top = gaussian(3, M, top) if top else None
+    if top > 2:                                             # the row's token among the alternatives, and one of them twice
+        r.top_tokens[:, 1] = r.top_tokens[:, 0]
+        r.top_tokens[:, 2] = torch.where(tokens >= 0, tokens, -1)
+    want, bound = plain_gradient(x, tokens, r, d_logp, d_entropy, d_top, scale)
+    got = ops.token_logprobs_grad(x, tokens, r, d_logp, d_entropy, d_top, scale=scale)
+    assert got.dtype == dtype
+    error, room = (got.double() - want).abs(), bound + half_step(dtype) * want.abs()
+    assert (error <= room).all(), f"worst {(error / room.clamp(min=1e-300)).max()}"
+    over = x.clone()
+    assert ops.token_logprobs_grad(over, tokens, r, d_logp, d_entropy, d_top, scale=scale, out=over) is over
+    assert torch.equal(over, got)
+    whole = torch.full((M + 2, V + 9), 7.0, dtype=dtype, device="cuda")       # another alignment than the logits'
+    ops.token_logprobs_grad(x, tokens, r, d_logp, d_entropy, d_top, scale=scale, out=whole[1:-1, 3:3 + V])
+    assert torch.equal(whole[1:-1, 3:3 + V], got)
+    whole[1:-1, 3:3 + V] = 7
+    assert (whole == 7).all()
+    ops.check()
+
+
+def test_gradient_against_differences(ops):
+    """The definition's values in 64 bits at two points on either side."""
+    M, V, scale = 4, 30, 0.8
+    x = gaussian(1, M, V).double()
+    tokens = torch.tensor([3, 0, 29, 7], dtype=torch.int32, device="cuda")
+    a, b, c = (gaussian(s, M).double() for s in (2, 3, 4))
+
+    def value(x):
+        r = plain_logprobs(x, tokens, 2, scale)
+        return (a * r[0] + b * r[1] + c * r[3][:, 1]).sum()
+
+    r = ops.token_logprobs(x.float(), tokens, top=2, scale=scale)
+    got = ops.token_logprobs_grad(x.float(), tokens, r, a.float(), b.float(), torch.stack([torch.zeros_like(c), c], 1).float(), scale=scale).double()
+    for row, col in ((0, 3), (0, 4), (1, 0), (2, 29), (3, 8), (3, int(r.top_tokens[3, 1]))):
+        up, down = x.clone(), x.clone()
+        up[row, col] += 1e-5
+        down[row, col] -= 1e-5
+        assert abs(float(value(up) - value(down)) / 2e-5 - float(got[row, col])) <= 1e-5
+
+
+def test_more_than_2_to_the_31_logits(ops):
+    M, V = 40000, 65536
+    x = torch.empty(M, V, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, M, 4000):
+        x[a:a + 4000] = gaussian(a, 4000, V, dtype=torch.bfloat16)
+    t = torch.randint(0, V, (M,), device="cuda", dtype=torch.int32)
+    r = ops.token_logprobs(x, t, top=2)
+    last = slice(M - 500, M)
+    assert_logprobs(type(r)(*(v[last] for v in r)), x[last], t[last], 2, 1.0)
+    g = torch.ones(M, device="cuda")
+    want = ops.token_logprobs_grad(x[last], t[last], type(r)(*(v[last].contiguous() for v in r)), g[last])
+    ops.token_logprobs_grad(x, t, r, g, out=x)
+    assert torch.equal(x[last], want)
+    ops.check()
+
+
+def test_captured_and_replayed_and_on_another_stream(ops):
+    """One graph of a whole way there and back: the same bits as the calls, and new ones for new inputs."""
+    T, k, E, D, V = 600, 2, 16, 128, 16
+    logits, x, dy = gaussian(1, T, V), gaussian(2, T, D), gaussian(3, T, D)
+
+    def way():
+        r = ops.token_logprobs(logits, top=k)
+        plan = ops.expert_sort(r.top_tokens, E)
+        w = r.top_logp.exp()
+        rows = ops.expert_rows(x, plan)
+        y = ops.expert_join(rows, plan, w)
+        drows, dw = ops.expert_join_grad(dy, rows, plan, w)
+        dl = ops.token_logprobs_grad(logits, None, r, d_top=dw * w)
+        return y, ops.expert_rows_grad(drows, plan), dl, plan.order
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        way()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out = way()
+    torch.cuda.current_stream().wait_stream(s)
+    for seed in (5, 6):
+        logits.copy_(gaussian(seed, T, V))
+        x.copy_(gaussian(seed + 10, T, D))
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(out, way()))
+    ops.check()
+
+
+def test_the_same_bits_every_time(ops):
+    x, t = gaussian(1, 50, 30000, dtype=torch.bfloat16), torch.arange(50, dtype=torch.int32, device="cuda")
+    first = ops.token_logprobs(x, t, top=20)
+    plan = ops.expert_sort(choices(1, 5000, 4, 64), 64)
+    ys, dy, w = gaussian(2, 20000, 256), gaussian(3, 5000, 256), gaussian(4, 5000, 4)
+    grads = ops.expert_join_grad(dy, ys, plan, w)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, ops.token_logprobs(x, t, top=20)))
+        assert all(torch.equal(a, b) for a, b in zip(grads, ops.expert_join_grad(dy, ys, plan, w)))
