@@ -1,8 +1,8 @@
 """Build the CUDA libraries in-tree for sm_100a with plain nvcc (cross-compiles without a GPU).
 
-    libcocod.so         the engine (C boundary of include/cocod.h, cocod_mlp.h, cocod_lm.h)
+    libcocod.so         the engine (C boundary of include/cocod.h, cocod_mlp.h, cocod_lm.h, cocod_adamw.h)
     libcocod_inputs.so  the device build of the synthetic-input generator (not part of the path)
-    _lm_binding.so      Python binding of the language-model operators (host code, g++)
+    _lm_binding.so      Python binding of the language-model operators and of AdamW (host code, g++)
 """
 from __future__ import annotations
 
@@ -18,7 +18,7 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 TARGETS = {
-    "libcocod.so": ["cocod_engine.cu", "cocod_mlp.cu", "cocod_lm.cu", "cocod_lm_rows.cu"],
+    "libcocod.so": ["cocod_engine.cu", "cocod_mlp.cu", "cocod_lm.cu", "cocod_lm_rows.cu", "cocod_adamw.cu"],
     "libcocod_inputs.so": ["inputs_gen.cu"],
 }
 

@@ -1,4 +1,4 @@
-// Python binding of the language-model operators (include/cocod_lm.h): looks the tensors over, allocates results and scratch through
+// Python binding of the language-model operators and of AdamW (include/cocod_lm.h, cocod_adamw.h): looks the tensors over, allocates results and scratch through
 // torch and makes the C call on torch's current stream.  Marshalling only.  The same in Python and ctypes took 5 to 8 us a
 // call, as long as the kernels of a small call themselves.
 //
@@ -16,7 +16,9 @@
 #include <sstream>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
+#include "cocod_adamw.h"
 #include "cocod_lm.h"
 
 namespace {
@@ -492,6 +494,48 @@ PyObject *token_logprobs_grad(PyObject *const *a)
     return rc == COCOD_OK && a[11] != Py_None ? given(a[11]) : code_or(rc, out);
 }
 
+// ------------------------------------------------------------------------------------------ AdamW
+// (handle, device, parameters, gradients, copies or None, gradients' factor or None): lists of n tensors; a gradient or a copy may be None
+PyObject *adamw_step(PyObject *const *a)
+{
+    auto *h = reinterpret_cast<cocod_adamw_handle *>(handle(a[0]));
+    const int64_t dev = device(a[1]);
+    const bool copied = a[4] != Py_None;
+    if (!PyList_Check(a[2]) || !PyList_Check(a[3]) || (copied && !PyList_Check(a[4]))) throw std::invalid_argument("need lists of tensors");
+    const Py_ssize_t n = PyList_GET_SIZE(a[2]);
+    if (PyList_GET_SIZE(a[3]) != n || (copied && PyList_GET_SIZE(a[4]) != n))
+        throw std::invalid_argument("grads: need " + std::to_string(n) + ", one for each parameter (None: it stays as it is)");
+    std::vector<void *> params(n), copies(copied ? n : 0);
+    std::vector<const void *> grads(n);
+    at::ScalarType types[2] = {at::kFloat, at::kFloat};
+    bool first[2] = {true, true};
+    const auto one = [&](PyObject *o, const char *name, int64_t size, int which) -> const Tensor & {
+        const Tensor &t = tensor(o, name, -1);
+        if (first[which]) types[which] = value_type(t, name), first[which] = false;
+        if (!there(t, types[which], dev) || t.numel() != size || !t.is_contiguous())
+            refuse(name, std::to_string(size) + " contiguous " + c10::toString(types[which]) + place(dev) + ", as the first one", t);
+        return t;
+    };
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const int64_t size = tensor(PyList_GET_ITEM(a[2], i), "params", -1).numel();
+        params[i] = one(PyList_GET_ITEM(a[2], i), "params", size, 0).data_ptr();
+        PyObject *g = PyList_GET_ITEM(a[3], i), *c = copied ? PyList_GET_ITEM(a[4], i) : Py_None;
+        grads[i] = g == Py_None ? nullptr : one(g, "grads", size, 1).data_ptr();
+        if (grads[i] != nullptr && grads[i] == params[i]) throw std::invalid_argument("grads: lies on its parameter");
+        if (c == Py_None) continue;
+        const Tensor &t = tensor(c, "copies", -1);
+        if (!there(t, at::kBFloat16, dev) || t.numel() != size || !t.is_contiguous()) refuse("copies", std::to_string(size) + " contiguous BFloat16" + place(dev), t);
+        copies[i] = t.data_ptr();
+    }
+    const float *factor = a[5] == Py_None ? nullptr : [&] {
+        const Tensor &t = tensor(a[5], "grad_scale", -1);
+        if (!there(t, at::kFloat, dev) || t.numel() != 1) refuse("grad_scale", "one Float" + place(dev), t);
+        return static_cast<const float *>(t.data_ptr());
+    }();
+    return PyLong_FromLong(cocod_adamw_step(h, params.data(), type_code(types[0]), grads.data(), type_code(types[1]), copied ? copies.data() : nullptr, factor,
+                                            current(dev)));
+}
+
 #define METHOD(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     METHOD("grouped_forward", rows_product<true>, 7),
@@ -510,6 +554,7 @@ PyMethodDef methods[] = {
     METHOD("expert_join_grad", expert_join_grad, 7),
     METHOD("token_logprobs", token_logprobs, 6),
     METHOD("token_logprobs_grad", token_logprobs_grad, 12),
+    METHOD("adamw_step", adamw_step, 6),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lm_binding", "Marshalling for the language-model operators (used by lm.py).", -1, methods,

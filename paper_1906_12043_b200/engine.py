@@ -85,6 +85,20 @@ SIGNATURES = {
     "cocod_vocab_loss_grad": (_i, [_vp, _i, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp,
                                    _vp, _i64, _vp, _i64, _i64, _i, _vp, _i64, _vp]),
     "cocod_grouped_wait_selftest": (_i, [_i, _i, _vp]),
+    # include/cocod_adamw.h (bound by optim.py)
+    "cocod_adamw_values": (_i64, [_i, ctypes.POINTER(_i64)]),
+    "cocod_adamw_create": (_i, [ctypes.POINTER(_vp), _i, ctypes.POINTER(_i64), ctypes.POINTER(_f), ctypes.POINTER(_i64), _i, _vp, _vp, _vp, _vp, _f,
+                                ctypes.c_double, ctypes.c_double, _f]),
+    "cocod_adamw_destroy": (_i, [_vp]),
+    "cocod_adamw_step": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _vp]),
+    "cocod_adamw_flat_step": (_i, [_vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp]),
+    "cocod_adamw_local_step": (_i, [_vp, _vp, _vp, _vp]),
+    "cocod_adamw_set_lr": (_i, [_vp, _f, _vp]),
+    "cocod_adamw_set_step": (_i, [_vp, _i64, _vp]),
+    "cocod_adamw_get_step": (_i, [_vp, ctypes.POINTER(_i64), _vp]),
+    "cocod_adamw_moments": (_i, [_vp, _vp, _vp, _vp]),
+    "cocod_adamw_load": (_i, [_vp, _vp, _vp, _vp]),
+    "cocod_adamw_launch_count": (_i64, [_vp]),
     "cocod_expert_workspace": (_i64, [_i64, _i, _i]),
     "cocod_expert_sort": (_i, [_vp, _i64, _i, _i, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "cocod_expert_rows": (_i, [_vp, _i64, _i, _i64, _vp, _i64, _vp, _vp, _i64, _i, _vp]),
