@@ -89,8 +89,7 @@ int64_t sort_span(int64_t N)
 }
 
 // ------------------------------------------------------------------------------------------ log probabilities
-constexpr int64_t MAX_WARP_ROW = 1024;
-constexpr int ROW_THREADS = 512;
+constexpr int64_t MAX_WARP_ROW = 256;
 
 template <typename T>
 int run_logprobs_warp(cocod_lm *h, const TokenRows &p, cudaStream_t s)
@@ -111,14 +110,12 @@ int row_blocks(int64_t M, int64_t V)
     return blocks;
 }
 
-template <typename T>
-int run_logprobs_row(cocod_lm *h, const TokenRows &p, cudaStream_t s)
+template <typename T, int THREADS>
+int run_logprobs_row(cocod_lm *h, const TokenRows &p, int blocks, cudaStream_t s)
 {
-    const int blocks = row_blocks(p.rows, p.vocab);
-    if (p.rows > MAX_DIM / blocks) return COCOD_ERR_TOO_LARGE;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(p.rows * blocks));
-    cfg.blockDim = dim3(ROW_THREADS);
+    cfg.gridDim = dim3((unsigned)(THREADS == 32 ? ceil_div(p.rows, ROW_BLOCK<32> / 32) : p.rows * blocks));
+    cfg.blockDim = dim3(ROW_BLOCK<THREADS>);
     cfg.stream = s;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -128,21 +125,38 @@ int run_logprobs_row(cocod_lm *h, const TokenRows &p, cudaStream_t s)
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = blocks > 1 ? 2 : 1;
-    auto kernel = p.top ? token_logprobs_row<T, ROW_THREADS, true> : token_logprobs_row<T, ROW_THREADS, false>;
+    auto kernel = p.top ? token_logprobs_row<T, THREADS, true> : token_logprobs_row<T, THREADS, false>;
     TRY_CUDA(cudaLaunchKernelEx(&cfg, kernel, p, blocks));
     return COCOD_OK;
+}
+template <typename T>
+int run_logprobs(cocod_lm *h, const TokenRows &p, cudaStream_t s)
+{
+    if (p.vocab <= MAX_WARP_ROW) return run_logprobs_warp<T>(h, p, s);
+    const int blocks = row_blocks(p.rows, p.vocab);
+    if (p.rows > MAX_DIM / blocks) return COCOD_ERR_TOO_LARGE;
+    if (blocks > 1) return run_logprobs_row<T, 512>(h, p, blocks, s);
+    // A row's threads: what follows the pass over a row costs every one of them, and leaves HBM idle unless other rows are under way (32768 x 4000, five
+    // alternatives: 86 us with 32 threads, 108 with 64; 16384 x 16000: 114 and 109, 125 with 128; 4096 x 50001 with twenty: 133 with 64, 108 and 103 with 128
+    // and 256, whose threads have less to look at again).
+    return p.vocab <= 12000 ? run_logprobs_row<T, 32>(h, p, 1, s) : p.vocab <= 24000 ? run_logprobs_row<T, 64>(h, p, 1, s)
+         : p.vocab <= 48000 ? run_logprobs_row<T, 128>(h, p, 1, s) : run_logprobs_row<T, 256>(h, p, 1, s);
 }
 
 template <typename T>
 int run_logprobs_grad(cocod_lm *h, const TokenGrads &p, cudaStream_t s)
 {
-    constexpr int N = Word<T>::N;
-    const int64_t words = ((int64_t)p.vocab + 2 * N - 2) / N, parts = ceil_div(words, GRAD_THREADS * GRAD_WORDS);
+    constexpr int N = Word<T>::N, STEP = GRAD_THREADS * GRAD_WORDS;
+    const int64_t words = ((int64_t)p.vocab + 2 * N - 2) / N, steps = ceil_div(words, STEP);
+    // a thread block takes up to eight steps of a row, as long as there are sixteen thread blocks for every SM
+    int64_t at_once = std::min<int64_t>(steps, 8);
+    while (at_once > 1 && p.rows * ceil_div(steps, at_once) < 16 * (int64_t)sm_count()) --at_once;
+    const int64_t parts = ceil_div(steps, at_once);
     if (p.rows > MAX_DIM / parts) return COCOD_ERR_TOO_LARGE;
     const bool together = (reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.out)) % 16 == 0 &&
                           (p.rows <= 1 || (p.ld - p.ld_out) * (int64_t)sizeof(T) % 16 == 0);
     TRY_CUDA(launch_dependent(true, together ? token_logprobs_grad<T, true> : token_logprobs_grad<T, false>, dim3((unsigned)(p.rows * parts)), dim3(GRAD_THREADS), 0,
-                              s, p, (int)parts));
+                              s, p, (int)parts, (int)(at_once * STEP)));
     return COCOD_OK;
 }
 
@@ -254,8 +268,7 @@ int cocod_token_logprobs(cocod_lm_handle *h, int64_t M, int64_t V, const void *l
     p.logits = logits; p.ld = ld; p.rows = M; p.vocab = (int)V; p.top = top; p.scale = scale; p.tokens = tokens; p.logp = logp; p.entropy = entropy;
     p.log_sum = log_sum; p.top_logp = top_logp; p.top_tokens = top_tokens; p.error_flag = h->flag;
     const cudaStream_t s = (cudaStream_t)stream;
-    if (V <= MAX_WARP_ROW) return es == 2 ? run_logprobs_warp<bf16>(h, p, s) : run_logprobs_warp<float>(h, p, s);
-    return es == 2 ? run_logprobs_row<bf16>(h, p, s) : run_logprobs_row<float>(h, p, s);
+    return es == 2 ? run_logprobs<bf16>(h, p, s) : run_logprobs<float>(h, p, s);
 }
 
 int cocod_token_logprobs_grad(cocod_lm_handle *h, int64_t M, int64_t V, const void *logits, int64_t ld, int type, const int32_t *tokens, float scale, int top,

@@ -2,13 +2,14 @@
 //
 // With y = scale * l, the row's reference m (its largest logit) and t = (l - m) * scale * log2(e):
 //     S1 = sum 2^t,  S2 = sum 2^t t,   Z = scale m + ln S1,  log p_v = scale (l_v - m) - ln S1,  H = ln S1 - ln 2 * S2 / S1
-// in one pass over the row: every thread holds a reference of its own, raised when a batch of its values exceeds it (S1' = c S1,
-// S2' = c (S2 + d S1) with d = old - new reference in units of t, c = 2^d), and threads are joined by the same rule at the end.
+// in one pass over the row: every thread holds a reference of its own, a value of its first batch, and takes a higher one when a batch exceeds it by so
+// much that the powers could leave fp32 (S1' = c S1, S2' = c (S2 + d S1) with d = old - new reference in units of t, c = 2^d); threads are joined by the
+// same rule at the end.
 //
-// The top alternatives cost that pass nothing.  A thread's reference is its largest value, so that the k-th largest of 64 groups' maxima
-// is a bound that at least k values reach and, as a rule, few more.  Only the threads that hold such a value look at their part of the row once
-// more (it lies in L2), and the few values found are ranked by pairs: larger first, of equal ones the lower index, by whole numbers that are in
-// the values' order (NaN above all, -0 equal to 0).
+// The top alternatives cost that pass next to nothing.  The largest of each batch of 32 values is needed there anyway; every thread keeps those of its
+// batches (up to eight, or of as many groups of batches).  The k-th largest of 64 groups' maxima is a bound that at least k values reach and, as a rule, few more.
+// Only the batches that hold such a value are looked at once more (they lie in L2), a warp for each, and the few values found are ranked by
+// pairs: larger first, of equal ones the lower index, by whole numbers that are in the values' order (NaN above all, -0 equal to 0).
 //
 // Values that are not finite: a row with a NaN or +inf has NaN for its log probabilities and its entropy; -inf is a masked entry (p = 0); a
 // row of nothing else has Z = -inf, log p = -inf, H = 0 and gradient 0.
@@ -281,29 +282,23 @@ __device__ __forceinline__ RowWords row_words(const T *x, int vocab)
     return w;
 }
 
-constexpr int TOP_GROUPS = 64, TOP_FOUND = 512;
+constexpr int TOP_GROUPS = 64, TOP_SLOTS = 8, TOP_BATCHES = 256;
+template <int THREADS> constexpr int TOP_FOUND = THREADS == 32 ? 256 : 512;
 
 template <int THREADS>
 struct LogprobsShared {
-    uint32_t group[TOP_GROUPS];              // the largest key of each group of threads
-    float s1[THREADS / 32], s2[THREADS / 32];
+    __align__(16) uint32_t group[TOP_GROUPS];  // the largest key of each group of batches
+    uint32_t slot[TOP_SLOTS][THREADS];       // the largest key of each batch (or group of batches) of a thread
+    float s1[(THREADS + 31) / 32], s2[(THREADS + 31) / 32];
     Sums part;                               // this thread block's
     uint32_t bound;
-    int found;
+    int batches, found;
     int scan[THREADS / 32];
-    unsigned long long list[TOP_FOUND];
+    int batch[TOP_BATCHES];                  // the first words of those that reach the bound
+    unsigned long long list[TOP_FOUND<THREADS>];
     unsigned long long best[MAX_ALTERNATIVES];
     unsigned long long round[THREADS / 32];
 };
-
-// A value that reaches the bound (above: exceeds it) goes into the list, as long as there is room; all are counted.
-__device__ __forceinline__ void note_found(unsigned long long *list, int *found, uint32_t key, uint32_t bound, bool above, int index)
-{
-    if (above ? key > bound : key >= bound) {
-        const int at = atomicAdd(found, 1);
-        if (at < TOP_FOUND) list[at] = ranked(key, index);
-    }
-}
 
 // The slice of a row that a thread block works on.
 template <typename T>
@@ -313,57 +308,121 @@ struct Slice {
     int from, to;                            // words that are full: word from + thread + n * THREADS is the thread's
     long long first, last;                   // values
     int ends;                                // this thread's value of a word that is not full: its index, or -1
+    int per_slot;                            // a slot is so many batches of a thread
 };
+// A batch is what a thread takes at once: BATCH values.
+constexpr int BATCH = 32;
+template <typename T> constexpr int BATCH_WORDS = BATCH / Word<T>::N;
 
-// The k best of a slice, in order, in sh.best (0 where there are fewer).  most: the thread's largest value's key (0: it had none).
-template <typename T, int THREADS>
-__device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, uint32_t most, int k)
+// A row's threads: the whole block, or, where 32 take it, one warp of a block that works on several rows.
+template <int THREADS> __device__ __forceinline__ void team_sync()
 {
-    constexpr int N = Word<T>::N;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if constexpr (THREADS == 32) __syncwarp();
+    else __syncthreads();
+}
+
+// Where the lanes of a warp that have something to put into a list put it, for N such things at a time (all lanes call; `count`: what the list holds,
+// and would hold if it were longer).
+template <int N>
+__device__ __forceinline__ void places_in(const bool (&mine)[N], int (&at)[N], int *count, int lane)
+{
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const unsigned who = __ballot_sync(~0u, mine[i]);
+        at[i] = total + __popc(who & ((1u << lane) - 1));
+        total += __popc(who);
+    }
+    if (total == 0) return;
+    int first = 0;
+    if (lane == 0) first = atomicAdd(count, total);
+    first = __shfl_sync(~0u, first, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] += first;
+}
+
+// The k best of a slice, in order, in sh.best (0 where there are fewer).  slots: of this thread.
+template <typename T, int THREADS>
+__device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, int slots, int k)
+{
+    constexpr int N = Word<T>::N, U = BATCH_WORDS<T>, WARPS = THREADS / 32;
+    const int tid = threadIdx.x % THREADS, lane = tid & 31, warp = tid >> 5;
     if (warp == 0) {                         // the k-th largest of the groups' maxima
         const uint32_t a = sh.group[lane], b = sh.group[lane + 32];
-        int before_a = 0, before_b = 0;
-#pragma unroll 8
-        for (int i = 0; i < TOP_GROUPS; ++i) {
-            const uint32_t o = sh.group[i];
-            before_a += o > a || (o == a && i < lane);
-            before_b += o > b || (o == b && i < lane + 32);
+        uint32_t more = max(a, b), less = min(a, b), most = 0;
+        for (int n = 0; n < k;) {            // (a lane whose larger one is taken has its smaller one left)
+            most = __reduce_max_sync(~0u, more);
+            const bool taken = more == most;
+            n += __popc(__ballot_sync(~0u, taken));
+            more = taken ? less : more;
+            less = taken ? 0 : less;
         }
-        if (before_a == k - 1) sh.bound = a;
-        if (before_b == k - 1) sh.bound = b;
-        if (lane == 0) sh.found = 0;
+        if (lane == 0) {
+            sh.bound = most;
+            sh.found = sh.batches = 0;
+        }
     }
-    __syncthreads();
+    team_sync<THREADS>();
     const uint32_t bound = sh.bound;
-    // Every value that reaches it (above: exceeds it), from the threads whose largest does: their warp reads their words together.
+    const int my_word = lane / N * THREADS, my_value = lane % N - s.w.lead, slot_words = s.per_slot * U * THREADS;
+    // Every value that reaches it (above: exceeds it): the batches that hold one are listed, and a warp reads each.
     auto collect = [&](bool above) {
-        unsigned who = __ballot_sync(~0u, most != 0 && (above ? most > bound : most >= bound));
-        if (s.ends >= 0) note_found(sh.list, &sh.found, key_of(load_one(s.x + s.ends)), bound, above, s.ends);
-        while (who) {
-            const int l = __ffs(who) - 1;
-            who &= who - 1;
-            for (int i = s.from + warp * 32 + l + lane * THREADS; i < s.to; i += 32 * THREADS) {
-                const uint4 r = reinterpret_cast<const uint4 *>(s.x - s.w.lead)[i];
-                float x[N];
-                values_of<T>(r, x);
-                const int at = i * N - s.w.lead;
+        {
+            bool mine[TOP_SLOTS];
+            int at[TOP_SLOTS];
 #pragma unroll
-                for (int e = 0; e < N; ++e) note_found(sh.list, &sh.found, key_of(x[e]), bound, above, at + e);
+            for (int i = 0; i < TOP_SLOTS; ++i) {
+                const uint32_t most = i < slots ? sh.slot[i][tid] : 0;
+                mine[i] = i < slots && (above ? most > bound : most >= bound);
+            }
+            places_in<TOP_SLOTS>(mine, at, &sh.batches, lane);
+#pragma unroll
+            for (int i = 0; i < TOP_SLOTS; ++i)
+                if (mine[i] && at[i] < TOP_BATCHES) sh.batch[at[i]] = s.from + tid + i * slot_words;
+        }
+        if (warp == 0) {                     // (the ends are its lanes')
+            const uint32_t key = s.ends >= 0 ? key_of(load_one(s.x + s.ends)) : 0;
+            const bool mine[1] = {s.ends >= 0 && (above ? key > bound : key >= bound)};
+            int at[1];
+            places_in<1>(mine, at, &sh.found, lane);
+            if (mine[0] && at[0] < TOP_FOUND<THREADS>) sh.list[at[0]] = ranked(key, s.ends);
+        }
+        team_sync<THREADS>();
+        const int n = min(sh.batches, TOP_BATCHES);
+        constexpr int AT_ONCE = 4;
+        for (int b0 = warp; b0 < n; b0 += AT_ONCE * WARPS) {
+            for (int g = 0; g < s.per_slot; ++g) {
+                uint32_t key[AT_ONCE];
+                int value[AT_ONCE], at[AT_ONCE];
+                bool mine[AT_ONCE];
+#pragma unroll
+                for (int a = 0; a < AT_ONCE; ++a) {
+                    const int b = b0 + a * WARPS, word = sh.batch[min(b, n - 1)] + g * (U * THREADS) + my_word;
+                    value[a] = word * N + my_value;
+                    mine[a] = b < n && word < s.to;
+                    key[a] = mine[a] ? key_of(load_one(s.x + value[a])) : 0;
+                }
+#pragma unroll
+                for (int a = 0; a < AT_ONCE; ++a) mine[a] = mine[a] && (above ? key[a] > bound : key[a] >= bound);
+                places_in<AT_ONCE>(mine, at, &sh.found, lane);
+#pragma unroll
+                for (int a = 0; a < AT_ONCE; ++a)
+                    if (mine[a] && at[a] < TOP_FOUND<THREADS>) sh.list[at[a]] = ranked(key[a], value[a]);
             }
         }
-        __syncthreads();
+        team_sync<THREADS>();
+        return sh.batches <= TOP_BATCHES && sh.found <= TOP_FOUND<THREADS>;
     };
-    collect(false);
+    bool fits = collect(false);
     int n = sh.found;
-    __syncthreads();
-    if (n > TOP_FOUND) {                     // many equal values: those above the bound ...
-        if (tid == 0) sh.found = 0;
-        __syncthreads();
-        collect(true);
+    team_sync<THREADS>();
+    if (!fits) {                             // many equal values: those above the bound ...
+        if (tid == 0) sh.found = sh.batches = 0;
+        team_sync<THREADS>();
+        fits = collect(true);
         n = sh.found;
-        __syncthreads();
-        if (n <= TOP_FOUND - MAX_ALTERNATIVES) {
+        team_sync<THREADS>();
+        if (fits && n <= TOP_FOUND<THREADS> - MAX_ALTERNATIVES) {
             // ... and of those equal to it the first ones, in the row's order
             const int need = max(0, k - n);
             int have = 0;
@@ -381,7 +440,7 @@ __device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, uint32_
                     if (lane >= d) sum += o;
                 }
                 if (lane == 31) sh.scan[warp] = sum;
-                __syncthreads();
+                team_sync<THREADS>();
                 int at = have + sum - own, all = 0;
                 for (int w = 0; w < THREADS / 32; ++w) {
                     if (w < warp) at += sh.scan[w];
@@ -394,7 +453,7 @@ __device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, uint32_
                         ++at;
                     }
                 have += all;
-                __syncthreads();
+                team_sync<THREADS>();
             }
             n += min(have, need);
         } else {
@@ -409,7 +468,7 @@ __device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, uint32_
             if (before < k) sh.best[before] = r;
         }
         for (int i = n + tid; i < k; i += THREADS) sh.best[i] = 0;
-        __syncthreads();
+        team_sync<THREADS>();
         return;
     }
     // A row made so that many values lie above the bound: one after the other.
@@ -436,20 +495,100 @@ __device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, uint32_
             best = o > best ? o : best;
         }
         if (lane == 0) sh.round[warp] = best;
-        __syncthreads();
+        team_sync<THREADS>();
         best = 0;
         for (int w = 0; w < THREADS / 32; ++w) best = sh.round[w] > best ? sh.round[w] : best;
         if (tid == 0) sh.best[j] = best;
         last = best;
-        __syncthreads();
+        team_sync<THREADS>();
     }
 }
 
-// The two sums of U words' values relative to `most`.
-template <typename T, int U>
-__device__ __forceinline__ void add_words(const uint4 (&r)[U], float most, float unit, uint64_t &s1, uint64_t &s2)
+// A thread's running sums (two of each, for the even and the odd values).
+//
+// The exponent of a value is x * unit - R with R = ref * unit rounded: one instruction for two values.  What the rounding of R left out, rho = ref * unit
+// - R, is the same factor 2^-rho for all of them and is made good when the sums go on.  Values below `low` count as `low`, whose power is 0 as
+// theirs, so that a masked entry adds 0 * (a finite number) to S2.  Both need R below 2^16 (rho below 2^-8); rows beyond that, or whose reference is no
+// number, take (x - ref) * unit (`plain`).
+struct Running {
+    float ref, r;
+    float limit;                             // what a batch's largest may reach without another reference
+    uint32_t low;                            // fp32, or two bf16
+    bool plain;
+    uint64_t s1, s2;
+};
+constexpr float FUSED_LIMIT = 65536.0f, UNIT_LIMIT = 1.0e-30f;
+// The value below which 2^(x unit - R) is 0 whatever the rounding to T: 256 below R, and a 64th of the reference for that rounding.
+template <typename T>
+__device__ __forceinline__ uint32_t low_of(float reference, float unit)
 {
-    const float ref = most == minus_inf() ? 0.0f : -most;
+    const float low = reference - 256.0f / unit - fabsf(reference) * (1.0f / 64.0f);
+    return sizeof(T) == 2 ? pack_bf16x2(low, low) : __float_as_uint(low);
+}
+template <typename T>
+__device__ __forceinline__ uint4 not_below(const uint4 &w, uint32_t low)
+{
+    if constexpr (sizeof(T) == 2) {
+        return make_uint4(max_bf16x2(w.x, low), max_bf16x2(w.y, low), max_bf16x2(w.z, low), max_bf16x2(w.w, low));
+    } else {
+        const float l = __uint_as_float(low);
+        return make_uint4(__float_as_uint(max_nan(__uint_as_float(w.x), l)), __float_as_uint(max_nan(__uint_as_float(w.y), l)),
+                          __float_as_uint(max_nan(__uint_as_float(w.z), l)), __float_as_uint(max_nan(__uint_as_float(w.w), l)));
+    }
+}
+// Both sums times 2^-shift, S2's exponents less `shift`.
+__device__ __forceinline__ void shift_sums(Running &a, float shift)
+{
+    const float c = exp2_fast(-shift);
+    a.s2 = mul2(pack2(c, c), fma2(pack2(-shift, -shift), a.s1, a.s2));
+    a.s1 = mul2(pack2(c, c), a.s1);
+}
+__device__ __forceinline__ float left_out(const Running &a, float unit) { return a.plain || a.ref == minus_inf() ? 0.0f : fmaf(a.ref, unit, -a.r); }
+template <typename T>
+__device__ __forceinline__ void refer_to(Running &a, float ref, float unit)
+{
+    a.ref = ref;
+    const float m = ref == minus_inf() ? 0.0f : ref;
+    a.r = m * unit;
+    a.limit = ref + 64.0f / unit;            // (from -inf on: every value is above)
+    a.plain = !(fabsf(a.r) <= FUSED_LIMIT && unit >= UNIT_LIMIT);
+    a.low = low_of<T>(m, unit);
+}
+template <typename T>
+__device__ __forceinline__ void raise(Running &a, float most, float unit)
+{
+    const float next = max_nan(a.ref, most), before = a.ref;
+    if (before != minus_inf()) {
+        shift_sums(a, left_out(a, unit));
+        const float d = (before - next) * unit, c = exp2_fast(d), d_ = c == 0.0f ? 0.0f : d;
+        a.s2 = mul2(pack2(c, c), fma2(pack2(d_, d_), a.s1, a.s2));
+        a.s1 = mul2(pack2(c, c), a.s1);
+    }
+    refer_to<T>(a, next, unit);
+    if (before != minus_inf()) shift_sums(a, -left_out(a, unit));
+}
+template <typename T, int U>
+__device__ __forceinline__ void add_words(Running &a, const uint4 (&r)[U], float unit)
+{
+    if (!a.plain) {
+        const uint64_t units = pack2(unit, unit), minus = pack2(-a.r, -a.r);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[Word<T>::N];
+            values_of<T>(not_below<T>(r[u], a.low), x);
+#pragma unroll
+            for (int e = 0; e < Word<T>::N; e += 2) {
+                const uint64_t d = fma2(pack2(x[e], x[e + 1]), units, minus);
+                float d0, d1;
+                unpack2(d, d0, d1);
+                const uint64_t y = pack2(exp2_fast(d0), exp2_fast(d1));
+                a.s1 = add2(a.s1, y);
+                a.s2 = fma2(y, d, a.s2);
+            }
+        }
+        return;
+    }
+    const float ref = a.ref == minus_inf() ? 0.0f : -a.ref;
     const uint64_t shift = pack2(ref, ref), factor = pack2(unit, unit);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -460,40 +599,39 @@ __device__ __forceinline__ void add_words(const uint4 (&r)[U], float most, float
             float d0, d1;
             unpack2(mul2(add2(pack2(x[e], x[e + 1]), shift), factor), d0, d1);
             const uint64_t y = pack2(exp2_fast(d0), exp2_fast(d1));
-            s1 = add2(s1, y);
-            s2 = fma2(y, pack2(fmaxf(d0, -1.0e4f), fmaxf(d1, -1.0e4f)), s2);          // (0 * -inf)
+            a.s1 = add2(a.s1, y);
+            a.s2 = fma2(y, pack2(fmaxf(d0, -1.0e4f), fmaxf(d1, -1.0e4f)), a.s2);          // (0 * -inf)
         }
     }
 }
-// A thread's running sums (two of each, for the even and the odd values).
-struct Running {
-    float most;
-    uint64_t s1, s2;
-};
-__device__ __forceinline__ void raise(Running &a, float most, float unit)
+// (the largest of the words)
+template <typename T, int U>
+__device__ __forceinline__ float take_words(Running &a, const uint4 (&r)[U], float unit)
 {
-    const float next = max_nan(a.most, most);
-    if (a.most != minus_inf()) {
-        const float d = (a.most - next) * unit, c = exp2_fast(d), d_ = c == 0.0f ? 0.0f : d;
-        a.s2 = mul2(pack2(c, c), fma2(pack2(d_, d_), a.s1, a.s2));
-        a.s1 = mul2(pack2(c, c), a.s1);
-    }
-    a.most = next;
+    const float most = largest<T, U>(r);
+    if (!(most <= a.limit)) raise<T>(a, most, unit);
+    add_words<T, U>(a, r, unit);
+    return most;
 }
 
 // `blocks` thread blocks (a cluster where there are more than one) take a row; each takes a stretch of its words.
+// 32 warps an SM: 64 registers (4096 x 65536: 89 us; with 24 or 40 warps 94 and 106).
+template <int THREADS> constexpr int ROW_BLOCK = THREADS == 32 ? 128 : THREADS;
 template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(ROW_BLOCK<THREADS>, 1024 / ROW_BLOCK<THREADS>)
 token_logprobs_row(const TokenRows p, int blocks)
 {
-    constexpr int N = Word<T>::N, U = 4;
-    __shared__ LogprobsShared<THREADS> sh;
+    constexpr int TEAMS = THREADS == 32 ? 4 : 1;
+    constexpr int N = Word<T>::N, U = BATCH_WORDS<T>;
+    __shared__ LogprobsShared<THREADS> shared[TEAMS];
+    LogprobsShared<THREADS> &sh = shared[threadIdx.x / THREADS];
     namespace cg = cooperative_groups;
     pdl_launch_dependents();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % blocks;
-    if (tid < TOP_GROUPS) sh.group[tid] = 0;
+    const int tid = threadIdx.x % THREADS, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % blocks;
+    for (int g = tid; g < TOP_GROUPS; g += THREADS) sh.group[g] = 0;
     pdl_wait();
-    const long long row = blockIdx.x / blocks;
+    const long long row = TEAMS > 1 ? (long long)blockIdx.x * TEAMS + threadIdx.x / THREADS : blockIdx.x / blocks;
+    if (row >= p.rows) return;
     const RowToken t = row_token(p.tokens, row, p.vocab, p.error_flag, tid == 0);
     if (!t.part) {                           // (the whole cluster)
         if (rank == 0) write_nothing(p, row, tid, THREADS);
@@ -509,40 +647,89 @@ token_logprobs_row(const TokenRows p, int blocks)
     s.last = min((long long)p.vocab, (long long)hi * N - s.w.lead);
     s.ends = -1;
     if (lo == 0 && lo < hi && tid >= s.w.lead && tid < N && s.w.lead > 0) s.ends = tid - s.w.lead;
-    if (hi == s.w.words && lo < hi && s.w.full_to < s.w.words && tid >= 32 && tid < 32 + N) {
-        const long long at = (long long)s.w.full_to * N - s.w.lead + (tid - 32);
+    if (hi == s.w.words && lo < hi && s.w.full_to < s.w.words && tid >= 16 && tid < 16 + N) {
+        const long long at = (long long)s.w.full_to * N - s.w.lead + (tid - 16);
         if (at < p.vocab) s.ends = (int)at;
     }
     const float own = tid == 0 && rank == 0 && t.token >= 0 ? load_one(s.x + t.token) : 0.0f;
     const float unit = p.scale * LOG2E;
-    Running a{minus_inf(), 0, 0};
+    Running a{};
+    refer_to<T>(a, minus_inf(), unit);
     const uint4 *words = reinterpret_cast<const uint4 *>(s.x - s.w.lead);
-    for (int i = s.from + tid; i < s.to; i += U * THREADS) {
-        uint4 r[U];
+    // (a thread's batches: the same number for all but the last threads; groups of them where there are more than slots)
+    const int batches = (max(0, s.to - s.from) + U * THREADS - 1) / (U * THREADS);
+    s.per_slot = (batches + TOP_SLOTS - 1) / TOP_SLOTS;
+    uint32_t even = 0, odd = 0;              // the largest keys of the even and the odd slots
+    float most = minus_inf();                // (without alternatives: of all)
+    int slots = 0;
+    float slot_most = minus_inf();
+    int i = s.from + tid, in_slot = 0;
+    const auto note = [&](float batch_most) {
+        if constexpr (TOP) {
+            slot_most = max_nan(slot_most, batch_most);
+            if (++in_slot == s.per_slot || i + U * THREADS >= s.to) {
+                const uint32_t key = key_of(slot_most);
+                sh.slot[slots][tid] = key;
+                if (slots & 1) odd = max(odd, key);
+                else even = max(even, key);
+                ++slots;
+                in_slot = 0;
+                slot_most = minus_inf();
+            }
+        } else {
+            most = max_nan(most, batch_most);
+        }
+    };
+    // bf16: the next batch is under way while one is taken (fp32, whose batches are twice the words, does without: 94 us, with it 110, for 2048 x 50001)
+    constexpr bool AHEAD = sizeof(T) == 2;
+    uint4 r[U];
+    const auto fetch = [&](int from) {
+        if (from + (U - 1) * THREADS < s.to) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) r[u] = i + u * THREADS < s.to ? words[i + u * THREADS] : all_masked<T>();
-        const float most = largest<T, U>(r);
-        if (!(most <= a.most)) raise(a, most, unit);
-        add_words<T, U>(r, a.most, unit, a.s1, a.s2);
+            for (int u = 0; u < U; ++u) r[u] = words[from + u * THREADS];
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = from + u * THREADS < s.to ? words[from + u * THREADS] : all_masked<T>();
+        }
+    };
+    if (AHEAD && i < s.to) fetch(i);
+    for (; i < s.to; i += U * THREADS) {
+        if constexpr (AHEAD) {
+            uint4 now[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) now[u] = r[u];
+            if (i + U * THREADS < s.to) fetch(i + U * THREADS);
+            note(take_words<T, U>(a, now, unit));
+        } else {
+            fetch(i);
+            note(take_words<T, U>(a, r, unit));
+        }
     }
-    const bool any = s.from + tid < s.to || s.ends >= 0;
     if (s.ends >= 0) {
-        const float x = load_one(s.x + s.ends);
-        if (!(x <= a.most)) raise(a, x, unit);
-        const float d = (x - (a.most == minus_inf() ? 0.0f : a.most)) * unit, e = exp2_fast(d);
-        a.s1 = add2(a.s1, pack2(e, 0.0f));
-        a.s2 = add2(a.s2, pack2(e * fmaxf(d, -1.0e4f), 0.0f));
+        Piece<T, true> one;
+        one.raw = all_masked<T>();
+        const T x = s.x[s.ends];
+        memcpy(&one.raw, &x, sizeof(T));
+        const uint4 r[1] = {one.raw};
+        const float value = take_words<T, 1>(a, r, unit);
+        even = max(even, key_of(value));
+        most = max_nan(most, value);
     }
+    shift_sums(a, left_out(a, unit));
     // the threads' sums, relative to the largest of all
-    const uint32_t most = any ? key_of(a.most) : 0;
-    __syncthreads();                         // (the groups are zero)
-    if (any) atomicMax(&sh.group[tid % TOP_GROUPS], most);
-    __syncthreads();
+    team_sync<THREADS>();                         // (the groups are zero)
+    if constexpr (TOP) {
+        if (even) atomicMax(&sh.group[tid % TOP_GROUPS], even);
+        if (odd) atomicMax(&sh.group[(tid + 32) % TOP_GROUPS], odd);
+    } else {
+        if (s.from + tid < s.to || s.ends >= 0) atomicMax(&sh.group[tid % TOP_GROUPS], key_of(most));
+    }
+    team_sync<THREADS>();
     const uint32_t top = __reduce_max_sync(~0u, max(sh.group[lane], sh.group[lane + 32]));
     float lo1, hi1, lo2, hi2;
     unpack2(a.s1, lo1, hi1);
     unpack2(a.s2, lo2, hi2);
-    Sums b = relative_to(Sums{a.most, lo1 + hi1, lo2 + hi2}, top ? value_of(top) : minus_inf(), unit);
+    Sums b = relative_to(Sums{a.ref, lo1 + hi1, lo2 + hi2}, top ? value_of(top) : minus_inf(), unit);
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) {
         b.s1 += __shfl_xor_sync(~0u, b.s1, d);
@@ -552,7 +739,7 @@ token_logprobs_row(const TokenRows p, int blocks)
         sh.s1[warp] = b.s1;
         sh.s2[warp] = b.s2;
     }
-    __syncthreads();
+    team_sync<THREADS>();
     if (warp == 0) {
         float s1 = lane < THREADS / 32 ? sh.s1[lane] : 0.0f, s2 = lane < THREADS / 32 ? sh.s2[lane] : 0.0f;
 #pragma unroll
@@ -564,9 +751,10 @@ token_logprobs_row(const TokenRows p, int blocks)
         b.s2 = s2;
         if (lane == 0) sh.part = b;
     }
-    if constexpr (TOP) find_top<T, THREADS>(sh, s, most, p.top);
+    if constexpr (TOP) find_top<T, THREADS>(sh, s, slots, p.top);
     if (blocks == 1) {
-        const float log_s1 = TOP || tid == 0 ? logf(TOP ? sh.part.s1 : b.s1) : 0.0f;      // (thread 0 wrote sh.part itself; find_top ends with a barrier)
+        if (tid >= max(1, p.top)) return;
+        const float log_s1 = logf(TOP ? sh.part.s1 : b.s1);      // (thread 0 wrote sh.part itself; find_top ends with a barrier)
         if (tid == 0) write_row(p, row, b, log_s1, own);
         if (TOP && tid < p.top) write_top(p, row, tid, sh.best[tid], sh.part, log_s1);
         return;
@@ -588,7 +776,7 @@ token_logprobs_row(const TokenRows p, int blocks)
         if constexpr (TOP) {
             const int n = blocks * p.top;    // (up to 8 * 32)
             for (int i = tid; i < n; i += THREADS) sh.list[i] = cluster.map_shared_rank(&sh, i / p.top)->best[i % p.top];
-            __syncthreads();
+            team_sync<THREADS>();
             for (int i = tid; i < n; i += THREADS) {
                 const unsigned long long r = sh.list[i];
                 int before = 0;
@@ -618,10 +806,47 @@ struct TokenGrads {
 };
 constexpr int GRAD_THREADS = 256, GRAD_WORDS = 4;
 
-// TOGETHER: in every row the result lies at the same alignment as the logits.
+// Eight bf16 or four fp32 gradients from as many logits.  With q = x unit - zl (zl = z log2 e rounded, rho what that left out), out = 2^q (b + g q) with all the
+// row's factors in b and g; as in the forward pass, values below `low` count as it, and `plain` rows take the formula as it stands.
+struct GradRow {
+    float scale, z, gh, base;                // plain
+    float unit, zl, b, g;
+    uint32_t low;
+    bool plain, nothing;
+};
+template <typename T>
+__device__ __forceinline__ void gradients_of(const GradRow &c, const uint4 &w, float (&v)[Word<T>::N])
+{
+    constexpr int N = Word<T>::N;
+    if (c.nothing) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = 0.0f;
+        return;
+    }
+    if (!c.plain) {
+        values_of<T>(not_below<T>(w, c.low), v);
+        const uint64_t unit = pack2(c.unit, c.unit), minus = pack2(-c.zl, -c.zl), b = pack2(c.b, c.b), g = pack2(c.g, c.g);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const uint64_t q = fma2(pack2(v[e], v[e + 1]), unit, minus);
+            float q0, q1;
+            unpack2(q, q0, q1);
+            unpack2(mul2(pack2(exp2_fast(q0), exp2_fast(q1)), fma2(q, g, b)), v[e], v[e + 1]);
+        }
+        return;
+    }
+    values_of<T>(w, v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float lp = fmaf(v[e], c.scale, -c.z);
+        v[e] = -c.scale * exp2_fast(lp * LOG2E) * fmaf(c.gh, fmaxf(lp, -1.0e4f), c.base);
+    }
+}
+
+// A thread block takes `chunk` words of one row.  TOGETHER: in every row the result lies at the same alignment as the logits.
 template <typename T, bool TOGETHER>
 __global__ void __launch_bounds__(GRAD_THREADS)
-token_logprobs_grad(const TokenGrads p, int parts)
+token_logprobs_grad(const TokenGrads p, int parts, int chunk)
 {
     constexpr int N = Word<T>::N;
     pdl_launch_dependents();
@@ -634,57 +859,49 @@ token_logprobs_grad(const TokenGrads p, int parts)
     const T *x = static_cast<const T *>(p.logits) + row * p.ld;
     T *out = static_cast<T *>(p.out) + row * p.ld_out;
     const RowWords w = row_words(x, p.vocab);
-    const int from = part * GRAD_THREADS * GRAD_WORDS, to = min(from + GRAD_THREADS * GRAD_WORDS, w.words);
+    const int from = part * chunk, to = min(from + chunk, w.words);
     if (from >= to) return;
     const RowToken t = row_token(p.tokens, row, p.vocab, p.error_flag, tid == 0 && part == 0);
-    const float z = p.log_sum[row];
-    const bool nothing = !t.part || z == minus_inf();
-    const uint4 *words = reinterpret_cast<const uint4 *>(x - w.lead);
-    uint4 r[GRAD_WORDS];
-#pragma unroll
-    for (int u = 0; u < GRAD_WORDS; ++u) {
-        const int i = from + tid + u * GRAD_THREADS;
-        if (i < to && i >= w.full_from && i < w.full_to) {
-            r[u] = words[i];
-        } else if (i < to) {
-            float v[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const long long c = (long long)i * N + e - w.lead;
-                v[e] = c >= 0 && c < p.vocab ? load_one(x + c) : 0.0f;
-            }
-            if constexpr (sizeof(T) == 2) r[u] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4 % N], v[5 % N]), pack_bf16x2(v[6 % N], v[7 % N]));
-            else r[u] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        }
-    }
+    GradRow c{};
+    c.scale = p.scale;
+    c.z = p.log_sum[row];
+    c.nothing = !t.part || c.z == minus_inf();
     // the row's few entries of their own
     const int n = p.top + 1;
     if (tid < n) {
-        int c = -1;
+        int v = -1;
         float g = 0.0f;
         if (tid == 0 && t.token >= 0 && p.d_logp != nullptr) {
-            c = t.token;
+            v = t.token;
             g = p.d_logp[row];
         }
         if (tid > 0 && t.part) {
-            c = p.top_tokens[row * p.top + tid - 1];
+            v = p.top_tokens[row * p.top + tid - 1];
             g = p.d_top[row * p.top + tid - 1];
-            if (c >= p.vocab && part == 0) atomicExch(p.error_flag, ERR_LABEL);
-            if (c < 0 || c >= p.vocab) c = -1, g = 0.0f;
+            if (v >= p.vocab && part == 0) atomicExch(p.error_flag, ERR_LABEL);
+            if (v < 0 || v >= p.vocab) v = -1, g = 0.0f;
         }
-        at[tid] = c;
+        at[tid] = v;
         given[tid] = g;
     }
+    c.gh = p.d_entropy != nullptr && t.part ? p.d_entropy[row] : 0.0f;
+    const float h = c.gh != 0.0f ? p.entropy[row] : 0.0f;
     __syncthreads();
     float every = 0.0f;
     for (int j = 0; j < n; ++j) every += given[j];
-    const float gh = p.d_entropy != nullptr && t.part ? p.d_entropy[row] : 0.0f, h = gh != 0.0f ? p.entropy[row] : 0.0f;
-    const float base = fmaf(gh, h, every);
+    c.base = fmaf(c.gh, h, every);
+    c.unit = p.scale * LOG2E;
+    c.zl = c.z * LOG2E;
+    c.plain = !(fabsf(c.zl) <= FUSED_LIMIT && c.unit >= UNIT_LIMIT && c.unit <= 1.0f / UNIT_LIMIT);
+    c.low = low_of<T>(c.z / p.scale, c.unit);
+    const float rho = fmaf(c.z, LOG2E, -c.zl), k = -p.scale * exp2_fast(-rho);
+    c.g = k * c.gh * LN2;
+    c.b = fmaf(k, c.base, -rho * c.g);
     // (the entries' own: the first of equal ones takes them all; its logit is read before anything is written)
     const long long c0 = (long long)from * N - w.lead, c1 = (long long)to * N - w.lead;
     bool special = false;
     float special_x = 0.0f, special_g = 0.0f;
-    if (tid < n && at[tid] >= 0 && at[tid] >= c0 && at[tid] < c1 && !nothing) {
+    if (tid < n && at[tid] >= 0 && at[tid] >= c0 && at[tid] < c1 && !c.nothing) {
         special = true;
         for (int j = 0; j < n; ++j) {
             if (at[j] != at[tid]) continue;
@@ -694,41 +911,55 @@ token_logprobs_grad(const TokenGrads p, int parts)
         special_x = load_one(x + at[tid]);
     }
     __syncthreads();
-    const uint64_t mul = pack2(p.scale, p.scale), sub = pack2(-z, -z), l2 = pack2(LOG2E, LOG2E), ghs = pack2(gh, gh), bases = pack2(base, base),
-                   minus = pack2(-p.scale, -p.scale);
+    const uint4 *words = reinterpret_cast<const uint4 *>(x - w.lead);
+    uint4 *out_words = reinterpret_cast<uint4 *>(out - w.lead);
+    for (int i0 = from; i0 < to; i0 += GRAD_THREADS * GRAD_WORDS) {
+        if (TOGETHER && i0 >= w.full_from && i0 + GRAD_THREADS * GRAD_WORDS <= min(to, w.full_to)) {
+            uint4 r[GRAD_WORDS];
 #pragma unroll
-    for (int u = 0; u < GRAD_WORDS; ++u) {
-        const int i = from + tid + u * GRAD_THREADS;
-        if (i >= to) break;
-        float v[N];
-        values_of<T>(r[u], v);
+            for (int u = 0; u < GRAD_WORDS; ++u) r[u] = words[i0 + tid + u * GRAD_THREADS];
 #pragma unroll
-        for (int e = 0; e < N; e += 2) {
-            float d0, d1, e0, e1;
-            const uint64_t lp = fma2(pack2(v[e], v[e + 1]), mul, sub);
-            unpack2(lp, d0, d1);
-            unpack2(mul2(lp, l2), e0, e1);
-            const uint64_t prob = mul2(pack2(exp2_fast(e0), exp2_fast(e1)), minus);
-            unpack2(mul2(prob, fma2(ghs, pack2(fmaxf(d0, -1.0e4f), fmaxf(d1, -1.0e4f)), bases)), v[e], v[e + 1]);
+            for (int u = 0; u < GRAD_WORDS; ++u) {
+                float v[N];
+                gradients_of<T>(c, r[u], v);
+                store_values<T, N>(reinterpret_cast<T *>(out_words + i0 + tid + u * GRAD_THREADS), v);
+            }
+            continue;
         }
-        if (nothing)
+#pragma unroll 1
+        for (int i = i0 + tid; i < min(i0 + GRAD_THREADS * GRAD_WORDS, to); i += GRAD_THREADS) {
+            const bool full = i >= w.full_from && i < w.full_to;
+            float v[N];
+            uint4 r = make_uint4(0, 0, 0, 0);
+            if (full) {
+                r = words[i];
+            } else {
+                T one[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = 0.0f;
-        if (TOGETHER && i >= w.full_from && i < w.full_to) {
-            store_values<T, N>(out + ((long long)i * N - w.lead), v);
-        } else {
+                for (int e = 0; e < N; ++e) {
+                    const long long j = (long long)i * N + e - w.lead;
+                    one[e] = j >= 0 && j < p.vocab ? x[j] : T(0.0f);
+                }
+                memcpy(&r, one, sizeof(r));
+            }
+            gradients_of<T>(c, r, v);
+            if (TOGETHER && full) {
+                store_values<T, N>(reinterpret_cast<T *>(out_words + i), v);
+            } else {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const long long c = (long long)i * N + e - w.lead;
-                if (c >= 0 && c < p.vocab) store_values<T, 1>(out + c, reinterpret_cast<const float (&)[1]>(v[e]));
+                for (int e = 0; e < N; ++e) {
+                    const long long j = (long long)i * N + e - w.lead;
+                    const float one[1] = {v[e]};
+                    if (j >= 0 && j < p.vocab) store_values<T, 1>(out + j, one);
+                }
             }
         }
     }
     __syncthreads();
     if (special) {
         // c (1 - p) - p (the others' + g_H (log p + H)): as exact near p = 1 as 1 - p itself
-        const float lp = fmaf(special_x, p.scale, -z), prob = exp2_fast(lp * LOG2E);
-        const float g[1] = {p.scale * (special_g * -expm1f(lp) - prob * fmaf(gh, fmaxf(lp, -1.0e4f), base - special_g))};
+        const float lp = fmaf(special_x, p.scale, -c.z), prob = exp2_fast(lp * LOG2E);
+        const float g[1] = {p.scale * (special_g * -expm1f(lp) - prob * fmaf(c.gh, fmaxf(lp, -1.0e4f), c.base - special_g))};
         store_values<T, 1>(out + at[tid], g);
     }
 }
