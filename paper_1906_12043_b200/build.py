@@ -63,7 +63,7 @@ def build_binding(force: bool = False) -> str:
         tmp = out + f".tmp{os.getpid()}"
         subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include")] +
                               [a for p in include for a in ("-isystem", p)] + [src, "-o", tmp, "-L", HERE, "-l:libcocod.so",
-                              "-L", os.path.join(home, "lib"), "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python",
+                              "-L", os.path.join(home, "lib"), "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-Wl,-rpath,$ORIGIN"])
         os.replace(tmp, out)
     return out

@@ -7,6 +7,7 @@
 //
 // What bounds them: the sort its launches, the others HBM (each row of either side is touched once).
 #pragma once
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -37,11 +38,14 @@ __device__ __forceinline__ int bucket_of(const ExpertSlots &p, int s, bool tell)
     return e < 0 || e >= p.experts_n ? p.experts_n : e;
 }
 
-// Thread block b counts slots b * span .. of each bucket into counts[b].
-static __global__ void __launch_bounds__(SORT_THREADS)
-expert_count(const ExpertSlots p, int span, int *counts)
+// Thread block b counts its slots b * span .. of each bucket.  before[b]: what the blocks before it in its cluster hold; totals[c]: what cluster c holds.
+constexpr int SORT_CLUSTER = 8;
+static __global__ void __cluster_dims__(SORT_CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS)
+expert_count(const ExpertSlots p, int span, int *before, int *totals)
 {
     extern __shared__ int sums[];
+    namespace cg = cooperative_groups;
+    auto cluster = cg::this_cluster();
     pdl_launch_dependents();
     const int buckets = p.experts_n + 1;
     for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) sums[e] = 0;
@@ -49,15 +53,37 @@ expert_count(const ExpertSlots p, int span, int *counts)
     __syncthreads();
     const long long from = (long long)blockIdx.x * span, to = min(from + span, (long long)p.total);
     for (long long s = from + threadIdx.x; s < to; s += SORT_THREADS) atomicAdd(&sums[bucket_of(p, (int)s, false)], 1);
-    __syncthreads();
-    for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) counts[(long long)blockIdx.x * buckets + e] = sums[e];
+    cluster.sync();
+    const int rank = blockIdx.x % SORT_CLUSTER;
+    for (int e = threadIdx.x; e < buckets; e += SORT_THREADS) {
+        int n[SORT_CLUSTER - 1], sum = 0;
+#pragma unroll
+        for (int r = 0; r < SORT_CLUSTER - 1; ++r) n[r] = r < rank ? cluster.map_shared_rank(sums, r)[e] : 0;
+#pragma unroll
+        for (int r = 0; r < SORT_CLUSTER - 1; ++r) sum += n[r];
+        before[blockIdx.x * buckets + e] = sum;
+        if (rank == SORT_CLUSTER - 1) totals[blockIdx.x / SORT_CLUSTER * buckets + e] = sum + sums[e];
+    }
+    cluster.sync();                          // (the others' counts are read until here)
 }
 
-// Thread block b puts its slots into place.  A warp takes a stretch of them, 32 at a time; those of one bucket find each other
-// (match), so that a slot's row is: the bucket's first row + what blocks, warps and tiles before hold of the bucket + how many lanes
-// before it.  counts: of all blocks (expert_count), not looked at where there is only one block.
+// The lanes with the same bucket, by the bits of its number (64 experts: 7 votes).
+__device__ __forceinline__ unsigned peers_of(int bucket, int bits)
+{
+    unsigned peers = ~0u;
+    for (int b = 0; b < bits; ++b) {
+        const bool one = bucket >> b & 1;
+        const unsigned ones = __ballot_sync(~0u, one);
+        peers &= one ? ones : ~ones;
+    }
+    return peers;
+}
+
+// Thread block b puts its slots into place.  A warp takes a stretch of them, 32 at a time; those of one bucket find each other,
+// so that a slot's row is: the bucket's first row + what blocks, warps and tiles before hold of the bucket + how many lanes
+// before it.  block_before, totals: expert_count's, not looked at where there is only one block.
 static __global__ void __launch_bounds__(SORT_THREADS)
-expert_place(const ExpertSlots p, int span, const int *counts, int *offsets, int *per_expert, int *order, int *place)
+expert_place(const ExpertSlots p, int span, int bits, const int *block_before, const int *totals, int *offsets, int *per_expert, int *order, int *place)
 {
     extern __shared__ int shared[];
     pdl_launch_dependents();
@@ -74,22 +100,19 @@ expert_place(const ExpertSlots p, int span, const int *counts, int *offsets, int
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) e[u] = s0 + 32 * u + lane < to ? bucket_of(p, (int)(s0 + 32 * u + lane), true) : -1;
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const unsigned peers = __match_any_sync(~0u, e[u]);
-            if (e[u] >= 0 && lane == __ffs(peers) - 1) mine[e[u]] += __popc(peers);
-            __syncwarp();
-        }
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (e[u] >= 0) atomicAdd(&mine[e[u]], 1);
     }
-    if (gridDim.x > 1) {                     // (all threads add up the blocks' counts)
-        const int parts = max(1, SORT_THREADS / buckets), blocks = gridDim.x;
+    if (gridDim.x > 1) {                     // (all threads add up the clusters' counts)
+        const int parts = max(1, SORT_THREADS / buckets), clusters = gridDim.x / SORT_CLUSTER, own = blockIdx.x / SORT_CLUSTER;
         for (int i = threadIdx.x; i < parts * buckets; i += SORT_THREADS) {
             const int e = i % buckets, part = i / buckets;
-            int sum = 0, early = 0;
-#pragma unroll 4
-            for (int b = part; b < blocks; b += parts) {
-                const int c = counts[(long long)b * buckets + e];
-                sum += c;
-                if (b < (int)blockIdx.x) early += c;
+            int sum = 0, early = part == 0 ? block_before[blockIdx.x * buckets + e] : 0;
+#pragma unroll 10
+            for (int c = part; c < clusters; c += parts) {
+                const int n = totals[c * buckets + e];
+                sum += n;
+                if (c < own) early += n;
             }
             atomicAdd(&all[e], sum);
             atomicAdd(&before[e], early);
@@ -140,7 +163,7 @@ expert_place(const ExpertSlots p, int span, const int *counts, int *offsets, int
         for (int u = 0; u < AT_ONCE; ++u) e[u] = s0 + 32 * u + lane < to ? bucket_of(p, (int)(s0 + 32 * u + lane), false) : -1;
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
-            const unsigned peers = __match_any_sync(~0u, e[u]);
+            const unsigned peers = peers_of(e[u] >= 0 ? e[u] : buckets, bits);        // (slots behind the end: a bucket of their own)
             const int s = (int)(s0 + 32 * u + lane);
             const int row = e[u] >= 0 ? mine[e[u]] + __popc(peers & ((1u << lane) - 1)) : 0;
             __syncwarp();
@@ -169,7 +192,7 @@ template <typename T, bool WIDE>
 __device__ __forceinline__ Piece<T, WIDE> load_piece(const T *p)
 {
     Piece<T, WIDE> r;
-    r.raw = *reinterpret_cast<const decltype(r.raw) *>(p);
+    r.raw = __ldg(reinterpret_cast<const decltype(r.raw) *>(p));      // (no kernel here writes what it reads)
     return r;
 }
 template <typename T, bool WIDE>
@@ -275,12 +298,13 @@ expert_rows(const ExpertRows p, const T *x, long long ldx, T *out, long long ld_
     }
 }
 
-// The way back: y[t] = sum_j w[t][j] rows[place[t][j]] (weights == nullptr: the plain sum), fp32 in the order of j.  A warp takes
-// JOIN_PIECES x 32 pieces; four rows' pieces are under way together.
+// The way back: y[t] = sum_j w[t][j] rows[place[t][j]] (weights == nullptr: the plain sum), fp32 in the order of j, in two forms with the same bits.  More than
+// two choices: a warp takes JOIN_PIECES x 32 pieces of one token, and four rows' pieces are under way together (16384 x 8 of 2048: 96 us, the other
+// form 113; x 4: 62 and 70; 4999 x 6 of 1032: 16.9 and 15.9).
 constexpr int JOIN_PIECES = 2;
 template <typename T, typename O, bool WIDE>
 __global__ void __launch_bounds__(256)
-expert_join(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
+expert_join_many(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -327,8 +351,72 @@ expert_join(const ExpertRows p, const T *rows, long long ld, const float *weight
         if (first + 32 * i < p.pieces) store_values<O, N>(y + (long long)token * ldy + (long long)(first + 32 * i) * N, sum[i]);
 }
 
+// One or two choices: a thread takes PIECES pieces of tokens' rows, 256 apart, whatever the rows' length, and ROWS rows' pieces of each are under way
+// together (65536 x 1 of 1024: 58 us, the other form 90; x 2: 89 and 99).
+template <typename T, typename O, bool WIDE, int ROWS, int PIECES>
+__global__ void __launch_bounds__(256)
+expert_join_few(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int N = Piece<T, WIDE>::N;
+    const long long first = (long long)blockIdx.x * (256 * PIECES), token0 = first / p.pieces;
+    const unsigned begin = (unsigned)(first - token0 * p.pieces) + threadIdx.x;
+    long long token[PIECES], at[PIECES];
+    float sum[PIECES][N];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const unsigned local = begin + 256 * i, ahead = local / (unsigned)p.pieces;
+        token[i] = token0 + ahead;
+        at[i] = (long long)(local - ahead * p.pieces) * N;
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[i][e] = 0.0f;
+    }
+    for (int j0 = 0; j0 < p.top; j0 += ROWS) {
+        int row[PIECES][ROWS];
+        float f[PIECES][ROWS];
+        Piece<T, WIDE> v[PIECES][ROWS];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+            for (int u = 0; u < ROWS; ++u) {
+                const bool there = token[i] < p.tokens && j0 + u < p.top;
+                row[i][u] = there ? p.place[token[i] * p.top + j0 + u] : -1;
+                f[i][u] = there && weights != nullptr ? weights[token[i] * p.top + j0 + u] : 1.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+            for (int u = 0; u < ROWS; ++u) {
+                if (row[i][u] >= p.rows || ~row[i][u] >= p.rows) {
+                    atomicExch(p.error_flag, ERR_PLACE);
+                    row[i][u] = -1;
+                }
+                if (row[i][u] >= 0) v[i][u] = load_piece<T, WIDE>(rows + row[i][u] * ld + at[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+            for (int u = 0; u < ROWS; ++u) {
+                if (row[i][u] < 0) continue;
+                float a[N];
+                widen<T, WIDE>(v[i][u], a);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[i][e] = fmaf(f[i][u], a[e], sum[i][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        if (token[i] < p.tokens) store_values<O, N>(y + token[i] * ldy + at[i], sum[i]);
+}
+
 // The gradient of that: back[place[t][j]] = w[t][j] dy[t] (0 where the slot takes no part), dw[t][j] = <dy[t], rows[place[t][j]]>.
 // WARPS warps take a token; each sum runs over a thread's pieces, the lanes and the warps, always in the same order.
+// (two rounds of loads under way together: 16384 x 8 of 2048 184 -> 175 us)
+constexpr int GRAD_AT_ONCE = 2;
 template <typename T, bool WIDE, int WARPS>
 __global__ void __launch_bounds__(256)
 expert_join_grad(const ExpertRows p, const T *dy, long long lddy, const T *rows, long long ld, const float *weights, T *back, long long ld_back, float *dw)
@@ -355,6 +443,7 @@ expert_join_grad(const ExpertRows p, const T *dy, long long lddy, const T *rows,
                 there[u] = __shfl_sync(~0u, (int)s.there, j);
                 f[u] = __shfl_sync(~0u, w, j);
             }
+#pragma unroll GRAD_AT_ONCE
             for (int c = of * 32 + lane; c < p.pieces; c += 32 * WARPS) {
                 const long long at = (long long)c * N;
                 const Piece<T, WIDE> d = load_piece<T, WIDE>(d_row + at);

@@ -55,9 +55,16 @@ int run_expert_join(cocod_lm *h, int64_t tokens, int k, int64_t D, const void *r
 {
     const ExpertRows p = expert_rows_of(h, tokens, k, D, place, Piece<T, WIDE>::N);
     unsigned blocks;
-    if (!warp_blocks(tokens, p.pieces, JOIN_PIECES, &blocks)) return COCOD_ERR_TOO_LARGE;
-    TRY_CUDA(launch_dependent(true, expert_join<T, O, WIDE>, dim3(blocks), dim3(256), 0, s, p, static_cast<const T *>(rows), (long long)ld, weights,
-                              static_cast<O *>(y), (long long)ldy));
+    if (k > 2) {
+        if (!warp_blocks(tokens, p.pieces, JOIN_PIECES, &blocks)) return COCOD_ERR_TOO_LARGE;
+        TRY_CUDA(launch_dependent(true, expert_join_many<T, O, WIDE>, dim3(blocks), dim3(256), 0, s, p, static_cast<const T *>(rows), (long long)ld, weights,
+                                  static_cast<O *>(y), (long long)ldy));
+        return COCOD_OK;
+    }
+    if (tokens > MAX_DIM * 256 / p.pieces) return COCOD_ERR_TOO_LARGE;
+    blocks = (unsigned)ceil_div(tokens * p.pieces, k > 1 ? 512 : 1024);
+    TRY_CUDA(launch_dependent(true, k > 1 ? expert_join_few<T, O, WIDE, 2, 2> : expert_join_few<T, O, WIDE, 1, 4>, dim3(blocks), dim3(256), 0, s, p,
+                              static_cast<const T *>(rows), (long long)ld, weights, static_cast<O *>(y), (long long)ldy));
     return COCOD_OK;
 }
 template <typename T, bool WIDE, int WARPS>
@@ -73,33 +80,43 @@ int run_expert_join_grad(cocod_lm *h, int64_t tokens, int k, int64_t D, const vo
                          const float *weights, void *back, int64_t ld_back, float *dw, cudaStream_t s)
 {
     const ExpertRows p = expert_rows_of(h, tokens, k, D, place, Piece<T, WIDE>::N);
-    // as many warps as have a piece for each lane
-    if (p.pieces <= 32) return run_join_grad<T, WIDE, 1>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
-    if (p.pieces <= 64) return run_join_grad<T, WIDE, 2>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
-    if (p.pieces <= 128) return run_join_grad<T, WIDE, 4>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    // 4999 x 6 of 129 pieces: one, two, four, eight warps 33.8, 32.3, 37.4, 40.5 us; 30000 x 2 of 64: one, two 39, 50; 16384 x 8 of 256: 196, 186, 188, 184
+    if (p.pieces <= 64) return run_join_grad<T, WIDE, 1>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    if (p.pieces <= 192) return run_join_grad<T, WIDE, 2>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
     return run_join_grad<T, WIDE, 8>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
 }
 
-// How the slots are divided among thread blocks: a multiple of SORT_THREADS for each.  One block needs no count before it.
-constexpr int64_t SORT_ALONE = 4096;
-int64_t sort_span(int64_t N)
+// How the slots are divided among thread blocks: a multiple of SORT_THREADS for each.  One block needs no count before it (2048 slots in 4.3 us, in several
+// blocks 5); several come in whole clusters.
+constexpr int64_t SORT_ALONE = 2048, SORT_LEAST = 1024;
+struct SortPlan {
+    int64_t blocks, span;
+};
+SortPlan sort_plan(int64_t N)
 {
-    const int64_t blocks = N <= SORT_ALONE ? 1 : std::max(1, sm_count());
-    return std::max<int64_t>(1, ceil_div(ceil_div(N, blocks), SORT_THREADS)) * SORT_THREADS;
+    if (N <= SORT_ALONE) return SortPlan{1, std::max<int64_t>(1, ceil_div(N, SORT_THREADS)) * SORT_THREADS};
+    const int64_t most = std::max<int64_t>(1, sm_count() / SORT_CLUSTER), clusters = std::min(most, ceil_div(N, SORT_LEAST * SORT_CLUSTER));
+    const int64_t blocks = clusters * SORT_CLUSTER;
+    return SortPlan{blocks, ceil_div(ceil_div(N, blocks), SORT_THREADS) * SORT_THREADS};
 }
 
 // ------------------------------------------------------------------------------------------ log probabilities
-constexpr int64_t MAX_WARP_ROW = 256;
+constexpr int64_t SHORT_ROW = 256;
 
-template <typename T>
-int run_logprobs_warp(cocod_lm *h, const TokenRows &p, cudaStream_t s)
+template <typename T, int LANES, int NR>
+int launch_short(cocod_lm *h, const TokenRows &p, cudaStream_t s)
 {
-    const dim3 grid((unsigned)ceil_div(p.rows, 8));
-    const int n = (p.vocab + 31) / 32;
-    auto kernel = n <= 1 ? token_logprobs_warp<T, 1> : n <= 2 ? token_logprobs_warp<T, 2> : n <= 4 ? token_logprobs_warp<T, 4> : n <= 8 ? token_logprobs_warp<T, 8>
-                : n <= 16 ? token_logprobs_warp<T, 16> : token_logprobs_warp<T, 32>;
-    TRY_CUDA(launch_dependent(true, kernel, grid, dim3(256), 0, s, p));
+    TRY_CUDA(launch_dependent(true, token_logprobs_short<T, LANES, NR>, dim3((unsigned)ceil_div(p.rows, 256 / LANES)), dim3(256), 0, s, p));
     return COCOD_OK;
+}
+template <typename T>
+int run_logprobs_short(cocod_lm *h, const TokenRows &p, cudaStream_t s)
+{
+    // (65536 x 64, two alternatives: half a warp 13.6 us, a whole one 18; 16384 x 64, four: 6.5 and 6.2)
+    if (p.vocab <= 16) return launch_short<T, 8, 2>(h, p, s);
+    if (p.vocab <= 32) return launch_short<T, 16, 2>(h, p, s);
+    if (p.vocab <= 64) return p.top <= 2 ? launch_short<T, 16, 4>(h, p, s) : launch_short<T, 32, 2>(h, p, s);
+    return p.vocab <= 128 ? launch_short<T, 32, 4>(h, p, s) : launch_short<T, 32, 8>(h, p, s);
 }
 
 // Thread blocks for a row: one while there are rows for every SM; for fewer rows up to eight, each with at least 2048 values.
@@ -132,7 +149,7 @@ int run_logprobs_row(cocod_lm *h, const TokenRows &p, int blocks, cudaStream_t s
 template <typename T>
 int run_logprobs(cocod_lm *h, const TokenRows &p, cudaStream_t s)
 {
-    if (p.vocab <= MAX_WARP_ROW) return run_logprobs_warp<T>(h, p, s);
+    if (p.vocab <= SHORT_ROW) return run_logprobs_short<T>(h, p, s);
     const int blocks = row_blocks(p.rows, p.vocab);
     if (p.rows > MAX_DIM / blocks) return COCOD_ERR_TOO_LARGE;
     if (blocks > 1) return run_logprobs_row<T, 512>(h, p, blocks, s);
@@ -179,8 +196,8 @@ extern "C" {
 int64_t cocod_expert_workspace(int64_t T, int k, int E)
 {
     if (T < 0 || k < 1 || k > MAX_CHOICES || T > MAX_DIM / k || E < 1 || E > COCOD_LM_MAX_GROUPS) return COCOD_ERR_INVALID;
-    const int64_t blocks = ceil_div(T * k, sort_span(T * k));
-    return blocks > 1 ? blocks * (E + 1) * 4 : 0;
+    const int64_t blocks = sort_plan(T * k).blocks;
+    return blocks > 1 ? (blocks + blocks / SORT_CLUSTER) * (E + 1) * 4 : 0;
 }
 
 int cocod_expert_sort(cocod_lm_handle *h, int64_t T, int k, int E, const int32_t *experts, int64_t ld, int32_t *offsets, int32_t *counts, int32_t *order,
@@ -201,14 +218,16 @@ int cocod_expert_sort(cocod_lm_handle *h, int64_t T, int k, int E, const int32_t
         }
         configured[dev] = true;
     }
-    const int64_t N = T * k, span = sort_span(N), blocks = std::max<int64_t>(1, ceil_div(N, span));
+    const int64_t N = T * k;
+    const SortPlan plan = sort_plan(N);
     ExpertSlots p{};
     p.experts = experts; p.ld = T > 1 ? ld : k; p.top = k; p.total = (int)N; p.experts_n = E; p.error_flag = h->flag;
-    int *sums = static_cast<int *>(workspace);
+    int *before = static_cast<int *>(workspace), *totals = before + plan.blocks * (E + 1);
+    const dim3 grid((unsigned)plan.blocks);
     const cudaStream_t s = (cudaStream_t)stream;
-    if (blocks > 1) TRY_CUDA(launch_dependent(true, expert_count, dim3((unsigned)blocks), dim3(SORT_THREADS), (E + 1) * 4, s, p, (int)span, sums));
-    TRY_CUDA(launch_dependent(true, expert_place, dim3((unsigned)blocks), dim3(SORT_THREADS), (SORT_WARPS + 2) * (E + 1) * 4, s, p, (int)span,
-                              static_cast<const int *>(sums), offsets, counts, order, place));
+    if (plan.blocks > 1) TRY_CUDA(launch_dependent(true, expert_count, grid, dim3(SORT_THREADS), (E + 1) * 4, s, p, (int)plan.span, before, totals));
+    TRY_CUDA(launch_dependent(true, expert_place, grid, dim3(SORT_THREADS), (SORT_WARPS + 2) * (E + 1) * 4, s, p, (int)plan.span,
+                              32 - __builtin_clz((unsigned)E + 1), static_cast<const int *>(before), static_cast<const int *>(totals), offsets, counts, order, place));
     return COCOD_OK;
 }
 

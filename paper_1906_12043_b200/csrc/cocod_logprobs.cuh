@@ -121,35 +121,36 @@ __device__ __forceinline__ void write_top(const TokenRows &p, long long row, int
     p.top_tokens[row * p.top + j] = index_of(r);
 }
 
-// ------------------------------------------------------------------------------------------ short rows: a warp for each
-// The row (at most 32 * NR entries) lies in the lanes' registers: lane + 32 i is value i.
-template <typename T, int NR>
+// ------------------------------------------------------------------------------------------ short rows: LANES lanes for each
+// The row (at most LANES * NR entries) lies in the lanes' registers: lane + LANES * i is value i.
+template <typename T, int LANES, int NR>
 __global__ void __launch_bounds__(256)
-token_logprobs_warp(const TokenRows p)
+token_logprobs_short(const TokenRows p)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x % LANES;
+    const unsigned mask = LANES == 32 ? ~0u : ((1u << (LANES % 32)) - 1) << ((threadIdx.x & 31) / LANES * LANES);
+    const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     if (row >= p.rows) return;
-    const RowToken t = row_token(p.tokens, row, p.vocab, p.error_flag, lane == 0);
-    if (!t.part) {
-        write_nothing(p, row, lane, 32);
-        return;
-    }
     const T *x = static_cast<const T *>(p.logits) + row * p.ld;
-    const float own = t.token >= 0 ? load_one(x + t.token) : 0.0f;
     float v[NR];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) v[i] = lane + 32 * i < p.vocab ? load_one(x + lane + 32 * i) : minus_inf();
+    for (int i = 0; i < NR; ++i) v[i] = lane + LANES * i < p.vocab ? load_one(x + lane + LANES * i) : minus_inf();
+    const RowToken t = row_token(p.tokens, row, p.vocab, p.error_flag, lane == 0);
+    if (!t.part) {
+        write_nothing(p, row, lane, LANES);
+        return;
+    }
+    const float own = t.token >= 0 && lane == 0 ? load_one(x + t.token) : 0.0f;
     uint32_t key[NR], best = 0;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-        key[i] = lane + 32 * i < p.vocab ? key_of(v[i]) : 0;
+        key[i] = lane + LANES * i < p.vocab ? key_of(v[i]) : 0;
         best = max(best, key[i]);
     }
     Sums a{0.0f, 0.0f, 0.0f};
-    a.most = value_of(__reduce_max_sync(~0u, best));
+    a.most = value_of(__reduce_max_sync(mask, best));
     const float unit = p.scale * LOG2E, m = a.most == minus_inf() ? 0.0f : a.most;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
@@ -158,34 +159,32 @@ token_logprobs_warp(const TokenRows p)
         a.s2 = fmaf(e, fmaxf(d, -1.0e4f), a.s2);          // (0 * -inf)
     }
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) {
-        a.s1 += __shfl_xor_sync(~0u, a.s1, d);
-        a.s2 += __shfl_xor_sync(~0u, a.s2, d);
+    for (int d = LANES / 2; d > 0; d /= 2) {
+        a.s1 += __shfl_xor_sync(mask, a.s1, d);
+        a.s2 += __shfl_xor_sync(mask, a.s2, d);
     }
     const float log_s1 = logf(a.s1);
     if (lane == 0) write_row(p, row, a, log_s1, own);
     // one after the other: the lanes' largest, the lowest index that has it, and its lane takes it out
-    unsigned long long mine = 0;
     for (int j = 0; j < p.top; ++j) {
-        const uint32_t most = __reduce_max_sync(~0u, best);
-        int at = 0x7fffffff;
+        const uint32_t most = __reduce_max_sync(mask, best);
+        unsigned at = 0x7fffffff;
         if (best == most) {
 #pragma unroll
             for (int i = NR - 1; i >= 0; --i)
-                if (key[i] == most) at = lane + 32 * i;
+                if (key[i] == most) at = lane + LANES * i;
         }
-        const int first = (int)__reduce_min_sync(~0u, (unsigned)at);
-        if (lane == j) mine = ranked(most, first);
+        const unsigned first = __reduce_min_sync(mask, at);
         if (at == first) {
+            write_top(p, row, j, ranked(most, (int)first), a, log_s1);
             best = 0;
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
-                if (lane + 32 * i == first) key[i] = 0;
+                if (lane + LANES * i == (int)first) key[i] = 0;
                 best = max(best, key[i]);
             }
         }
     }
-    if (lane < p.top) write_top(p, row, lane, mine, a, log_s1);
 }
 
 // ------------------------------------------------------------------------------------------ long rows: one to eight thread blocks for each
@@ -777,9 +776,10 @@ token_logprobs_row(const TokenRows p, int blocks)
             const int n = blocks * p.top;    // (up to 8 * 32)
             for (int i = tid; i < n; i += THREADS) sh.list[i] = cluster.map_shared_rank(&sh, i / p.top)->best[i % p.top];
             team_sync<THREADS>();
-            for (int i = tid; i < n; i += THREADS) {
+            for (int i = tid; i < n; i += THREADS) {      // (by pairs: a search in the blocks' ordered lists takes 1 us longer)
                 const unsigned long long r = sh.list[i];
                 int before = 0;
+#pragma unroll 8
                 for (int o = 0; o < n; ++o) before += sh.list[o] > r;
                 if (r != 0 && before < p.top) write_top(p, row, before, r, all, log_s1);
             }

@@ -8,6 +8,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/MemoryOverlap.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -121,7 +122,17 @@ at::ScalarType result_type(PyObject *out, int64_t code, at::ScalarType usual)
     return type;
 }
 inline int type_code(at::ScalarType t) { return t == at::kFloat ? COCOD_F32 : COCOD_BF16; }
-inline Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type) { return at::empty(shape, like.options().dtype(type)); }
+// (the allocation itself, without the dispatcher's way to it)
+inline Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type) { return at::detail::empty_cuda(shape, type, like.device(), std::nullopt); }
+// A contiguous part of a buffer, `at` bytes behind its start, as a tensor of its own.
+inline Tensor part_of(const Tensor &buffer, int64_t at, at::IntArrayRef shape, at::ScalarType type)
+{
+    const caffe2::TypeMeta meta = c10::scalarTypeToTypeMeta(type);
+    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(buffer.storage()), buffer.key_set(), meta);
+    t.unsafeGetTensorImpl()->set_storage_offset(at / (int64_t)meta.itemsize());
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+    return t;
+}
 
 inline cocod_stream_t current(int64_t device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 inline PyObject *code_or(int rc, const Tensor &t) { return rc == COCOD_OK ? THPVariable_Wrap(t) : PyLong_FromLong(rc); }
@@ -349,14 +360,13 @@ PyObject *expert_sort(PyObject *const *a)
         throw std::invalid_argument("experts: 1 to " + std::to_string(COCOD_LM_MAX_CHOICES) + " choices among 1 to " + std::to_string(COCOD_LM_MAX_GROUPS) + " experts");
     const int64_t bytes = cocod_expert_workspace(T, (int)k, (int)E);
     if (bytes < 0) return PyLong_FromLong((long)bytes);
-    const Tensor all = fresh(e, {2 * E + 1 + 2 * T * k + bytes / 4}, at::kInt);
+    const int64_t N = T * k, at[5] = {0, E + 1, 2 * E + 1, 2 * E + 1 + N, 2 * E + 1 + 2 * N};      // offsets, counts, order, place, scratch
+    const Tensor all = fresh(e, {at[4] + bytes / 4}, at::kInt);
     int32_t *p = static_cast<int32_t *>(all.data_ptr());
-    const int64_t N = T * k;
-    const int rc = cocod_expert_sort(h, T, (int)k, (int)E, static_cast<const int32_t *>(m.data), m.ld, p, p + E + 1, p + 2 * E + 1, p + 2 * E + 1 + N,
-                                     p + 2 * E + 1 + 2 * N, bytes, current(dev));
+    const int rc = cocod_expert_sort(h, T, (int)k, (int)E, static_cast<const int32_t *>(m.data), m.ld, p, p + at[1], p + at[2], p + at[3], p + at[4], bytes, current(dev));
     if (rc != COCOD_OK) return PyLong_FromLong(rc);
-    const auto part = [&](int64_t from, at::IntArrayRef size, at::IntArrayRef strides) { return THPVariable_Wrap(all.as_strided(size, strides, from)); };
-    return Py_BuildValue("(NNNN)", part(0, {E + 1}, {1}), part(E + 1, {E}, {1}), part(2 * E + 1, {N}, {1}), part(2 * E + 1 + N, {T, k}, {k, 1}));
+    const auto part = [&](int i, at::IntArrayRef shape) { return THPVariable_Wrap(part_of(all, 4 * at[i], shape, at::kInt)); };
+    return Py_BuildValue("(NNNN)", part(0, {E + 1}), part(1, {E}), part(2, {N}), part(3, {T, k}));
 }
 
 // (handle, device, x, place, out or None)
@@ -444,16 +454,17 @@ PyObject *token_logprobs(PyObject *const *a)
     const Matrix m = any_rows(x, "logits", M, V, type, dev);
     const int32_t *tokens = given_tokens(a[3], M, dev);
     const float scale = number(a[5]);
-    const Tensor all = fresh(x, {3, M}, at::kFloat);
+    const int64_t padded = (M + 3) / 4 * 4, wide = (M * top + 3) / 4 * 4;          // (parts at multiples of 16 bytes)
+    const Tensor all = fresh(x, {3 * padded + 2 * wide}, at::kFloat);
     float *p = static_cast<float *>(all.data_ptr());
-    Tensor top_logp, top_tokens;
-    if (top) top_logp = fresh(x, {M, top}, at::kFloat), top_tokens = fresh(x, {M, top}, at::kInt);
-    const int rc = cocod_token_logprobs(h, M, V, m.data, m.ld, type_code(type), tokens, scale, (int)top, p, p + M, p + 2 * M,
-                                        top ? static_cast<float *>(top_logp.data_ptr()) : nullptr, top ? static_cast<int32_t *>(top_tokens.data_ptr()) : nullptr, current(dev));
+    const int rc = cocod_token_logprobs(h, M, V, m.data, m.ld, type_code(type), tokens, scale, (int)top, p, p + padded, p + 2 * padded, p + 3 * padded,
+                                        reinterpret_cast<int32_t *>(p + 3 * padded + wide), current(dev));
     if (rc != COCOD_OK) return PyLong_FromLong(rc);
-    const auto part = [&](int64_t i) { return THPVariable_Wrap(all.as_strided({M}, {1}, i * M)); };
-    return Py_BuildValue("(NNNNN)", tokens ? part(0) : given(Py_None), part(1), part(2), top ? THPVariable_Wrap(top_logp) : given(Py_None),
-                         top ? THPVariable_Wrap(top_tokens) : given(Py_None));
+    const auto part = [&](bool there, int64_t at, at::IntArrayRef shape, at::ScalarType kind) {
+        return there ? THPVariable_Wrap(part_of(all, 4 * at, shape, kind)) : given(Py_None);
+    };
+    return Py_BuildValue("(NNNNN)", part(tokens != nullptr, 0, {M}, at::kFloat), part(true, padded, {M}, at::kFloat), part(true, 2 * padded, {M}, at::kFloat),
+                         part(top > 0, 3 * padded, {M, top}, at::kFloat), part(top > 0, 3 * padded + wide, {M, top}, at::kInt));
 }
 
 // (handle, device, logits, tokens or None, scale, top_tokens or None, log_sum, entropy or None, d_logp or None, d_entropy or None, d_top or None,

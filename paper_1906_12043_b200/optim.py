@@ -88,9 +88,9 @@ class _Moments:
 
     def moments(self):
         """(m, v) in float32, the tensors one behind the other, each starting at a multiple of 128 values.  With 32 bits the state itself, with 8 a copy."""
-        stream = self._stream()
         if self.state_bits == 32:
             return tuple(self._state)
+        stream = self._stream()
         m, v = (torch.empty(self.values, dtype=torch.float32, device=self._state[0].device) for _ in range(2))
         self._ck(self._lib.cocod_adamw_moments(self._h, m.data_ptr(), v.data_ptr(), stream), "cocod_adamw_moments")
         return m, v
