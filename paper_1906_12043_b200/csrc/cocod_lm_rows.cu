@@ -80,9 +80,12 @@ int run_expert_join_grad(cocod_lm *h, int64_t tokens, int k, int64_t D, const vo
                          const float *weights, void *back, int64_t ld_back, float *dw, cudaStream_t s)
 {
     const ExpertRows p = expert_rows_of(h, tokens, k, D, place, Piece<T, WIDE>::N);
-    // 4999 x 6 of 129 pieces: one, two, four, eight warps 33.8, 32.3, 37.4, 40.5 us; 30000 x 2 of 64: one, two 39, 50; 16384 x 8 of 256: 196, 186, 188, 184
+    // Warps of a token: the most whose lanes have a piece in four of five places.  16384 x 8 of 256 pieces: one, two, four, eight warps 196, 186, 188, 184 us; 4999 x 6
+    // of 129: 33.8, 32.3, 37.4, 40.5; 30000 x 2 of 64: one, two 39, 50.
+    const auto filled = [&](int warps) { return p.pieces * 5ll >= 4 * ceil_div(p.pieces, 32 * warps) * 32 * warps; };
     if (p.pieces <= 64) return run_join_grad<T, WIDE, 1>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
-    if (p.pieces <= 192) return run_join_grad<T, WIDE, 2>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    if (p.pieces < 256 || (!filled(8) && !filled(4))) return run_join_grad<T, WIDE, 2>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    if (!filled(8)) return run_join_grad<T, WIDE, 4>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
     return run_join_grad<T, WIDE, 8>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
 }
 
