@@ -1,7 +1,7 @@
 #!/usr/bin/env python
 """K workers train a next-token model with CoCoD-SGD on one GPU, every gradient formed by the language-model operators.
 
-    python examples/lm_workers.py [--workers 8] [--vocab 2048] [--width 512] [--rounds 60]
+    python examples/lm_workers.py [--workers 8] [--vocab 2048] [--width 512] [--rounds 60] [--optimizer adamw --lr 0.001 --bits 8]
 
 The model: a fixed embedding of the token before, two ReLU layers, a vocabulary.  Every worker has weights and a mini-batch of
 its own, of its own size (Algorithm 1's M_i).  One local step:
@@ -10,7 +10,7 @@ its own, of its own size (Algorithm 1's M_i).  One local step:
     loss       softmax cross-entropy over the vocabulary and its gradient (vocab_loss_grad), straight into the K x P gradients
     backward   the ReLU's gate from the checkpoint (act_relu_grad), the weight gradient from the checkpoint
                (grouped_weight_grad), the gradient of the layer's input (grouped_input_grad)
-    update     Engine.local_step on the K x P gradients, which also keeps the bf16 copy that the products read
+    update     Engine.local_step on the K x P gradients, which also keeps the bf16 copy that the products read (or EngineAdamW.local_step)
 
 and a round is k of them between comm_begin and comm_end.  The text is a Markov chain: every token is followed by one of four
 others, so that no model gets below log 4 = 1.386.
@@ -27,14 +27,14 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
 
-from paper_1906_12043_b200 import engine as E, lm  # noqa: E402
+from paper_1906_12043_b200 import engine as E, lm, optim  # noqa: E402
 
 FOLLOWERS = 4
 
 
 class Workers:
-    def __init__(self, sizes, vocab, embed, width, lr, mu, seed=0):
-        """sizes: tokens in each worker's mini-batch."""
+    def __init__(self, sizes, vocab, embed, width, lr, mu, seed=0, adamw_bits=0):
+        """sizes: tokens in each worker's mini-batch.  adamw_bits: 0 (momentum SGD), or AdamW with its moments in 8 or 32 bits."""
         self.K, self.vocab, self.embed, self.width = len(sizes), vocab, embed, width
         self.shapes = [(width, embed), (width, width), (vocab, width)]
         self.starts, at = [], 0
@@ -52,6 +52,10 @@ class Workers:
         self.engine.set_option(E.OPT_BF16_SHADOW, 1)
         self.engine.set_params(x0.cuda())
         self.engine.set_batch_sizes([float(s) for s in sizes])
+        self.local_step = self.engine.local_step
+        if adamw_bits:
+            self.opt = optim.EngineAdamW(self.engine, [(n * k, 0.01) for n, k in self.shapes], lr=lr, betas=(0.9, 0.95), state_bits=adamw_bits)
+            self.local_step = self.opt.local_step
         self.ops = lm.LMOps()
         self.grads = torch.zeros(self.K, self.P, device="cuda")
         ends = torch.tensor([0] + list(sizes)).cumsum(0)
@@ -89,7 +93,7 @@ class Workers:
         self.engine.comm_begin(side)
         for _ in range(k):
             losses.append(self.gradients(*self.batch()))
-            self.engine.local_step(self.grads)
+            self.local_step(self.grads)
         self.engine.comm_end()
         return torch.stack(losses)
 
@@ -104,9 +108,11 @@ def main():
     ap.add_argument("--rounds", type=int, default=60)
     ap.add_argument("--k", type=int, default=4, help="local steps in a round")
     ap.add_argument("--lr", type=float, default=0.5)
+    ap.add_argument("--optimizer", default="sgd", choices=("sgd", "adamw"))
+    ap.add_argument("--bits", type=int, default=8, choices=(8, 32), help="of AdamW's moments")
     a = ap.parse_args()
     sizes = [a.tokens // (1 + i % 2) for i in range(a.workers)]
-    w = Workers(sizes, a.vocab, a.embed, a.width, a.lr, 0.9)
+    w = Workers(sizes, a.vocab, a.embed, a.width, a.lr, 0.9, adamw_bits=a.bits if a.optimizer == "adamw" else 0)
     side = torch.cuda.Stream(priority=-1)
     print(f"{a.workers} workers of {sum(n * k for n, k in w.shapes):,} parameters, {sum(sizes)} tokens a step")
     for r in range(a.rounds):
