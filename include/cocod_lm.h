@@ -163,7 +163,7 @@ int cocod_expert_join_grad(cocod_lm_handle *h, int64_t T, int k, int64_t D, cons
                            const float *weights, void *drows, int64_t ld_drows, float *dweights, int type, cocod_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
- * Log probabilities of given tokens.  logits: M x V (type COCOD_BF16 or COCOD_F32, any row stride and alignment); y = scale * logits, scale > 0;
+ * Log probabilities of given tokens.  logits: M x V (type COCOD_BF16 or COCOD_F32, any row stride and alignment); y = scale * logits, 1e-30 <= scale <= 1e30;
  *     log_sum[r] = log sum_v exp y[r][v],   log p = y - log_sum,   logp[r] = log p[r][tokens[r]],
  *     entropy[r] = - sum_v p log p,   top_tokens[r][j]: the token with the j-th largest logit (of equal ones the lower first), top_logp: its log p.
  * tokens: M int32, or NULL: no tokens, logp is not written.  A row whose token is negative takes no part whatever it holds: its results are 0, its

@@ -182,8 +182,8 @@ int run_logprobs_grad(cocod_lm *h, const TokenGrads &p, cudaStream_t s)
 
 bool good_tokens(const cocod_lm *h, int64_t M, int64_t V, const void *logits, int64_t ld, int es, const int32_t *tokens, float scale, int top)
 {
-    return h && es && M >= 0 && M <= MAX_DIM && V >= 1 && V <= MAX_DIM && good_matrix(logits, ld, V, M, es) && aligned_to(tokens, 4) && scale > 0.0f &&
-           scale <= 3.0e38f && top >= 0 && top <= MAX_ALTERNATIVES && top <= V;
+    return h && es && M >= 0 && M <= MAX_DIM && V >= 1 && V <= MAX_DIM && good_matrix(logits, ld, V, M, es) && aligned_to(tokens, 4) && scale >= 1.0e-30f &&
+           scale <= 1.0e30f && top >= 0 && top <= MAX_ALTERNATIVES && top <= V;
 }
 bool words_aligned(std::initializer_list<const void *> all)
 {

@@ -463,7 +463,7 @@ PyObject *token_logprobs(PyObject *const *a)
     const auto part = [&](bool there, int64_t at, at::IntArrayRef shape, at::ScalarType kind) {
         return there ? THPVariable_Wrap(part_of(all, 4 * at, shape, kind)) : given(Py_None);
     };
-    return Py_BuildValue("(NNNNN)", part(tokens != nullptr, 0, {M}, at::kFloat), part(true, padded, {M}, at::kFloat), part(true, 2 * padded, {M}, at::kFloat),
+    return Py_BuildValue("(NNNNN)", part(a[3] != Py_None, 0, {M}, at::kFloat), part(true, padded, {M}, at::kFloat), part(true, 2 * padded, {M}, at::kFloat),
                          part(top > 0, 3 * padded, {M, top}, at::kFloat), part(top > 0, 3 * padded + wide, {M, top}, at::kInt));
 }
 
@@ -482,12 +482,12 @@ PyObject *token_logprobs_grad(PyObject *const *a)
     const auto row_values = [&](PyObject *o, const char *name) {
         return o == Py_None ? nullptr : static_cast<const float *>(vector(tensor(o, name, 1), name, M, at::kFloat, dev));
     };
-    if (a[8] != Py_None && !tokens) throw std::invalid_argument("d_logp: there are no tokens whose log probabilities it could belong to");
+    if (a[8] != Py_None && a[3] == Py_None) throw std::invalid_argument("d_logp: there are no tokens whose log probabilities it could belong to");
     if (a[9] != Py_None && a[7] == Py_None) throw std::invalid_argument("d_entropy: the entropy is needed");
     if (a[10] != Py_None && a[5] == Py_None) throw std::invalid_argument("d_top: the top tokens are needed");
     const float *log_sum = row_values(a[6], "log_sum"), *entropy = row_values(a[7], "entropy"), *d_logp = row_values(a[8], "d_logp"),
                 *d_entropy = row_values(a[9], "d_entropy"), *d_top = nullptr;
-    if (!log_sum && M > 0) throw std::invalid_argument("log_sum: need a tensor");
+    if (a[6] == Py_None) throw std::invalid_argument("log_sum: need a tensor");
     const int32_t *top_tokens = nullptr;
     int64_t top = 0;
     if (a[10] != Py_None) {

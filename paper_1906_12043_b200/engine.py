@@ -172,6 +172,7 @@ class Engine:
         if not torch.cuda.is_available():
             raise RuntimeError("the CoCoD-SGD engine needs a CUDA device (there is no CPU fallback)")
         self.K, self.P = int(K), int(P)
+        self._compute = 0                      # address of the compute stream (0: the legacy default stream)
         self._lib = load()
         self._h = _vp()
         rc = self._lib.cocod_create(ctypes.byref(self._h), self.K, self.P, lr, mu, wd)
@@ -249,6 +250,7 @@ class Engine:
     # -- around it
     def set_stream(self, stream):
         self._ck(self._lib.cocod_set_stream(self._h, _stream(stream)), "cocod_set_stream")
+        self._compute = _stream(stream) or 0
 
     def set_params(self, x0):
         self._ck(self._lib.cocod_set_params(self._h, _ptr(x0), self._check_tensor(x0, self.P, "x0")),

@@ -112,8 +112,9 @@ class _Moments:
         if d["state_bits"] != self.state_bits or len(d["state"]) != len(self._state) or \
                 any(a.shape != b.shape or a.dtype != b.dtype for a, b in zip(d["state"], self._state)):
             raise ValueError("the state of another model, or with another number of bits")
-        for a, b in zip(self._state, d["state"]):
-            a.copy_(b)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream)) if stream else torch.cuda.stream(torch.cuda.default_stream()):
+            for a, b in zip(self._state, d["state"]):
+                a.copy_(b)
         self._ck(self._lib.cocod_adamw_set_step(self._h, int(d["steps"]), stream), "cocod_adamw_set_step")
         self.lr = d["lr"]
 
@@ -134,7 +135,7 @@ class _Moments:
 
 
 class AdamW(_Moments):
-    """AdamW over a list of contiguous CUDA tensors, all bf16 or all float32."""
+    """AdamW over a list of contiguous CUDA tensors, all bf16 or all float32, that do not overlap."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, state_bits: int = 32, copies=None):
         """weight_decay: one number, or one for each tensor.  state_bits: 32, or 8 (blocks of 128 values share a unit).  copies: bf16 tensors that are
@@ -153,7 +154,7 @@ class AdamW(_Moments):
         self._b = _lm_binding
 
     def step(self, grads=None, grad_scale=None):
-        """One step on torch's current stream.  grads: one for each parameter, all bf16 or all float32 (default: the parameters' .grad); a parameter whose
+        """One step on torch's current stream (order the steps of one object).  grads: one for each parameter, all bf16 or all float32 (default: the parameters' .grad); a parameter whose
         gradient is None keeps its value and its moments.  grad_scale: one float32 on the device, a factor of all gradients."""
         if grads is None:
             grads = [p.grad for p in self.params]
@@ -179,11 +180,16 @@ class EngineAdamW(_Moments):
             for n, d in tensors:
                 sizes.append(n), decays.append(d), starts.append(at)
                 at += n
-        super().__init__(sizes, lr, betas, eps, decays, state_bits, starts)
         self.engine = engine
+        super().__init__(sizes, lr, betas, eps, decays, state_bits, starts)
+
+    def _stream(self):
+        """The engine's compute stream: everything here is ordered there, as the engine's own calls are."""
+        super()._stream()
+        return self.engine._compute
 
     def local_step(self, grads, grad_scale=None):
-        """Step II, one iteration for all workers, on the engine's compute stream.  grads: K x P float32 CUDA tensor."""
+        """Step II, one iteration for all workers.  grads: K x P float32 CUDA tensor."""
         self._stream()
         e = self.engine
         if not e._h:

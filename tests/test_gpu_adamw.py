@@ -212,6 +212,23 @@ def test_small_and_absent_gradients(optim):
             assert (m[128:256] == 0).all() and (v[128:256] == 0).all()
 
 
+def test_moments_that_are_loaded(optim):
+    """Zeros of either sign, and values over many orders of magnitude: coded as the definition says."""
+    n = 128 * 40
+    m, v = gaussian(1, n) * torch.exp(3 * gaussian(2, n)), (gaussian(3, n) * torch.exp(3 * gaussian(4, n))) ** 2
+    m[::3], v[::5], v[1::5] = -0.0, 0.0, -0.0
+    m[128:256], v[256:384] = 0.0, -0.0
+    m[384:512] *= 1e-36
+    v[384:512] *= 1e-30
+    v[512:640] *= 1e-34                                      # roots of numbers near the least normal one
+    v[640:650] = 1e-44
+    opt = optim.AdamW([torch.zeros(n, device="cuda")], state_bits=8)
+    opt.load_moments(7, m, v)
+    want = coded(m.double(), f32(v.double().abs().sqrt()))
+    got = opt.moments()
+    assert torch.equal(got[0].double(), want[0]) and torch.equal(got[1].double(), want[1]) and opt.steps == 7
+
+
 def test_states_go_out_and_back(optim):
     sizes = [1000, 77, 5000]
     for bits in (8, 32):
@@ -275,7 +292,7 @@ def test_gradients_of_torch_and_agreement_with_its_own_optimizer(optim):
         opt.step()
         ref.step()
     for p, q in zip(w, d):
-        assert float((p.double() - q).abs().max()) <= 5 * 24 * U * 3      # five steps; |p| < 3 or so, updates of 0.01
+        assert float((p.detach().double() - q.detach()).abs().max()) <= 5 * 24 * U * 3      # five steps; |p| < 3 or so, updates of 0.01
 
 
 @pytest.mark.parametrize("bits", [8, 32])
@@ -350,6 +367,33 @@ def test_local_steps_of_the_workers(optim, K, P, bits):
         for i in range(K):
             models[i].copy_(x[i])
     assert opt.steps == 6 and eng.step_count == 6
+
+
+def test_an_engine_on_a_stream_of_its_own(optim):
+    """Rates, moments and steps are ordered with the engine's calls."""
+    from paper_1906_12043_b200 import engine as E
+    K, P = 2, 300_000
+    s = torch.cuda.Stream()
+    for bits in (8, 32):
+        x0, g = gaussian(1, K, P), gaussian(2, K, P)
+        torch.cuda.synchronize()
+        got = []
+        for stream in (s, None):
+            eng = E.Engine(K, P, 0.1, 0.9, 0.0, stream=stream)
+            eng.set_params_all(x0)
+            opt = optim.EngineAdamW(eng, lr=0.01, state_bits=bits)
+            for t in range(6):
+                opt.local_step(g)
+                opt.lr = 0.01 * (t + 1)
+            d = opt.state_dict()
+            opt.load_state_dict(d)
+            m, v = opt.moments()
+            eng.sync()
+            torch.cuda.synchronize()
+            got.append((eng.get_params(), m.clone(), v.clone()))
+            eng.sync()
+            assert opt.steps == 6
+        assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
 def test_refusals(optim):

@@ -260,7 +260,7 @@ def test_refusals(ops, lm):
         with pytest.raises(ValueError):
             call()
     from paper_1906_12043_b200.engine import CocodError
-    for bad in (0.0, -1.0, float("nan"), INF):
+    for bad in (0.0, -1.0, float("nan"), INF, 1e-31, 1e31):
         with pytest.raises(CocodError):
             ops.token_logprobs(ys, scale=bad)
     t = plan.order % D
@@ -511,6 +511,53 @@ def test_more_than_2_to_the_31_logits(ops):
     ops.token_logprobs_grad(x, t, r, g, out=x)
     assert torch.equal(x[last], want)
     ops.check()
+
+
+def test_no_rows_at_all(ops):
+    for k, E in ((1, 3), (4, 9)):
+        plan = ops.expert_sort(torch.empty(0, k, dtype=torch.int32, device="cuda"), E)
+        assert plan.offsets.tolist() == [0] * (E + 1) and plan.counts.tolist() == [0] * E and plan.order.shape == (0,) and plan.place.shape == (0, k)
+        x, w = torch.empty(0, 24, device="cuda"), torch.empty(0, k, device="cuda")
+        rows = ops.expert_rows(x, plan)
+        assert rows.shape == (0, 24) and ops.expert_rows_grad(rows, plan).shape == (0, 24) and ops.expert_join(rows, plan, w).shape == (0, 24)
+        d, dw = ops.expert_join_grad(x, rows, plan, w)
+        assert d.shape == (0, 24) and dw.shape == (0, k)
+    for V in (5, 500, 50000):
+        x, t = torch.empty(0, V, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+        r = ops.token_logprobs(x, t, top=3)
+        assert r.logp.shape == r.entropy.shape == r.log_sum.shape == (0,) and r.top_logp.shape == r.top_tokens.shape == (0, 3)
+        assert ops.token_logprobs_grad(x, t, r, torch.empty(0, device="cuda")).shape == (0, V)
+    ops.check()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-6, 1e6, 1e30])
+def test_scales_far_from_one(ops, scale):
+    """The softmax of scale * logits, from all equal to a single one."""
+    for V in (60, 3000, 40000):
+        x = gaussian(V, 5, V)
+        x[1, ::2] = -INF
+        x[2, 3] = x[2].max()
+        t = torch.full((5,), 3, dtype=torch.int32, device="cuda")
+        assert_logprobs(ops.token_logprobs(x, t, top=4, scale=scale), x, t, 4, scale)
+    ops.check()
+
+
+def test_two_streams_at_once(ops):
+    """Calls that share nothing but the report of errors."""
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    x, y = gaussian(1, 300, 30000, dtype=torch.bfloat16), gaussian(2, 300, 30000, dtype=torch.bfloat16)
+    e, f = choices(3, 9000, 4, 64), choices(4, 9000, 4, 64)
+    want = [ops.token_logprobs(x, top=5), ops.token_logprobs(y, top=5), ops.expert_sort(e, 64), ops.expert_sort(f, 64)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for s, logits, experts in ((a, x, e), (b, y, f)):
+            with torch.cuda.stream(s):
+                got.append((ops.token_logprobs(logits, top=5), ops.expert_sort(experts, 64)))
+    torch.cuda.synchronize()
+    for i, (r, plan) in enumerate(got):
+        assert all(p is None and q is None or torch.equal(p, q) for p, q in zip(r, want[i % 2]))
+        assert all(torch.equal(p, q) for p, q in zip(plan, want[2 + i % 2]))
 
 
 def test_captured_and_replayed_and_on_another_stream(ops):

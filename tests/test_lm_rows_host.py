@@ -1,0 +1,102 @@
+"""Experts, log probabilities and AdamW without a GPU: refusals at the C boundary and of the binding, and sizes."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_1906_12043_b200 import build, engine
+    build.build()
+    return engine.load()
+
+
+def test_calls_without_a_handle_are_refused(lib):
+    from paper_1906_12043_b200.engine import ERR_INVALID, OK
+    assert lib.cocod_expert_sort(None, 1, 1, 1, 16, 1, 16, 16, 16, 16, None, 0, None) == ERR_INVALID
+    assert lib.cocod_expert_rows(None, 1, 1, 8, 16, 8, 16, 16, 8, 0, None) == ERR_INVALID
+    assert lib.cocod_expert_join(None, 1, 1, 8, 16, 8, 0, 16, 16, 16, 8, 0, None) == ERR_INVALID
+    assert lib.cocod_expert_join_grad(None, 1, 1, 8, 16, 8, 16, 8, 16, 16, 16, 8, 16, 0, None) == ERR_INVALID
+    assert lib.cocod_token_logprobs(None, 1, 8, 16, 8, 1, None, 1.0, 0, 16, 16, 16, None, None, None) == ERR_INVALID
+    assert lib.cocod_token_logprobs_grad(None, 1, 8, 16, 8, 1, None, 1.0, 0, None, 16, 16, None, 16, None, 16, 8, None) == ERR_INVALID
+    assert lib.cocod_adamw_destroy(None) == OK
+    assert lib.cocod_adamw_step(None, None, 1, None, 1, None, None, None) == ERR_INVALID
+    assert lib.cocod_adamw_flat_step(None, 16, 16, 1, 16, 1, None, None, None) == ERR_INVALID
+    assert lib.cocod_adamw_local_step(None, None, None, None) == ERR_INVALID
+    assert lib.cocod_adamw_set_lr(None, 1.0, None) == ERR_INVALID
+    assert lib.cocod_adamw_set_step(None, 1, None) == ERR_INVALID
+    assert lib.cocod_adamw_get_step(None, None, None) == ERR_INVALID
+    assert lib.cocod_adamw_moments(None, 16, 16, None) == ERR_INVALID
+    assert lib.cocod_adamw_load(None, 16, 16, None) == ERR_INVALID
+    assert lib.cocod_adamw_launch_count(None) == -1
+
+
+@pytest.mark.parametrize("T,k,E", [(-1, 1, 1), (1, 0, 1), (1, 33, 40), (1, 1, 0), (1, 1, 1025), (2 ** 31, 1, 4), (2 ** 27, 16, 4)])
+def test_sizes_of_experts_out_of_range(lib, T, k, E):
+    assert lib.cocod_expert_workspace(T, k, E) < 0
+
+
+def test_workspaces_of_the_sort(lib):
+    """Few slots need none, and no number of slots needs more than counts for a thread block on every SM and a cluster of them."""
+    assert lib.cocod_expert_workspace(0, 1, 1) == lib.cocod_expert_workspace(1, 1, 1024) == lib.cocod_expert_workspace(64, 32, 7) == 0
+    for T in (5000, 10 ** 6, 2 ** 31 - 2000):
+        assert 0 < lib.cocod_expert_workspace(T, 1, 100) <= 148 * 9 // 8 * 101 * 4
+
+
+def sizes(*n):
+    return len(n), (ctypes.c_int64 * max(1, len(n)))(*n)
+
+
+def test_values_of_the_moments(lib):
+    assert lib.cocod_adamw_values(*sizes(1)) == 128 and lib.cocod_adamw_values(*sizes(128, 129, 1)) == 512
+    for bad in (sizes(), sizes(0), sizes(5, -1), sizes(2 ** 40), sizes(*[2 ** 39] * 3), (1, None), (-1, sizes(1)[1])):
+        assert lib.cocod_adamw_values(*bad) < 0
+
+
+def test_adamw_is_looked_over_before_anything_is_made(lib):
+    from paper_1906_12043_b200.engine import ERR_INVALID
+    out, nan, inf = ctypes.c_void_p(), float("nan"), float("inf")
+    good = dict(out=ctypes.byref(out), n=2, sizes=sizes(3, 4)[1], decay=None, starts=None, bits=8, m=256, v=256, mu=256, vu=256, lr=0.1, b1=0.9, b2=0.99, eps=1e-8)
+    decays = (ctypes.c_float * 2)
+    starts = (ctypes.c_int64 * 2)
+    for bad in (dict(out=None), dict(n=0), dict(sizes=None), dict(sizes=sizes(3, 0)[1]), dict(bits=16), dict(bits=0), dict(m=None), dict(v=None), dict(m=8), dict(mu=None),
+                dict(vu=None), dict(vu=2), dict(lr=nan), dict(lr=inf), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=nan), dict(eps=-1.0), dict(eps=nan), dict(eps=inf),
+                dict(decay=decays(0.1, nan)), dict(starts=starts(0, -1))):
+        assert lib.cocod_adamw_create(*{**good, **bad}.values()) == ERR_INVALID, bad
+    assert not out.value
+
+
+def test_operators_refuse_to_run_without_a_gpu(lib):
+    from paper_1906_12043_b200 import optim
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    with pytest.raises(RuntimeError):
+        optim.AdamW([torch.zeros(3)])
+
+
+def test_the_binding_refuses_without_a_gpu(lib):
+    from paper_1906_12043_b200 import _lm_binding as b
+    for f, n in (("expert_sort", 4), ("expert_rows", 5), ("expert_join", 7), ("expert_join_grad", 7), ("token_logprobs", 6), ("token_logprobs_grad", 12), ("adamw_step", 6)):
+        with pytest.raises(ValueError, match="number of arguments"):
+            getattr(b, f)(*[0] * (n - 1))
+        with pytest.raises(ValueError, match="destroyed"):
+            getattr(b, f)(*[0] * n)
+
+
+def test_the_measured_cases_are_of_their_ranges():
+    """perf/more_operators.py: names, work and draws, without a GPU."""
+    import importlib.util
+    import os
+    import random
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    spec = importlib.util.spec_from_file_location("more_operators", os.path.join(root, "perf", "more_operators.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    listed = m.listed()
+    assert len({c["name"] for c in listed}) == len(listed) and not m.own
+    rng = random.Random(1)
+    most = max(m.work(c)["bytes"] for c in listed)
+    for c in listed + [m.draw(rng) for _ in range(200)]:
+        assert 0 < m.work(c)["bytes"] <= most
