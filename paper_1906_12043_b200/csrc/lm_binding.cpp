@@ -543,8 +543,29 @@ PyObject *adamw_step(PyObject *const *a)
         if (!there(t, at::kFloat, dev) || t.numel() != 1) refuse("grad_scale", "one Float" + place(dev), t);
         return static_cast<const float *>(t.data_ptr());
     }();
-    return PyLong_FromLong(cocod_adamw_step(h, params.data(), type_code(types[0]), grads.data(), type_code(types[1]), copied ? copies.data() : nullptr, factor,
-                                            current(dev)));
+    const int rc = cocod_adamw_step(h, params.data(), type_code(types[0]), grads.data(), type_code(types[1]), copied ? copies.data() : nullptr, factor, current(dev));
+    // (what autograd kept of a parameter is not what is there now: it is told, as by an operation in place)
+    const auto changed = [](PyObject *o) {
+        if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+    };
+    for (Py_ssize_t i = 0; i < n && rc == COCOD_OK; ++i) {
+        if (grads[i] == nullptr) continue;
+        changed(PyList_GET_ITEM(a[2], i));
+        if (copied) changed(PyList_GET_ITEM(a[4], i));
+    }
+    return PyLong_FromLong(rc);
+}
+
+// (handle, device, values, a tensor of the state, stream or None: the current one): the moments in fp32
+PyObject *adamw_moments(PyObject *const *a)
+{
+    auto *h = reinterpret_cast<cocod_adamw_handle *>(handle(a[0]));
+    const int64_t dev = device(a[1]), values = whole(a[2]);
+    const Tensor &like = tensor(a[3], "state", -1);
+    const Tensor m = fresh(like, {values}, at::kFloat), v = fresh(like, {values}, at::kFloat);
+    cocod_stream_t stream = a[4] == Py_None ? current(dev) : reinterpret_cast<cocod_stream_t>(whole(a[4]));
+    const int rc = cocod_adamw_moments(h, static_cast<float *>(m.data_ptr()), static_cast<float *>(v.data_ptr()), stream);
+    return rc == COCOD_OK ? Py_BuildValue("(NN)", THPVariable_Wrap(m), THPVariable_Wrap(v)) : PyLong_FromLong(rc);
 }
 
 #define METHOD(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<f, n>)), METH_FASTCALL, nullptr}
@@ -566,6 +587,7 @@ PyMethodDef methods[] = {
     METHOD("token_logprobs", token_logprobs, 6),
     METHOD("token_logprobs_grad", token_logprobs_grad, 12),
     METHOD("adamw_step", adamw_step, 6),
+    METHOD("adamw_moments", adamw_moments, 5),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lm_binding", "Marshalling for the language-model operators (used by lm.py).", -1, methods,

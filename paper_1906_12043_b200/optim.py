@@ -33,6 +33,8 @@ class _Moments:
         if len(decays) != n:
             raise ValueError(f"weight_decay: one number, or one for each of the {n} tensors")
         self._lib = _E.load()
+        from . import _lm_binding
+        self._b = _lm_binding
         c_sizes = (ctypes.c_int64 * n)(*sizes)
         self.values = int(self._lib.cocod_adamw_values(n, c_sizes))
         if self.values < 0:
@@ -54,14 +56,19 @@ class _Moments:
         if rc != _E.OK:
             raise _E.CocodError(rc, name)
 
+    def _own_stream(self):
+        """None: everything is ordered on torch's current stream."""
+        return None
+
     def _stream(self):
-        """The current stream.  The handle's device has to be the current one."""
+        """The stream of the next call.  The handle's device has to be the current one."""
         if not self._h:
             raise ValueError("the optimizer was destroyed")
         if torch.cuda.current_device() != self._device:
             raise ValueError(f"the current device is cuda:{torch.cuda.current_device()}, this optimizer was made on cuda:{self._device}: "
                              f"call it under torch.cuda.device({self._device})")
-        return torch.cuda.current_stream().cuda_stream
+        own = self._own_stream()
+        return torch.cuda.current_stream().cuda_stream if own is None else own
 
     @property
     def lr(self) -> float:
@@ -90,10 +97,10 @@ class _Moments:
         """(m, v) in float32, the tensors one behind the other, each starting at a multiple of 128 values.  With 32 bits the state itself, with 8 a copy."""
         if self.state_bits == 32:
             return tuple(self._state)
-        stream = self._stream()
-        m, v = (torch.empty(self.values, dtype=torch.float32, device=self._state[0].device) for _ in range(2))
-        self._ck(self._lib.cocod_adamw_moments(self._h, m.data_ptr(), v.data_ptr(), stream), "cocod_adamw_moments")
-        return m, v
+        both = self._b.adamw_moments(self._h, self._device, self.values, self._state[0], self._own_stream())
+        if type(both) is int:
+            raise _E.CocodError(both, "cocod_adamw_moments")
+        return both
 
     def load_moments(self, steps: int, m, v):
         """Continue after `steps` steps with these moments (float32, as moments() returns them; what lies between the tensors has to be 0)."""
@@ -117,6 +124,9 @@ class _Moments:
                 a.copy_(b)
         self._ck(self._lib.cocod_adamw_set_step(self._h, int(d["steps"]), stream), "cocod_adamw_set_step")
         self.lr = d["lr"]
+
+    def __reduce__(self):
+        raise TypeError("an optimizer is not copied or pickled: save its state_dict(), and load it into another one")
 
     @property
     def launch_count(self) -> int:
@@ -150,8 +160,6 @@ class AdamW(_Moments):
         if self.copies is not None and (len(self.copies) != len(self.params) or self.params[0].dtype != torch.float32):
             raise ValueError("copies: one for each float32 parameter (None: none)")
         super().__init__([p.numel() for p in self.params], lr, betas, eps, weight_decay, state_bits)
-        from . import _lm_binding
-        self._b = _lm_binding
 
     def step(self, grads=None, grad_scale=None):
         """One step on torch's current stream (order the steps of one object).  grads: one for each parameter, all bf16 or all float32 (default: the parameters' .grad); a parameter whose
@@ -183,9 +191,8 @@ class EngineAdamW(_Moments):
         self.engine = engine
         super().__init__(sizes, lr, betas, eps, decays, state_bits, starts)
 
-    def _stream(self):
+    def _own_stream(self):
         """The engine's compute stream: everything here is ordered there, as the engine's own calls are."""
-        super()._stream()
         return self.engine._compute
 
     def local_step(self, grads, grad_scale=None):

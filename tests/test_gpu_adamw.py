@@ -255,6 +255,26 @@ def test_states_go_out_and_back(optim):
             optim.AdamW(other, state_bits=40 - bits).load_state_dict(d)
 
 
+def test_what_autograd_kept_of_a_parameter_is_not_used_after_a_step(optim):
+    w = torch.nn.Parameter(gaussian(1, 30))
+    opt = optim.AdamW([w])
+    y = (w * w).sum()
+    opt.step([gaussian(2, 30)])
+    with pytest.raises(RuntimeError):
+        y.backward()
+    (w * w).sum().backward()
+    opt.step()
+
+
+def test_an_optimizer_is_not_copied(optim):
+    import copy
+    import pickle
+    opt = optim.AdamW([gaussian(1, 30)])
+    for f in (copy.copy, copy.deepcopy, pickle.dumps):
+        with pytest.raises(TypeError):
+            f(opt)
+
+
 def test_captured_steps_count_their_replays_and_follow_the_rate(optim):
     sizes = [3000, 10, 777]
     for bits in (8, 32):

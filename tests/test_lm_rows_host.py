@@ -78,7 +78,8 @@ def test_operators_refuse_to_run_without_a_gpu(lib):
 
 def test_the_binding_refuses_without_a_gpu(lib):
     from paper_1906_12043_b200 import _lm_binding as b
-    for f, n in (("expert_sort", 4), ("expert_rows", 5), ("expert_join", 7), ("expert_join_grad", 7), ("token_logprobs", 6), ("token_logprobs_grad", 12), ("adamw_step", 6)):
+    for f, n in (("expert_sort", 4), ("expert_rows", 5), ("expert_join", 7), ("expert_join_grad", 7), ("token_logprobs", 6), ("token_logprobs_grad", 12), ("adamw_step", 6),
+                 ("adamw_moments", 5)):
         with pytest.raises(ValueError, match="number of arguments"):
             getattr(b, f)(*[0] * (n - 1))
         with pytest.raises(ValueError, match="destroyed"):
