@@ -192,7 +192,7 @@ template <typename T, bool WIDE>
 __device__ __forceinline__ Piece<T, WIDE> load_piece(const T *p)
 {
     Piece<T, WIDE> r;
-    r.raw = __ldg(reinterpret_cast<const decltype(r.raw) *>(p));      // (no kernel here writes what it reads)
+    r.raw = *reinterpret_cast<const decltype(r.raw) *>(p);      // (an ordinary load: the read-only one of bf16 is assembly, which may be moved before its condition)
     return r;
 }
 template <typename T, bool WIDE>

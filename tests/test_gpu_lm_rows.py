@@ -203,6 +203,44 @@ def test_views_and_their_surroundings(ops, dtype, lead):
     assert ((dw - dw2).abs().double() <= 2 * (D + 16) * 2.0 ** -24 * products.sum(2)).all()
 
 
+def at_the_end(t):
+    """The same values where a segment of the allocator's memory ends: a read behind them leaves mapped memory."""
+    size = max(32 << 20, -(-t.numel() * t.element_size() // (2 << 20)) * (2 << 20))
+    whole = torch.empty(size, dtype=torch.uint8, device="cuda")
+    bytes_ = t.numel() * t.element_size()
+    view = whole[size - bytes_:].view(t.dtype).view(t.shape)
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("T,k,D", [(1, 1, 1), (76, 8, 3), (33, 1, 5), (40, 2, 33), (20, 4, 130), (9, 3, 264), (5, 2, 2056), (7, 6, 1031)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_operands_that_end_where_memory_ends(ops, T, k, D, dtype):
+    """Read-only loads of bf16 are assembly that the compiler may move before the condition they stand behind: lanes without a piece read behind the
+    last row (seen as an illegal address once in thousands of calls, where the operand lay at the end of mapped memory)."""
+    torch.cuda.empty_cache()
+    plan = ops.expert_sort(at_the_end(choices(1, T, k, 4, 0.2)), 4)
+    plan = plan._replace(place=at_the_end(plan.place))
+    x, ys, dy, w = (at_the_end(t) for t in (gaussian(1, T, D, dtype=dtype), gaussian(2, T * k, D, dtype=dtype), gaussian(3, T, D, dtype=dtype), gaussian(4, T, k)))
+    own = [t.clone() for t in (x, ys, dy, w)]
+    assert torch.equal(ops.expert_rows(x, plan), ops.expert_rows(own[0], plan))
+    assert torch.equal(ops.expert_join(ys, plan, w), ops.expert_join(own[1], plan, own[3]))
+    assert torch.equal(ops.expert_rows_grad(ys, plan), ops.expert_rows_grad(own[1], plan))
+    got, want = ops.expert_join_grad(dy, ys, plan, w, out=at_the_end(torch.zeros_like(ys))), ops.expert_join_grad(own[2], own[1], plan, own[3])
+    assert torch.equal(got[0], want[0])
+    products = (own[2].double().abs()[:, None] * own[1].double().abs()[torch.where(plan.place >= 0, plan.place, ~plan.place).long()]).sum(2)
+    assert ((got[1] - want[1]).abs().double() <= 2 * (D + 16) * 2.0 ** -24 * products).all()
+    for V in (D, 70 * D):
+        logits = at_the_end(gaussian(5, T, V, dtype=dtype))
+        top = min(V, 5)
+        a, b = ops.token_logprobs(logits, top=top), ops.token_logprobs(logits.clone(), top=top)
+        assert torch.equal(a.top_tokens, b.top_tokens)
+        g = gaussian(6, T)
+        ops.token_logprobs_grad(logits, None, a, d_entropy=g, out=logits)
+        assert torch.isfinite(logits).all()
+    ops.check()
+
+
 def test_a_place_beyond_the_rows_is_left_out_and_reported(ops, lm):
     from paper_1906_12043_b200.engine import CocodError
     T, k, E, D = 20, 2, 4, 64
