@@ -192,7 +192,7 @@ template <typename T, bool WIDE>
 __device__ __forceinline__ Piece<T, WIDE> load_piece(const T *p)
 {
     Piece<T, WIDE> r;
-    r.raw = *reinterpret_cast<const decltype(r.raw) *>(p);      // (an ordinary load: the read-only one of bf16 is assembly, which may be moved before its condition)
+    r.raw = *reinterpret_cast<const decltype(r.raw) *>(p);      // (an ordinary load: a read-only one of bf16 is assembly that may be moved before its condition)
     return r;
 }
 template <typename T, bool WIDE>
@@ -415,10 +415,10 @@ expert_join_few(const ExpertRows p, const T *rows, long long ld, const float *we
 
 // The gradient of that: back[place[t][j]] = w[t][j] dy[t] (0 where the slot takes no part), dw[t][j] = <dy[t], rows[place[t][j]]>.
 // WARPS warps take a token; each sum runs over a thread's pieces, the lanes and the warps, always in the same order.
-// (two rounds of loads under way together: 16384 x 8 of 2048 184 -> 175 us)
-constexpr int GRAD_AT_ONCE = 2;
-template <typename T, bool WIDE, int WARPS>
-__global__ void __launch_bounds__(256)
+// The loads of a piece of U slots are under way together, and as many blocks share an SM as their registers allow without spilling (16384 x 8 of 2048, U = 4: four
+// blocks 176 us, three 198, five 187; U = 2, of one or two choices: six blocks, 100000 x 1 of 512 66 us against 82 with U = 4; U = 8 was behind at all sizes: 184).
+template <typename T, bool WIDE, int WARPS, int U>
+__global__ void __launch_bounds__(256, U == 2 ? 6 : 4)
 expert_join_grad(const ExpertRows p, const T *dy, long long lddy, const T *rows, long long ld, const float *weights, T *back, long long ld_back, float *dw)
 {
     pdl_launch_dependents();
@@ -431,45 +431,46 @@ expert_join_grad(const ExpertRows p, const T *dy, long long lddy, const T *rows,
         const Slot s = slot_of(p, token, lane);
         const float w = lane < p.top ? weights[(long long)token * p.top + lane] : 0.0f;
         const T *d_row = dy + (long long)token * lddy;
-        for (int j0 = 0; j0 < p.top; j0 += 4) {
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, f[4];
-            int r[4];
-            bool there[4];
+        for (int j0 = 0; j0 < p.top; j0 += U) {
+            float sum[U], f[U];
+            int r[U];
+            unsigned there = __ballot_sync(~0u, s.there) >> j0;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const int j = min(j0 + u, 31);
+                sum[u] = 0.0f;
                 r[u] = __shfl_sync(~0u, s.row, j);
                 if (j0 + u >= p.top) r[u] = -1;
-                there[u] = __shfl_sync(~0u, (int)s.there, j);
+                if (r[u] < 0) there &= ~(1u << u);
                 f[u] = __shfl_sync(~0u, w, j);
             }
-#pragma unroll GRAD_AT_ONCE
             for (int c = of * 32 + lane; c < p.pieces; c += 32 * WARPS) {
                 const long long at = (long long)c * N;
                 const Piece<T, WIDE> d = load_piece<T, WIDE>(d_row + at);
-                Piece<T, WIDE> v[4];
+                Piece<T, WIDE> v[U];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (r[u] >= 0 && there[u]) v[u] = load_piece<T, WIDE>(rows + (long long)r[u] * ld + at);
+                for (int u = 0; u < U; ++u)
+                    if (there >> u & 1) v[u] = load_piece<T, WIDE>(rows + (long long)r[u] * ld + at);
                 float g[N];
                 widen<T, WIDE>(d, g);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+                for (int u = 0; u < U; ++u) {
                     if (r[u] < 0) continue;
+                    const bool here = there >> u & 1;
                     float out[N];
-                    if (there[u]) {
+                    if (here) {
                         float a[N];
                         widen<T, WIDE>(v[u], a);
 #pragma unroll
                         for (int e = 0; e < N; ++e) sum[u] = fmaf(g[e], a[e], sum[u]);
                     }
 #pragma unroll
-                    for (int e = 0; e < N; ++e) out[e] = there[u] ? f[u] * g[e] : 0.0f;
+                    for (int e = 0; e < N; ++e) out[e] = here ? f[u] * g[e] : 0.0f;
                     store_values<T, N>(back + (long long)r[u] * ld_back + at, out);
                 }
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < U; ++u) {
 #pragma unroll
                 for (int d = 16; d > 0; d /= 2) sum[u] += __shfl_xor_sync(~0u, sum[u], d);
                 if (lane == 0 && j0 + u < p.top) part[warp][j0 + u] = sum[u];

@@ -71,7 +71,8 @@ template <typename T, bool WIDE, int WARPS>
 int run_join_grad(cocod_lm *h, const ExpertRows &p, const void *dy, int64_t lddy, const void *rows, int64_t ld, const float *weights, void *back, int64_t ld_back,
                   float *dw, cudaStream_t s)
 {
-    TRY_CUDA(launch_dependent(true, expert_join_grad<T, WIDE, WARPS>, dim3((unsigned)ceil_div(p.tokens, 8 / WARPS)), dim3(256), 0, s, p, static_cast<const T *>(dy),
+    auto kernel = p.top <= 2 ? expert_join_grad<T, WIDE, WARPS, 2> : expert_join_grad<T, WIDE, WARPS, 4>;
+    TRY_CUDA(launch_dependent(true, kernel, dim3((unsigned)ceil_div(p.tokens, 8 / WARPS)), dim3(256), 0, s, p, static_cast<const T *>(dy),
                               (long long)lddy, static_cast<const T *>(rows), (long long)ld, weights, static_cast<T *>(back), (long long)ld_back, dw));
     return COCOD_OK;
 }
@@ -80,12 +81,14 @@ int run_expert_join_grad(cocod_lm *h, int64_t tokens, int k, int64_t D, const vo
                          const float *weights, void *back, int64_t ld_back, float *dw, cudaStream_t s)
 {
     const ExpertRows p = expert_rows_of(h, tokens, k, D, place, Piece<T, WIDE>::N);
-    // Warps of a token: the most whose lanes have a piece in four of five places.  16384 x 8 of 256 pieces: one, two, four, eight warps 196, 186, 188, 184 us; 4999 x 6
-    // of 129: 33.8, 32.3, 37.4, 40.5; 30000 x 2 of 64: one, two 39, 50.
-    const auto filled = [&](int warps) { return p.pieces * 5ll >= 4 * ceil_div(p.pieces, 32 * warps) * 32 * warps; };
-    if (p.pieces <= 64) return run_join_grad<T, WIDE, 1>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
-    if (p.pieces < 256 || (!filled(8) && !filled(4))) return run_join_grad<T, WIDE, 2>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
-    if (!filled(8)) return run_join_grad<T, WIDE, 4>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    // Warps of a token: as many as leave each lane two pieces, and more while there are SMs without a block and lanes would still have one.  16384 x 8 of 256 pieces: one,
+    // two, four, eight warps 196, 183, 176, 185 us; 4999 x 6 of 129: 33.8, 31.7, 33.8, 41.0; 40000 x 6 of 64: 93, 99, 148, 246; 4096 x 12 of 512: 160, 148, 140, 133;
+    // 64 x 8 of 256: 15.4, 9.2, 6.7, 5.1.
+    int warps = p.pieces >= 512 ? 8 : p.pieces >= 256 ? 4 : p.pieces > 64 ? 2 : 1;
+    while (warps < 8 && (int64_t)p.tokens * warps < 8 * (int64_t)sm_count() && p.pieces > 32 * warps) warps *= 2;
+    if (warps == 1) return run_join_grad<T, WIDE, 1>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    if (warps == 2) return run_join_grad<T, WIDE, 2>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
+    if (warps == 4) return run_join_grad<T, WIDE, 4>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
     return run_join_grad<T, WIDE, 8>(h, p, dy, lddy, rows, ld, weights, back, ld_back, dw, s);
 }
 
