@@ -7,6 +7,7 @@
 //
 // What bounds them: the sort its launches, the others HBM (each row of either side is touched once).
 #pragma once
+
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -267,8 +268,9 @@ __device__ __forceinline__ Slot slot_of(const ExpertRows &p, int token, int lane
     return s;
 }
 
-// A warp takes ROW_PIECES x 32 pieces of a token's row and writes them to its k rows (zeros for a slot that takes no part).
-constexpr int ROW_PIECES = 4;
+// A warp takes ROW_PIECES x 32 pieces of a token's row and writes them to its k rows (zeros for a slot that takes no part).  With the sort before it, two pieces and
+// four: 16384 x 4 of 2048 62.5 and 63.5 us, 100000 x 1 of 512 42.5 and 50.2, 64 x 8 of 2048 7.2 and 8.2; one piece 60.4 where two are 49.7 (65536 x 1 of 1024).
+constexpr int ROW_PIECES = 2;
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 expert_rows(const ExpertRows p, const T *x, long long ldx, T *out, long long ld_out)
@@ -298,47 +300,47 @@ expert_rows(const ExpertRows p, const T *x, long long ldx, T *out, long long ld_
     }
 }
 
-// The way back: y[t] = sum_j w[t][j] rows[place[t][j]] (weights == nullptr: the plain sum), fp32 in the order of j, in two forms with the same bits.  More than
-// two choices: a warp takes JOIN_PIECES x 32 pieces of one token, and four rows' pieces are under way together (16384 x 8 of 2048: 96 us, the other
-// form 113; x 4: 62 and 70; 4999 x 6 of 1032: 16.9 and 15.9).
-constexpr int JOIN_PIECES = 2;
-template <typename T, typename O, bool WIDE>
-__global__ void __launch_bounds__(256)
+// The way back: y[t] = sum_j w[t][j] rows[place[t][j]] (weights == nullptr: the plain sum), fp32 in the order of j, in two forms with the same bits.  A warp takes
+// PIECES x 32 pieces of one token, and U rows' pieces are under way together; BLOCKS of 256 threads share an SM (16384 x 8 of 2048, U = 4, two pieces: three blocks
+// 95.8 us, four 91.7, one piece and six blocks 96.3, four 109; 65536 x 2 of 1024, U = 2: four blocks 78, five 73, six 77; 65536 x 1 of 1024, U = 1: eight blocks 50.7, four
+// pieces and four blocks 49.1, but 54.8 against 39.4 at half the width).  A launch that leaves SMs idle takes one piece (64 x 8 of 2048, in a graph: 2.2 us instead of 2.6).
+template <typename T, typename O, bool WIDE, int U, int PIECES, int BLOCKS>
+__global__ void __launch_bounds__(256, BLOCKS)
 expert_join_many(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
 {
     pdl_launch_dependents();
     pdl_wait();
     constexpr int N = Piece<T, WIDE>::N;
-    const int lane = threadIdx.x & 31, parts = (p.pieces + 32 * JOIN_PIECES - 1) / (32 * JOIN_PIECES);
+    const int lane = threadIdx.x & 31, parts = (p.pieces + 32 * PIECES - 1) / (32 * PIECES);
     const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int token = (int)min(unit / parts, (long long)p.tokens);
     if (token >= p.tokens) return;
-    const int first = (int)(unit - (long long)token * parts) * 32 * JOIN_PIECES + lane;
+    const int first = (int)(unit - (long long)token * parts) * 32 * PIECES + lane;
     const Slot s = slot_of(p, token, lane);
     const float w = weights != nullptr && lane < p.top ? weights[(long long)token * p.top + lane] : 1.0f;
-    float sum[JOIN_PIECES][N];
+    float sum[PIECES][N];
 #pragma unroll
-    for (int i = 0; i < JOIN_PIECES; ++i)
+    for (int i = 0; i < PIECES; ++i)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[i][e] = 0.0f;
-    for (int j0 = 0; j0 < p.top; j0 += 4) {
-        Piece<T, WIDE> v[4][JOIN_PIECES];
-        bool there[4];
-        float f[4];
+    for (int j0 = 0; j0 < p.top; j0 += U) {
+        Piece<T, WIDE> v[U][PIECES];
+        bool there[U];
+        float f[U];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int j = min(j0 + u, 31), r = __shfl_sync(~0u, s.row, j);
             there[u] = __shfl_sync(~0u, (int)s.there, j) && j0 + u < p.top;
             f[u] = __shfl_sync(~0u, w, j);
 #pragma unroll
-            for (int i = 0; i < JOIN_PIECES; ++i)
+            for (int i = 0; i < PIECES; ++i)
                 if (there[u] && first + 32 * i < p.pieces) v[u][i] = load_piece<T, WIDE>(rows + (long long)r * ld + (long long)(first + 32 * i) * N);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             if (!there[u]) continue;
 #pragma unroll
-            for (int i = 0; i < JOIN_PIECES; ++i) {
+            for (int i = 0; i < PIECES; ++i) {
                 float a[N];
                 widen<T, WIDE>(v[u][i], a);
 #pragma unroll
@@ -347,14 +349,14 @@ expert_join_many(const ExpertRows p, const T *rows, long long ld, const float *w
         }
     }
 #pragma unroll
-    for (int i = 0; i < JOIN_PIECES; ++i)
+    for (int i = 0; i < PIECES; ++i)
         if (first + 32 * i < p.pieces) store_values<O, N>(y + (long long)token * ldy + (long long)(first + 32 * i) * N, sum[i]);
 }
 
-// One or two choices: a thread takes PIECES pieces of tokens' rows, 256 apart, whatever the rows' length, and ROWS rows' pieces of each are under way
-// together (65536 x 1 of 1024: 58 us, the other form 90; x 2: 89 and 99).
+// One or two choices, where the rows' length would leave a quarter of those lanes idle: a thread takes PIECES pieces of tokens' rows, 256 apart, whatever the rows'
+// length, and ROWS rows' pieces of each are under way together (30000 x 2 of 520: 21.5 us, the other form 28.2; of 1024 with 65536 tokens 81 and 73).
 template <typename T, typename O, bool WIDE, int ROWS, int PIECES>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, ROWS == 1 ? 6 : 8)
 expert_join_few(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
 {
     pdl_launch_dependents();

@@ -55,15 +55,20 @@ int run_expert_join(cocod_lm *h, int64_t tokens, int k, int64_t D, const void *r
 {
     const ExpertRows p = expert_rows_of(h, tokens, k, D, place, Piece<T, WIDE>::N);
     unsigned blocks;
-    if (k > 2) {
-        if (!warp_blocks(tokens, p.pieces, JOIN_PIECES, &blocks)) return COCOD_ERR_TOO_LARGE;
-        TRY_CUDA(launch_dependent(true, expert_join_many<T, O, WIDE>, dim3(blocks), dim3(256), 0, s, p, static_cast<const T *>(rows), (long long)ld, weights,
-                                  static_cast<O *>(y), (long long)ldy));
+    if (k > 2 || p.pieces * 4ll >= 3 * ceil_div(p.pieces, 64) * 64) {
+        if (!warp_blocks(tokens, p.pieces, 2, &blocks)) return COCOD_ERR_TOO_LARGE;
+        auto kernel = k > 2 ? expert_join_many<T, O, WIDE, 4, 2, 4> : k > 1 ? expert_join_many<T, O, WIDE, 2, 2, 5> : expert_join_many<T, O, WIDE, 1, 2, 8>;
+        if (blocks < (unsigned)sm_count()) {
+            warp_blocks(tokens, p.pieces, 1, &blocks);
+            kernel = expert_join_many<T, O, WIDE, 4, 1, 4>;
+        }
+        TRY_CUDA(launch_dependent(true, kernel, dim3(blocks), dim3(256), 0, s, p, static_cast<const T *>(rows), (long long)ld, weights, static_cast<O *>(y),
+                                  (long long)ldy));
         return COCOD_OK;
     }
     if (tokens > MAX_DIM * 256 / p.pieces) return COCOD_ERR_TOO_LARGE;
-    blocks = (unsigned)ceil_div(tokens * p.pieces, k > 1 ? 512 : 1024);
-    TRY_CUDA(launch_dependent(true, k > 1 ? expert_join_few<T, O, WIDE, 2, 2> : expert_join_few<T, O, WIDE, 1, 4>, dim3(blocks), dim3(256), 0, s, p,
+    blocks = (unsigned)ceil_div(tokens * p.pieces, k > 1 ? 256 : 512);
+    TRY_CUDA(launch_dependent(true, k > 1 ? expert_join_few<T, O, WIDE, 2, 1> : expert_join_few<T, O, WIDE, 1, 2>, dim3(blocks), dim3(256), 0, s, p,
                               static_cast<const T *>(rows), (long long)ld, weights, static_cast<O *>(y), (long long)ldy));
     return COCOD_OK;
 }
