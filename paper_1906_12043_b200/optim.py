@@ -11,6 +11,7 @@ streams.  No CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -51,6 +52,8 @@ class _Moments:
         if rc != _E.OK:
             raise _E.CocodError(rc, "cocod_adamw_create")
         self._h = h.value
+        with self._in_order():                  # (the first step may come on another stream than the zeros)
+            pass
 
     def _ck(self, rc, name):
         if rc != _E.OK:
@@ -70,9 +73,27 @@ class _Moments:
         own = self._own_stream()
         return torch.cuda.current_stream().cuda_stream if own is None else own
 
+    @contextlib.contextmanager
+    def _in_order(self):
+        """The stream of the handle's calls (None: torch's current one).  Another than the current one works behind what that one holds, and the current one goes on
+        behind what is done inside: so the current stream's tensors are read and written there, and used, changed or freed afterwards, in the order of the calls."""
+        own = self._own_stream()
+        if own is None:
+            yield None
+            return
+        here, there = torch.cuda.current_stream(), torch.cuda.ExternalStream(own) if own else torch.cuda.default_stream()
+        if here.cuda_stream == own:
+            yield here
+            return
+        there.wait_stream(here)
+        try:
+            yield there
+        finally:
+            here.wait_stream(there)
+
     @property
     def lr(self) -> float:
-        """The learning rate.  Setting it is ordered on the current stream; captured steps follow it."""
+        """The learning rate.  Setting it is ordered on the stream of the steps (EngineAdamW: the engine's compute stream); captured steps follow it."""
         return self._lr
 
     @lr.setter
@@ -82,7 +103,7 @@ class _Moments:
 
     @property
     def steps(self) -> int:
-        """Steps done (synchronises the current stream)."""
+        """Steps done (synchronises the stream of the steps)."""
         got = ctypes.c_int64()
         self._ck(self._lib.cocod_adamw_get_step(self._h, ctypes.byref(got), self._stream()), "cocod_adamw_get_step")
         return int(got.value)
@@ -94,10 +115,12 @@ class _Moments:
         return t.data_ptr()
 
     def moments(self):
-        """(m, v) in float32, the tensors one behind the other, each starting at a multiple of 128 values.  With 32 bits the state itself, with 8 a copy."""
-        if self.state_bits == 32:
+        """(m, v) in float32, the tensors one behind the other, each starting at a multiple of 128 values.  A copy; of an AdamW with 32 bits the state itself, which its
+        next step changes.  (An engine's is a copy always: its steps run on another stream than what reads the moments.)"""
+        if self.state_bits == 32 and self._own_stream() is None:
             return tuple(self._state)
-        both = self._b.adamw_moments(self._h, self._device, self.values, self._state[0], self._own_stream())
+        with self._in_order():
+            both = self._b.adamw_moments(self._h, self._device, self.values, self._state[0], self._own_stream())
         if type(both) is int:
             raise _E.CocodError(both, "cocod_adamw_moments")
         return both
@@ -107,19 +130,24 @@ class _Moments:
         stream, at = self._stream(), (self._flat(m, "m"), self._flat(v, "v"))
         if steps < 0:
             raise ValueError(f"steps: 0 or more, got {steps}")
-        self._ck(self._lib.cocod_adamw_load(self._h, *at, stream), "cocod_adamw_load")
+        with self._in_order():
+            self._ck(self._lib.cocod_adamw_load(self._h, *at, stream), "cocod_adamw_load")
         self._ck(self._lib.cocod_adamw_set_step(self._h, int(steps), stream), "cocod_adamw_set_step")
 
     def state_dict(self):
         """A copy of the state as it is held."""
-        return {"state_bits": self.state_bits, "steps": self.steps, "lr": self.lr, "state": [t.clone() for t in self._state]}
+        steps, copies = self.steps, [torch.empty_like(t) for t in self._state]
+        with self._in_order() as there, torch.cuda.stream(there):
+            for a, b in zip(copies, self._state):
+                a.copy_(b)
+        return {"state_bits": self.state_bits, "steps": steps, "lr": self.lr, "state": copies}
 
     def load_state_dict(self, d):
         stream = self._stream()
         if d["state_bits"] != self.state_bits or len(d["state"]) != len(self._state) or \
                 any(a.shape != b.shape or a.dtype != b.dtype for a, b in zip(d["state"], self._state)):
             raise ValueError("the state of another model, or with another number of bits")
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream)) if stream else torch.cuda.stream(torch.cuda.default_stream()):
+        with self._in_order() as there, torch.cuda.stream(there):
             for a, b in zip(self._state, d["state"]):
                 a.copy_(b)
         self._ck(self._lib.cocod_adamw_set_step(self._h, int(d["steps"]), stream), "cocod_adamw_set_step")
@@ -192,11 +220,12 @@ class EngineAdamW(_Moments):
         super().__init__(sizes, lr, betas, eps, decays, state_bits, starts)
 
     def _own_stream(self):
-        """The engine's compute stream: everything here is ordered there, as the engine's own calls are."""
+        """The engine's compute stream: everything here is ordered there, as the engine's own calls are, and what goes in and out with the current stream."""
         return self.engine._compute
 
     def local_step(self, grads, grad_scale=None):
-        """Step II, one iteration for all workers.  grads: K x P float32 CUDA tensor."""
+        """Step II, one iteration for all workers, on the engine's compute stream.  grads: K x P float32 CUDA tensor, complete and kept in that stream's order, as
+        Engine.local_step's."""
         self._stream()
         e = self.engine
         if not e._h:

@@ -462,3 +462,54 @@ def test_refusals(optim):
     opt.destroy()
     with pytest.raises(ValueError):
         opt.step(g)
+
+
+def queue_work(ms=30):
+    """Ordinary work that keeps the current stream busy for a while (a product of 8192^3 takes more than 0.7 ms)."""
+    a = torch.ones(8192, 8192, dtype=torch.bfloat16, device="cuda")
+    for _ in range(int(ms / 0.7)):
+        torch.mm(a, a)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_an_engine_on_a_stream_of_its_own_and_a_busy_current_stream(optim, bits):
+    """The zeros of a new state, copies of the state and moments that are handed out or in come from the current stream: the engine's steps and they wait for each other."""
+    from paper_1906_12043_b200 import engine as E
+    K, P = 2, 3_000_001
+    x0, g = gaussian(1, K, P), gaussian(2, K, P)
+    torch.cuda.synchronize()
+    got = []
+    for stream in (None, torch.cuda.Stream()):
+        busy = queue_work if stream is not None else lambda: None
+        eng = E.Engine(K, P, 0.1, 0.9, 0.0, stream=stream)
+        eng.set_params_all(x0)
+        torch.cuda.synchronize()
+        busy()
+        opt = optim.EngineAdamW(eng, lr=0.01, state_bits=bits)
+        opt.local_step(g)
+        opt.local_step(g)
+        busy()
+        d = opt.state_dict()
+        opt.local_step(g)
+        seen = [t.clone() for t in d["state"]]
+        busy()
+        opt.load_state_dict(d)
+        for t in d["state"]:                                 # (what was read may be changed)
+            t.zero_()
+        opt.local_step(g)
+        busy()
+        before = [torch.full((opt.values,), 7.0, device="cuda") for _ in range(2)]
+        del before                                           # (the next results may lie where this is still being written)
+        moments = [t.clone() for t in opt.moments()]
+        opt.local_step(g)
+        busy()
+        m, v = (t * 2 for t in moments)
+        opt.load_moments(5, m, v)
+        m.zero_(), v.zero_()
+        opt.local_step(g)
+        eng.sync()
+        torch.cuda.synchronize()
+        got.append([eng.get_params(), *seen, *moments, *(t.clone() for t in opt.moments())])
+        torch.cuda.synchronize()
+        assert opt.steps == 6
+    assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -101,3 +101,67 @@ def test_the_measured_cases_are_of_their_ranges():
     most = max(m.work(c)["bytes"] for c in listed)
     for c in listed + [m.draw(rng) for _ in range(200)]:
         assert 0 < m.work(c)["bytes"] <= most
+
+
+class FakeStream:
+    def __init__(self, at, log):
+        self.cuda_stream, self.log = at, log
+
+    def wait_stream(self, other):
+        self.log.append((self.cuda_stream, "waits for", other.cuda_stream))
+
+
+def test_an_engines_optimizer_orders_its_stream_with_the_current_one(lib, monkeypatch):
+    """Every tensor that goes in or out, and the zeros of the new state: the engine's stream (7) waits for the current one (5) before, the current one for it after."""
+    import contextlib
+    from types import SimpleNamespace
+
+    from paper_1906_12043_b200 import _lm_binding, engine, optim
+    log, here = [], None
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*a):
+                log.append(name)
+                if name == "cocod_adamw_create":
+                    a[0]._obj.value = 1
+                return 256 if name == "cocod_adamw_values" else 0
+            return call
+
+    @contextlib.contextmanager
+    def stream(s):
+        log.append(("on", s.cuda_stream))
+        yield
+        log.append("off")
+
+    here = FakeStream(5, log)
+    zeros = torch.zeros
+    for name, f in (("is_available", lambda: True), ("current_device", lambda: 0), ("current_stream", lambda: here), ("stream", stream), ("ExternalStream", lambda at: FakeStream(at, log))):
+        monkeypatch.setattr(torch.cuda, name, f)
+    monkeypatch.setattr(torch, "zeros", lambda *a, device, **k: log.append("zeros") or zeros(*a, **k))
+    monkeypatch.setattr(engine, "load", Library)
+    monkeypatch.setattr(_lm_binding, "adamw_moments", lambda *a: log.append(("moments", a[-1])) or (zeros(256),) * 2)
+    monkeypatch.setattr(optim._Moments, "_flat", lambda self, t, name: t.data_ptr())
+    first, last = (7, "waits for", 5), (5, "waits for", 7)
+    e = SimpleNamespace(K=2, P=100, _compute=7, _h=1)
+    for bits in (8, 32):
+        log.clear()
+        opt = optim.EngineAdamW(e, state_bits=bits)
+        assert log.index("zeros") < log.index(first)
+        log.clear()
+        d = opt.state_dict()
+        assert log == ["cocod_adamw_get_step", first, ("on", 7), "off", last]
+        log.clear()
+        opt.load_state_dict(d)
+        assert log[:4] == [first, ("on", 7), "off", last]
+        log.clear()
+        opt.load_moments(1, *(zeros(256),) * 2)
+        assert log[:3] == [first, "cocod_adamw_load", last]
+        log.clear()
+        opt.moments()
+        assert log == [first, ("moments", 7), last]
+        here.cuda_stream = 7                                 # (the same stream: nothing to wait for)
+        log.clear()
+        opt.moments()
+        assert log == [("moments", 7)]
+        here.cuda_stream = 5
