@@ -46,8 +46,10 @@ int64_t cocod_adamw_values(int n, const int64_t *sizes);
 int cocod_adamw_create(cocod_adamw_handle **out, int n, const int64_t *sizes, const float *decay, const int64_t *starts, int state_bits, void *m, void *v,
                        float *m_units, float *v_units, float lr, double beta1, double beta2, float eps);
 int cocod_adamw_destroy(cocod_adamw_handle *h);
+/* The n sizes given at creation (the handle's memory), or NULL without a handle. */
+const int64_t *cocod_adamw_sizes(const cocod_adamw_handle *h, int *n);
 
-/* One step.  params, grads, copies: host arrays of n device addresses (the arrays are read before the call returns); a tensor whose
+/* One step.  params, grads, copies: host arrays of n device addresses (the arrays are read before the call returns), tensor i of sizes[i] values; a tensor whose
  * gradient is NULL keeps its parameters and moments.  copies (or NULL): bf16 copies of fp32 parameters, written with them; single ones may be NULL.
  * param_type, grad_type: COCOD_BF16 or COCOD_F32; any alignment of whole values (16 bytes are faster).  bf16 parameters are rounded to nearest.
  * grad_scale: device, one fp32 value, or NULL. */

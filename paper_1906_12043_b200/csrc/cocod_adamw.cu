@@ -15,6 +15,7 @@ struct cocod_adamw {
     long long covered = 0;                 // flat: the values that the tensors cover one behind the other, 0 if they do not
     long long values = 0, launches = 0;
     std::vector<int> first_chunk;          // n + 1
+    std::vector<int64_t> sizes;
     cocod::adamw::Tensor *tensors = nullptr;
     int *chunk_tensor = nullptr;
     cocod::adamw::Clock *clock = nullptr;
@@ -140,6 +141,7 @@ int cocod_adamw_create(cocod_adamw_handle **out, int n, const int64_t *sizes, co
         h->state = State{m, v, m_units, v_units};
         h->beta1 = beta1; h->beta2 = beta2; h->eps = eps;
         h->first_chunk.resize(n + 1);
+        h->sizes.assign(sizes, sizes + n);
         std::vector<Tensor> tensors(n);
         std::vector<int> chunk_tensor(chunks);
         long long state = 0, covered = 0;
@@ -191,6 +193,13 @@ int cocod_adamw_destroy(cocod_adamw_handle *h)
     if (now != h->device && now >= 0) cudaSetDevice(now);
     adamw_free(h);
     return COCOD_OK;
+}
+
+const int64_t *cocod_adamw_sizes(const cocod_adamw_handle *h, int *n)
+{
+    if (!h || !n) return nullptr;
+    *n = h->n;
+    return h->sizes.data();
 }
 
 int cocod_adamw_step(cocod_adamw_handle *h, void *const *params, int param_type, const void *const *grads, int grad_type, void *const *copies,

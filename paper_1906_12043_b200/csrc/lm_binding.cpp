@@ -506,15 +506,19 @@ PyObject *token_logprobs_grad(PyObject *const *a)
 }
 
 // ------------------------------------------------------------------------------------------ AdamW
-// (handle, device, parameters, gradients, copies or None, gradients' factor or None): lists of n tensors; a gradient or a copy may be None
+// (handle, device, parameters, gradients, copies or None, gradients' factor or None): lists or tuples of the tensors the optimizer was made for, as many and
+// of the same sizes (the kernels go by those); a gradient or a copy may be None
 PyObject *adamw_step(PyObject *const *a)
 {
     auto *h = reinterpret_cast<cocod_adamw_handle *>(handle(a[0]));
     const int64_t dev = device(a[1]);
     const bool copied = a[4] != Py_None;
-    if (!PyList_Check(a[2]) || !PyList_Check(a[3]) || (copied && !PyList_Check(a[4]))) throw std::invalid_argument("need lists of tensors");
-    const Py_ssize_t n = PyList_GET_SIZE(a[2]);
-    if (PyList_GET_SIZE(a[3]) != n || (copied && PyList_GET_SIZE(a[4]) != n))
+    const auto sequence = [](PyObject *o) { return PyList_Check(o) || PyTuple_Check(o); };
+    if (!sequence(a[2]) || !sequence(a[3]) || (copied && !sequence(a[4]))) throw std::invalid_argument("need lists of tensors");
+    int n = 0;
+    const int64_t *sizes = cocod_adamw_sizes(h, &n);
+    if (PySequence_Fast_GET_SIZE(a[2]) != n) throw std::invalid_argument("params: need the " + std::to_string(n) + " that the optimizer was made for");
+    if (PySequence_Fast_GET_SIZE(a[3]) != n || (copied && PySequence_Fast_GET_SIZE(a[4]) != n))
         throw std::invalid_argument("grads: need " + std::to_string(n) + ", one for each parameter (None: it stays as it is)");
     std::vector<void *> params(n), copies(copied ? n : 0);
     std::vector<const void *> grads(n);
@@ -527,15 +531,14 @@ PyObject *adamw_step(PyObject *const *a)
             refuse(name, std::to_string(size) + " contiguous " + c10::toString(types[which]) + place(dev) + ", as the first one", t);
         return t;
     };
-    for (Py_ssize_t i = 0; i < n; ++i) {
-        const int64_t size = tensor(PyList_GET_ITEM(a[2], i), "params", -1).numel();
-        params[i] = one(PyList_GET_ITEM(a[2], i), "params", size, 0).data_ptr();
-        PyObject *g = PyList_GET_ITEM(a[3], i), *c = copied ? PyList_GET_ITEM(a[4], i) : Py_None;
-        grads[i] = g == Py_None ? nullptr : one(g, "grads", size, 1).data_ptr();
+    for (int i = 0; i < n; ++i) {
+        params[i] = one(PySequence_Fast_GET_ITEM(a[2], i), "params", sizes[i], 0).data_ptr();
+        PyObject *g = PySequence_Fast_GET_ITEM(a[3], i), *c = copied ? PySequence_Fast_GET_ITEM(a[4], i) : Py_None;
+        grads[i] = g == Py_None ? nullptr : one(g, "grads", sizes[i], 1).data_ptr();
         if (grads[i] != nullptr && grads[i] == params[i]) throw std::invalid_argument("grads: lies on its parameter");
         if (c == Py_None) continue;
         const Tensor &t = tensor(c, "copies", -1);
-        if (!there(t, at::kBFloat16, dev) || t.numel() != size || !t.is_contiguous()) refuse("copies", std::to_string(size) + " contiguous BFloat16" + place(dev), t);
+        if (!there(t, at::kBFloat16, dev) || t.numel() != sizes[i] || !t.is_contiguous()) refuse("copies", std::to_string(sizes[i]) + " contiguous BFloat16" + place(dev), t);
         copies[i] = t.data_ptr();
     }
     const float *factor = a[5] == Py_None ? nullptr : [&] {
@@ -548,10 +551,10 @@ PyObject *adamw_step(PyObject *const *a)
     const auto changed = [](PyObject *o) {
         if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
     };
-    for (Py_ssize_t i = 0; i < n && rc == COCOD_OK; ++i) {
+    for (int i = 0; i < n && rc == COCOD_OK; ++i) {
         if (grads[i] == nullptr) continue;
-        changed(PyList_GET_ITEM(a[2], i));
-        if (copied) changed(PyList_GET_ITEM(a[4], i));
+        changed(PySequence_Fast_GET_ITEM(a[2], i));
+        if (copied) changed(PySequence_Fast_GET_ITEM(a[4], i));
     }
     return PyLong_FromLong(rc);
 }

@@ -90,6 +90,7 @@ SIGNATURES = {
     "cocod_adamw_create": (_i, [ctypes.POINTER(_vp), _i, ctypes.POINTER(_i64), ctypes.POINTER(_f), ctypes.POINTER(_i64), _i, _vp, _vp, _vp, _vp, _f,
                                 ctypes.c_double, ctypes.c_double, _f]),
     "cocod_adamw_destroy": (_i, [_vp]),
+    "cocod_adamw_sizes": (ctypes.POINTER(_i64), [_vp, ctypes.POINTER(_i)]),
     "cocod_adamw_step": (_i, [_vp, _vp, _i, _vp, _i, _vp, _vp, _vp]),
     "cocod_adamw_flat_step": (_i, [_vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp]),
     "cocod_adamw_local_step": (_i, [_vp, _vp, _vp, _vp]),

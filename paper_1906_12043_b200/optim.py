@@ -178,11 +178,11 @@ class AdamW(_Moments):
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, state_bits: int = 32, copies=None):
         """weight_decay: one number, or one for each tensor.  state_bits: 32, or 8 (blocks of 128 values share a unit).  copies: bf16 tensors that are
         written with float32 parameters, for example those that products read (None in the list: that one has none)."""
-        self.params = list(params)
+        self.params = tuple(params)             # (as many and as large as the state: step refuses others)
         if not self.params or any(not isinstance(p, torch.Tensor) for p in self.params):
             raise ValueError("params: need tensors")
-        self.copies = None if copies is None else list(copies)
-        written = [t for t in self.params + (self.copies or []) if t is not None]
+        self.copies = None if copies is None else tuple(copies)
+        written = [t for t in self.params + (self.copies or ()) if t is not None]
         if len({t.data_ptr() for t in written}) != len(written):
             raise ValueError("params: a tensor is there twice")
         if self.copies is not None and (len(self.copies) != len(self.params) or self.params[0].dtype != torch.float32):
@@ -194,7 +194,7 @@ class AdamW(_Moments):
         gradient is None keeps its value and its moments.  grad_scale: one float32 on the device, a factor of all gradients."""
         if grads is None:
             grads = [p.grad for p in self.params]
-        rc = self._b.adamw_step(self._h, self._device, self.params, grads if type(grads) is list else list(grads), self.copies, grad_scale)
+        rc = self._b.adamw_step(self._h, self._device, self.params, grads if type(grads) in (list, tuple) else list(grads), self.copies, grad_scale)
         if rc != _E.OK:
             raise _E.CocodError(rc, "cocod_adamw_step")
 

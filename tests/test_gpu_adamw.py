@@ -513,3 +513,35 @@ def test_an_engine_on_a_stream_of_its_own_and_a_busy_current_stream(optim, bits)
         torch.cuda.synchronize()
         assert opt.steps == 6
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("n", [3, 70])
+def test_tensors_of_other_sizes_than_the_state_are_refused(optim, bits, n):
+    """The kernels go by the sizes given at creation: a parameter that was taken out, shortened or lengthened since is refused before anything is read or written."""
+    for change in ("fewer", "more", "shorter", "longer", "a shorter copy", "a longer gradient"):
+        params = [torch.nn.Parameter(gaussian(i, 300)) for i in range(n)]
+        opt = optim.AdamW(params, state_bits=bits, copies=[p.detach().bfloat16() for p in params])
+        opt.step([gaussian(i, 300) for i in range(n)])
+        grads = [gaussian(i, 300) for i in range(n)]
+        with pytest.raises((AttributeError, TypeError)):
+            opt.params.pop()
+        if change == "fewer":
+            opt.params, opt.copies = opt.params[:-1], opt.copies[:-1]
+            grads.pop()
+        elif change == "more":
+            opt.params, opt.copies = opt.params + (gaussian(1, 300),), opt.copies + (None,)
+            grads.append(gaussian(2, 300))
+        elif change == "a shorter copy":
+            opt.copies = opt.copies[:-1] + (opt.copies[-1][:299],)
+        else:
+            size = 299 if change == "shorter" else 301
+            if change != "a longer gradient":
+                params[-1].data = gaussian(1, size)
+            grads[-1] = gaussian(2, size)
+        kept = [p.detach().clone() for p in params] + [t.clone() for t in opt.moments()]
+        with pytest.raises(ValueError):
+            opt.step(grads)
+        with pytest.raises(ValueError):
+            opt.step(tuple(grads))
+        assert all(torch.equal(a, b) for a, b in zip(kept, [p.detach() for p in params] + list(opt.moments()))) and opt.steps == 1

@@ -165,3 +165,8 @@ def test_an_engines_optimizer_orders_its_stream_with_the_current_one(lib, monkey
         opt.moments()
         assert log == [("moments", 7)]
         here.cuda_stream = 5
+
+
+def test_no_sizes_without_a_handle(lib):
+    n = ctypes.c_int(5)
+    assert not lib.cocod_adamw_sizes(None, ctypes.byref(n)) and n.value == 5
