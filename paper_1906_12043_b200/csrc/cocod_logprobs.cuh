@@ -2,9 +2,11 @@
 //
 // With y = scale * l, the row's reference m (its largest logit) and t = (l - m) * scale * log2(e):
 //     S1 = sum 2^t,  S2 = sum 2^t t,   Z = scale m + ln S1,  log p_v = scale (l_v - m) - ln S1,  H = ln S1 - ln 2 * S2 / S1
-// in one pass over the row: every thread holds a reference of its own, a value of its first batch, and takes a higher one when a batch exceeds it by so
-// much that the powers could leave fp32 (S1' = c S1, S2' = c (S2 + d S1) with d = old - new reference in units of t, c = 2^d); threads are joined by the
-// same rule at the end.
+// in one pass over the row: a warp's threads share a reference, the largest logit that the warp has seen, and change it together when a batch exceeds it (S1' = c S1,
+// S2' = c (S2 + d S1) with d = old - new reference in units of t, c = 2^d); warps are joined by the same rule at the end.  The largest logit's own term, (1, 0)
+// exactly, is not in the thread's sums but counted beside them: S1 = n + (the others), so that ln S1 = log1p(n - 1 + the others) and what a confident row has beside its
+// largest logit is not lost in rounding; no log p is above 0, and no entropy below.  (With references of a thread that stayed until a value was 2^64 times the
+// reference's, log p and H were off by up to 7e-6 there, of either sign.)
 //
 // The top alternatives cost that pass next to nothing.  The largest of each batch of 32 values is needed there anyway; every thread keeps those of its
 // batches (up to eight, or of as many groups of batches).  The k-th largest of 64 groups' maxima is a bound that at least k values reach and, as a rule, few more.
@@ -51,6 +53,12 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float reciprocal_fast(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
 
 // Whole numbers in the order of the values; 0 is below every value's.
@@ -68,17 +76,26 @@ __device__ __forceinline__ float value_of(uint32_t key)
 __device__ __forceinline__ unsigned long long ranked(uint32_t key, int index) { return (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)index); }
 __device__ __forceinline__ int index_of(unsigned long long r) { return (int)(0xffffffffu - (uint32_t)r); }
 
-// What is known of a part of a row: its reference and the two sums.
+// What is known of a part of a row: its reference and the two sums, of S1 without n terms that are the reference's own (1 each, and 0 in S2).
 struct Sums {
     float most, s1, s2;
+    int n;
 };
 // The same sums relative to another reference that is not below (unit: scale * log2 e).
 __device__ __forceinline__ Sums relative_to(const Sums &a, float most, float unit)
 {
-    if (a.most == minus_inf()) return Sums{most, 0.0f, 0.0f};
-    const float d = (a.most - most) * unit, c = a.most == most ? 1.0f : exp2_fast(d);
-    if (a.most == most || c == 0.0f) return Sums{most, c * a.s1, c * a.s2};
-    return Sums{most, c * a.s1, c * fmaf(d, a.s1, a.s2)};
+    if (a.most == most) return a;
+    if (a.most == minus_inf()) return Sums{most, 0.0f, 0.0f, 0};
+    const float d = (a.most - most) * unit, c = exp2_fast(d), s1 = a.s1 + (float)a.n;
+    return c == 0.0f ? Sums{most, 0.0f, 0.0f, 0} : Sums{most, c * s1, c * fmaf(d, s1, a.s2), 0};
+}
+// ln S1 of a whole row; then its S1 is the whole sum.  (S2 has no positive term: what roundings leave above 0 is 0.)
+__device__ __forceinline__ float complete(Sums &a)
+{
+    const float log_s1 = log1pf((float)(a.n - 1) + a.s1);
+    a.s1 += (float)a.n;
+    a.s2 = a.s2 > 0.0f ? 0.0f : a.s2;
+    return log_s1;
 }
 
 // The row's token: the label, -1 where the row takes no part (or has none).
@@ -151,7 +168,7 @@ token_logprobs_short(const TokenRows p)
         key[i] = lane + LANES * i < p.vocab ? key_of(v[i]) : 0;
         best = max(best, key[i]);
     }
-    Sums a{0.0f, 0.0f, 0.0f};
+    Sums a{0.0f, 0.0f, 0.0f, 0};
     a.most = value_of(__reduce_max_sync(mask, best));
     const float unit = p.scale * LOG2E, m = a.most == minus_inf() ? 0.0f : a.most;
 #pragma unroll
@@ -227,6 +244,12 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float warp_max_nan(float x)
+{
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
 // 16 bytes of logits: N values.
 template <typename T> struct Word {
     static constexpr int N = 16 / sizeof(T);
@@ -291,6 +314,7 @@ struct LogprobsShared {
     __align__(16) uint32_t group[TOP_GROUPS];  // the largest key of each group of batches
     uint32_t slot[TOP_SLOTS][THREADS];       // the largest key of each batch (or group of batches) of a thread
     float s1[(THREADS + 31) / 32], s2[(THREADS + 31) / 32];
+    int n[(THREADS + 31) / 32];
     Sums part;                               // this thread block's
     uint32_t bound;
     int batches, found;
@@ -505,17 +529,16 @@ __device__ void find_top(LogprobsShared<THREADS> &sh, const Slice<T> &s, int slo
     }
 }
 
-// A thread's running sums (two of each, for the even and the odd values).
+// A thread's running sums (two of each, for the even and the odd values), relative to its warp's reference.
 //
 // The exponent of a value is x * unit - R with R = ref * unit rounded: one instruction for two values.  What the rounding of R left out, rho = ref * unit
-// - R, is the same factor 2^-rho for all of them and is made good when the sums go on.  Values below `low` count as `low`, whose power is 0 as
+// - R, is the reference's own exponent, known exactly, and taken into account whenever the reference changes.  Values below `low` count as `low`, whose power is 0 as
 // theirs, so that a masked entry adds 0 * (a finite number) to S2.  Both need R below 2^16 (rho below 2^-8); rows beyond that, or whose reference is no
 // number, take (x - ref) * unit (`plain`).
 struct Running {
-    float ref, r;
-    float limit;                             // what a batch's largest may reach without another reference
+    float ref, r, base;                      // base: 0, or (`plain`) the reference, and r = 0
     uint32_t low;                            // fp32, or two bf16
-    bool plain;
+    bool own;                                // this thread has met the reference: that term is not in the sums
     uint64_t s1, s2;
 };
 constexpr float FUSED_LIMIT = 65536.0f, UNIT_LIMIT = 1.0e-30f;
@@ -523,7 +546,7 @@ constexpr float FUSED_LIMIT = 65536.0f, UNIT_LIMIT = 1.0e-30f;
 template <typename T>
 __device__ __forceinline__ uint32_t low_of(float reference, float unit)
 {
-    const float low = reference - 256.0f / unit - fabsf(reference) * (1.0f / 64.0f);
+    const float low = reference - 256.0f * reciprocal_fast(unit) - fabsf(reference) * (1.0f / 64.0f);
     return sizeof(T) == 2 ? pack_bf16x2(low, low) : __float_as_uint(low);
 }
 template <typename T>
@@ -537,41 +560,42 @@ __device__ __forceinline__ uint4 not_below(const uint4 &w, uint32_t low)
                           __float_as_uint(max_nan(__uint_as_float(w.z), l)), __float_as_uint(max_nan(__uint_as_float(w.w), l)));
     }
 }
-// Both sums times 2^-shift, S2's exponents less `shift`.
-__device__ __forceinline__ void shift_sums(Running &a, float shift)
-{
-    const float c = exp2_fast(-shift);
-    a.s2 = mul2(pack2(c, c), fma2(pack2(-shift, -shift), a.s1, a.s2));
-    a.s1 = mul2(pack2(c, c), a.s1);
-}
-__device__ __forceinline__ float left_out(const Running &a, float unit) { return a.plain || a.ref == minus_inf() ? 0.0f : fmaf(a.ref, unit, -a.r); }
+// The exponent of the value m under the present reference.
+__device__ __forceinline__ float exponent_of(const Running &a, float m, float unit) { return fmaf(m - a.base, unit, -a.r); }
 template <typename T>
 __device__ __forceinline__ void refer_to(Running &a, float ref, float unit)
 {
     a.ref = ref;
-    const float m = ref == minus_inf() ? 0.0f : ref;
-    a.r = m * unit;
-    a.limit = ref + 64.0f / unit;            // (from -inf on: every value is above)
-    a.plain = !(fabsf(a.r) <= FUSED_LIMIT && unit >= UNIT_LIMIT);
+    const float m = ref == minus_inf() ? 0.0f : ref, r = m * unit;
+    const bool fused = fabsf(r) <= FUSED_LIMIT;
+    a.r = fused ? r : 0.0f;
+    a.base = fused ? 0.0f : m;
     a.low = low_of<T>(m, unit);
 }
+// A term y with the exponent d, or 0, is added to the sums of the even or of the odd values.
+__device__ __forceinline__ void add_one(Running &a, bool even, float y, float d)
+{
+    const uint64_t both = even ? pack2(y, 0.0f) : pack2(0.0f, y);
+    a.s1 = add2(a.s1, both);
+    a.s2 = fma2(both, pack2(d, d), a.s2);
+}
+// All lanes: the warp's largest is the reference now (NaN above all).
 template <typename T>
 __device__ __forceinline__ void raise(Running &a, float most, float unit)
 {
-    const float next = max_nan(a.ref, most), before = a.ref;
-    if (before != minus_inf()) {
-        shift_sums(a, left_out(a, unit));
-        const float d = (before - next) * unit, c = exp2_fast(d), d_ = c == 0.0f ? 0.0f : d;
-        a.s2 = mul2(pack2(c, c), fma2(pack2(d_, d_), a.s1, a.s2));
-        a.s1 = mul2(pack2(c, c), a.s1);
-    }
-    refer_to<T>(a, next, unit);
-    if (before != minus_inf()) shift_sums(a, -left_out(a, unit));
+    const Running old = a;
+    refer_to<T>(a, warp_max_nan(max_nan(a.ref, most)), unit);
+    // (the new reference's exponent under itself less the one that it has under the old one)
+    const float d = old.ref == minus_inf() ? minus_inf() : exponent_of(a, a.ref, unit) - exponent_of(old, a.ref, unit), c = exp2_fast(d), d_ = c == 0.0f ? 0.0f : d;
+    a.s2 = mul2(pack2(c, c), fma2(pack2(d_, d_), a.s1, a.s2));
+    a.s1 = mul2(pack2(c, c), a.s1);
+    const float before = fmaxf(exponent_of(a, old.ref, unit), -1.0e4f);      // (0 * -inf)
+    add_one(a, true, old.own ? exp2_fast(before) : 0.0f, before);
 }
 template <typename T, int U>
 __device__ __forceinline__ void add_words(Running &a, const uint4 (&r)[U], float unit)
 {
-    if (!a.plain) {
+    if (a.base == 0.0f) {
         const uint64_t units = pack2(unit, unit), minus = pack2(-a.r, -a.r);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -589,8 +613,7 @@ __device__ __forceinline__ void add_words(Running &a, const uint4 (&r)[U], float
         }
         return;
     }
-    const float ref = a.ref == minus_inf() ? 0.0f : -a.ref;
-    const uint64_t shift = pack2(ref, ref), factor = pack2(unit, unit);
+    const uint64_t shift = pack2(-a.base, -a.base), factor = pack2(unit, unit);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         float x[Word<T>::N];
@@ -605,14 +628,34 @@ __device__ __forceinline__ void add_words(Running &a, const uint4 (&r)[U], float
         }
     }
 }
-// (the largest of the words)
+// (all lanes; the largest of the lane's words)
 template <typename T, int U>
 __device__ __forceinline__ float take_words(Running &a, const uint4 (&r)[U], float unit)
 {
     const float most = largest<T, U>(r);
-    if (!(most <= a.limit)) raise<T>(a, most, unit);
+    const bool higher = __any_sync(~0u, !(most <= a.ref));
+    if (higher) raise<T>(a, most, unit);
     add_words<T, U>(a, r, unit);
+    if (higher) {                            // (the reference's term lies in the larger sum)
+        float e, o;
+        unpack2(a.s1, e, o);
+        a.own = most == a.ref;
+        const float d = exponent_of(a, a.ref, unit);
+        add_one(a, e >= o, a.own ? -exp2_fast(d) : 0.0f, d);
+    }
     return most;
+}
+// A thread's sums, relative to the row's (or the part's) largest.
+__device__ __forceinline__ Sums sums_of(Running a, float most, float unit)
+{
+    if (a.ref == minus_inf()) return Sums{most, 0.0f, 0.0f, 0};
+    const bool own = a.own && a.ref == most;
+    if (a.own && !own) add_one(a, true, exp2_fast(exponent_of(a, a.ref, unit)), exponent_of(a, a.ref, unit));
+    float e1, o1, e2, o2;
+    unpack2(a.s1, e1, o1);
+    unpack2(a.s2, e2, o2);
+    const float d = exponent_of(a, most, unit), c = exp2_fast(-d), s1 = e1 + o1;
+    return c == 0.0f ? Sums{most, 0.0f, 0.0f, own} : Sums{most, c * s1, c * fmaf(-d, s1, e2 + o2), own};
 }
 
 // `blocks` thread blocks (a cluster where there are more than one) take a row; each takes a stretch of its words.
@@ -666,6 +709,7 @@ token_logprobs_row(const TokenRows p, int blocks)
     float slot_most = minus_inf();
     int i = s.from + tid, in_slot = 0;
     const auto note = [&](float batch_most) {
+        if (i >= s.to) return;               // (the last lanes of the last batch)
         if constexpr (TOP) {
             slot_most = max_nan(slot_most, batch_most);
             if (++in_slot == s.per_slot || i + U * THREADS >= s.to) {
@@ -693,30 +737,34 @@ token_logprobs_row(const TokenRows p, int blocks)
             for (int u = 0; u < U; ++u) r[u] = from + u * THREADS < s.to ? words[from + u * THREADS] : all_masked<T>();
         }
     };
-    if (AHEAD && i < s.to) fetch(i);
-    for (; i < s.to; i += U * THREADS) {
+    if (AHEAD || TOP) fetch(i);              // (fp32: loads behind their use with alternatives, before it without: 8192 x 4000 34.4 us, the other way 36.0; 2048 x 50001 69.2 and 73.1)
+    if (warp == 0 && __any_sync(~0u, s.ends >= 0)) {
+        Piece<T, true> one;
+        one.raw = all_masked<T>();
+        if (s.ends >= 0) {
+            const T x = s.x[s.ends];
+            memcpy(&one.raw, &x, sizeof(T));
+        }
+        const uint4 word[1] = {one.raw};
+        const float value = take_words<T, 1>(a, word, unit);
+        if (s.ends >= 0) {
+            even = max(even, key_of(value));
+            most = max_nan(most, value);
+        }
+    }
+    for (; i - lane < s.to; i += U * THREADS) {      // (all lanes of a warp)
         if constexpr (AHEAD) {
             uint4 now[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) now[u] = r[u];
-            if (i + U * THREADS < s.to) fetch(i + U * THREADS);
+            if (i - lane + U * THREADS < s.to) fetch(i + U * THREADS);
             note(take_words<T, U>(a, now, unit));
         } else {
-            fetch(i);
+            if (!TOP) fetch(i);
             note(take_words<T, U>(a, r, unit));
+            if (TOP && i - lane + U * THREADS < s.to) fetch(i + U * THREADS);
         }
     }
-    if (s.ends >= 0) {
-        Piece<T, true> one;
-        one.raw = all_masked<T>();
-        const T x = s.x[s.ends];
-        memcpy(&one.raw, &x, sizeof(T));
-        const uint4 r[1] = {one.raw};
-        const float value = take_words<T, 1>(a, r, unit);
-        even = max(even, key_of(value));
-        most = max_nan(most, value);
-    }
-    shift_sums(a, left_out(a, unit));
     // the threads' sums, relative to the largest of all
     team_sync<THREADS>();                    // (the groups are zero)
     if constexpr (TOP) {
@@ -727,10 +775,8 @@ token_logprobs_row(const TokenRows p, int blocks)
     }
     team_sync<THREADS>();
     const uint32_t top = __reduce_max_sync(~0u, max(sh.group[lane], sh.group[lane + 32]));
-    float lo1, hi1, lo2, hi2;
-    unpack2(a.s1, lo1, hi1);
-    unpack2(a.s2, lo2, hi2);
-    Sums b = relative_to(Sums{a.ref, lo1 + hi1, lo2 + hi2}, top ? value_of(top) : minus_inf(), unit);
+    Sums b = sums_of(a, top ? value_of(top) : minus_inf(), unit);
+    const int n = __popc(__ballot_sync(~0u, b.n != 0));
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) {
         b.s1 += __shfl_xor_sync(~0u, b.s1, d);
@@ -739,10 +785,12 @@ token_logprobs_row(const TokenRows p, int blocks)
     if (lane == 0) {
         sh.s1[warp] = b.s1;
         sh.s2[warp] = b.s2;
+        sh.n[warp] = n;
     }
     team_sync<THREADS>();
     if (warp == 0) {
         float s1 = lane < THREADS / 32 ? sh.s1[lane] : 0.0f, s2 = lane < THREADS / 32 ? sh.s2[lane] : 0.0f;
+        b.n = __reduce_add_sync(~0u, lane < THREADS / 32 ? sh.n[lane] : 0);
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) {
             s1 += __shfl_xor_sync(~0u, s1, d);
@@ -755,26 +803,29 @@ token_logprobs_row(const TokenRows p, int blocks)
     if constexpr (TOP) find_top<T, THREADS>(sh, s, slots, p.top);
     if (blocks == 1) {
         if (tid >= max(1, p.top)) return;
-        const float log_s1 = logf(TOP ? sh.part.s1 : b.s1);      // (thread 0 wrote sh.part itself; find_top ends with a barrier)
+        if (TOP) b = sh.part;                // (thread 0 wrote it itself; find_top ends with a barrier)
+        const float log_s1 = complete(b);
         if (tid == 0) write_row(p, row, b, log_s1, own);
-        if (TOP && tid < p.top) write_top(p, row, tid, sh.best[tid], sh.part, log_s1);
+        if (TOP && tid < p.top) write_top(p, row, tid, sh.best[tid], b, log_s1);
         return;
     }
     auto cluster = cg::this_cluster();
     cluster.sync();
     if (rank == 0) {
         // (every warp for itself, a lane for each block: their sums come together)
-        Sums all{minus_inf(), 0.0f, 0.0f};
+        Sums all{minus_inf(), 0.0f, 0.0f, 0};
         if (lane < blocks) all = cluster.map_shared_rank(&sh, lane)->part;
         all = relative_to(all, value_of(__reduce_max_sync(~0u, key_of(all.most))), unit);
 #pragma unroll
         for (int d = 4; d > 0; d /= 2) {
             all.s1 += __shfl_xor_sync(~0u, all.s1, d);
             all.s2 += __shfl_xor_sync(~0u, all.s2, d);
+            all.n += __shfl_xor_sync(~0u, all.n, d);
         }
         all.s1 = __shfl_sync(~0u, all.s1, 0);
         all.s2 = __shfl_sync(~0u, all.s2, 0);
-        const float log_s1 = logf(all.s1);
+        all.n = __shfl_sync(~0u, all.n, 0);
+        const float log_s1 = complete(all);
         if (tid == 0) write_row(p, row, all, log_s1, own);
         if constexpr (TOP) {
             const int n = blocks * p.top;    // (up to 8 * 32)

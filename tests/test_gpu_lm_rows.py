@@ -638,3 +638,60 @@ def test_the_same_bits_every_time(ops):
     for _ in range(5):
         assert all(torch.equal(a, b) for a, b in zip(first, ops.token_logprobs(x, t, top=20)))
         assert all(torch.equal(a, b) for a, b in zip(grads, ops.expert_join_grad(dy, ys, plan, w)))
+
+
+def spread(x, scale):
+    """In 64 bits, without cancellation: what all terms but the largest add up to, relative to it; the same weighted with their distances from it; and the sum over the
+    terms of e^-d (2^-20 + 8 * 2^-24 d / ln 2) and of d times that."""
+    y = x.double() * scale
+    most, at = y.max(1, keepdim=True)
+    d = most - y                                             # (distances in natural units)
+    e = torch.exp(-d)
+    e.scatter_(1, at, 0.0)
+    near = torch.where(e > 0, d, 0.0)
+    each = e * (2.0 ** -20 + 8 * 2.0 ** -24 * near / math.log(2))
+    return e.sum(1), (e * near).sum(1), each.sum(1), (near * each).sum(1), d
+
+
+@pytest.mark.parametrize("V", [257, 1000, 4000, 9001, 20000, 40000, 65536, 128256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M", [5, 230])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+def test_confident_rows(ops, V, dtype, M, scale):
+    """Rows with a logit far above the others, wherever it lies: log probabilities are not above 0 and entropies not below, and both are as near to those of 64 bits as
+    sums of the other terms allow.
+
+    Let O be the sum of all terms but the largest, relative to it.  A term at distance d is off by a relative 2^-20 (the exponential and the factors of up to four changes of
+    reference, 2^-22 each at most, the rounding of scale log2 e) and 8 * 2^-24 d / ln 2 (the roundings of its exponent and of the changes').  Sums add (V / 128 + 64) * 2^-24 of O.
+    The largest term is exact, but for the other values of its batch, at most 17 of which are added to it and rounded with it: 18 * 2^-24 * (1 + O).  So log (1 + O) is off by
+    at most E = these three over 1 + O, and the entropy log (1 + O) + D / (1 + O), D the terms times their distances, by E + D / (1 + O) E + the errors of D's terms, each of
+    which has another 2^-23, the sums' of D, and 18 * 2^-24 * 2^-8 for the largest term's exponent, which is a rounding of at most 2^-8.  Results: 2^-22 of themselves."""
+    x = gaussian(V + M, M, V, scale=2.0, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    tokens = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    far = (20 + 25 * torch.rand(M, generator=g, device="cuda")).to(dtype)
+    x.scatter_(1, tokens.long()[:, None], far[:, None])
+    x[0] = torch.linspace(-50, 10, V).to(dtype)              # (every batch's largest exceeds all before)
+    x[1] = torch.linspace(10, -50, V).to(dtype)
+    if M > 5:
+        x[2, V // 3] = x[2].max()                            # (twice)
+        x[3, ::3] = -INF
+    tokens[4] = (tokens[4] + 1) % V                          # (not the confident token)
+    O, D, each, weighted, d = spread(x, scale)
+    sums = (V / 128 + 64) * 2.0 ** -24
+    E = (each + sums * O) / (1 + O) + 18 * 2.0 ** -24
+    H = torch.log1p(O) + D / (1 + O)
+    lp = -d.gather(1, tokens.long()[:, None])[:, 0] - torch.log1p(O)
+    for top in (0, 3):
+        r = ops.token_logprobs(x, tokens, top=top, scale=scale)
+        assert (r.logp <= 0).all() and (r.entropy >= 0).all()
+        error = torch.where(r.logp.double() == lp, 0.0, (r.logp.double() - lp).abs())      # (a masked token: -inf)
+        room = E + 2.0 ** -22 * lp.abs()
+        assert (error <= room).all(), f"log p: worst {(error / room).max()} of the bound"
+        error = (r.entropy.double() - H).abs()
+        room = E + (D * E + weighted + (2.0 ** -23 + sums) * D) / (1 + O) + 18 * 2.0 ** -32 + 2.0 ** -22 * H
+        assert (error <= room).all(), f"entropy: worst {(error / room).max()} of the bound"
+        if top:
+            assert (r.top_logp <= 0).all()
+            assert torch.equal(r.top_tokens.long(), torch.sort(x.double(), dim=1, descending=True, stable=True).indices[:, :top])
+    ops.check()
