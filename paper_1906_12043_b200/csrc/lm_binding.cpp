@@ -136,10 +136,23 @@ inline Tensor part_of(const Tensor &buffer, int64_t at, at::IntArrayRef shape, a
 
 inline cocod_stream_t current(int64_t device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 inline PyObject *code_or(int rc, const Tensor &t) { return rc == COCOD_OK ? THPVariable_Wrap(t) : PyLong_FromLong(rc); }
+// A tensor that was written: what autograd kept of it is not what is there now; it is told, as by an operation in place.
+inline void written(PyObject *o)
+{
+    const Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// A result that was given, which has been written.
 inline PyObject *given(PyObject *o)
 {
+    written(o);
     Py_INCREF(o);
     return o;
+}
+inline PyObject *none()
+{
+    Py_INCREF(Py_None);
+    return Py_None;
 }
 
 template <PyObject *(*F)(PyObject *const *), int N>
@@ -461,7 +474,7 @@ PyObject *token_logprobs(PyObject *const *a)
                                         reinterpret_cast<int32_t *>(p + 3 * padded + wide), current(dev));
     if (rc != COCOD_OK) return PyLong_FromLong(rc);
     const auto part = [&](bool there, int64_t at, at::IntArrayRef shape, at::ScalarType kind) {
-        return there ? THPVariable_Wrap(part_of(all, 4 * at, shape, kind)) : given(Py_None);
+        return there ? THPVariable_Wrap(part_of(all, 4 * at, shape, kind)) : none();
     };
     return Py_BuildValue("(NNNNN)", part(a[3] != Py_None, 0, {M}, at::kFloat), part(true, padded, {M}, at::kFloat), part(true, 2 * padded, {M}, at::kFloat),
                          part(top > 0, 3 * padded, {M, top}, at::kFloat), part(top > 0, 3 * padded + wide, {M, top}, at::kInt));
@@ -547,14 +560,10 @@ PyObject *adamw_step(PyObject *const *a)
         return static_cast<const float *>(t.data_ptr());
     }();
     const int rc = cocod_adamw_step(h, params.data(), type_code(types[0]), grads.data(), type_code(types[1]), copied ? copies.data() : nullptr, factor, current(dev));
-    // (what autograd kept of a parameter is not what is there now: it is told, as by an operation in place)
-    const auto changed = [](PyObject *o) {
-        if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
-    };
     for (int i = 0; i < n && rc == COCOD_OK; ++i) {
         if (grads[i] == nullptr) continue;
-        changed(PySequence_Fast_GET_ITEM(a[2], i));
-        if (copied) changed(PySequence_Fast_GET_ITEM(a[4], i));
+        written(PySequence_Fast_GET_ITEM(a[2], i));
+        if (copied && copies[i] != nullptr) written(PySequence_Fast_GET_ITEM(a[4], i));
     }
     return PyLong_FromLong(rc);
 }

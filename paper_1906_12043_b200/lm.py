@@ -103,7 +103,8 @@ class TokenLogprobs(NamedTuple):
 
 
 class LMOps:
-    """The operators, with the scratch their kernels share: order the calls of one object (one stream, or events)."""
+    """The operators, with the scratch their kernels share: order the calls of one object (one stream, or events).  A result that is given (out, dw) is written as by
+    an operation in place, also for autograd."""
 
     def __init__(self, workspace_limit: int = 2 << 30, widen: bool = True):
         """workspace_limit: bytes that a call of the vocabulary operators may take for what it keeps of the rows it works on

@@ -695,3 +695,33 @@ def test_confident_rows(ops, V, dtype, M, scale):
             assert (r.top_logp <= 0).all()
             assert torch.equal(r.top_tokens.long(), torch.sort(x.double(), dim=1, descending=True, stable=True).indices[:, :top])
     ops.check()
+
+
+def test_a_result_that_is_given_is_an_operation_in_place_for_autograd(ops):
+    """Every out= and dw=: what autograd kept of the tensor is not used for a backward pass after it was written."""
+    M, k, n = 32, 64, 48
+    off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    x, w, dy = gaussian(1, M, k, dtype=torch.bfloat16), gaussian(2, 1, n, k, dtype=torch.bfloat16), gaussian(3, M, n, dtype=torch.bfloat16)
+    packed, labels, experts = ops.act_pack(x), torch.zeros(M, dtype=torch.int32, device="cuda"), choices(1, M, 2, 4)
+    plan, p = ops.expert_sort(experts, 4), gaussian(4, M, 2)
+    rows = ops.expert_rows(x, plan)
+    known = ops.token_logprobs(dy, labels)
+    calls = [(lambda out: ops.grouped_forward(x, w, off, out=out), dy), (lambda out: ops.grouped_input_grad(dy, w, off, out=out), x),
+             (lambda out: ops.grouped_weight_grad(dy, x, off, out=out), w), (lambda out: ops.grouped_weight_grad(dy, packed, off, out=out), w),
+             (lambda out: ops.act_unpack(packed, out=out), x), (lambda out: ops.act_relu_grad(x, packed, out=out), x),
+             (lambda out: ops.vocab_loss_grad(x, w, labels, off, dw=out), w), (lambda out: ops.expert_rows(x, plan, out=out), rows),
+             (lambda out: ops.expert_rows_grad(rows, plan, out=out), x), (lambda out: ops.expert_join(rows, plan, p, out=out), x),
+             (lambda out: ops.expert_join_grad(x, rows, plan, p, out=out), rows), (lambda out: ops.token_logprobs_grad(dy, labels, known, gaussian(1, M), out=out), dy)]
+    for call, like in calls:
+        leaf = torch.zeros_like(like, requires_grad=True)
+        kept = leaf.exp()                                    # (whose own value is its gradient)
+        whole = kept.sum()
+        call(kept.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            whole.backward()
+        with torch.inference_mode():
+            call(torch.zeros_like(like))
+    logits = torch.zeros_like(dy, requires_grad=True).exp()
+    ops.token_logprobs_grad(logits.detach(), labels, known, gaussian(1, M), out=logits.detach())
+    assert logits._version == 1
+    ops.check()
