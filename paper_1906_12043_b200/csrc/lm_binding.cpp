@@ -7,8 +7,10 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/Context.h>
 #include <ATen/MemoryOverlap.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -122,8 +124,14 @@ at::ScalarType result_type(PyObject *out, int64_t code, at::ScalarType usual)
     return type;
 }
 inline int type_code(at::ScalarType t) { return t == at::kFloat ? COCOD_F32 : COCOD_BF16; }
-// (the allocation itself, without the dispatcher's way to it)
-inline Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type) { return at::detail::empty_cuda(shape, type, like.device(), std::nullopt); }
+// (the allocation itself, without the dispatcher's way to it, 0.4 us, where nobody listens there: no mode of the dispatcher, and no filling of new memory)
+inline Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type)
+{
+    const at::Context &c = at::globalContext();
+    if (c10::impl::TorchDispatchModeTLS::any_modes_set() || (c.deterministicAlgorithms() && c.deterministicFillUninitializedMemory()))
+        return at::empty(shape, like.options().dtype(type));
+    return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
+}
 // A contiguous part of a buffer, `at` bytes behind its start, as a tensor of its own.
 inline Tensor part_of(const Tensor &buffer, int64_t at, at::IntArrayRef shape, at::ScalarType type)
 {

@@ -725,3 +725,42 @@ def test_a_result_that_is_given_is_an_operation_in_place_for_autograd(ops):
     ops.token_logprobs_grad(logits.detach(), labels, known, gaussian(1, M), out=logits.detach())
     assert logits._version == 1
     ops.check()
+
+
+def test_new_results_are_seen_by_dispatch_modes_and_filled_where_torch_fills_them(ops):
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Seen(TorchDispatchMode):
+        def __init__(self):
+            super().__init__()
+            self.names = []
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            self.names.append(str(func))
+            return func(*args, **(kwargs or {}))
+
+    M, k, n = 32, 64, 48
+    off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    x, w = gaussian(1, M, k, dtype=torch.bfloat16), gaussian(2, 1, n, k, dtype=torch.bfloat16)
+    plan = ops.expert_sort(choices(1, M, 2, 4), 4)
+    place = plan.place.clone()
+    place[place == 2 * M - 1] = place[place == 0].item()     # (a row that no place names is not written)
+    calls = [lambda: ops.grouped_forward(x, w, off), lambda: ops.expert_rows(x, plan._replace(place=place))]
+    before = [call() for call in calls]
+    with Seen() as seen:
+        for call in calls:
+            call()
+        ops.token_logprobs(x, top=2)
+        ops.expert_sort(plan.place.abs() % 4, 4)
+    assert sum("aten.empty" in name for name in seen.names) >= 4
+    was = torch.are_deterministic_algorithms_enabled(), torch.utils.deterministic.fill_uninitialized_memory
+    try:
+        torch.use_deterministic_algorithms(True, warn_only=True)
+        torch.utils.deterministic.fill_uninitialized_memory = True
+        torch.cuda.empty_cache()
+        y, rows = (call() for call in calls)
+        assert torch.equal(y, before[0]) and rows[-1].isnan().all() and torch.equal(rows[:-1], before[1][:-1])
+    finally:
+        torch.use_deterministic_algorithms(was[0])
+        torch.utils.deterministic.fill_uninitialized_memory = was[1]
+    ops.check()
