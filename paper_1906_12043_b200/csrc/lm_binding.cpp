@@ -113,6 +113,12 @@ void apart(const Tensor &out, const char *out_name, const Tensor &in, const char
         throw std::invalid_argument(std::string(out_name) + ": lies on " + name);
 }
 
+// The same for an operand that may be None.
+void apart(const Tensor &out, const char *out_name, PyObject *in, const char *name)
+{
+    if (in != Py_None) apart(out, out_name, tensor(in, name, -1), name);
+}
+
 // The result's type: the caller's choice (0 bf16, 1 fp32, -1 none), which has to be the type of a result that is given.
 at::ScalarType result_type(PyObject *out, int64_t code, at::ScalarType usual)
 {
@@ -402,7 +408,7 @@ PyObject *expert_rows(PyObject *const *a)
     const int32_t *places = static_cast<const int32_t *>(table(at, "place", T, k, at::kInt, dev));
     const Tensor out = a[4] == Py_None ? fresh(x, {T * k, D}, type) : tensor(a[4], "out", 2);
     const Matrix mo = any_rows(out, "out", T * k, D, type, dev);
-    if (a[4] != Py_None) apart(out, "out", x, "x");
+    if (a[4] != Py_None) apart(out, "out", x, "x"), apart(out, "out", at, "place");
     const int rc = cocod_expert_rows(h, T, (int)k, D, m.data, m.ld, places, mo.data, mo.ld, type_code(type), current(dev));
     return rc == COCOD_OK && a[4] != Py_None ? given(a[4]) : code_or(rc, out);
 }
@@ -420,7 +426,7 @@ PyObject *expert_join(PyObject *const *a)
     const float *w = a[4] == Py_None ? nullptr : static_cast<const float *>(table(tensor(a[4], "weights", 2), "weights", T, k, at::kFloat, dev));
     const Tensor out = a[5] == Py_None ? fresh(x, {T, D}, out_type) : tensor(a[5], "out", 2);
     const Matrix mo = any_rows(out, "out", T, D, out_type, dev);
-    if (a[5] != Py_None) apart(out, "out", x, "rows");
+    if (a[5] != Py_None) apart(out, "out", x, "rows"), apart(out, "out", at, "place"), apart(out, "out", a[4], "weights");
     const int rc = cocod_expert_join(h, T, (int)k, D, m.data, m.ld, type_code(type), places, w, mo.data, mo.ld, type_code(out_type), current(dev));
     return rc == COCOD_OK && a[5] != Py_None ? given(a[5]) : code_or(rc, out);
 }
@@ -438,7 +444,7 @@ PyObject *expert_join_grad(PyObject *const *a)
     const float *w = static_cast<const float *>(table(tensor(a[5], "weights", 2), "weights", T, k, at::kFloat, dev));
     const Tensor out = a[6] == Py_None ? fresh(x, {T * k, D}, type) : tensor(a[6], "out", 2), dw = fresh(x, {T, k}, at::kFloat);
     const Matrix mo = any_rows(out, "out", T * k, D, type, dev);
-    if (a[6] != Py_None) apart(out, "out", dy, "dy"), apart(out, "out", x, "rows");
+    if (a[6] != Py_None) apart(out, "out", dy, "dy"), apart(out, "out", x, "rows"), apart(out, "out", at, "place"), apart(out, "out", a[5], "weights");
     const int rc = cocod_expert_join_grad(h, T, (int)k, D, md.data, md.ld, m.data, m.ld, places, w, mo.data, mo.ld, static_cast<float *>(dw.data_ptr()),
                                           type_code(type), current(dev));
     if (rc != COCOD_OK) return PyLong_FromLong(rc);
@@ -520,7 +526,16 @@ PyObject *token_logprobs_grad(PyObject *const *a)
     }
     const Tensor out = a[11] == Py_None ? fresh(x, {M, V}, type) : tensor(a[11], "out", 2);
     const Matrix mo = any_rows(out, "out", M, V, type, dev);
-    if (a[11] != Py_None) apart(out, "out", x, "logits", true);
+    if (a[11] != Py_None) {
+        apart(out, "out", x, "logits", true);
+        apart(out, "out", a[3], "tokens");
+        apart(out, "out", a[6], "log_sum");
+        apart(out, "out", a[8], "d_logp");
+        apart(out, "out", a[9], "d_entropy");
+        apart(out, "out", a[10], "d_top");
+        if (d_entropy != nullptr) apart(out, "out", a[7], "entropy");
+        if (d_top != nullptr) apart(out, "out", a[5], "top_tokens");
+    }
     const int rc = cocod_token_logprobs_grad(h, M, V, m.data, m.ld, type_code(type), tokens, scale, (int)top, top_tokens, log_sum, entropy, d_logp, d_entropy, d_top,
                                              mo.data, mo.ld, current(dev));
     return rc == COCOD_OK && a[11] != Py_None ? given(a[11]) : code_or(rc, out);

@@ -764,3 +764,37 @@ def test_new_results_are_seen_by_dispatch_modes_and_filled_where_torch_fills_the
         torch.use_deterministic_algorithms(was[0])
         torch.utils.deterministic.fill_uninitialized_memory = was[1]
     ops.check()
+
+
+def test_a_result_does_not_lie_on_any_operand(ops):
+    """... the small ones among them, which threads still read when others have written."""
+    T, k, E = 64, 8, 16
+    plan = ops.expert_sort(choices(1, T, k, E), E)
+    x, ys, w = gaussian(1, T, k), gaussian(2, T * k, k), gaussian(3, T, k)
+    place = plan.place.view(torch.float32)
+    wide = torch.zeros(T * k, k, device="cuda")
+    on_rows = wide[:T].copy_(w)
+    kept = [t.clone() for t in (plan.place, w)]
+    wide_plan = plan._replace(place=wide.view(torch.int32)[T:2 * T].copy_(plan.place))
+    for call in (lambda: ops.expert_join(ys, plan, w, out=w), lambda: ops.expert_join(ys, plan, w, out=place), lambda: ops.expert_rows_grad(ys, plan, out=place),
+                 lambda: ops.expert_join_grad(x, ys, plan, on_rows, out=wide), lambda: ops.expert_join_grad(x, ys, wide_plan, w, out=wide),
+                 lambda: ops.expert_rows(x, wide_plan, out=wide)):
+        with pytest.raises(ValueError, match="lies on"):
+            call()
+    M, V = 12, 20
+    logits, all_ = gaussian(4, M, V), torch.zeros(M, V, device="cuda")
+    t = torch.zeros(M, dtype=torch.int32, device="cuda")
+    known, g, d_top = ops.token_logprobs(logits, t, top=2), gaussian(5, M), gaussian(6, M, 2)
+
+    def inside(v):                                           # (the same values somewhere in the result)
+        return all_.view(v.dtype).view(-1)[7:7 + v.numel()].view(v.shape).copy_(v)
+
+    for call in (lambda: ops.token_logprobs_grad(logits, inside(t), known, g, out=all_), lambda: ops.token_logprobs_grad(logits, t, known, inside(g), out=all_),
+                 lambda: ops.token_logprobs_grad(logits, t, known, d_entropy=inside(g), out=all_), lambda: ops.token_logprobs_grad(logits, t, known, d_top=inside(d_top), out=all_),
+                 lambda: ops.token_logprobs_grad(logits, t, known._replace(log_sum=inside(known.log_sum)), g, out=all_),
+                 lambda: ops.token_logprobs_grad(logits, t, known._replace(entropy=inside(known.entropy)), d_entropy=g, out=all_),
+                 lambda: ops.token_logprobs_grad(logits, t, known._replace(top_tokens=inside(known.top_tokens)), d_top=d_top, out=all_)):
+        with pytest.raises(ValueError, match="lies on"):
+            call()
+    assert all(torch.equal(a, b) for a, b in zip(kept, (plan.place, w)))
+    ops.check()
