@@ -62,7 +62,7 @@ int cocod_adamw_flat_step(cocod_adamw_handle *h, const void *params_in, void *pa
 
 /* The local step of Algorithm 1 (Step II) for every worker of an engine with AdamW in place of momentum SGD: what cocod_local_step does to the
  * engine's models, its bf16 copy, its step count and its state of communication.  The tensors have to cover the K x P values one behind the other.
- * Runs on the engine's compute stream.  grads: device, K x P fp32.  The engine's momentum, lr, mu and wd take no part. */
+ * Runs on the engine's compute stream; both handles are of the same device.  grads: device, K x P fp32.  The engine's momentum, lr, mu and wd take no part. */
 int cocod_adamw_local_step(cocod_adamw_handle *h, cocod_handle *engine, const float *grads, const float *grad_scale);
 
 /* Ordered on the stream. */

@@ -229,7 +229,7 @@ int cocod_adamw_local_step(cocod_adamw_handle *h, cocod_handle *engine, const fl
     if (!h || !engine || !grads) return COCOD_ERR_INVALID;
     cocod_step_plan plan{};
     if (int rc = cocod_internal_plan_step(engine, &plan)) return rc;
-    if (!h->flat || h->covered != (long long)plan.K * plan.P) return COCOD_ERR_INVALID;
+    if (!h->flat || h->covered != (long long)plan.K * plan.P || h->device != plan.device) return COCOD_ERR_INVALID;
     if (int rc = cocod_adamw_flat_step(h, plan.x_in, plan.x_out, COCOD_F32, grads, COCOD_F32, plan.shadow, grad_scale, plan.compute)) return rc;
     return cocod_internal_finish_step(engine, 1);
 }

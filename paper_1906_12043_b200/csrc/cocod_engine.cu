@@ -1161,6 +1161,7 @@ int cocod_internal_plan_step(cocod_handle *h, cocod_step_plan *plan)
     plan->lr = h->lr; plan->mu = h->mu; plan->wd = h->wd;
     plan->K = h->K; plan->P = h->P;
     plan->compute = h->compute;
+    plan->device = h->device;
     return COCOD_OK;
 }
 

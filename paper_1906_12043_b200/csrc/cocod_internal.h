@@ -16,6 +16,7 @@ struct cocod_step_plan {
     int K;
     int64_t P;
     cudaStream_t compute;
+    int device;
 };
 
 // Describe the local step the engine would run now.  Fails like cocod_local_step would.

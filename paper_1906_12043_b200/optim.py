@@ -234,4 +234,7 @@ class EngineAdamW(_Moments):
             raise ValueError("grads must be a CUDA tensor")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or not grad_scale.is_cuda or grad_scale.numel() != 1):
             raise ValueError("grad_scale: need one float32 on the device")
+        for t, name in ((grads, "grads"), (grad_scale, "grad_scale")):
+            if t is not None and t.get_device() != self._device:
+                raise ValueError(f"{name}: on cuda:{t.get_device()}, need cuda:{self._device} (the current device at creation)")
         self._ck(self._lib.cocod_adamw_local_step(self._h, e._h, _E._ptr(grads), _E._ptr(grad_scale)), "cocod_adamw_local_step")

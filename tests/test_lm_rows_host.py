@@ -170,3 +170,26 @@ def test_an_engines_optimizer_orders_its_stream_with_the_current_one(lib, monkey
 def test_no_sizes_without_a_handle(lib):
     n = ctypes.c_int(5)
     assert not lib.cocod_adamw_sizes(None, ctypes.byref(n)) and n.value == 5
+
+
+def test_an_engines_optimizer_refuses_tensors_of_another_device(monkeypatch):
+    """... before their addresses get to a kernel."""
+    from types import SimpleNamespace
+
+    from paper_1906_12043_b200 import optim
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    opt = optim.EngineAdamW.__new__(optim.EngineAdamW)
+    called = []
+    opt._h, opt._device = 1, 0
+    opt._lib = SimpleNamespace(cocod_adamw_local_step=lambda *a: called.append(a) or 0, cocod_adamw_destroy=lambda h: 0)
+    opt.engine = SimpleNamespace(K=1, P=4, _h=1, _compute=7, _check_tensor=lambda *a: 0)
+
+    def on(device, n):
+        return SimpleNamespace(get_device=lambda: device, is_cuda=True, dtype=torch.float32, numel=lambda: n, data_ptr=lambda: 256)
+
+    opt.local_step(on(0, 4), on(0, 1))
+    assert len(called) == 1
+    for bad in ((on(1, 4), None), (on(0, 4), on(1, 1))):
+        with pytest.raises(ValueError, match="cuda:1"):
+            opt.local_step(*bad)
+    assert len(called) == 1
