@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 
 import torch
 
@@ -147,11 +148,14 @@ class _Moments:
         if d["state_bits"] != self.state_bits or len(d["state"]) != len(self._state) or \
                 any(a.shape != b.shape or a.dtype != b.dtype for a, b in zip(d["state"], self._state)):
             raise ValueError("the state of another model, or with another number of bits")
+        steps, lr = int(d["steps"]), float(d["lr"])
+        if steps < 0 or not math.isfinite(lr):
+            raise ValueError(f"a state after {steps} steps with the rate {lr}")
         with self._in_order() as there, torch.cuda.stream(there):
             for a, b in zip(self._state, d["state"]):
                 a.copy_(b)
-        self._ck(self._lib.cocod_adamw_set_step(self._h, int(d["steps"]), stream), "cocod_adamw_set_step")
-        self.lr = d["lr"]
+        self._ck(self._lib.cocod_adamw_set_step(self._h, steps, stream), "cocod_adamw_set_step")
+        self.lr = lr
 
     def __reduce__(self):
         raise TypeError("an optimizer is not copied or pickled: save its state_dict(), and load it into another one")

@@ -545,3 +545,20 @@ def test_tensors_of_other_sizes_than_the_state_are_refused(optim, bits, n):
         with pytest.raises(ValueError):
             opt.step(tuple(grads))
         assert all(torch.equal(a, b) for a, b in zip(kept, [p.detach() for p in params] + list(opt.moments()))) and opt.steps == 1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_state_that_is_refused_changes_nothing(optim, bits):
+    p = [gaussian(1, 300)]
+    opt, other = optim.AdamW(p, state_bits=bits), optim.AdamW([gaussian(1, 300)], state_bits=bits)
+    for o in (opt, other):
+        o.step([gaussian(2, 300)])
+    other.step([gaussian(3, 300)])
+    kept = [t.clone() for t in opt.moments()]
+    d = other.state_dict()
+    for bad in (dict(d, steps=-1), dict(d, lr=float("nan")), dict(d, lr=float("inf")), dict(d, state=d["state"][:1]), dict(d, state_bits=40 - bits)):
+        with pytest.raises(ValueError):
+            opt.load_state_dict(bad)
+        assert all(torch.equal(a, b) for a, b in zip(kept, opt.moments())) and opt.steps == 1
+    opt.load_state_dict(d)
+    assert all(torch.equal(a, b) for a, b in zip(other.moments(), opt.moments())) and opt.steps == 2
