@@ -562,3 +562,61 @@ def test_a_state_that_is_refused_changes_nothing(optim, bits):
         assert all(torch.equal(a, b) for a, b in zip(kept, opt.moments())) and opt.steps == 1
     opt.load_state_dict(d)
     assert all(torch.equal(a, b) for a, b in zip(other.moments(), opt.moments())) and opt.steps == 2
+
+
+LARGE = [[1_000_003, 150 * 4096 + 5, 7, 300_000], [40_000_000, 333, 5_000_001]]
+
+
+@pytest.mark.parametrize("sizes", LARGE)
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("ptype,gtype", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16)])
+def test_steps_of_large_models(optim, sizes, bits, ptype, gtype):
+    """Chunks of 4096 values and more, whose 8-bit form loads a step ahead: three steps against the formulas, by the bounds above."""
+    lr, betas, eps, decays = 1e-2, (0.9, 0.99), 1e-8, [0.1 * (i % 3) for i in range(len(sizes))]
+    params = [gaussian(i, n, scale=0.5, dtype=ptype) for i, n in enumerate(sizes)]
+    plain = Plain(params, lr, betas, eps, decays, bits)
+    opt = optim.AdamW(params, lr=lr, betas=betas, eps=eps, weight_decay=decays, state_bits=bits)
+    for t in range(3):
+        grads = [gaussian(1000 * t + i, n, scale=10.0 ** (i % 5 - 3), dtype=gtype) for i, n in enumerate(sizes)]
+        grads[0][::3] = 0
+        old = [x.clone() for x in plain.m]
+        bounds = plain.step(grads)
+        opt.step(grads)
+        m, v = opt.moments()
+        at = 0
+        for i, n in enumerate(sizes):
+            got, want = params[i].double(), plain.p[i]
+            room = bounds[i] + (torch.finfo(ptype).eps / 2 if ptype == torch.bfloat16 else U) * want.abs() + 1e-40
+            assert ((got - want).abs() <= 1.01 * room).all(), (t, i)
+            L = -(-n // 128) * 128
+            gm, gv = m[at:at + L].double(), v[at:at + L].double()
+            at += L
+            if bits == 8:
+                assert torch.equal(gm, plain.m[i]) and torch.equal(gv, plain.v[i])
+            else:
+                assert ((gm - plain.m[i]).abs() <= 4 * U * (0.9 * old[i].abs() + 0.2 * padded(grads[i].double()).abs())).all()
+                assert ((gv - plain.v[i]).abs() <= 6 * U * plain.v[i] + 1e-44).all()
+            assert (gm[n:] == 0).all() and (gv[n:] == 0).all()
+        plain.follow(params, (m, v))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("first", [128, 10])
+def test_local_steps_of_large_models(optim, bits, first):
+    """The workers' tensors one behind the other, all of them aligned or, behind ten values, none: the same bits as lists of tensors."""
+    from paper_1906_12043_b200 import engine as E
+    K, sizes = 3, [first, 1_500_000, 2047, 400_000]
+    P = sum(sizes)
+    x0 = gaussian(1, K, P)
+    eng = E.Engine(K, P, 0.1, 0.9, 0.0)
+    eng.set_params_all(x0)
+    opt = optim.EngineAdamW(eng, [(n, 0.1 * (i % 2)) for i, n in enumerate(sizes)], lr=0.01, state_bits=bits)
+    tensors = [t.clone() for i in range(K) for t in x0[i].split(sizes)]
+    alone = optim.AdamW(tensors, lr=0.01, weight_decay=[0.1 * (i % 2) for i in range(len(sizes))] * K, state_bits=bits)
+    for t in range(3):
+        g = gaussian(10 + t, K, P)
+        opt.local_step(g)
+        alone.step([p.clone() for i in range(K) for p in g[i].split(sizes)])
+    eng.sync()
+    x = eng.get_params()
+    assert torch.equal(x.view(-1), torch.cat(tensors)) and all(torch.equal(a, b) for a, b in zip(opt.moments(), alone.moments()))

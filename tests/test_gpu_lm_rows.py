@@ -798,3 +798,54 @@ def test_a_result_does_not_lie_on_any_operand(ops):
             call()
     assert all(torch.equal(a, b) for a, b in zip(kept, (plan.place, w)))
     ops.check()
+
+
+# ------------------------------------------------------------------------------------------------------- the forms that large batches take
+@pytest.mark.parametrize("T,k,D", [(2500, 1, 512), (20000, 1, 64), (2500, 2, 1024), (1300, 2, 768), (6000, 1, 1027), (9000, 2, 520), (3000, 1, 2048), (1500, 5, 1032), (700, 12, 4096)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_joins_of_large_batches(ops, T, k, D, dtype):
+    """Enough rows for every SM: the forms for one and two choices with full and with ragged widths, and the gradient's; the same bounds as above."""
+    E = 32
+    plan = ops.expert_sort(choices(T, T, k, E, 0.1), E)
+    there = plan.place >= 0
+    at = torch.where(there, plan.place, ~plan.place).long()
+    ys, dy, w = gaussian(2, T * k, D, dtype=dtype), gaussian(3, T, D, dtype=dtype), gaussian(4, T, k)
+    ys[at[~there]] = float("nan")
+    wide = torch.where(there[..., None], ys.double()[at], 0.0)
+    for out_dtype in (torch.bfloat16, torch.float32):
+        for f, got in ((w.double(), ops.expert_join(ys, plan, w, out_dtype=out_dtype)), (torch.ones_like(w).double(), ops.expert_rows_grad(ys, plan, out_dtype=out_dtype))):
+            y, size = (f[..., None] * wide).sum(1), (f[..., None] * wide).abs().sum(1)
+            assert ((got.double() - y).abs() <= half_step(out_dtype) * y.abs() + 1.01 * (k + 1) * 2.0 ** -24 * size).all()
+    drows, dw = ops.expert_join_grad(dy, ys, plan, w)
+    back = torch.zeros(T * k, D, dtype=torch.float64, device="cuda")
+    back[at[there]] = (w.double()[..., None] * dy.double()[:, None])[there]
+    assert ((drows.double() - back).abs() <= 1.01 * (half_step(dtype) + 2.0 ** -24) * back.abs()).all() and (drows[at[~there]] == 0).all()
+    products = wide * dy.double()[:, None]
+    assert ((dw.double() - products.sum(2)).abs() <= (D / 32 + 16) * 2.0 ** -24 * products.abs().sum(2)).all() and (dw[~there] == 0).all()
+    ops.check()
+
+
+@pytest.mark.parametrize("M,V", [(2000, 300), (2000, 4000), (2000, 9001), (1300, 12000), (1200, 20000), (650, 47999), (400, 50001), (200, 128256), (160, 300000)])
+@pytest.mark.parametrize("top", [0, 5, 32])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["plain", "masked", "coarse"])
+def test_log_probabilities_of_large_batches(ops, M, V, top, dtype, kind):
+    """Enough rows for every SM: 32, 64, 128 and 256 threads a row, each with more batches than it has slots among the longest rows; the same bounds as above."""
+    x = gaussian(M + V, M, V, scale=2.0, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    if kind == "masked":
+        x = x.masked_fill(torch.rand(M, V, generator=g, device="cuda") < torch.rand(M, 1, generator=g, device="cuda"), -INF)
+        x[3] = -INF
+        x[4, :-2] = -INF
+    elif kind == "coarse":                                  # many equal values: the lowest index first
+        x = (x * 2).round() / 2
+        x[5] = 1.0
+        x[6, V // 2:] = 40.0
+    tokens = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    tokens[::9] = -1
+    for a in range(0, M, 400):                              # (a part of the rows at a time in 64 bits)
+        if a == 0:
+            r = ops.token_logprobs(x, tokens, top=top)
+        part = type(r)(*(None if v is None else v[a:a + 400] for v in r))
+        assert_logprobs(part, x[a:a + 400], tokens[a:a + 400], top, 1.0)
+    ops.check()
