@@ -4,8 +4,8 @@
  * Step t of a tensor with parameters p, gradient g (times *grad_scale where that is given), moments m and v:
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *     p = p (1 - lr decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps).
- * All tensors are updated by one launch (by one for every 1024 of them where they are given one by one).  The number of steps, the powers of the
- * betas and lr live on the device, so that a step captured into a CUDA graph counts its replays and follows cocod_adamw_set_lr.
+ * All tensors are updated by one launch (by one for every 1024 of them where they are given one by one).  t is the number of the handle's steps, also for a tensor
+ * that had no gradient in some of them: its moments stay as they were, their correction goes on.  The number of steps, the powers of the betas and lr live on the device, so that a step captured into a CUDA graph counts its replays and follows cocod_adamw_set_lr.
  *
  * State.  The moments lie in the caller's memory, tensors one behind the other, each starting at a multiple of 128 values; L = the sum
  * of the sizes, each rounded up to 128 (cocod_adamw_values).  What lies behind a tensor's values stays 0.
@@ -42,7 +42,7 @@ int64_t cocod_adamw_values(int n, const int64_t *sizes);
 
 /* sizes, decay (NULL: 0), starts: host, n values; the arrays are copied.  starts: where the tensors lie in one flat buffer (cocod_adamw_flat_step,
  * cocod_adamw_local_step), or NULL if every step gives their addresses (cocod_adamw_step).  Allocates its tables (about 40 bytes a tensor and 4 for each
- * 2048 values).  m_units, v_units: NULL with 32 bits.  The state is not touched.  Errors: INVALID (0 <= beta < 1, eps >= 0, lr and decay finite), OOM, CUDA. */
+ * chunk of 1024 to 16384 values, at least one a tensor).  m_units, v_units: NULL with 32 bits.  The state is not touched.  Errors: INVALID (0 <= beta < 1, eps >= 0, lr and decay finite), OOM, CUDA. */
 int cocod_adamw_create(cocod_adamw_handle **out, int n, const int64_t *sizes, const float *decay, const int64_t *starts, int state_bits, void *m, void *v,
                        float *m_units, float *v_units, float lr, double beta1, double beta2, float eps);
 int cocod_adamw_destroy(cocod_adamw_handle *h);

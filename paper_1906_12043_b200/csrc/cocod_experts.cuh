@@ -303,7 +303,7 @@ expert_rows(const ExpertRows p, const T *x, long long ldx, T *out, long long ld_
 // The way back: y[t] = sum_j w[t][j] rows[place[t][j]] (weights == nullptr: the plain sum), fp32 in the order of j, in two forms with the same bits.  A warp takes
 // PIECES x 32 pieces of one token, and U rows' pieces are under way together; BLOCKS of 256 threads share an SM (16384 x 8 of 2048, U = 4, two pieces: three blocks
 // 95.8 us, four 91.7, one piece and six blocks 96.3, four 109; 65536 x 2 of 1024, U = 2: four blocks 78, five 73, six 77; 65536 x 1 of 1024, U = 1: eight blocks 50.7, four
-// pieces and four blocks 49.1, but 54.8 against 39.4 at half the width).  A launch that leaves SMs idle takes one piece (64 x 8 of 2048, in a graph: 2.2 us instead of 2.6).
+// pieces and four blocks 49.1, but 54.8 against 39.4 at half the width; eight blocks of U = 1 spill 12 words with a bf16 result and 23 with fp32, and take 50.4 and 72.6, six 56.4 and 73.9 with two words).  A launch that leaves SMs idle takes one piece (64 x 8 of 2048, in a graph: 2.2 us instead of 2.6).
 template <typename T, typename O, bool WIDE, int U, int PIECES, int BLOCKS>
 __global__ void __launch_bounds__(256, BLOCKS)
 expert_join_many(const ExpertRows p, const T *rows, long long ld, const float *weights, O *y, long long ldy)
@@ -417,8 +417,8 @@ expert_join_few(const ExpertRows p, const T *rows, long long ld, const float *we
 
 // The gradient of that: back[place[t][j]] = w[t][j] dy[t] (0 where the slot takes no part), dw[t][j] = <dy[t], rows[place[t][j]]>.
 // WARPS warps take a token; each sum runs over a thread's pieces, the lanes and the warps, always in the same order.
-// The loads of a piece of U slots are under way together, and as many blocks share an SM as their registers allow without spilling (16384 x 8 of 2048, U = 4: four
-// blocks 176 us, three 198, five 187; U = 2, of one or two choices: six blocks, 100000 x 1 of 512 66 us against 82 with U = 4; U = 8 was behind at all sizes: 184).
+// The loads of a piece of U slots are under way together.  Blocks that share an SM: U = 4, four (16384 x 8 of 2048: 176 us, three 198, five 187); U = 2, of one or two
+// choices, six, for which up to twelve words are spilled (100000 x 1 of 512: 65 us, with five blocks and two words 70, with U = 4 82).  U = 8 was behind at all sizes: 184.
 template <typename T, bool WIDE, int WARPS, int U>
 __global__ void __launch_bounds__(256, U == 2 ? 6 : 4)
 expert_join_grad(const ExpertRows p, const T *dy, long long lddy, const T *rows, long long ld, const float *weights, T *back, long long ld_back, float *dw)

@@ -165,8 +165,8 @@ int run_logprobs(cocod_lm *h, const TokenRows &p, cudaStream_t s)
     if (p.rows > MAX_DIM / blocks) return COCOD_ERR_TOO_LARGE;
     if (blocks > 1) return run_logprobs_row<T, 512>(h, p, blocks, s);
     // A row's threads: what follows the pass over a row costs every one of them, and leaves HBM idle unless other rows are under way (32768 x 4000, five
-    // alternatives: 86 us with 32 threads, 108 with 64; 16384 x 16000: 114 and 109, 125 with 128; 4096 x 50001 with twenty: 133 with 64, 108 and 103 with 128
-    // and 256, whose threads have less to look at again).  Where few rows leave SMs without warps, more: 200 x 5000 with twenty: 10.7 us with 32, 7.2 with 256.
+    // alternatives: 84 us with 32 threads, 107 with 64; 16384 x 16000: 114 and 113, 133 with 128; 4096 x 50001 with twenty: 131 with 64, 99 and 100 with 128
+    // and 256, whose threads have less to look at again).  Where few rows leave SMs without warps, more: 200 x 5000 with twenty: 12.9 us with 32, 8.5 with 256.
     int threads = p.vocab <= 12000 ? 32 : p.vocab <= 24000 ? 64 : p.vocab <= 48000 ? 128 : 256;
     while (threads < 256 && p.rows * (threads / 32) * 2 <= 16 * (int64_t)sm_count() && p.vocab >= 16 * threads) threads *= 2;
     return threads == 32 ? run_logprobs_row<T, 32>(h, p, 1, s) : threads == 64 ? run_logprobs_row<T, 64>(h, p, 1, s)

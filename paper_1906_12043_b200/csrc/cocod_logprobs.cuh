@@ -5,8 +5,8 @@
 // in one pass over the row: a warp's threads share a reference, the largest logit that the warp has seen, and change it together when a batch exceeds it (S1' = c S1,
 // S2' = c (S2 + d S1) with d = old - new reference in units of t, c = 2^d); warps are joined by the same rule at the end.  The largest logit's own term, (1, 0)
 // exactly, is not in the thread's sums but counted beside them: S1 = n + (the others), so that ln S1 = log1p(n - 1 + the others) and what a confident row has beside its
-// largest logit is not lost in rounding; no log p is above 0, and no entropy below.  (With references of a thread that stayed until a value was 2^64 times the
-// reference's, log p and H were off by up to 7e-6 there, of either sign.)
+// largest logit is not lost in rounding; no log p is above 0, and no entropy below.  (Rows of 4000 to 128256 entries with one 20 to 40 above
+// the others: log p and H are off by up to 2.1e-7; with a thread's references, kept until a value was 2^64 times the reference's, by 3.1e-6 and 2.0e-5, of either sign.)
 //
 // The top alternatives cost that pass next to nothing.  The largest of each batch of 32 values is needed there anyway; every thread keeps those of its
 // batches (up to eight, or of as many groups of batches).  The k-th largest of 64 groups' maxima is a bound that at least k values reach and, as a rule, few more.
@@ -16,10 +16,10 @@
 // Values that are not finite: a row with a NaN or +inf has NaN for its log probabilities and its entropy; -inf is a masked entry (p = 0); a
 // row of nothing else has Z = -inf, log p = -inf, H = 0 and gradient 0.
 //
-// What bounds them: HBM, one reading (forward) or one reading and one writing (gradient) of the logits, of long rows in bf16 (4096 x 65536: 88 us and 6.1 TB/s
-// without alternatives, 103 with five; the gradient of 4096 x 50001 138 us, 5.9 TB/s): the forward pass takes eight issue slots a value of the eleven that the
+// What bounds them: HBM, one reading (forward) or one reading and one writing (gradient) of the logits, of long rows in bf16 (4096 x 65536, other logits every time: 97 us and
+// 5.5 TB/s without alternatives, 108 with five; the gradient of 4096 x 50001 138 us, 5.9 TB/s): the forward pass takes eight issue slots a value of the eleven that the
 // copy rate leaves.  Of short rows what follows the pass: its barriers, the second look and the ranking wait for one another, and a thread block has
-// nothing else to do (32768 x 4000: 55 us without alternatives, 86 with five, 131 with twenty; one reading would take 40).
+// nothing else to do (32768 x 4000: 58 us without alternatives, 86 with five, 130 with twenty; one reading would take 40).
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -659,7 +659,7 @@ __device__ __forceinline__ Sums sums_of(Running a, float most, float unit)
 }
 
 // `blocks` thread blocks (a cluster where there are more than one) take a row; each takes a stretch of its words.
-// 32 warps an SM: 64 registers (4096 x 65536: 89 us; with 24 or 40 warps 94 and 106).
+// 32 warps an SM: 64 registers (4096 x 65536: 89 us; with 24 or 40 warps 94 and 106).  32 threads with alternatives spill three words for it.
 template <int THREADS> constexpr int ROW_BLOCK = THREADS == 32 ? 128 : THREADS;
 template <typename T, int THREADS, bool TOP>
 __global__ void __launch_bounds__(ROW_BLOCK<THREADS>, 1024 / ROW_BLOCK<THREADS>)
@@ -725,7 +725,7 @@ token_logprobs_row(const TokenRows p, int blocks)
             most = max_nan(most, batch_most);
         }
     };
-    // bf16: the next batch is under way while one is taken (fp32, whose batches are twice the words, does without: 94 us, with it 110, for 2048 x 50001)
+    // bf16: the next batch is under way while one is taken (fp32, whose batches are twice the words, does without: 68 us, with it 126, for 2048 x 50001)
     constexpr bool AHEAD = sizeof(T) == 2;
     uint4 r[U];
     const auto fetch = [&](int from) {

@@ -87,7 +87,7 @@ class PackedActivations:
 
 class ExpertPlan(NamedTuple):
     """Slots (token t's j-th choice) in the order of their experts.  A slot that takes no part has the bitwise complement of its row in `place`; such
-    rows lie behind the last expert's, count as its own in `offsets`, and are zero."""
+    rows lie behind the last expert's, count as its own in `offsets`, and are zero.  The four are parts of one allocation: clone the one that is kept or saved alone."""
     offsets: torch.Tensor          # E + 1: row offsets[e] is expert e's first, as the products by group take them
     counts: torch.Tensor           # E: slots of each expert
     order: torch.Tensor            # the slot (t * k + j) of each row
@@ -95,6 +95,7 @@ class ExpertPlan(NamedTuple):
 
 
 class TokenLogprobs(NamedTuple):
+    """Parts of one allocation: clone the one that is kept or saved alone."""
     logp: Optional[torch.Tensor]          # of the rows' tokens (None without tokens)
     entropy: torch.Tensor
     log_sum: torch.Tensor                 # log of the sum of exp(scale * logits)
@@ -225,7 +226,7 @@ class LMOps:
         return self._checked(self._b.expert_join(self._h, self._device, rows, plan.place, weights, out, self._code(out_dtype)), "cocod_expert_join")
 
     def expert_join_grad(self, dy, rows, plan: ExpertPlan, weights, out=None):
-        """(drows, dweights): the gradients of expert_join's rows (T k x D; zeros where a slot takes no part) and weights (T x k float32)."""
+        """(drows, dweights): the gradients of expert_join's rows (T k x D; zeros where a slot takes no part) and weights (T x k float32).  dy and rows are of one type."""
         return self._checked(self._b.expert_join_grad(self._h, self._device, dy, rows, plan.place, weights, out), "cocod_expert_join_grad")
 
     # ------------------------------------------------------------------------------------------ log probabilities

@@ -195,7 +195,7 @@ class AdamW(_Moments):
 
     def step(self, grads=None, grad_scale=None):
         """One step on torch's current stream (order the steps of one object).  grads: one for each parameter, all bf16 or all float32 (default: the parameters' .grad); a parameter whose
-        gradient is None keeps its value and its moments.  grad_scale: one float32 on the device, a factor of all gradients."""
+        gradient is None keeps its value and its moments (the number of steps, by which moments are corrected, is the optimizer's).  grad_scale: one float32 on the device, a factor of all gradients."""
         if grads is None:
             grads = [p.grad for p in self.params]
         rc = self._b.adamw_step(self._h, self._device, self.params, grads if type(grads) in (list, tuple) else list(grads), self.copies, grad_scale)
