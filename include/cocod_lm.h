@@ -172,7 +172,8 @@ int cocod_expert_join_grad(cocod_lm_handle *h, int64_t T, int k, int64_t D, cons
  * +inf: NaN for logp, entropy, log_sum and top_logp; top_tokens orders NaN before all others.
  *
  * token_logprobs_grad   dlogits = scale * (given - p * (sum of given + d_entropy * (log p + entropy))), with `given` the sum of d_logp at the row's token
- *   and d_top at its top_tokens (a repeated or negative one is allowed: added up, left out).  log_sum and entropy are those of the forward call.
+ *   and d_top at its top_tokens (a repeated or negative one is allowed: added up, left out).  log_sum and entropy are those of the forward call; log p
+ *   is y - log_sum in fp32, off by up to 2^-23 (|y| + |log_sum|) also where p is near 1.
  *   d_logp, d_entropy, d_top: NULL where there are none (entropy is read only with d_entropy; top_tokens and d_top are M x top).  dlogits:
  *   M x V of the logits' type; may be the logits themselves (same address and stride). */
 #define COCOD_LM_MAX_TOP 32
